@@ -545,6 +545,121 @@ int32_t llama_swiglu_quantise(const void *gu, int64_t ldgu, int64_t rows, int64_
  */
 int32_t llama_residual_add(const void *a, const void *b, void *out, int64_t n, void *stream);
 
+/*
+ * ---- paged key/value cache of the decoder layer --------------------------
+ * Token-by-token and chunked inference: the keys and values of earlier tokens
+ * are kept in pages, in FP8 with one power-of-two scaling bias per token and
+ * key/value head (Sec. 2.3 Eq. 3 over the head's d_head values, Sec. 2.1 Eq. 1
+ * cast), or in bf16; a call's new tokens are appended and then attend over the
+ * cache.  A bias per token needs no second look at earlier tokens, and a
+ * cached value never changes.
+ *
+ * llama_cache -- the cache, pages shared by all sequences (a host struct, read
+ * before a call returns; its pointers are device pointers, 16-byte aligned):
+ *   k:     [n_pages, n_kv_heads, page_size, d_head] codes (1 byte) or bf16
+ *   v:     [n_pages, n_kv_heads, page_size / 16, d_head, 16] codes or bf16:
+ *          blocks of 16 tokens, the tokens innermost (the order in which the
+ *          product of probabilities and values reads them)
+ *   k_exp, v_exp: [n_pages, n_kv_heads, page_size] bytes, 127 - b for a bias b
+ *          (clamped to b <= 126): value = code * 2^(exp - 127).  NULL for bf16.
+ * fmt: FP8_E4M3, FP8_E5M2 or LLAMA_CACHE_BF16.  (The paper's (a) formats are
+ * FP8_ENOTSUP: the matrix cores do not read them.)  d_head 64 or 128
+ * (FP8_ENOTSUP otherwise).  page_size: a power of two, 16 to 1024.
+ * 1 <= n_pages <= INT32_MAX.
+ *
+ * llama_cache_seqs -- the sequences of a call (host struct of device pointers):
+ *   cu_rows: int32 [n_seqs + 1], nondecreasing from 0: rows cu_rows[s] <= r <
+ *          cu_rows[s+1] of the call belong to sequence s.  Rows behind
+ *          cu_rows[n_seqs] belong to none and are neither read nor written.
+ *   kv_len: int32 [n_seqs]: tokens of the sequence in the cache, the call's own
+ *          rows included.  The n rows of sequence s are its last n tokens: row
+ *          cu_rows[s] + i is at position kv_len[s] - n + i.
+ *   pages: int32 [n_seqs, max_pages], row stride ld_pages: the page that holds
+ *          positions page_size i .. page_size i + page_size - 1.
+ * They are read on the device, so a captured graph follows their contents.
+ * max_pages * page_size is at most 2^30 positions, n_seqs 2^20, the rows of a
+ * call 2^27, n_kv_heads 4096, n_heads 65536 (FP8_ENOTSUP beyond, for n_heads
+ * FP8_EINVAL).
+ * Whatever they hold, nothing outside the buffers is read or written:
+ * a page number outside [0, n_pages) is a page that is absent, and so is every
+ * position below 0 or from max_pages * page_size on.  Tokens at absent places
+ * are not stored, read back as zeros, and are seen by no query.
+ * Sequences may share pages that none of them writes.  Two rows of one call
+ * that write the same slot leave either's codes there.
+ */
+#define LLAMA_CACHE_BF16 16
+typedef struct llama_cache {
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;
+    int64_t n_pages;
+    int32_t n_kv_heads, d_head, page_size, fmt;
+} llama_cache;
+typedef struct llama_cache_seqs {
+    const int32_t *cu_rows, *kv_len, *pages;
+    int64_t n_seqs, max_pages, ld_pages;
+} llama_cache_seqs;
+
+/*
+ * llama_cache_append -- rotary embedding at each token's own position and the
+ * write into the cache, in one launch:
+ *   q = round(rot(Q)); K' = rot(K) and V quantised per (token, head) from
+ *   their fp32 values (one rounding), or rounded to bf16.
+ * qkv:   [rows, ld], the QKV projection's output: n_heads query heads, then
+ *        n_kv_heads key heads, then n_kv_heads value heads, d_head columns each.
+ *        Not changed (unless q is its query columns).
+ * table: llama_rope_table of table_len positions, table_len >= max_pages *
+ *        page_size; NULL: no rotation.
+ * q:     out, optional, [rows, ldq >= n_heads d_head]: the rotated queries; may
+ *        be qkv itself (ldq = ld, in place).  Rows at absent positions give 0.
+ * An amax of 0, an infinite or a NaN one gives bias 0, as fp8_scale_bias; NaN
+ * values keep NaN codes, infinities clip.  rows == 0 or n_seqs == 0 is a no-op.
+ */
+int32_t llama_cache_append(const void *qkv, int64_t rows, int64_t ld, int32_t n_heads, const llama_cache *cache,
+                           const llama_cache_seqs *seqs, const float *table, int64_t table_len, void *q, int64_t ldq,
+                           void *stream);
+
+/*
+ * llama_cache_read -- cached values back as bf16 rows: row cu_rows[s] + i of k
+ * and v gets the key and value heads of sequence s at position kv_len[s] - n + i
+ * (n_kv_heads d_head columns each), 2^(exp - 127) times the codes, which is
+ * exact in bf16 but for results below its normal range (rounded to nearest
+ * even).  To read a whole sequence, give it kv_len[s] rows.
+ * k, v: out, [rows, ldk], [rows, ldv]; one of them may be NULL.
+ */
+int32_t llama_cache_read(const llama_cache *cache, const llama_cache_seqs *seqs, int64_t rows, void *k, int64_t ldk,
+                         void *v, int64_t ldv, void *stream);
+
+/*
+ * llama_cache_attention -- causal grouped-query attention of the call's rows
+ * over the cache (which already holds their own keys and values):
+ *   o_r = sum_j softmax_j(q_r . k_j / sqrt(d_head)) v_j
+ * over the present positions j of r's sequence with j <= p, p the position of
+ * r, and, if window > 0, j > p - window.  A row that sees no position gives 0.
+ * What a row does not see does not reach it, whatever it holds (NaN included).
+ * q:     [rows, ldq], n_heads heads; head h reads key/value head
+ *        h / (n_heads / n_kv_heads).
+ * max_rows: at least the rows of every sequence (the sizes of the launch follow
+ *        it); of a longer sequence the rows after the first max_rows are left.
+ * o:     out, [rows, ldo].
+ * fmt .. ldq8: fused quantise of o as in llama_attention (q8 == NULL: none); its
+ *        amax is over the rows of sequences only.
+ * ws:    workspace of llama_cache_attention_ws_bytes(...) bytes, 16-byte aligned;
+ *        scratch, distinct for concurrent calls.  It holds the partial results
+ *        of key ranges that are computed apart and then joined.
+ * Softmax statistics and sums in fp32; the probabilities are rounded to bf16
+ * for the product with the values, and o is rounded once.  The key ranges
+ * depend on the sizes of the call alone (n_heads, rows, n_seqs, max_rows,
+ * max_pages) and on a sequence's own length: a call gives the same bits every
+ * time.
+ */
+size_t llama_cache_attention_ws_bytes(int64_t rows, int32_t n_heads, const llama_cache *cache,
+                                      const llama_cache_seqs *seqs, int64_t max_rows);
+int32_t llama_cache_attention(const void *q, int64_t rows, int64_t ldq, int32_t n_heads, const llama_cache *cache,
+                              const llama_cache_seqs *seqs, int64_t max_rows, int64_t window, void *o, int64_t ldo,
+                              int32_t fmt, int32_t margin, const int32_t *bias_pred, int32_t *bias,
+                              uint32_t *amax_bits, uint32_t *flags, uint8_t *q8, int64_t ldq8, void *ws,
+                              size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -575,6 +575,108 @@ int32_t llama_residual_add(const void* a, const void* b, void* out, int64_t n, v
     return launch_residual_add((const uint16_t*)a, (const uint16_t*)b, (uint16_t*)out, n, as_stream(stream));
 }
 
+// ---- paged key/value cache
+}  // extern "C"
+
+namespace {
+// Checks a cache and the sequences of a call of `rows` rows and fills *v.
+int32_t cache_checks(const llama_cache* c, const llama_cache_seqs* s, int64_t rows, CacheView* v) {
+    if (!c || !s || rows < 0 || s->n_seqs < 0 || s->max_pages < 0 || c->n_pages < 1 || c->n_kv_heads < 1)
+        return FP8_EINVAL;
+    const int ps = c->page_size;
+    if (ps < 16 || ps > 1024 || (ps & (ps - 1))) return FP8_EINVAL;
+    const bool fp8 = c->fmt == FP8_E4M3 || c->fmt == FP8_E5M2;
+    if (c->fmt == FP8_E4_A || c->fmt == FP8_E5_A) return FP8_ENOTSUP;
+    if (!fp8 && c->fmt != LLAMA_CACHE_BF16) return FP8_EINVAL;
+    if (c->d_head != 64 && c->d_head != 128) return FP8_ENOTSUP;
+    if (!c->k || !c->v || !a16(c->k) || !a16(c->v)) return FP8_EINVAL;
+    if (fp8 && (!c->k_exp || !c->v_exp || !a16(c->k_exp) || !a16(c->v_exp))) return FP8_EINVAL;
+    if (c->n_pages > INT32_MAX || s->n_seqs > ((int64_t)1 << 20) || s->max_pages > ((int64_t)1 << 30) / ps ||
+        rows > ((int64_t)1 << 27) || c->n_kv_heads > 4096)
+        return FP8_ENOTSUP;
+    if (rows > 0 && s->n_seqs > 0) {
+        if (!s->cu_rows || !s->kv_len || !aligned(s->cu_rows, 4) || !aligned(s->kv_len, 4)) return FP8_EINVAL;
+        if (s->max_pages > 0 && (!s->pages || !aligned(s->pages, 4) || s->ld_pages < s->max_pages)) return FP8_EINVAL;
+    }
+    int shift = 4;
+    while ((1 << shift) < ps) ++shift;
+    *v = CacheView{(uint8_t*)c->k, (uint8_t*)c->v, c->k_exp, c->v_exp, c->n_pages, s->ld_pages, s->cu_rows, s->kv_len,
+                   s->pages, c->n_kv_heads, shift, (int)s->n_seqs, (int)s->max_pages, rows};
+    return FP8_OK;
+}
+
+bool heads_ok(int32_t n_heads, const llama_cache* c) {
+    return n_heads >= 1 && n_heads <= 65536 && n_heads % c->n_kv_heads == 0;
+}
+}  // namespace
+
+extern "C" {
+
+int32_t llama_cache_append(const void* qkv, int64_t rows, int64_t ld, int32_t n_heads, const llama_cache* cache,
+                           const llama_cache_seqs* seqs, const float* table, int64_t table_len, void* q, int64_t ldq,
+                           void* stream) {
+    CacheView v;
+    const int32_t st = cache_checks(cache, seqs, rows, &v);
+    if (st != FP8_OK) return st;
+    if (!heads_ok(n_heads, cache)) return FP8_EINVAL;
+    if (rows == 0 || v.n_seqs == 0) return FP8_OK;
+    const int64_t dh = cache->d_head;
+    if (!qkv || !a16(qkv) || !rows_ok(ld, (n_heads + 2 * (int64_t)v.nkv) * dh)) return FP8_EINVAL;
+    if (q && (!a16(q) || !rows_ok(ldq, n_heads * dh))) return FP8_EINVAL;
+    if (table && (!aligned(table, 16) || table_len < (int64_t)v.max_pages << v.page_shift)) return FP8_EINVAL;
+    return launch_cache_append((const uint16_t*)qkv, ld, n_heads, v, cache->fmt, (int)dh, table, (uint16_t*)q, ldq,
+                               as_stream(stream));
+}
+
+int32_t llama_cache_read(const llama_cache* cache, const llama_cache_seqs* seqs, int64_t rows, void* k, int64_t ldk,
+                         void* v, int64_t ldv, void* stream) {
+    CacheView cv;
+    const int32_t st = cache_checks(cache, seqs, rows, &cv);
+    if (st != FP8_OK) return st;
+    if (rows == 0 || cv.n_seqs == 0) return FP8_OK;
+    const int64_t cols = (int64_t)cv.nkv * cache->d_head;
+    if (!k && !v) return FP8_EINVAL;
+    if ((k && (!a16(k) || !rows_ok(ldk, cols))) || (v && (!a16(v) || !rows_ok(ldv, cols)))) return FP8_EINVAL;
+    return launch_cache_read(cv, cache->fmt, cache->d_head, (uint16_t*)k, ldk, (uint16_t*)v, ldv, as_stream(stream));
+}
+
+size_t llama_cache_attention_ws_bytes(int64_t rows, int32_t n_heads, const llama_cache* cache,
+                                      const llama_cache_seqs* seqs, int64_t max_rows) {
+    if (!cache || !seqs || rows <= 0 || rows > ((int64_t)1 << 27) || max_rows < 1 || cache->n_kv_heads < 1 ||
+        !heads_ok(n_heads, cache) || (cache->d_head != 64 && cache->d_head != 128) || seqs->n_seqs < 1 ||
+        seqs->n_seqs > ((int64_t)1 << 20) || seqs->max_pages < 0 || cache->page_size < 16 || cache->page_size > 1024 ||
+        seqs->max_pages > ((int64_t)1 << 30) / cache->page_size)
+        return 0;
+    return (size_t)cache_attn_plan(rows, n_heads, cache->n_kv_heads, cache->d_head, seqs->n_seqs, max_rows,
+                                   seqs->max_pages * cache->page_size)
+        .ws_bytes;
+}
+
+int32_t llama_cache_attention(const void* q, int64_t rows, int64_t ldq, int32_t n_heads, const llama_cache* cache,
+                              const llama_cache_seqs* seqs, int64_t max_rows, int64_t window, void* o, int64_t ldo,
+                              int32_t fmt, int32_t margin, const int32_t* bias_pred, int32_t* bias,
+                              uint32_t* amax_bits, uint32_t* flags, uint8_t* q8, int64_t ldq8, void* ws,
+                              size_t ws_bytes, void* stream) {
+    CacheView v;
+    const int32_t st = cache_checks(cache, seqs, rows, &v);
+    if (st != FP8_OK) return st;
+    if (!heads_ok(n_heads, cache) || max_rows < 0 || window < 0) return FP8_EINVAL;
+    if (rows == 0 || v.n_seqs == 0 || max_rows == 0)
+        return glue_empty(fmt, margin, bias, amax_bits, flags, q8, stream);
+    const int64_t cols = (int64_t)n_heads * cache->d_head;
+    if (!q || !o || !a16(q) || !a16(o) || !rows_ok(ldq, cols) || !rows_ok(ldo, cols)) return FP8_EINVAL;
+    const CacheAttnPlan plan = cache_attn_plan(rows, n_heads, v.nkv, cache->d_head, v.n_seqs, max_rows,
+                                               (int64_t)v.max_pages << v.page_shift);
+    if (plan.parts >= ((int64_t)1 << 24)) return FP8_ENOTSUP;  // workgroups of one launch
+    if (plan.ws_bytes > 0 && (!ws || !a16(ws) || ws_bytes < (size_t)plan.ws_bytes)) return FP8_EINVAL;
+    FusedQuant fq;
+    const int32_t qst = glue_quant(fmt, margin, bias_pred, bias, amax_bits, flags, q8, ldq8, cols, ws, ws_bytes,
+                                   1 + plan.parts, &fq);
+    if (qst != FP8_OK) return qst;
+    return launch_cache_attention((const uint16_t*)q, ldq, n_heads, v, cache->fmt, cache->d_head, max_rows, window,
+                                  (uint16_t*)o, ldo, &fq, ws, as_stream(stream));
+}
+
 }  // extern "C"
 
 // ---- for the tests and measurements: not declared in fp8lin.h, not part of the ABI

@@ -190,6 +190,31 @@ int32_t launch_swiglu(const uint16_t* gu, int64_t ldgu, int64_t rows, int64_t ff
 int32_t launch_attention(const uint16_t* qkv, int64_t rows, int64_t ld, int64_t seq_len, int nh, int nkv,
                          uint16_t* o, int64_t ldo, const FusedQuant* fq, hipStream_t s);
 
+// ---- paged key/value cache (fp8lin_cache.hip); arguments checked
+// Device view of llama_cache and llama_cache_seqs.
+struct CacheView {
+    uint8_t *k, *v, *ke, *ve;
+    int64_t n_pages, ld_pages;
+    const int32_t *cu, *kv_len, *pages;
+    int nkv, page_shift, n_seqs, max_pages;
+    int64_t rows;
+};
+int32_t launch_cache_append(const uint16_t* qkv, int64_t ld, int nh, const CacheView& c, int fmt, int d_head,
+                            const float* table, uint16_t* q, int64_t ldq, hipStream_t s);
+int32_t launch_cache_read(const CacheView& c, int fmt, int d_head, uint16_t* k, int64_t ldk, uint16_t* v, int64_t ldv,
+                          hipStream_t s);
+// Sizes of an attention call: workspace bytes for the partial results, and
+// the workgroups that write outputs (maxima of a fused quantise).
+struct CacheAttnPlan {
+    int64_t parts;       // workgroups that write the output
+    int64_t ws_bytes;    // everything: 1 + parts words, then the partials
+};
+CacheAttnPlan cache_attn_plan(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t max_rows,
+                              int64_t max_len);
+int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const CacheView& c, int fmt, int d_head,
+                               int64_t max_rows, int64_t window, uint16_t* o, int64_t ldo, const FusedQuant* fq,
+                               void* ws, hipStream_t s);
+
 // *p = v on the stream (one word).
 int32_t launch_fill_u32(uint32_t* p, uint32_t v, hipStream_t s);
 

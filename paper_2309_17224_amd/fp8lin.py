@@ -18,6 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfp8lin.so")
 
 E4M3, E5M2 = 0, 1
+CACHE_BF16 = 16     # format of an unquantised key/value cache
 E4_A, E5_A = 2, 3   # the paper's formats (Table 7 rows "(a)"); bias and cast calls only
 DT_BF16, DT_F32 = 0, 1
 FLAG_NONFINITE, FLAG_ZERO, FLAG_SATURATED = 1, 2, 4
@@ -37,6 +38,7 @@ EXPORTS = (
     "llama_rmsnorm_ws_bytes", "llama_rmsnorm_quantise", "llama_rope_table", "llama_rope",
     "llama_attention_ws_bytes", "llama_attention", "llama_swiglu_ws_bytes", "llama_swiglu_quantise",
     "llama_residual_add",
+    "llama_cache_append", "llama_cache_read", "llama_cache_attention_ws_bytes", "llama_cache_attention",
 )
 
 
@@ -134,6 +136,15 @@ def lib() -> ctypes.CDLL:
                                             sz, vp]
         L.llama_residual_add.restype = i32
         L.llama_residual_add.argtypes = [vp, vp, vp, i64, vp]
+        L.llama_cache_append.restype = i32
+        L.llama_cache_append.argtypes = [vp, i64, i64, i32, vp, vp, vp, i64, vp, i64, vp]
+        L.llama_cache_read.restype = i32
+        L.llama_cache_read.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp]
+        L.llama_cache_attention_ws_bytes.restype = sz
+        L.llama_cache_attention_ws_bytes.argtypes = [i64, i32, vp, vp, i64]
+        L.llama_cache_attention.restype = i32
+        L.llama_cache_attention.argtypes = [vp, i64, i64, i32, vp, vp, i64, i64, vp, i64, i32, i32, vp, vp, vp, vp,
+                                            vp, i64, vp, sz, vp]
         L.ptq_quantise_weights.restype = i32
         L.ptq_quantise_weights.argtypes = [vp, i32, i64, i64, vp, vp, vp, vp, vp, sz, vp]
         _lib = L
@@ -669,3 +680,157 @@ def llama_residual_add(a, b, out=None, stream=None):
     st = lib().llama_residual_add(_p(a), _p(b), _p(out), a.numel(), _stream(stream))
     _check("llama_residual_add", st)
     return out
+
+
+# ------------------------------------------------------------------ paged key/value cache
+class CacheStruct(ctypes.Structure):
+    """llama_cache of the C header."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32),
+                ("d_head", ctypes.c_int32), ("page_size", ctypes.c_int32), ("fmt", ctypes.c_int32)]
+
+
+class SeqsStruct(ctypes.Structure):
+    """llama_cache_seqs of the C header."""
+    _fields_ = [("cu_rows", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("pages", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("ld_pages", ctypes.c_int64)]
+
+
+def _shaped(t: torch.Tensor, name: str, shape, dtype, device) -> torch.Tensor:
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the rest on {device}")
+    return t
+
+
+class KVCache:
+    """Pages of keys and values (llama_cache): fmt E4M3 or E5M2 (codes with one
+    exponent byte per token and head, value = code * 2^(exp - 127)) or
+    CACHE_BF16.  k [n_pages, n_kv_heads, page_size, d_head], v [n_pages,
+    n_kv_heads, page_size / 16, d_head, 16], k_exp and v_exp [n_pages,
+    n_kv_heads, page_size]; buffers that are not given are allocated, empty."""
+
+    def __init__(self, n_pages: int, n_kv_heads: int, d_head: int, page_size: int, fmt: int, device, k=None, v=None,
+                 k_exp=None, v_exp=None):
+        dev = torch.empty(0, device=device).device  # with its index
+        self.device, self.fmt = dev, int(fmt)
+        self.n_pages, self.n_kv_heads, self.d_head, self.page_size = n_pages, n_kv_heads, d_head, page_size
+        dt = torch.bfloat16 if fmt == CACHE_BF16 else torch.uint8
+        ks, vs = (n_pages, n_kv_heads, page_size, d_head), (n_pages, n_kv_heads, page_size // 16, d_head, 16)
+        self.k = torch.empty(ks, dtype=dt, device=dev) if k is None else _shaped(k, "k", ks, dt, dev)
+        self.v = torch.empty(vs, dtype=dt, device=dev) if v is None else _shaped(v, "v", vs, dt, dev)
+        self.k_exp = self.v_exp = None
+        if fmt != CACHE_BF16:
+            es, u8 = ks[:3], torch.uint8
+            self.k_exp = torch.empty(es, dtype=u8, device=dev) if k_exp is None else _shaped(k_exp, "k_exp", es, u8, dev)
+            self.v_exp = torch.empty(es, dtype=u8, device=dev) if v_exp is None else _shaped(v_exp, "v_exp", es, u8, dev)
+        self._c = CacheStruct(_p(self.k), _p(self.v), _p(self.k_exp), _p(self.v_exp), n_pages, n_kv_heads, d_head,
+                              page_size, self.fmt)
+        self._ref = ctypes.addressof(self._c)
+
+
+class CacheSeqs:
+    """The sequences of a call (llama_cache_seqs), int32 device tensors: cu_rows
+    [n + 1], kv_len [n] (tokens cached, the call's own included), pages [n,
+    max_pages].  Their contents may change between calls."""
+
+    def __init__(self, cu_rows: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor):
+        n = kv_len.numel()
+        _shaped(kv_len, "kv_len", (n,), torch.int32, kv_len.device)
+        _shaped(cu_rows, "cu_rows", (n + 1,), torch.int32, kv_len.device)
+        if pages.dtype != torch.int32:
+            raise TypeError(f"pages: expected torch.int32, got {pages.dtype}")
+        if pages.dim() != 2 or pages.shape[0] != n or pages.device != kv_len.device:
+            raise ValueError("pages: expected [n_seqs, max_pages] on the device of kv_len")
+        self.cu_rows, self.kv_len, self.pages = cu_rows, kv_len, pages
+        self.n_seqs, self.max_pages, self.device = n, pages.shape[1], kv_len.device
+        self._c = SeqsStruct(_p(cu_rows), _p(kv_len), _p(pages), n, self.max_pages, _ld(pages))
+        self._ref = ctypes.addressof(self._c)
+
+
+def _on_device(cache: KVCache, seqs: CacheSeqs, *tensors) -> None:
+    """Every tensor of a call sits on the current GPU (its stream runs the call)."""
+    dev = cache.device
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {dev}, which is not the current GPU")
+    if seqs.device != dev or any(t is not None and t.device != dev for t in tensors):
+        raise ValueError(f"every tensor of the call must be on {dev}")
+
+
+def _cols(t: torch.Tensor, name: str, rows: int, cols: int) -> None:
+    _bf16(t, name)
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols:
+        raise ValueError(f"{name}: expected [{rows}, {cols}], got {tuple(t.shape)}")
+
+
+def llama_cache_append(qkv, cache: KVCache, seqs: CacheSeqs, n_heads: int, table=None, q=None, stream=None):
+    """Rotate the queries and keys of the call's rows (table: llama_rope_table of
+    at least max_pages * page_size positions; None: no rotation) and write keys
+    and values into the cache.  qkv: [rows, (n_heads + 2 n_kv_heads) d_head].
+    q: [rows, n_heads d_head], may be a view of qkv's query columns.  Returns q."""
+    rows, dh = qkv.shape[0], cache.d_head
+    _cols(qkv, "qkv", rows, (n_heads + 2 * cache.n_kv_heads) * dh)
+    q = torch.empty((rows, n_heads * dh), dtype=torch.bfloat16, device=qkv.device) if q is None else q
+    _cols(q, "q", rows, n_heads * dh)
+    _on_device(cache, seqs, qkv, table, q)
+    if table is not None and (table.dtype != torch.float32 or not table.is_contiguous()):
+        raise TypeError("table: expected a contiguous float32 tensor")
+    st = lib().llama_cache_append(_p(qkv), rows, _ld(qkv), n_heads, cache._ref, seqs._ref, _p(table),
+                                  table.numel() // dh if table is not None else 0, _p(q), _ld(q), _stream(stream))
+    _check("llama_cache_append", st)
+    return q
+
+
+def llama_cache_read(cache: KVCache, seqs: CacheSeqs, rows: int, k=None, v=None, want_k=True, want_v=True,
+                     stream=None):
+    """Cached keys and values of the positions that the call's rows stand for, as
+    bf16 [rows, n_kv_heads d_head].  Returns (k, v)."""
+    cols = cache.n_kv_heads * cache.d_head
+    bf = dict(dtype=torch.bfloat16, device=cache.device)
+    if want_k and k is None:
+        k = torch.empty((rows, cols), **bf)
+    if want_v and v is None:
+        v = torch.empty((rows, cols), **bf)
+    for t, name in ((k, "k"), (v, "v")):
+        if t is not None:
+            _cols(t, name, rows, cols)
+    _on_device(cache, seqs, k, v)
+    st = lib().llama_cache_read(cache._ref, seqs._ref, rows, _p(k), _ld(k) if k is not None else 0, _p(v),
+                                _ld(v) if v is not None else 0, _stream(stream))
+    _check("llama_cache_read", st)
+    return k, v
+
+
+def llama_cache_attention_ws_bytes(rows: int, n_heads: int, cache: KVCache, seqs: CacheSeqs, max_rows: int) -> int:
+    return int(lib().llama_cache_attention_ws_bytes(int(rows), int(n_heads), cache._ref, seqs._ref, int(max_rows)))
+
+
+def cache_attention_workspace(rows: int, n_heads: int, cache: KVCache, seqs: CacheSeqs, max_rows: int) -> torch.Tensor:
+    return torch.empty(max(llama_cache_attention_ws_bytes(rows, n_heads, cache, seqs, max_rows), 16),
+                       dtype=torch.uint8, device=cache.device)
+
+
+def llama_cache_attention(q, cache: KVCache, seqs: CacheSeqs, n_heads: int, max_rows: int, window: int = 0, o=None,
+                          fq: FusedQuant | None = None, ws=None, stream=None):
+    """Causal grouped-query attention of the call's rows (q [rows, n_heads
+    d_head]) over the cache, optionally with the fused quantise of o (its ws is
+    this call's).  max_rows: at least the rows of every sequence.  Returns o."""
+    rows, cols = q.shape[0], n_heads * cache.d_head
+    _cols(q, "q", rows, cols)
+    o = torch.empty((rows, cols), dtype=torch.bfloat16, device=q.device) if o is None else o
+    _cols(o, "o", rows, cols)
+    if fq is not None:
+        ws = fq.ws
+        if fq.q.shape != (rows, cols) or fq.q.dtype != torch.uint8:
+            raise ValueError(f"fq.q: expected uint8 [{rows}, {cols}]")
+    elif ws is None:
+        ws = cache_attention_workspace(rows, n_heads, cache, seqs, max_rows)
+    _on_device(cache, seqs, q, o, ws)
+    quant = fq.args()[:-2] if fq else _NO_QUANT[:-2]
+    st = lib().llama_cache_attention(_p(q), rows, _ld(q), n_heads, cache._ref, seqs._ref, max_rows, window, _p(o),
+                                     _ld(o), *quant, _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+    _check("llama_cache_attention", st)
+    return o
