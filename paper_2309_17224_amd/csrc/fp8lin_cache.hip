@@ -333,96 +333,743 @@ __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restr
 }
 
 // ------------------------------------------------------------- attention
-// One wave per (row, head): keys in tiles of 64, one per lane; running maximum
-// and sum of the softmax; each lane then sums two (or one) dimensions of the
-// values.
-template <int FMT, int DH, bool QUANT, int QF>
-__global__ __launch_bounds__(kT) void attn_kernel(CacheView c, const uint16_t* __restrict__ q, int64_t ldq, int nh,
-                                                  int64_t max_rows, int64_t window, uint16_t* __restrict__ o,
-                                                  int64_t ldo, const int32_t* __restrict__ pred,
-                                                  int32_t* __restrict__ used, uint32_t* __restrict__ parts,
-                                                  uint8_t* __restrict__ q8, int64_t ldq8) {
-    constexpr int kE = FMT == kBf16 ? 1 : FMT, kPer = DH / 64;
-    __shared__ float qs[kT / 64][DH];
+// A call's rows of one sequence and key/value head form the packed rows m =
+// token * group + head of the group: all of them read the same keys.  Two
+// kernels, both with the scores transposed (S^T = K . Q^T, then O^T += V^T . P^T),
+// so that the probabilities a lane holds are already the operand of the second
+// product:
+//   few_kernel   up to 16 packed rows (single tokens): each wave takes tiles of
+//                64 keys on its own, keys and values from memory straight into
+//                the operand registers; bound by reading the cache;
+//   many_kernel  tiles of 128 packed rows: keys and values through LDS, there in
+//                bf16; bound by the matrix cores and the exponentials.
+// FP8 codes become bf16 exactly (v_cvt_scalef32_pk_bf16_*).  Both products run
+// on the bf16 matrix instructions: those of FP8 operands keep about 14 bits of
+// the largest product of a sum (measured: up to 1e-4 of sum |q k| off, against
+// 1e-7), which scores do not tolerate.  A key's exponent is applied by that
+// conversion; a value's multiplies its probability, whose lanes are along keys.
+//
+// The key range of a tile of rows can be split over several workgroups, which
+// leave (maximum, sum, unnormalised output) in fp32 for combine_kernel.
+typedef float f16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kFew = 16;      // packed rows of few_kernel
+constexpr int kMany = 128;    // packed rows of a workgroup of many_kernel
+constexpr int kTile = 64;     // keys of a tile
+constexpr int kWant = 512;    // workgroups of a launch that key ranges are split for
+constexpr int kLeast = 512;   // keys of a range at least (of the longest sequence)
+
+struct AttnArgs {
+    CacheView c;
+    const uint16_t* q;
+    int64_t ldq;
+    int nh, grp;
+    int max_rows;
+    int window;           // 0: none
+    int few_on;           // few_kernel takes the sequences of up to kFew packed rows
+    int splits;           // of this kernel's key ranges
+    int few_splits, many_splits;
+    float c2;             // log2(e) / sqrt(d_head)
+    uint16_t* o;
+    int64_t ldo;
+    // fused quantise (q8 null: none)
+    const int32_t* pred;
+    int32_t* used;
+    uint32_t* parts;      // this launch's
+    uint8_t* q8;
+    int64_t ldq8;
+    int qfmt;
+    float* part_o;        // [split][row][head][d_head]
+    float2* part_ml;      // [split][row][head]: maximum, sum
+};
+
+__device__ __forceinline__ f16_t mfma32(u32x4 a, u32x4 b, f16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                   0, 0, 0);
+}
+
+// Two codes (the low or high half of w) times scale (a power of two) -> two bf16.
+template <int FMT, bool HI>
+__device__ __forceinline__ uint32_t cvt2b(uint32_t w, float scale) {
+    if (FMT == FP8_E5M2) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, HI));
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
+}
+// Eight codes -> eight bf16.
+template <int FMT>
+__device__ __forceinline__ u32x4 cvt8b(uint32_t w0, uint32_t w1, float scale) {
+    return u32x4{cvt2b<FMT, false>(w0, scale), cvt2b<FMT, true>(w0, scale), cvt2b<FMT, false>(w1, scale),
+                 cvt2b<FMT, true>(w1, scale)};
+}
+__device__ __forceinline__ float exp_float(uint32_t e) { return __uint_as_float(e << 23); }
+
+// Key range of the packed rows m0 .. m1 - 1 of a sequence, as tiles of 64 keys
+// from a multiple of 64 on, and the part of it that split i of n takes.
+struct Range {
+    int start;      // first key of tile 0
+    int kend;       // keys below this
+    int t0, t1;     // tiles of this split
+    int live;       // splits that have tiles
+    int first, last;  // positions of the first and last row
+};
+__device__ __forceinline__ Range range_of(const AttnArgs& p, const Seq& sq, int m0, int m1, int split, int n) {
+    Range r;
+    r.first = sq.p0 + m0 / p.grp;
+    r.last = sq.p0 + (m1 - 1) / p.grp;
+    r.kend = max(min(r.last + 1, sq.len), 0);
+    const int lo = p.window > 0 ? max(r.first - p.window + 1, 0) : 0;
+    r.start = lo & ~(kTile - 1);
+    const int nt = r.kend > r.start ? (r.kend - r.start + kTile - 1) / kTile : 0;
+    const int per = max((nt + n - 1) / n, 1);
+    r.live = (nt + per - 1) / per;
+    r.t0 = split * per;
+    r.t1 = min(r.t0 + per, nt);
+    return r;
+}
+
+// Nonfinite values of bf16 pairs: their exponent is all ones.
+__device__ __forceinline__ uint32_t nonfinite2(uint32_t w) { return ((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u; }
+
+// A value operand that holds infinities or NaN: what a row does not see (weight
+// 0) must not reach it, but 0 * NaN would.  The finite part, and indicators (1.0)
+// of +inf or NaN and of -inf or NaN, whose sums over the keys with weight say
+// what to add.
+__device__ __forceinline__ void split_nonfinite(u32x4 v, u32x4& fin, u32x4& up, u32x4& down) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t w = v[k];
+        const uint32_t bad = nonfinite2(w) >> 15;                                     // a 1 in a half that is not finite
+        const uint32_t nan = (((w & 0x007F007Fu) + 0x007F007Fu) >> 7) & 0x00010001u;  // whose mantissa is not zero
+        const uint32_t neg = (w >> 15) & 0x00010001u;
+        fin[k] = w & ~(bad * 0xFFFFu);
+        up[k] = (bad & (nan | ~neg)) * 0x3F80u;
+        down[k] = (bad & (nan | neg)) * 0x3F80u;
+    }
+}
+__device__ __forceinline__ u32x4 weight_mask(u32x4 p) {  // 1.0 where a probability is not zero
+    u32x4 m;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] = ((((p[k] & 0x7FFF7FFFu) + 0x7FFF7FFFu) >> 15) & 0x00010001u) * 0x3F80u;
+    return m;
+}
+__device__ __forceinline__ float add_nonfinite(float o, float up, float down) {
+    if (up > 0.0f) o += INFINITY;
+    if (down > 0.0f) o -= INFINITY;
+    return o;
+}
+
+// Masks that keep the first n (0 .. 16) of 16 codes (W = 4 words) or bf16 values (8).
+template <int W>
+__device__ __forceinline__ void token_masks(int n, uint32_t (&mk)[W]) {
+    constexpr int kPer = W == 4 ? 4 : 2;  // tokens of a word
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        const int bits = max(min(n - kPer * k, kPer), 0) * (32 / kPer);
+        mk[k] = (uint32_t)((1ull << bits) - 1);
+    }
+}
+
+// Eight output values (bf16) of a row: stored, and cast for the fused quantise.
+__device__ __forceinline__ uint32_t put8(const AttnArgs& p, bool cast, int bq, int64_t row, int64_t col, uint4 v) {
+    st16(p.o + row * p.ldo + col, v);
+    if (!p.q8) return 0u;
+    if (cast) {
+        uint2 u;
+        switch (p.qfmt) {
+            case FP8_E4M3: u = codes8<FP8_E4M3>(v, bq); break;
+            case FP8_E5M2: u = codes8<FP8_E5M2>(v, bq); break;
+            case FP8_E4_A: u = codes8<FP8_E4_A>(v, bq); break;
+            default: u = codes8<FP8_E5_A>(v, bq); break;
+        }
+        *(uint2*)(p.q8 + row * p.ldq8 + col) = u;
+    }
+    return mag8(v);
+}
+
+// ---- up to 16 packed rows
+// Wave w takes the tiles t0 + w, t0 + w + 4, ... of its workgroup.  In a tile,
+// lane (r, g) = (lane % 16, lane / 16) reads for key tile kt = 0..3 the 32 (or
+// 16) codes of dimensions 32 g .. of key 16 (r / 4) + 4 kt + r % 4: with this
+// order of the rows, the scores that lane (q, g) gets are of the 16 keys 16 g
+// + 4 kt + i, a block of the values' layout, whose codes for dimension 16 dt + r
+// it reads as one vector.  Nothing moves between lanes.
+template <int FMT, int DH>
+__global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
+    constexpr int kE = FMT == kBf16 ? 1 : FMT;
+    constexpr int kSteps = DH / 32;                    // of the contraction over d_head
+    constexpr int kKv = DH * kEsz<FMT> / 64;           // 16-byte vectors of a lane's keys
+    constexpr int kVv = kEsz<FMT>;                     // and of its values, for each of
+    constexpr int kDt = DH / 16;                       // these tiles of dimensions
+    __shared__ float so[4][kFew][DH + 4];
+    __shared__ float sm[4][kFew], sl[4][kFew];
     __shared__ uint32_t redm[kT / 64];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int bq = QUANT ? fused_bias(pred, used) : 0;
-    const int64_t item = (int64_t)blockIdx.x * (kT / 64) + w;
-    const int64_t r = item / nh;
-    const int h = (int)(item % nh), hk = h / (nh / c.nkv);
-    const int s = wave_search(c.n_seqs, r, [&](int i) { return row_at(c, i); });
+    const CacheView& c = p.c;
+    const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
+    // uniform to the compiler too: branches around matrix instructions, which
+    // do not heed the lane mask, are then scalar
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hk = blockIdx.x % c.nkv;
+    const int rest = blockIdx.x / c.nkv;
+    const int split = rest % p.splits, s = rest / p.splits;
+    const bool cast = p.q8 && p.pred;
+    const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
     const Seq sq = seq_of(c, s);
-    const bool live = r < c.rows && r >= sq.r0 && r < sq.r0 + sq.n && r - sq.r0 < max_rows;
-    uint32_t mag = 0;
-    if (live) {
-        for (int i = lane; i < DH; i += 64) qs[w][i] = lo_f(q[r * ldq + (int64_t)h * DH + i]);
+    const int m1 = min(sq.n, p.max_rows) * p.grp;
+    Range rg = range_of(p, sq, 0, max(m1, 1), split, p.splits);
+    if (m1 < 1 || m1 > kFew || (split > 0 && rg.t0 >= rg.t1)) {
+        if (p.q8 && tid == 0) p.parts[blockIdx.x] = 0u;
+        return;
+    }
+    // this lane's query (rows past the last one repeat it, and are not stored)
+    const int mq = min(r16, m1 - 1), tok = mq / p.grp;
+    const int pos = sq.p0 + tok;
+    const uint16_t* qp = p.q + (sq.r0 + tok) * p.ldq + (int64_t)(hk * p.grp + mq % p.grp) * DH;
+    u32x4 qf[kSteps];
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) qf[st] = ldg16(qp + kSteps * 8 * g + 8 * st);
+
+    const int lo = p.window > 0 ? pos - p.window : -1;  // the last key before those that the row sees
+
+    const int rb = r16 >> 2, rl = r16 & 3;  // block and place of this lane's keys
+    u32x4 kreg[4][kKv], vreg[kDt][kVv];
+    u32x4 ke4, ve4;
+    int kn, vn;  // valid keys of the two blocks (0 if the page is absent)
+    int64_t kbase, vbase;  // slots of the two blocks
+    auto where = [&](int t, int blk, int& n) {
+        const int b0 = rg.start + kTile * t + kBlk * blk;
+        const int page = b0 < rg.kend ? page_of(c, s, b0) : -1;
+        n = page >= 0 ? min(rg.kend - b0, kBlk) : 0;
+        return slot_of(c, max(page, 0), hk, b0);
+    };
+    auto load_k = [&](int t) {
+        kbase = where(t, rb, kn);
+        if (FMT != kBf16) ke4 = *(const u32x4*)(c.ke + kbase);
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int v = 0; v < kKv; ++v)
+                kreg[kt][v] = *(const u32x4*)(c.k + ((kbase + 4 * kt + rl) * DH + (DH / 4) * g) * kEsz<FMT> + 16 * v);
+    };
+    auto load_v = [&](int t) {
+        vbase = where(t, g, vn);
+        if (FMT != kBf16) ve4 = *(const u32x4*)(c.ve + vbase);
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+            for (int v = 0; v < kVv; ++v)
+                vreg[dt][v] = *(const u32x4*)(c.v + (vbase * DH + (16 * dt + r16) * kBlk) * kEsz<FMT> + 16 * v);
+    };
+
+    f4_t o[kDt];
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt) o[dt] = f4_t{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.0f;
+    int t = rg.t0 + w;
+    if (t < rg.t1) {
+        load_k(t);
+        load_v(t);
+    }
+    for (; t < rg.t1; t += 4) {
+        const bool more = t + 4 < rg.t1;  // its loads follow the last use of this tile's registers
+        const int kb = rg.start + kTile * t;
+        f4_t sc[4];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            sc[kt] = f4_t{0.f, 0.f, 0.f, 0.f};
+            const float ks = FMT == kBf16 ? 1.0f : exp_float((ke4[kt] >> (8 * rl)) & 0xFFu);
+#pragma unroll
+            for (int st = 0; st < kSteps; ++st) {
+                u32x4 kf;
+                if (FMT == kBf16) kf = kreg[kt][st];
+                else kf = cvt8b<kE>(kreg[kt][st / 2][2 * (st & 1)], kreg[kt][st / 2][2 * (st & 1) + 1], ks);
+                sc[kt] = mfma_bf16(kf, qf[st], sc[kt]);
+            }
+        }
+        if (more) load_k(t + 4);
+        const bool edge = kb + kTile - 1 > rg.first || (p.window > 0 && kb <= rg.last - p.window) || __any(vn < kBlk);
+        if (edge) {
+            // keys lo + 1 .. lo + seen are seen, of this lane's block if its page is present
+            const int seen = vn > 0 ? min(pos, rg.kend - 1) - lo : 0;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = kb + kBlk * g + 4 * kt + i;
+                    sc[kt][i] = (unsigned)(key - lo - 1) < (unsigned)max(seen, 0) ? sc[kt][i] : -INFINITY;
+                }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kt][i]);
+        mx = quad_max(mx);
+        if (__any(mx > m)) {
+            const float mn = fmaxf(m, mx);
+            const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * p.c2);
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
+        }
+        const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
+        u32x4 pf[2];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            float pr[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][i], p.c2, moff));
+                l += pr[i];
+                // an exponent of a masked slot may be anything, its weight is 0
+                if (FMT != kBf16) pr[i] *= exp_float(min((ve4[kt] >> (8 * i)) & 0xFFu, 254u));
+            }
+            pf[kt >> 1][2 * (kt & 1)] = pack_bf16x2(pr[0], pr[1]);
+            pf[kt >> 1][2 * (kt & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
+        }
+        const bool cut = edge && __any(vn < kBlk);
+        uint32_t mk[4 * kVv];  // slots that hold no token may hold NaN
+        if (cut) token_masks(vn, mk);
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt) {
+            uint32_t vw[4 * kVv];
+#pragma unroll
+            for (int k = 0; k < 4 * kVv; ++k) vw[k] = vreg[dt][k / 4][k % 4];
+            if (cut) {
+#pragma unroll
+                for (int k = 0; k < 4 * kVv; ++k) vw[k] &= mk[k];
+            }
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                u32x4 vf;
+                if (FMT == kBf16) vf = u32x4{vw[4 * st % (4 * kVv)], vw[(4 * st + 1) % (4 * kVv)], vw[(4 * st + 2) % (4 * kVv)], vw[(4 * st + 3) % (4 * kVv)]};
+                else vf = cvt8b<kE>(vw[2 * st], vw[2 * st + 1], 1.0f);
+                if (edge && __any(nonfinite2(vf[0]) | nonfinite2(vf[1]) | nonfinite2(vf[2]) | nonfinite2(vf[3]))) {
+                    u32x4 fin, up, down;
+                    split_nonfinite(vf, fin, up, down);
+                    const u32x4 wm = weight_mask(pf[st]);
+                    const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+                    const f4_t cu = mfma_bf16(up, wm, zero), cd = mfma_bf16(down, wm, zero);
+                    o[dt] = mfma_bf16(fin, pf[st], o[dt]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[dt][i] = add_nonfinite(o[dt][i], cu[i], cd[i]);
+                } else {
+                    o[dt] = mfma_bf16(vf, pf[st], o[dt]);
+                }
+            }
+        }
+        if (more) load_v(t + 4);
+    }
+    l = quad_sum(l);
+    // join the four waves
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt) *(f4_t*)&so[w][r16][16 * dt + 4 * g] = o[dt];
+    if (g == 0) {
+        sm[w][r16] = m;
+        sl[w][r16] = l;
     }
     __syncthreads();
-    if (live) {
-        const int64_t p = (int64_t)sq.p0 + (r - sq.r0);
-        const int64_t kend = min(p + 1, (int64_t)sq.len);
-        const int64_t klo = window > 0 ? max(p - window + 1, (int64_t)0) : 0;
-        const float scale = 1.4426950408889634f / sqrtf((float)DH);
-        float m = -INFINITY, l = 0.0f, acc[kPer];
-        for (int i = 0; i < kPer; ++i) acc[i] = 0.0f;
-        for (int64_t k0 = klo & ~(int64_t)63; k0 < kend; k0 += 64) {
-            const int64_t key = k0 + lane;
-            const int page = key >= klo && key < kend ? page_of(c, s, (int)key) : -1;
-            const int64_t slot = page >= 0 ? slot_of(c, page, hk, (int)key) : 0;
-            float sc = 0.0f, vs = 1.0f;
-            if (page >= 0) {
-                for (int d = 0; d < DH; d += 4) {
-                    float f[4];
-                    if (FMT == kBf16) {
-                        const uint2 u = *(const uint2*)((const uint16_t*)c.k + slot * DH + d);
-                        f[0] = lo_f(u.x); f[1] = hi_f(u.x); f[2] = lo_f(u.y); f[3] = hi_f(u.y);
-                    } else {
-                        decode4<kE>(*(const uint32_t*)(c.k + slot * DH + d), f);
-                    }
-                    for (int e = 0; e < 4; ++e) sc += f[e] * qs[w][d + e];
-                }
-                if (FMT != kBf16) {
-                    sc *= unscale_of(c.ke[slot]);
-                    vs = unscale_of(c.ve[slot]);
-                }
-            }
-            const float x = page >= 0 ? sc * scale : -INFINITY;
-            float mx = x;
-            for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
-            const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.0f : mn;
-            const float alpha = exp2f(m - ref);
-            const float pr = page >= 0 ? exp2f(x - ref) : 0.0f;
-            l = l * alpha + wave_sum(pr);
-            m = mn;
-            const float pv = pr * vs;
-            for (int i = 0; i < kPer; ++i) acc[i] *= alpha;
-            for (int k = 0; k < 64; ++k) {
-                const int pg = __shfl(page, k, 64);
-                if (pg < 0) continue;
-                const int64_t sl = slot_of(c, pg, hk, (int)(k0 + k));
-                const float pk = __shfl(pv, k, 64);
-                const int64_t vb = (sl & ~(int64_t)15) * DH + (sl & 15);
-                for (int i = 0; i < kPer; ++i) {
-                    const int64_t at = vb + (int64_t)(lane * kPer + i) * kBlk;
-                    const float v = FMT == kBf16 ? lo_f(((const uint16_t*)c.v)[at]) : decode<kE, 0>(c.v[at]);
-                    acc[i] += pk * v;
-                }
-            }
+    uint32_t mag = 0;
+    constexpr int kCh = DH / 8;
+    for (int i = tid; i < m1 * kCh; i += kT) {
+        const int row = i / kCh, ch = i % kCh;
+        float mm = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mm = fmaxf(mm, sm[k][row]);
+        float acc[8], ll = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = sm[k][row] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sm[k][row] - mm) * p.c2);
+            if (f == 0.0f && sl[k][row] == 0.0f) continue;
+            ll += f * sl[k][row];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += f * so[k][row][8 * ch + e];
         }
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        for (int i = 0; i < kPer; ++i) {
-            const uint32_t u = pack_bf16x2(acc[i] * inv, 0.0f) & 0xFFFFu;
-            const int64_t col = (int64_t)h * DH + lane * kPer + i;
-            o[r * ldo + col] = (uint16_t)u;
-            if (QUANT) {
-                mag = max(mag, u & 0x7FFFu);
-                if (pred) q8[r * ldq8 + col] = (uint8_t)codes8<QF>(make_uint4(u, 0u, 0u, 0u), bq).x;
-            }
+        const int64_t grow = sq.r0 + row / p.grp;
+        const int head = hk * p.grp + row % p.grp;
+        if (p.splits > 1) {
+            const int64_t at = ((int64_t)split * c.rows + grow) * p.nh + head;
+            if (ch == 0) p.part_ml[at] = make_float2(mm, ll);
+            float* d = p.part_o + at * DH + 8 * ch;
+            *(float4*)d = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            *(float4*)(d + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        } else {
+            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+            const uint4 v = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
+                                       pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
+            mag = max(mag, put8(p, cast, bq, grow, (int64_t)head * DH + 8 * ch, v));
         }
     }
-    if (QUANT) {
+    if (p.q8) {
         const uint32_t bm = block_max(mag, redm);
-        if (threadIdx.x == 0) parts[blockIdx.x] = bm;
+        if (tid == 0) p.parts[blockIdx.x] = bm;
+    }
+}
+
+// ---- tiles of 128 packed rows
+// Wave w owns packed rows 32 w .. 32 w + 31 of the tile, one per lane pair (the
+// queries stay in registers).  Tiles of 64 keys are double-buffered in LDS as
+// bf16: wave w brings in the 16 keys of block w, converts the codes on the way
+// (once for the four waves) and loads the tile after next meanwhile.
+//   K: rows of one key, 16-byte chunk c at c ^ (key mod 16 or 8);
+//   V: rows of one dimension, 64 keys each, a block's keys in the order 0-3,
+//      8-11, 4-7, 12-15 that the scores' registers have; chunk c at
+//      c ^ (d / 2 mod 8).  Any 16 rows of one chunk then cover the 64 banks.
+// Score register i of lane (q, h) is key 8 (i / 4) + 4 h + i % 4 of 32.
+template <int FMT, int DH>
+__global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
+    constexpr int kE = FMT == kBf16 ? 1 : FMT;
+    constexpr int kSteps = DH / 16;                       // of the contraction over d_head
+    constexpr int kDt = DH / 32;                          // tiles of dimensions
+    constexpr int kKb = kTile * DH * 2;                   // bytes of K (and of V) in LDS
+    constexpr int kKmask = DH / 8 - 1;                    // chunks of a key row, less one
+    constexpr int kKv = DH * kEsz<FMT> / 64;              // 16-byte vectors of keys a lane brings in
+    constexpr int kVd = DH / 64;                          // dimensions whose values it brings in
+    constexpr int kVv = kEsz<FMT>;                        // vectors of each
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kKb];  // K0 V0 K1 V1; output staging
+    __shared__ __attribute__((aligned(16))) float vsc[2][kTile];   // 2^(exp - 127) of the values
+    __shared__ __attribute__((aligned(16))) int info[2][4];        // valid keys of a block | nonfinite values << 8
+    __shared__ uint32_t redm[kT / 64];
+    const CacheView& c = p.c;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, h = lane >> 5;
+    const int hk = blockIdx.x % c.nkv;
+    int rest = blockIdx.x / c.nkv;
+    const int split = rest % p.splits;
+    rest = (int)(gridDim.x / (c.nkv * p.splits)) - 1 - rest / p.splits;  // the last rows, with the longest ranges, first
+    // tile slots: as many for each sequence as cu_rows[s + 1] / kMany + 1 - cu_rows[s] / kMany in packed rows
+    const int s = wave_search(c.n_seqs, rest, [&](int i) { return row_at(c, i) * p.grp / kMany + i; });
+    const Seq sq = seq_of(c, s);
+    const int m0 = (int)(rest - (sq.r0 * p.grp / kMany + s)) * kMany;
+    const int mtot = min(sq.n, p.max_rows) * p.grp;
+    const bool cast = p.q8 && p.pred;
+    const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
+    const int m1 = min(m0 + kMany, mtot);
+    const Range rg = range_of(p, sq, min(m0, mtot), max(m1, 1), split, p.splits);
+    if (m0 >= mtot || (p.few_on && mtot <= kFew) || (split > 0 && rg.t0 >= rg.t1)) {
+        if (p.q8 && tid == 0) p.parts[blockIdx.x] = 0u;
+        return;
+    }
+    const int mq = min(m0 + 32 * w + l32, m1 - 1), tok = mq / p.grp;
+    const int pos = sq.p0 + tok;
+    const uint16_t* qp = p.q + (sq.r0 + tok) * p.ldq + (int64_t)(hk * p.grp + mq % p.grp) * DH;
+    u32x4 qf[kSteps];
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks) qf[ks] = ldg16(qp + 16 * ks + 8 * h);
+
+    const int lo = p.window > 0 ? pos - p.window : -1;  // the last key before those that the row sees
+    const int seen = max(min(pos, rg.kend - 1) - lo, 0);
+
+    // this wave's block of a tile: raw codes on their way to LDS
+    u32x4 kraw[kKv], vraw[kVd][kVv];
+    uint32_t ke = 0, ve = 0;
+    int nval = 0;
+    auto page_at = [&](int t) {
+        const int b0 = rg.start + kTile * t + kBlk * w;
+        return b0 < rg.kend ? page_of(c, s, b0) : -1;
+    };
+    auto load = [&](int t, int page) {
+        const int b0 = rg.start + kTile * t + kBlk * w;
+        nval = page >= 0 ? min(rg.kend - b0, kBlk) : 0;
+        const int64_t slot = slot_of(c, max(page, 0), hk, b0);
+        const uint8_t* kp = c.k + (slot + (lane >> 2)) * (DH * kEsz<FMT>) + (lane & 3) * (DH / 4) * kEsz<FMT>;
+#pragma unroll
+        for (int v = 0; v < kKv; ++v) kraw[v] = *(const u32x4*)(kp + 16 * v);
+#pragma unroll
+        for (int d = 0; d < kVd; ++d)
+#pragma unroll
+            for (int v = 0; v < kVv; ++v)
+                vraw[d][v] = *(const u32x4*)(c.v + (slot * DH + (lane + 64 * d) * kBlk) * kEsz<FMT> + 16 * v);
+        if (FMT != kBf16) {
+            ke = c.ke[slot + (lane >> 2)];
+            ve = c.ve[slot + (lane & 15)];
+        }
+    };
+    auto store = [&](int buf) {
+        uint8_t* Kl = lds + buf * 2 * kKb;
+        uint8_t* Vl = Kl + kKb;
+        const int key = kBlk * w + (lane >> 2);
+#pragma unroll
+        for (int j = 0; j < DH / 32; ++j) {
+            u32x4 x;
+            if (FMT == kBf16) x = kraw[j % kKv];
+            else x = cvt8b<kE>(kraw[j / 2 % kKv][2 * (j & 1)], kraw[j / 2 % kKv][2 * (j & 1) + 1], exp_float(ke));
+            const int ch = (lane & 3) * (DH / 32) + j;
+            *(u32x4*)(Kl + key * DH * 2 + ((ch ^ (key & kKmask)) << 4)) = x;
+        }
+        bool bad = false;
+#pragma unroll
+        for (int d = 0; d < kVd; ++d) {
+            uint32_t vw[4 * kVv];
+#pragma unroll
+            for (int k = 0; k < 4 * kVv; ++k) vw[k] = vraw[d][k / 4][k % 4];
+            if (nval < kBlk) {  // slots that hold no token may hold NaN
+                uint32_t mk[4 * kVv];
+                token_masks(nval, mk);
+#pragma unroll
+                for (int k = 0; k < 4 * kVv; ++k) vw[k] &= mk[k];
+            }
+            u32x4 x[2];
+            if (FMT == kBf16) {
+                constexpr int kM = 4 * kVv - 1;
+                x[0] = u32x4{vw[0], vw[1], vw[4 & kM], vw[5 & kM]};
+                x[1] = u32x4{vw[2], vw[3], vw[6 & kM], vw[7 & kM]};
+                uint32_t any = 0;
+#pragma unroll
+                for (int k = 0; k < 4 * kVv; ++k) any |= nonfinite2(vw[k]);
+                bad |= any != 0;
+            } else {
+                x[0] = cvt8b<kE>(vw[0], vw[2], 1.0f);
+                x[1] = cvt8b<kE>(vw[1], vw[3], 1.0f);
+                constexpr uint32_t kOne = kE == FP8_E5M2 ? 0x04040404u : 0x01010101u;
+                uint32_t any = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) any |= (vw[k] & 0x7F7F7F7Fu) + kOne;
+                bad |= (any & 0x80808080u) != 0;
+            }
+            const int dim = lane + 64 * d;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                *(u32x4*)(Vl + dim * (kTile * 2) + (((2 * w + e) ^ ((dim >> 1) & 7)) << 4)) = x[e];
+        }
+        const uint64_t anybad = __ballot(bad);
+        if (lane < kBlk) vsc[buf][kBlk * w + lane] = lane < nval ? exp_float(ve) : 0.0f;
+        if (lane == 0) info[buf][w] = nval | (anybad ? 256 : 0);
+    };
+
+    f16_t o[kDt];
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+    const float lazy = 8.0f / p.c2;
+
+    if (rg.t0 < rg.t1) {
+        int page = page_at(rg.t0);
+        load(rg.t0, page);
+        page = page_at(min(rg.t0 + 1, rg.t1 - 1));
+        store(0);
+        load(min(rg.t0 + 1, rg.t1 - 1), page);
+        page = page_at(min(rg.t0 + 2, rg.t1 - 1));
+        __syncthreads();
+        for (int t = rg.t0; t < rg.t1; ++t) {
+            const int buf = (t - rg.t0) & 1;
+            // the next tile into the other buffer, which every wave has finished
+            // reading; after the last tile it is written once more for nothing
+            store(buf ^ 1);
+            load(min(t + 2, rg.t1 - 1), page);
+            page = page_at(min(t + 3, rg.t1 - 1));
+            const uint8_t* Kl = lds + buf * 2 * kKb;
+            const uint8_t* Vl = Kl + kKb;
+            f16_t sc[2];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[kt][i] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    const int key = 32 * kt + l32;
+                    const u32x4 kf = *(const u32x4*)(Kl + key * DH * 2 + (((2 * ks + h) ^ (key & kKmask)) << 4));
+                    sc[kt] = mfma32(kf, qf[ks], sc[kt]);
+                }
+            const int4 in4 = *(const int4*)info[buf];
+            const int in[4] = {__builtin_amdgcn_readfirstlane(in4.x), __builtin_amdgcn_readfirstlane(in4.y),
+                               __builtin_amdgcn_readfirstlane(in4.z), __builtin_amdgcn_readfirstlane(in4.w)};
+            const int kb = rg.start + kTile * t;
+            const bool full = ((in[0] & in[1] & in[2] & in[3]) & kBlk) != 0;
+            if (!full || kb + kTile - 1 > rg.first || (p.window > 0 && kb <= rg.last - p.window)) {
+                // keys lo + 1 .. lo + seen are seen, of blocks whose page is present
+                const int from = kb + 4 * h - lo - 1;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const unsigned n = (in[b] & 255) ? seen : 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int at = 8 * (b & 1) + i;
+                        const bool see = (unsigned)(from + 16 * b + 8 * (i >> 2) + (i & 3)) < n;
+                        sc[b >> 1][at] = see ? sc[b >> 1][at] : -INFINITY;
+                    }
+                }
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kt][i]);
+            {
+                const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+            }
+            // the exponent offset moves only when a score exceeds it by 2^8 in
+            // probability: rarely, and never by more than what fp32 and bf16 hold
+            const bool grow = mx > m + lazy;
+            if (__any(grow)) {
+                const float mn = grow ? mx : m;
+                const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * p.c2);
+                m = mn;
+                l *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
+            }
+            const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
+            u32x4 pf[4];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    float pr[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][4 * q4 + i], p.c2, moff));
+                        l += pr[i];
+                    }
+                    if (FMT != kBf16) {
+                        const f4_t vs = *(const f4_t*)&vsc[buf][32 * kt + 8 * q4 + 4 * h];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) pr[i] *= vs[i];
+                    }
+                    pf[2 * kt + (q4 >> 1)][2 * (q4 & 1)] = pack_bf16x2(pr[0], pr[1]);
+                    pf[2 * kt + (q4 >> 1)][2 * (q4 & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
+                }
+            auto vfrag = [&](int dt, int b) {
+                const int dim = 32 * dt + l32;
+                return *(const u32x4*)(Vl + dim * (kTile * 2) + (((2 * b + h) ^ ((dim >> 1) & 7)) << 4));
+            };
+            if (__builtin_expect(((in[0] | in[1] | in[2] | in[3]) & 256) == 0, 1)) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int dt = 0; dt < kDt; ++dt) o[dt] = mfma32(vfrag(dt, b), pf[b], o[dt]);
+            } else {
+                // one operand at a time, in a loop that is not unrolled: this
+                // path is not to cost the other one registers
+#pragma unroll 1
+                for (int b = 0; b < 4; ++b) {
+                    const u32x4 wm = weight_mask(pf[0]);
+#pragma unroll
+                    for (int dt = 0; dt < kDt; ++dt) {
+                        u32x4 fin, up, down;
+                        split_nonfinite(vfrag(dt, b), fin, up, down);
+                        o[dt] = mfma32(fin, pf[0], o[dt]);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int sgn = 0; sgn < 2; ++sgn) {
+                            f16_t cnt;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) cnt[i] = 0.0f;
+                            cnt = mfma32(sgn ? down : up, wm, cnt);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[dt][i] += cnt[i] > 0.0f ? (sgn ? -INFINITY : INFINITY) : 0.0f;
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                    pf[0] = pf[1];
+                    pf[1] = pf[2];
+                    pf[2] = pf[3];
+                }
+            }
+            __syncthreads();
+        }
+    }
+    {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    }
+    if (p.splits > 1) {
+        if (m0 + 32 * w + l32 < m1) {
+            const int64_t at = ((int64_t)split * c.rows + sq.r0 + tok) * p.nh + hk * p.grp + mq % p.grp;
+            if (h == 0) p.part_ml[at] = make_float2(m, l);
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4)
+                    *(float4*)(p.part_o + at * DH + 32 * dt + 8 * q4 + 4 * h) =
+                        make_float4(o[dt][4 * q4], o[dt][4 * q4 + 1], o[dt][4 * q4 + 2], o[dt][4 * q4 + 3]);
+        }
+        if (p.q8 && tid == 0) p.parts[blockIdx.x] = 0u;
+        return;
+    }
+    // rows of this head's d_head values through LDS (16-byte chunk c of row r at c ^ r)
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int rl = 32 * w + l32;
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const int ch = 4 * dt + q4;
+            *(uint2*)(lds + rl * DH * 2 + ((ch ^ (rl & kKmask)) << 4) + 8 * h) =
+                make_uint2(pack_bf16x2(o[dt][4 * q4] * inv, o[dt][4 * q4 + 1] * inv),
+                           pack_bf16x2(o[dt][4 * q4 + 2] * inv, o[dt][4 * q4 + 3] * inv));
+        }
+    __syncthreads();
+    uint32_t mag = 0;
+    constexpr int kCh = DH / 8;
+    for (int i = tid; i < (m1 - m0) * kCh; i += kT) {
+        const int row = i / kCh, ch = i % kCh, mm = m0 + row;
+        const uint4 v = *(const uint4*)(lds + row * DH * 2 + ((ch ^ (row & kKmask)) << 4));
+        mag = max(mag, put8(p, cast, bq, sq.r0 + mm / p.grp, (int64_t)(hk * p.grp + mm % p.grp) * DH + 8 * ch, v));
+    }
+    if (p.q8) {
+        const uint32_t bm = block_max(mag, redm);
+        if (tid == 0) p.parts[blockIdx.x] = bm;
+    }
+}
+
+// ---- join of the key ranges of one (row, head) by DH / 8 lanes
+template <int DH>
+__global__ __launch_bounds__(kT) void combine_kernel(AttnArgs p) {
+    constexpr int kCh = DH / 8;
+    __shared__ uint32_t redm[kT / 64];
+    const CacheView& c = p.c;
+    const bool cast = p.q8 && p.pred;
+    const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
+    const int64_t first = (int64_t)blockIdx.x * (kT / kCh);
+    const int64_t item = first + threadIdx.x / kCh;
+    const int ch = threadIdx.x % kCh;
+    const int64_t r = item / p.nh;
+    const int head = (int)(item % p.nh);
+    uint32_t mag = 0;
+    // a workgroup's items can lie in two sequences or more: search for each row
+    int s = wave_search(c.n_seqs, min(first / p.nh, c.rows - 1), [&](int i) { return row_at(c, i); });
+    while (s + 1 < c.n_seqs && row_at(c, s + 1) <= r) ++s;
+    const Seq sq = seq_of(c, s);
+    const int i = (int)(r - sq.r0);
+    if (r < c.rows && i >= 0 && i < min(sq.n, p.max_rows)) {
+        const int mtot = min(sq.n, p.max_rows) * p.grp;
+        const bool few = p.few_on && mtot <= kFew;
+        const int n = few ? p.few_splits : p.many_splits;
+        if (n > 1) {
+            const int mm = i * p.grp + head % p.grp, m0 = few ? 0 : mm / kMany * kMany;
+            const Range rg = range_of(p, sq, m0, few ? mtot : min(m0 + kMany, mtot), 0, n);
+            const int64_t step = c.rows * p.nh, at = r * p.nh + head;
+            float top = -INFINITY;
+            for (int k = 0; k < rg.live; ++k) top = fmaxf(top, p.part_ml[k * step + at].x);
+            float acc[8], ll = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+            for (int k = 0; k < rg.live; ++k) {
+                const float2 ml = p.part_ml[k * step + at];
+                const float* d = p.part_o + (k * step + at) * DH + 8 * ch;
+                const float4 x = *(const float4*)d, y = *(const float4*)(d + 4);
+                if (ml.x == -INFINITY && ml.y == 0.0f) continue;
+                const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml.x - top) * p.c2);
+                ll += f * ml.y;
+                acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
+                acc[4] += f * y.x; acc[5] += f * y.y; acc[6] += f * y.z; acc[7] += f * y.w;
+            }
+            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+            const uint4 v = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
+                                       pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
+            mag = put8(p, cast, bq, r, (int64_t)head * DH + 8 * ch, v);
+        }
+    }
+    if (p.q8) {
+        const uint32_t bm = block_max(mag, redm);
+        if (threadIdx.x == 0) p.parts[blockIdx.x] = bm;
     }
 }
 
@@ -499,38 +1146,99 @@ int32_t launch_cache_read(const CacheView& c, int fmt, int d_head, uint16_t* k, 
     return hip_status();
 }
 
+namespace {
+// How a call is split over workgroups, from its sizes alone.
+struct Plan {
+    bool few, many;            // which kernels run
+    int few_splits, many_splits;
+    int64_t few_wg, many_wg, join_wg;
+    int64_t parts, words, ws_bytes;
+};
+Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t max_rows, int64_t max_len) {
+    Plan p;
+    const int64_t grp = nh / nkv, cap = max_rows < rows ? max_rows : rows;
+    p.many = cap * grp > kFew;
+    // sequences of one length have no single tokens among them
+    p.few = !p.many || (grp <= kFew && n_seqs > 1 && rows < n_seqs * max_rows);
+    // Enough workgroups for two on each compute unit, each with at least 512
+    // keys of the longest sequence.
+    auto splits = [&](int64_t wg) {
+        const int64_t want = (kWant + wg - 1) / wg, most = (max_len + kLeast - 1) / kLeast;
+        const int64_t n = want < most ? want : most;
+        return (int)(n < 1 ? 1 : n);
+    };
+    const int64_t few = n_seqs * nkv, many = (rows * grp / kMany + n_seqs) * nkv;
+    p.few_splits = p.few ? splits(few) : 1;
+    p.many_splits = p.many ? splits(many) : 1;
+    p.few_wg = p.few ? few * p.few_splits : 0;
+    p.many_wg = p.many ? many * p.many_splits : 0;
+    const int most = p.few_splits > p.many_splits ? p.few_splits : p.many_splits;
+    const int64_t items = rows * nh, per = kT / (d_head / 8);
+    p.join_wg = most > 1 ? (items + per - 1) / per : 0;
+    p.parts = p.few_wg + p.many_wg + p.join_wg;
+    p.words = (1 + p.parts + 3) & ~(int64_t)3;
+    p.ws_bytes = 4 * p.words + (most > 1 ? most * items * (4 * (int64_t)d_head + 8) : 0);
+    return p;
+}
+}  // namespace
+
 CacheAttnPlan cache_attn_plan(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t max_rows,
                               int64_t max_len) {
-    CacheAttnPlan p;
-    p.parts = (rows * nh + kT / 64 - 1) / (kT / 64);
-    p.ws_bytes = (1 + p.parts) * (int64_t)sizeof(uint32_t);
-    return p;
+    const Plan p = plan_of(rows, nh, nkv, d_head, n_seqs, max_rows, max_len);
+    return CacheAttnPlan{p.parts, p.ws_bytes};
 }
 
 int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const CacheView& c, int fmt, int d_head,
                                int64_t max_rows, int64_t window, uint16_t* o, int64_t ldo, const FusedQuant* fq,
                                void* ws, hipStream_t s) {
     const bool quant = fq && fq->q;
-    const CacheAttnPlan p = cache_attn_plan(c.rows, nh, c.nkv, d_head, c.n_seqs, max_rows,
-                                            (int64_t)c.max_pages << c.page_shift);
+    const Plan pl = plan_of(c.rows, nh, c.nkv, d_head, c.n_seqs, max_rows, (int64_t)c.max_pages << c.page_shift);
+    const int most = pl.few_splits > pl.many_splits ? pl.few_splits : pl.many_splits;
     uint32_t* words = (uint32_t*)ws;
+    AttnArgs a;
+    a.c = c;
+    a.q = q;
+    a.ldq = ldq;
+    a.nh = nh;
+    a.grp = nh / c.nkv;
+    a.max_rows = (int)(max_rows < c.rows ? max_rows : c.rows);
+    a.window = (int)(window < ((int64_t)1 << 30) ? window : 0);  // beyond any position: none
+    a.few_on = pl.few;
+    a.few_splits = pl.few_splits;
+    a.many_splits = pl.many_splits;
+    a.c2 = (float)(1.4426950408889634 / sqrt((double)d_head));
+    a.o = o;
+    a.ldo = ldo;
+    a.pred = quant ? fq->pred : nullptr;
+    a.used = quant ? (int32_t*)words : nullptr;
+    a.q8 = quant ? fq->q : nullptr;
+    a.ldq8 = quant ? fq->ldq : 0;
+    a.qfmt = quant ? fq->fmt : FP8_E4M3;
+    a.part_o = (float*)(words + pl.words);
+    a.part_ml = (float2*)(a.part_o + (int64_t)most * c.rows * nh * d_head);
     with_cache(fmt, d_head, [&](auto F, auto D) {
-        with_fmt(quant ? fq->fmt : FP8_E4M3, [&](auto QF) {
-            constexpr int kF = decltype(F)::value, kD = decltype(D)::value, kQ = decltype(QF)::value;
-            if (quant)
-                hipLaunchKernelGGL((attn_kernel<kF, kD, true, kQ>), dim3((unsigned)p.parts), dim3(kT), 0, s, c, q, ldq,
-                                   nh, max_rows, window, o, ldo, fq->pred, (int32_t*)words, words + 1, fq->q, fq->ldq);
-            else
-                hipLaunchKernelGGL((attn_kernel<kF, kD, false, kQ>), dim3((unsigned)p.parts), dim3(kT), 0, s, c, q, ldq,
-                                   nh, max_rows, window, o, ldo, nullptr, nullptr, nullptr, nullptr, (int64_t)0);
-        });
+        constexpr int kF = decltype(F)::value, kD = decltype(D)::value;
+        if (pl.many) {
+            a.splits = pl.many_splits;
+            a.parts = words + 1 + pl.few_wg;
+            hipLaunchKernelGGL((many_kernel<kF, kD>), dim3((unsigned)pl.many_wg), dim3(kT), 0, s, a);
+        }
+        if (pl.few) {
+            a.splits = pl.few_splits;
+            a.parts = words + 1;
+            hipLaunchKernelGGL((few_kernel<kF, kD>), dim3((unsigned)pl.few_wg), dim3(kT), 0, s, a);
+        }
+        if (pl.join_wg) {
+            a.parts = words + 1 + pl.few_wg + pl.many_wg;
+            hipLaunchKernelGGL((combine_kernel<kD>), dim3((unsigned)pl.join_wg), dim3(kT), 0, s, a);
+        }
     });
     int32_t st = hip_status();
     if (st == FP8_OK && quant) {
         const int64_t cols = (int64_t)nh * d_head;
         with_fmt(fq->fmt, [&](auto QF) {
             hipLaunchKernelGGL((quant_finish_kernel<decltype(QF)::value>), dim3((unsigned)(c.rows < 512 ? c.rows : 512)),
-                               dim3(kT), 0, s, c, o, cols, ldo, max_rows, fq->margin, words, (int)p.parts, fq->bias,
+                               dim3(kT), 0, s, c, o, cols, ldo, max_rows, fq->margin, words, (int)pl.parts, fq->bias,
                                fq->amax_bits, fq->flags, fq->q, fq->ldq);
         });
         st = hip_status();
