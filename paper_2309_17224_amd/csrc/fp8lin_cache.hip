@@ -431,8 +431,8 @@ __device__ __forceinline__ uint32_t nonfinite2(uint32_t w) { return ((w & 0x7FFF
 
 // A value operand that holds infinities or NaN: what a row does not see (weight
 // 0) must not reach it, but 0 * NaN would.  The finite part, and indicators (1.0)
-// of +inf or NaN and of -inf or NaN, whose sums over the keys with weight say
-// what to add.
+// of +inf or NaN and of -inf or NaN, whose sums over the keys that a row sees say
+// whether to add +inf and -inf (both: NaN).
 __device__ __forceinline__ void split_nonfinite(u32x4 v, u32x4& fin, u32x4& up, u32x4& down) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -445,10 +445,11 @@ __device__ __forceinline__ void split_nonfinite(u32x4 v, u32x4& fin, u32x4& up, 
         down[k] = (bad & (nan | neg)) * 0x3F80u;
     }
 }
-__device__ __forceinline__ u32x4 weight_mask(u32x4 p) {  // 1.0 where a probability is not zero
+// 1.0 for each of eight keys whose bit is set.
+__device__ __forceinline__ u32x4 ones_where(uint32_t bits) {
     u32x4 m;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) m[k] = ((((p[k] & 0x7FFF7FFFu) + 0x7FFF7FFFu) >> 15) & 0x00010001u) * 0x3F80u;
+    for (int k = 0; k < 4; ++k) m[k] = ((bits >> (2 * k)) & 1u) * 0x3F80u + ((bits >> (2 * k + 1)) & 1u) * 0x3F800000u;
     return m;
 }
 __device__ __forceinline__ float add_nonfinite(float o, float up, float down) {
@@ -585,17 +586,18 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
             }
         }
         if (more) load_k(t + 4);
+        uint32_t sees = 0xFFFFu;  // bit i: key i of this lane's block
         const bool edge = kb + kTile - 1 > rg.first || (p.window > 0 && kb <= rg.last - p.window) || __any(vn < kBlk);
         if (edge) {
             // keys lo + 1 .. lo + seen are seen, of this lane's block if its page is present
-            const int seen = vn > 0 ? min(pos, rg.kend - 1) - lo : 0;
+            const int seen = vn > 0 ? max(min(pos, rg.kend - 1) - lo, 0) : 0, from = kb + kBlk * g - lo - 1;
+            sees = 0;
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = kb + kBlk * g + 4 * kt + i;
-                    sc[kt][i] = (unsigned)(key - lo - 1) < (unsigned)max(seen, 0) ? sc[kt][i] : -INFINITY;
-                }
+            for (int i = 0; i < 16; ++i) {
+                const bool see = (unsigned)(from + i) < (unsigned)seen;
+                sc[i >> 2][i & 3] = see ? sc[i >> 2][i & 3] : -INFINITY;
+                sees |= see ? 1u << i : 0u;
+            }
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -646,7 +648,7 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
                 if (edge && __any(nonfinite2(vf[0]) | nonfinite2(vf[1]) | nonfinite2(vf[2]) | nonfinite2(vf[3]))) {
                     u32x4 fin, up, down;
                     split_nonfinite(vf, fin, up, down);
-                    const u32x4 wm = weight_mask(pf[st]);
+                    const u32x4 wm = ones_where(sees >> (8 * st));
                     const f4_t zero = {0.f, 0.f, 0.f, 0.f};
                     const f4_t cu = mfma_bf16(up, wm, zero), cd = mfma_bf16(down, wm, zero);
                     o[dt] = mfma_bf16(fin, pf[st], o[dt]);
@@ -729,7 +731,8 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
     constexpr int kVv = kEsz<FMT>;                        // vectors of each
     __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kKb];  // K0 V0 K1 V1; output staging
     __shared__ __attribute__((aligned(16))) float vsc[2][kTile];   // 2^(exp - 127) of the values
-    __shared__ __attribute__((aligned(16))) int info[2][4];        // valid keys of a block | nonfinite values << 8
+    __shared__ __attribute__((aligned(16))) int info[2][4];        // valid keys of a block
+    __shared__ int hidden;                                         // values were left to the second sweep
     __shared__ uint32_t redm[kT / 64];
     const CacheView& c = p.c;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -786,7 +789,8 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
             ve = c.ve[slot + (lane & 15)];
         }
     };
-    auto store = [&](int buf) {
+    // finite: without infinities and NaN among the values
+    auto store = [&](int buf, auto finite) {
         uint8_t* Kl = lds + buf * 2 * kKb;
         uint8_t* Vl = Kl + kKb;
         const int key = kBlk * w + (lane >> 2);
@@ -798,44 +802,54 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
             const int ch = (lane & 3) * (DH / 32) + j;
             *(u32x4*)(Kl + key * DH * 2 + ((ch ^ (key & kKmask)) << 4)) = x;
         }
-        bool bad = false;
+        const int n = nval;
+        if (n < kBlk) {  // slots that hold no token may hold NaN
+            uint32_t mk[4 * kVv];
+            token_masks(n, mk);
+#pragma unroll
+            for (int d = 0; d < kVd; ++d)
+#pragma unroll
+                for (int k = 0; k < 4 * kVv; ++k) vraw[d][k / 4][k % 4] &= mk[k];
+        }
+        if constexpr (finite) {
+            // a 1 in the top bit of each value that is not
+            auto nf = [](uint32_t x) {
+                return FMT == kBf16 ? nonfinite2(x) : ((x & 0x7F7F7F7Fu) + (kE == FP8_E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u;
+            };
+            uint32_t any = 0;
+#pragma unroll
+            for (int d = 0; d < kVd; ++d)
+#pragma unroll
+                for (int k = 0; k < 4 * kVv; ++k) any |= nf(vraw[d][k / 4][k % 4]);
+            if (__builtin_expect(__any(any), 0)) {
+                hidden = 1;
+#pragma unroll
+                for (int d = 0; d < kVd; ++d)
+#pragma unroll
+                    for (int k = 0; k < 4 * kVv; ++k) {
+                        const uint32_t x = vraw[d][k / 4][k % 4];
+                        vraw[d][k / 4][k % 4] = x & ~((nf(x) >> (FMT == kBf16 ? 15 : 7)) * (FMT == kBf16 ? 0xFFFFu : 0xFFu));
+                    }
+            }
+        }
 #pragma unroll
         for (int d = 0; d < kVd; ++d) {
-            uint32_t vw[4 * kVv];
-#pragma unroll
-            for (int k = 0; k < 4 * kVv; ++k) vw[k] = vraw[d][k / 4][k % 4];
-            if (nval < kBlk) {  // slots that hold no token may hold NaN
-                uint32_t mk[4 * kVv];
-                token_masks(nval, mk);
-#pragma unroll
-                for (int k = 0; k < 4 * kVv; ++k) vw[k] &= mk[k];
-            }
             u32x4 x[2];
+            const u32x4 v0 = vraw[d][0], v1 = vraw[d][kVv - 1];
             if (FMT == kBf16) {
-                constexpr int kM = 4 * kVv - 1;
-                x[0] = u32x4{vw[0], vw[1], vw[4 & kM], vw[5 & kM]};
-                x[1] = u32x4{vw[2], vw[3], vw[6 & kM], vw[7 & kM]};
-                uint32_t any = 0;
-#pragma unroll
-                for (int k = 0; k < 4 * kVv; ++k) any |= nonfinite2(vw[k]);
-                bad |= any != 0;
+                x[0] = u32x4{v0[0], v0[1], v1[0], v1[1]};
+                x[1] = u32x4{v0[2], v0[3], v1[2], v1[3]};
             } else {
-                x[0] = cvt8b<kE>(vw[0], vw[2], 1.0f);
-                x[1] = cvt8b<kE>(vw[1], vw[3], 1.0f);
-                constexpr uint32_t kOne = kE == FP8_E5M2 ? 0x04040404u : 0x01010101u;
-                uint32_t any = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) any |= (vw[k] & 0x7F7F7F7Fu) + kOne;
-                bad |= (any & 0x80808080u) != 0;
+                x[0] = cvt8b<kE>(v0[0], v0[2], 1.0f);
+                x[1] = cvt8b<kE>(v0[1], v0[3], 1.0f);
             }
             const int dim = lane + 64 * d;
 #pragma unroll
             for (int e = 0; e < 2; ++e)
                 *(u32x4*)(Vl + dim * (kTile * 2) + (((2 * w + e) ^ ((dim >> 1) & 7)) << 4)) = x[e];
         }
-        const uint64_t anybad = __ballot(bad);
-        if (lane < kBlk) vsc[buf][kBlk * w + lane] = lane < nval ? exp_float(ve) : 0.0f;
-        if (lane == 0) info[buf][w] = nval | (anybad ? 256 : 0);
+        if (FMT != kBf16 && lane < kBlk) vsc[buf][kBlk * w + lane] = lane < n ? exp_float(ve) : 0.0f;
+        if (lane == 0) info[buf][w] = n;
     };
 
     f16_t o[kDt];
@@ -846,11 +860,11 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
     float m = -INFINITY, l = 0.0f;
     const float lazy = 8.0f / p.c2;
 
-    if (rg.t0 < rg.t1) {
+    auto sweep = [&](auto finite) {
         int page = page_at(rg.t0);
         load(rg.t0, page);
         page = page_at(min(rg.t0 + 1, rg.t1 - 1));
-        store(0);
+        store(0, finite);
         load(min(rg.t0 + 1, rg.t1 - 1), page);
         page = page_at(min(rg.t0 + 2, rg.t1 - 1));
         __syncthreads();
@@ -858,7 +872,7 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
             const int buf = (t - rg.t0) & 1;
             // the next tile into the other buffer, which every wave has finished
             // reading; after the last tile it is written once more for nothing
-            store(buf ^ 1);
+            store(buf ^ 1, finite);
             load(min(t + 2, rg.t1 - 1), page);
             page = page_at(min(t + 3, rg.t1 - 1));
             const uint8_t* Kl = lds + buf * 2 * kKb;
@@ -886,7 +900,7 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
                 const int from = kb + 4 * h - lo - 1;
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    const unsigned n = (in[b] & 255) ? seen : 0;
+                    const unsigned n = in[b] ? seen : 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int at = 8 * (b & 1) + i;
@@ -895,67 +909,67 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
                     }
                 }
             }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kt][i]);
-            {
-                const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-            }
-            // the exponent offset moves only when a score exceeds it by 2^8 in
-            // probability: rarely, and never by more than what fp32 and bf16 hold
-            const bool grow = mx > m + lazy;
-            if (__any(grow)) {
-                const float mn = grow ? mx : m;
-                const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * p.c2);
-                m = mn;
-                l *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
-            }
-            const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
-            u32x4 pf[4];
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    float pr[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][4 * q4 + i], p.c2, moff));
-                        l += pr[i];
-                    }
-                    if (FMT != kBf16) {
-                        const f4_t vs = *(const f4_t*)&vsc[buf][32 * kt + 8 * q4 + 4 * h];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) pr[i] *= vs[i];
-                    }
-                    pf[2 * kt + (q4 >> 1)][2 * (q4 & 1)] = pack_bf16x2(pr[0], pr[1]);
-                    pf[2 * kt + (q4 >> 1)][2 * (q4 & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
-                }
             auto vfrag = [&](int dt, int b) {
                 const int dim = 32 * dt + l32;
                 return *(const u32x4*)(Vl + dim * (kTile * 2) + (((2 * b + h) ^ ((dim >> 1) & 7)) << 4));
             };
-            if (__builtin_expect(((in[0] | in[1] | in[2] | in[3]) & 256) == 0, 1)) {
+            if constexpr (finite) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kt][i]);
+                {
+                    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+                }
+                // the exponent offset moves only when a score exceeds it by 2^8 in
+                // probability: rarely, and never by more than what fp32 and bf16 hold
+                const bool grow = mx > m + lazy;
+                if (__any(grow)) {
+                    const float mn = grow ? mx : m;
+                    const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * p.c2);
+                    m = mn;
+                    l *= alpha;
+#pragma unroll
+                    for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
+                }
+                const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
+                u32x4 pf[4];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        float pr[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][4 * q4 + i], p.c2, moff));
+                            l += pr[i];
+                        }
+                        if (FMT != kBf16) {
+                            const f4_t vs = *(const f4_t*)&vsc[buf][32 * kt + 8 * q4 + 4 * h];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) pr[i] *= vs[i];
+                        }
+                        pf[2 * kt + (q4 >> 1)][2 * (q4 & 1)] = pack_bf16x2(pr[0], pr[1]);
+                        pf[2 * kt + (q4 >> 1)][2 * (q4 & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
+                    }
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int dt = 0; dt < kDt; ++dt) o[dt] = mfma32(vfrag(dt, b), pf[b], o[dt]);
             } else {
-                // one operand at a time, in a loop that is not unrolled: this
-                // path is not to cost the other one registers
+                // what infinities and NaN among the values add to the rows that see them
 #pragma unroll 1
                 for (int b = 0; b < 4; ++b) {
-                    const u32x4 wm = weight_mask(pf[0]);
+                    uint32_t bits = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) bits |= sc[0][i] == -INFINITY ? 0u : 1u << i;
+                    const u32x4 wm = ones_where(bits);
 #pragma unroll
                     for (int dt = 0; dt < kDt; ++dt) {
                         u32x4 fin, up, down;
                         split_nonfinite(vfrag(dt, b), fin, up, down);
-                        o[dt] = mfma32(fin, pf[0], o[dt]);
-                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int sgn = 0; sgn < 2; ++sgn) {
                             f16_t cnt;
@@ -967,13 +981,24 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
                             __builtin_amdgcn_sched_barrier(0);
                         }
                     }
-                    pf[0] = pf[1];
-                    pf[1] = pf[2];
-                    pf[2] = pf[3];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        sc[0][i] = sc[0][8 + i];
+                        sc[0][8 + i] = sc[1][i];
+                        sc[1][i] = sc[1][8 + i];
+                    }
                 }
             }
             __syncthreads();
         }
+    };
+    if (rg.t0 < rg.t1) {
+        if (tid == 0) hidden = 0;
+        __syncthreads();
+        sweep(IC<1>{});
+        // The loop above has no branch for infinities and NaN among the values:
+        // a second one, if there were any, adds what they give.
+        if (hidden) sweep(IC<0>{});
     }
     {
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
