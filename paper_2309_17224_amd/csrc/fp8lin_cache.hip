@@ -430,17 +430,16 @@ __device__ __forceinline__ Range range_of(const AttnArgs& p, const Seq& sq, int 
 __device__ __forceinline__ uint32_t nonfinite2(uint32_t w) { return ((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u; }
 
 // A value operand that holds infinities or NaN: what a row does not see (weight
-// 0) must not reach it, but 0 * NaN would.  The finite part, and indicators (1.0)
-// of +inf or NaN and of -inf or NaN, whose sums over the keys that a row sees say
-// whether to add +inf and -inf (both: NaN).
-__device__ __forceinline__ void split_nonfinite(u32x4 v, u32x4& fin, u32x4& up, u32x4& down) {
+// 0) must not reach it, but 0 * NaN would.  So the product takes the finite part,
+// and these are indicators (1.0) of +inf or NaN and of -inf or NaN, whose sums over
+// the keys that a row sees say whether to add +inf and -inf (both: NaN).
+__device__ __forceinline__ void split_nonfinite(u32x4 v, u32x4& up, u32x4& down) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint32_t w = v[k];
         const uint32_t bad = nonfinite2(w) >> 15;                                     // a 1 in a half that is not finite
         const uint32_t nan = (((w & 0x007F007Fu) + 0x007F007Fu) >> 7) & 0x00010001u;  // whose mantissa is not zero
         const uint32_t neg = (w >> 15) & 0x00010001u;
-        fin[k] = w & ~(bad * 0xFFFFu);
         up[k] = (bad & (nan | ~neg)) * 0x3F80u;
         down[k] = (bad & (nan | neg)) * 0x3F80u;
     }
@@ -458,13 +457,12 @@ __device__ __forceinline__ float add_nonfinite(float o, float up, float down) {
     return o;
 }
 
-// Masks that keep the first n (0 .. 16) of 16 codes (W = 4 words) or bf16 values (8).
-template <int W>
+// Masks that keep the first n tokens of W words of PER tokens each.
+template <int PER, int W>
 __device__ __forceinline__ void token_masks(int n, uint32_t (&mk)[W]) {
-    constexpr int kPer = W == 4 ? 4 : 2;  // tokens of a word
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-        const int bits = max(min(n - kPer * k, kPer), 0) * (32 / kPer);
+        const int bits = max(min(n - PER * k, PER), 0) * (32 / PER);
         mk[k] = (uint32_t)((1ull << bits) - 1);
     }
 }
@@ -487,19 +485,21 @@ __device__ __forceinline__ uint32_t put8(const AttnArgs& p, bool cast, int bq, i
 }
 
 // ---- up to 16 packed rows
-// Wave w takes the tiles t0 + w, t0 + w + 4, ... of its workgroup.  In a tile,
-// lane (r, g) = (lane % 16, lane / 16) reads for key tile kt = 0..3 the 32 (or
-// 16) codes of dimensions 32 g .. of key 16 (r / 4) + 4 kt + r % 4: with this
-// order of the rows, the scores that lane (q, g) gets are of the 16 keys 16 g
-// + 4 kt + i, a block of the values' layout, whose codes for dimension 16 dt + r
-// it reads as one vector.  Nothing moves between lanes.
+// Wave w takes the tiles w, w + 4, ... of its workgroup's range: tiles of 64 keys
+// in FP8, 32 in bf16, 16 KB either way at d_head 128.  Of a tile's four equal groups of keys, of G = 16
+// (8) keys each, lane (r, g) = (lane % 16, lane / 16) reads for key tile kt the
+// dimensions (d_head / 4) g .. of key G (r / 4) + 4 kt + r % 4: with this order of
+// the rows, the scores that lane (q, g) gets are of the keys G g + 4 kt + i, whose
+// values for dimension 16 dt + r it reads as one vector.  Nothing moves between
+// lanes.
 template <int FMT, int DH>
 __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
     constexpr int kE = FMT == kBf16 ? 1 : FMT;
     constexpr int kSteps = DH / 32;                    // of the contraction over d_head
     constexpr int kKv = DH * kEsz<FMT> / 64;           // 16-byte vectors of a lane's keys
-    constexpr int kVv = kEsz<FMT>;                     // and of its values, for each of
-    constexpr int kDt = DH / 16;                       // these tiles of dimensions
+    constexpr int kDt = DH / 16;                       // tiles of dimensions, a vector of values each
+    constexpr int kG = 16 / kEsz<FMT>;                 // keys of a lane group in a tile
+    constexpr int kKeys = 4 * kG, kKt = kG / 4, kPv = kG / 8;  // keys, key tiles, steps of P . V
     __shared__ float so[4][kFew][DH + 4];
     __shared__ float sm[4][kFew], sl[4][kFew];
     __shared__ uint32_t redm[kT / 64];
@@ -531,50 +531,43 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
     const int lo = p.window > 0 ? pos - p.window : -1;  // the last key before those that the row sees
 
     const int rb = r16 >> 2, rl = r16 & 3;  // block and place of this lane's keys
-    u32x4 kreg[4][kKv], vreg[kDt][kVv];
+    u32x4 kreg[kKt][kKv], vreg[kDt];
     u32x4 ke4, ve4;
-    int kn, vn;  // valid keys of the two blocks (0 if the page is absent)
-    int64_t kbase, vbase;  // slots of the two blocks
-    auto where = [&](int t, int blk, int& n) {
-        const int b0 = rg.start + kTile * t + kBlk * blk;
-        const int page = b0 < rg.kend ? page_of(c, s, b0) : -1;
-        n = page >= 0 ? min(rg.kend - b0, kBlk) : 0;
-        return slot_of(c, max(page, 0), hk, b0);
+    int kn, vn;  // valid keys of the two groups (0 if the page is absent)
+    int64_t kbase, vbase;  // slots of their first keys
+    auto where = [&](int t, int grp, int& n) {
+        const int key = rg.start + kKeys * t + kG * grp;
+        const int page = key < rg.kend ? page_of(c, s, key) : -1;
+        n = page >= 0 ? min(rg.kend - key, kG) : 0;
+        return slot_of(c, max(page, 0), hk, key);
     };
     auto load_k = [&](int t) {
         kbase = where(t, rb, kn);
         if (FMT != kBf16) ke4 = *(const u32x4*)(c.ke + kbase);
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+        for (int kt = 0; kt < kKt; ++kt)
 #pragma unroll
             for (int v = 0; v < kKv; ++v)
                 kreg[kt][v] = *(const u32x4*)(c.k + ((kbase + 4 * kt + rl) * DH + (DH / 4) * g) * kEsz<FMT> + 16 * v);
+    };
+    auto v_at = [&](int dt) {
+        return c.v + ((vbase & ~(int64_t)(kBlk - 1)) * DH + (16 * dt + r16) * kBlk + (vbase & (kBlk - kG))) * kEsz<FMT>;
     };
     auto load_v = [&](int t) {
         vbase = where(t, g, vn);
         if (FMT != kBf16) ve4 = *(const u32x4*)(c.ve + vbase);
 #pragma unroll
-        for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-            for (int v = 0; v < kVv; ++v)
-                vreg[dt][v] = *(const u32x4*)(c.v + (vbase * DH + (16 * dt + r16) * kBlk) * kEsz<FMT> + 16 * v);
+        for (int dt = 0; dt < kDt; ++dt) vreg[dt] = *(const u32x4*)v_at(dt);
     };
 
     f4_t o[kDt];
 #pragma unroll
     for (int dt = 0; dt < kDt; ++dt) o[dt] = f4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.0f;
-    int t = rg.t0 + w;
-    if (t < rg.t1) {
-        load_k(t);
-        load_v(t);
-    }
-    for (; t < rg.t1; t += 4) {
-        const bool more = t + 4 < rg.t1;  // its loads follow the last use of this tile's registers
-        const int kb = rg.start + kTile * t;
-        f4_t sc[4];
+    // scores of the loaded tile (raw), and the masks of a tile at an edge
+    auto scores = [&](f4_t (&sc)[kKt]) {
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
+        for (int kt = 0; kt < kKt; ++kt) {
             sc[kt] = f4_t{0.f, 0.f, 0.f, 0.f};
             const float ks = FMT == kBf16 ? 1.0f : exp_float((ke4[kt] >> (8 * rl)) & 0xFFu);
 #pragma unroll
@@ -585,23 +578,69 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
                 sc[kt] = mfma_bf16(kf, qf[st], sc[kt]);
             }
         }
-        if (more) load_k(t + 4);
-        uint32_t sees = 0xFFFFu;  // bit i: key i of this lane's block
-        const bool edge = kb + kTile - 1 > rg.first || (p.window > 0 && kb <= rg.last - p.window) || __any(vn < kBlk);
-        if (edge) {
-            // keys lo + 1 .. lo + seen are seen, of this lane's block if its page is present
-            const int seen = vn > 0 ? max(min(pos, rg.kend - 1) - lo, 0) : 0, from = kb + kBlk * g - lo - 1;
-            sees = 0;
+    };
+    auto is_edge = [&](int kb) {
+        return kb + kKeys - 1 > rg.first || (p.window > 0 && kb <= rg.last - p.window) || __any(vn < kG);
+    };
+    // bit i: key i of this lane's group is seen by its row; keys lo + 1 .. lo +
+    // seen are, if the page is present
+    auto seen_bits = [&](int kb) {
+        const int seen = vn > 0 ? max(min(pos, rg.kend - 1) - lo, 0) : 0, from = kb + kG * g - lo - 1;
+        uint32_t bits = 0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool see = (unsigned)(from + i) < (unsigned)seen;
-                sc[i >> 2][i & 3] = see ? sc[i >> 2][i & 3] : -INFINITY;
-                sees |= see ? 1u << i : 0u;
+        for (int i = 0; i < kG; ++i) bits |= (unsigned)(from + i) < (unsigned)seen ? 1u << i : 0u;
+        return bits;
+    };
+    // a 1 in the top bit of each value that is not finite
+    auto nf = [](uint32_t x) {
+        return FMT == kBf16 ? nonfinite2(x) : ((x & 0x7F7F7F7Fu) + (kE == FP8_E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u;
+    };
+    auto vfrag = [&](u32x4 v, int st) {  // values of the keys 8 st .. 8 st + 7 of this lane's group
+        if (FMT == kBf16) return v;
+        return cvt8b<kE>(v[2 * st & 3], v[(2 * st + 1) & 3], 1.0f);
+    };
+
+    bool hidden = false;  // infinities or NaN among the values of an edge
+    const int tend = rg.t1 * (kTile / kKeys), tfirst = rg.t0 * (kTile / kKeys) + w;
+    int t = tfirst;
+    if (t < tend) {
+        load_k(t);
+        load_v(t);
+    }
+    auto tile = [&](int kb, auto edge) {
+        const bool more = t + 4 < tend;  // its loads follow the last use of this tile's registers
+        f4_t sc[kKt];
+        scores(sc);
+        if (more) load_k(t + 4);
+        if (edge) {
+            const uint32_t bits = seen_bits(kb);
+#pragma unroll
+            for (int i = 0; i < kG; ++i) sc[i >> 2][i & 3] = (bits >> i) & 1u ? sc[i >> 2][i & 3] : -INFINITY;
+            if (__any(vn < kG)) {  // slots that hold no token may hold NaN
+                uint32_t mk[4];
+                token_masks<kG / 4>(vn, mk);
+#pragma unroll
+                for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) vreg[dt][k] &= mk[k];
+            }
+            uint32_t any = 0;
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) any |= nf(vreg[dt][k]);
+            if (__any(any)) {  // their finite part here, what they add below
+                hidden = true;
+#pragma unroll
+                for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        vreg[dt][k] &= ~((nf(vreg[dt][k]) >> (FMT == kBf16 ? 15 : 7)) * (FMT == kBf16 ? 0xFFFFu : 0xFFu));
             }
         }
         float mx = -INFINITY;
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+        for (int kt = 0; kt < kKt; ++kt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kt][i]);
         mx = quad_max(mx);
@@ -614,9 +653,9 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
             for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
         }
         const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
-        u32x4 pf[2];
+        u32x4 pf[kPv];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
+        for (int kt = 0; kt < kKt; ++kt) {
             float pr[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -628,38 +667,49 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
             pf[kt >> 1][2 * (kt & 1)] = pack_bf16x2(pr[0], pr[1]);
             pf[kt >> 1][2 * (kt & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
         }
-        const bool cut = edge && __any(vn < kBlk);
-        uint32_t mk[4 * kVv];  // slots that hold no token may hold NaN
-        if (cut) token_masks(vn, mk);
 #pragma unroll
-        for (int dt = 0; dt < kDt; ++dt) {
-            uint32_t vw[4 * kVv];
+        for (int st = 0; st < kPv; ++st)
 #pragma unroll
-            for (int k = 0; k < 4 * kVv; ++k) vw[k] = vreg[dt][k / 4][k % 4];
-            if (cut) {
+            for (int dt = 0; dt < kDt; ++dt) o[dt] = mfma_bf16(vfrag(vreg[dt], st), pf[st], o[dt]);
+        if (more) load_v(t + 4);
+    };
+    // bf16 values are operands as they are loaded: there a tile at an edge takes
+    // code of its own, or the compiler copies the registers of every tile, and so
+    // waits for their loads early.  (FP8 codes pass through a conversion anyway;
+    // with two copies of that code they would not fit the registers.)
+    for (; t < tend; t += 4) {
+        const int kb = rg.start + kKeys * t;
+        if (FMT != kBf16) tile(kb, is_edge(kb));
+        else if (is_edge(kb)) tile(kb, std::true_type{});
+        else tile(kb, std::false_type{});
+    }
+    if (hidden) {
+#pragma unroll 1
+        for (t = tfirst; t < tend; t += 4) {
+            const int kb = rg.start + kKeys * t;
+            vbase = where(t, g, vn);
+            if (!is_edge(kb)) continue;
+            const uint32_t bits = seen_bits(kb);
+            uint32_t mk[4];
+            token_masks<kG / 4>(vn, mk);
 #pragma unroll
-                for (int k = 0; k < 4 * kVv; ++k) vw[k] &= mk[k];
-            }
+            for (int dt = 0; dt < kDt; ++dt) {  // one operand at a time: few registers
+                u32x4 vv = *(const u32x4*)v_at(dt);
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                u32x4 vf;
-                if (FMT == kBf16) vf = u32x4{vw[4 * st % (4 * kVv)], vw[(4 * st + 1) % (4 * kVv)], vw[(4 * st + 2) % (4 * kVv)], vw[(4 * st + 3) % (4 * kVv)]};
-                else vf = cvt8b<kE>(vw[2 * st], vw[2 * st + 1], 1.0f);
-                if (edge && __any(nonfinite2(vf[0]) | nonfinite2(vf[1]) | nonfinite2(vf[2]) | nonfinite2(vf[3]))) {
-                    u32x4 fin, up, down;
-                    split_nonfinite(vf, fin, up, down);
-                    const u32x4 wm = ones_where(sees >> (8 * st));
+                for (int k = 0; k < 4; ++k) vv[k] &= mk[k];
+#pragma unroll
+                for (int st = 0; st < kPv; ++st) {
+                    u32x4 up, down;
+                    split_nonfinite(vfrag(vv, st), up, down);
+                    const u32x4 wm = ones_where(bits >> (8 * st));
                     const f4_t zero = {0.f, 0.f, 0.f, 0.f};
                     const f4_t cu = mfma_bf16(up, wm, zero), cd = mfma_bf16(down, wm, zero);
-                    o[dt] = mfma_bf16(fin, pf[st], o[dt]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[dt][i] = add_nonfinite(o[dt][i], cu[i], cd[i]);
-                } else {
-                    o[dt] = mfma_bf16(vf, pf[st], o[dt]);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (more) load_v(t + 4);
     }
     l = quad_sum(l);
     // join the four waves
@@ -805,7 +855,7 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
         const int n = nval;
         if (n < kBlk) {  // slots that hold no token may hold NaN
             uint32_t mk[4 * kVv];
-            token_masks(n, mk);
+            token_masks<4 / kEsz<FMT>>(n, mk);
 #pragma unroll
             for (int d = 0; d < kVd; ++d)
 #pragma unroll
@@ -968,8 +1018,8 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
                     const u32x4 wm = ones_where(bits);
 #pragma unroll
                     for (int dt = 0; dt < kDt; ++dt) {
-                        u32x4 fin, up, down;
-                        split_nonfinite(vfrag(dt, b), fin, up, down);
+                        u32x4 up, down;
+                        split_nonfinite(vfrag(dt, b), up, down);
 #pragma unroll
                         for (int sgn = 0; sgn < 2; ++sgn) {
                             f16_t cnt;
