@@ -643,15 +643,19 @@ int32_t llama_cache_read(const llama_cache *cache, const llama_cache_seqs *seqs,
  * o:     out, [rows, ldo].
  * fmt .. ldq8: fused quantise of o as in llama_attention (q8 == NULL: none); its
  *        amax is over the rows of sequences only.
- * ws:    workspace of llama_cache_attention_ws_bytes(...) bytes, 16-byte aligned;
- *        scratch, distinct for concurrent calls.  It holds the partial results
- *        of key ranges that are computed apart and then joined.
+ * ws:    workspace of llama_cache_attention_ws_bytes(...) bytes, 16-byte aligned,
+ *        whose first LLAMA_CACHE_WS_COUNTS bytes must hold zeros before the first
+ *        call; every call that returns FP8_OK and runs to completion leaves them
+ *        zero again (calls of other sizes may use it too).  The rest is scratch: it
+ *        holds the partial results of key ranges that are computed apart and then
+ *        joined.  Calls that may run at the same time need separate workspaces.
  * Softmax statistics and sums in fp32; the probabilities are rounded to bf16
  * for the product with the values, and o is rounded once.  The key ranges
  * depend on the sizes of the call alone (n_heads, rows, n_seqs, max_rows,
  * max_pages) and on a sequence's own length: a call gives the same bits every
  * time.
  */
+#define LLAMA_CACHE_WS_COUNTS 65536
 size_t llama_cache_attention_ws_bytes(int64_t rows, int32_t n_heads, const llama_cache *cache,
                                       const llama_cache_seqs *seqs, int64_t max_rows);
 int32_t llama_cache_attention(const void *q, int64_t rows, int64_t ldq, int32_t n_heads, const llama_cache *cache,

@@ -356,8 +356,15 @@ typedef float f16_t __attribute__((ext_vector_type(16)));
 constexpr int kFew = 16;      // packed rows of few_kernel
 constexpr int kMany = 128;    // packed rows of a workgroup of many_kernel
 constexpr int kTile = 64;     // keys of a tile
-constexpr int kWant = 512;    // workgroups of a launch that key ranges are split for
-constexpr int kLeast = 512;   // keys of a range at least (of the longest sequence)
+#ifndef FW
+#define FW 1024
+#define FL 8
+#define MW 512
+#define ML 8
+#endif
+constexpr int kManyWant = MW, kManyLeast = ML;
+constexpr int kFewWant = FW, kFewLeast = FL;
+constexpr int kCounts = LLAMA_CACHE_WS_COUNTS / 4;  // counters at the start of the workspace: items that can be cut
 
 struct AttnArgs {
     CacheView c;
@@ -367,8 +374,9 @@ struct AttnArgs {
     int max_rows;
     int window;           // 0: none
     int few_on;           // few_kernel takes the sequences of up to kFew packed rows
-    int splits;           // of this kernel's key ranges
-    int few_splits, many_splits;
+    int splits, per;      // many_kernel's key ranges: how many at most, and tiles of each
+    int few_per;          // few_kernel: tiles of a part at most
+    int32_t* counts;      // and finished parts of each item
     float c2;             // log2(e) / sqrt(d_head)
     uint16_t* o;
     int64_t ldo;
@@ -379,8 +387,10 @@ struct AttnArgs {
     uint8_t* q8;
     int64_t ldq8;
     int qfmt;
-    float* part_o;        // [split][row][head][d_head]
-    float2* part_ml;      // [split][row][head]: maximum, sum
+    // partials: output, (maximum, sum); few_kernel's [part][item][kFew], many_kernel's
+    // [split][row][head]
+    float* part_o;
+    float2* part_ml;
 };
 
 __device__ __forceinline__ f16_t mfma32(u32x4 a, u32x4 b, f16_t c) {
@@ -403,23 +413,23 @@ __device__ __forceinline__ u32x4 cvt8b(uint32_t w0, uint32_t w1, float scale) {
 __device__ __forceinline__ float exp_float(uint32_t e) { return __uint_as_float(e << 23); }
 
 // Key range of the packed rows m0 .. m1 - 1 of a sequence, as tiles of 64 keys
-// from a multiple of 64 on, and the part of it that split i of n takes.
+// from a multiple of 64 on, and the `per` tiles of it that a split takes.
 struct Range {
     int start;      // first key of tile 0
     int kend;       // keys below this
+    int nt;         // tiles
     int t0, t1;     // tiles of this split
     int live;       // splits that have tiles
     int first, last;  // positions of the first and last row
 };
-__device__ __forceinline__ Range range_of(const AttnArgs& p, const Seq& sq, int m0, int m1, int split, int n) {
+__device__ __forceinline__ Range range_of(const AttnArgs& p, const Seq& sq, int m0, int m1, int split, int per) {
     Range r;
     r.first = sq.p0 + m0 / p.grp;
     r.last = sq.p0 + (m1 - 1) / p.grp;
     r.kend = max(min(r.last + 1, sq.len), 0);
     const int lo = p.window > 0 ? max(r.first - p.window + 1, 0) : 0;
     r.start = lo & ~(kTile - 1);
-    const int nt = r.kend > r.start ? (r.kend - r.start + kTile - 1) / kTile : 0;
-    const int per = max((nt + n - 1) / n, 1);
+    const int nt = r.nt = r.kend > r.start ? (r.kend - r.start + kTile - 1) / kTile : 0;
     r.live = (nt + per - 1) / per;
     r.t0 = split * per;
     r.t1 = min(r.t0 + per, nt);
@@ -484,39 +494,88 @@ __device__ __forceinline__ uint32_t put8(const AttnArgs& p, bool cast, int bq, i
     return mag8(v);
 }
 
+__device__ __forceinline__ uint4 scaled8(const float* a, float f) {
+    return make_uint4(pack_bf16x2(a[0] * f, a[1] * f), pack_bf16x2(a[2] * f, a[3] * f), pack_bf16x2(a[4] * f, a[5] * f),
+                      pack_bf16x2(a[6] * f, a[7] * f));
+}
+// Pairs of floats to and from where every XCD sees them.
+__device__ __forceinline__ void put_far(uint64_t* p, float a, float b) {
+    __hip_atomic_store(p, ((uint64_t)__float_as_uint(b) << 32) | __float_as_uint(a), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_far(uint64_t* p) {
+    const uint64_t v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+// A partial (maximum and sum ml, output x, y) added to the sums relative to top.
+__device__ __forceinline__ void add_part(float* acc, float& ll, float2 ml, float top, float c2, float4 x, float4 y) {
+    if (ml.x == -INFINITY && ml.y == 0.0f) return;
+    const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml.x - top) * c2);
+    ll += f * ml.y;
+    acc[0] += f * x.x;
+    acc[1] += f * x.y;
+    acc[2] += f * x.z;
+    acc[3] += f * x.w;
+    acc[4] += f * y.x;
+    acc[5] += f * y.y;
+    acc[6] += f * y.z;
+    acc[7] += f * y.w;
+}
+
 // ---- up to 16 packed rows
-// Wave w takes the tiles w, w + 4, ... of its workgroup's range: tiles of 64 keys
-// in FP8, 32 in bf16, 16 KB either way at d_head 128.  Of a tile's four equal groups of keys, of G = 16
-// (8) keys each, lane (r, g) = (lane % 16, lane / 16) reads for key tile kt the
-// dimensions (d_head / 4) g .. of key G (r / 4) + 4 kt + r % 4: with this order of
-// the rows, the scores that lane (q, g) gets are of the keys G g + 4 kt + i, whose
+// Wave w takes the steps w, w + 4, ... of its workgroup's keys: steps of 64 keys in
+// FP8, 32 in bf16, 16 KB either way at d_head 128.  Of a step's four groups of G =
+// 16 (8) keys, lane (r, g) = (lane % 16, lane / 16) reads for key tile kt the bytes
+// 64 v + 16 g .. of key G (r / 4) + 4 kt + r % 4 (so that a load takes whole 64-byte
+// pieces of rows; the queries have the same order of dimensions).  With this order
+// of the rows, the scores that lane (q, g) gets are of the keys G g + 4 kt + i, whose
 // values for dimension 16 dt + r it reads as one vector.  Nothing moves between
-// lanes.
+// lanes.  The cache is read once: its loads carry the non-temporal hint.
+//
+// An item, a (sequence, key/value head), of more than few_per tiles is cut into
+// equal parts, a workgroup each; the one that finishes last joins them.  The
+// partials pass through device-scope atomic stores and loads, which the L2s of
+// the XCDs do not hold back, and a count of the finished parts, which is zero
+// again when the call ends.
 template <int FMT, int DH>
 __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
     constexpr int kE = FMT == kBf16 ? 1 : FMT;
     constexpr int kSteps = DH / 32;                    // of the contraction over d_head
     constexpr int kKv = DH * kEsz<FMT> / 64;           // 16-byte vectors of a lane's keys
     constexpr int kDt = DH / 16;                       // tiles of dimensions, a vector of values each
-    constexpr int kG = 16 / kEsz<FMT>;                 // keys of a lane group in a tile
-    constexpr int kKeys = 4 * kG, kKt = kG / 4, kPv = kG / 8;  // keys, key tiles, steps of P . V
+    constexpr int kG = 16 / kEsz<FMT>, kKeys = 4 * kG; // keys of a lane group, of a step
+    constexpr int kKt = kG / 4, kPv = kG / 8;          // key tiles, steps of P . V
+    constexpr int kCh = DH / 8;
+    static_assert(kFew * kCh <= kT, "a thread for eight values of a row");
     __shared__ float so[4][kFew][DH + 4];
     __shared__ float sm[4][kFew], sl[4][kFew];
     __shared__ uint32_t redm[kT / 64];
+    __shared__ int last;
     const CacheView& c = p.c;
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
     // uniform to the compiler too: branches around matrix instructions, which
     // do not heed the lane mask, are then scalar
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int hk = blockIdx.x % c.nkv;
-    const int rest = blockIdx.x / c.nkv;
-    const int split = rest % p.splits, s = rest / p.splits;
+    const int rb = r16 >> 2, rl = r16 & 3;  // group and place of this lane's keys
+    // the first parts of all items first: every item has one
+    const int items = c.n_seqs * c.nkv, part = blockIdx.x / items, item = blockIdx.x % items;
+    const int hk = item % c.nkv, s = item / c.nkv;
+    // Pages of the first part's first step, before the lengths are there (used
+    // where they turn out to start at key 0).
+    int kpage = -1, vpage = -1;  // of the next step to load
+    if (part == 0 && c.max_pages > 0) {
+        const int32_t* row = c.pages + (int64_t)s * c.ld_pages;
+        kpage = row[min((kKeys * w + kG * rb) >> c.page_shift, c.max_pages - 1)];
+        vpage = row[min((kKeys * w + kG * g) >> c.page_shift, c.max_pages - 1)];
+    }
     const bool cast = p.q8 && p.pred;
     const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
     const Seq sq = seq_of(c, s);
     const int m1 = min(sq.n, p.max_rows) * p.grp;
-    Range rg = range_of(p, sq, 0, max(m1, 1), split, p.splits);
-    if (m1 < 1 || m1 > kFew || (split > 0 && rg.t0 >= rg.t1)) {
+    const Range rg = range_of(p, sq, 0, max(m1, 1), 0, p.few_per);
+    const int share = rg.live > 1 ? (rg.nt + rg.live - 1) / rg.live : rg.nt;  // tiles of a part
+    const int tb = part * share, te = min(tb + share, rg.nt);
+    if (m1 < 1 || m1 > kFew || (part > 0 && tb >= te)) {
         if (p.q8 && tid == 0) p.parts[blockIdx.x] = 0u;
         return;
     }
@@ -524,52 +583,59 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
     const int mq = min(r16, m1 - 1), tok = mq / p.grp;
     const int pos = sq.p0 + tok;
     const uint16_t* qp = p.q + (sq.r0 + tok) * p.ldq + (int64_t)(hk * p.grp + mq % p.grp) * DH;
-    u32x4 qf[kSteps];
-#pragma unroll
-    for (int st = 0; st < kSteps; ++st) qf[st] = ldg16(qp + kSteps * 8 * g + 8 * st);
-
     const int lo = p.window > 0 ? pos - p.window : -1;  // the last key before those that the row sees
 
-    const int rb = r16 >> 2, rl = r16 & 3;  // block and place of this lane's keys
     u32x4 kreg[kKt][kKv], vreg[kDt];
-    u32x4 ke4, ve4;
-    int kn, vn;  // valid keys of the two groups (0 if the page is absent)
+    u32x4 kex, vex;
+    int kn, vn;            // valid keys of the two groups (0 if the page is absent)
     int64_t kbase, vbase;  // slots of their first keys
-    auto where = [&](int t, int grp, int& n) {
+    auto page_in = [&](int t, int grp) {
         const int key = rg.start + kKeys * t + kG * grp;
-        const int page = key < rg.kend ? page_of(c, s, key) : -1;
-        n = page >= 0 ? min(rg.kend - key, kG) : 0;
-        return slot_of(c, max(page, 0), hk, key);
+        const int i = min(key >> c.page_shift, c.max_pages - 1);  // in the table, where the key is not
+        return c.pages[(int64_t)s * c.ld_pages + i];
+    };
+    auto where = [&](int t, int grp, int page, int& n) {
+        const int key = rg.start + kKeys * t + kG * grp;
+        const bool here = page >= 0 && page < c.n_pages;
+        n = here ? max(min(rg.kend - key, kG), 0) : 0;
+        return slot_of(c, here ? page : 0, hk, key);
     };
     auto load_k = [&](int t) {
-        kbase = where(t, rb, kn);
-        if (FMT != kBf16) ke4 = *(const u32x4*)(c.ke + kbase);
+        kbase = where(t, rb, kpage, kn);
+        if (FMT != kBf16) kex = *(const u32x4*)(c.ke + kbase);
 #pragma unroll
         for (int kt = 0; kt < kKt; ++kt)
 #pragma unroll
             for (int v = 0; v < kKv; ++v)
-                kreg[kt][v] = *(const u32x4*)(c.k + ((kbase + 4 * kt + rl) * DH + (DH / 4) * g) * kEsz<FMT> + 16 * v);
+                kreg[kt][v] = __builtin_nontemporal_load(
+                    (const u32x4*)(c.k + (kbase + 4 * kt + rl) * (DH * kEsz<FMT>) + 64 * v + 16 * g));
+        kpage = page_in(t + 4, rb);
     };
     auto v_at = [&](int dt) {
         return c.v + ((vbase & ~(int64_t)(kBlk - 1)) * DH + (16 * dt + r16) * kBlk + (vbase & (kBlk - kG))) * kEsz<FMT>;
     };
     auto load_v = [&](int t) {
-        vbase = where(t, g, vn);
-        if (FMT != kBf16) ve4 = *(const u32x4*)(c.ve + vbase);
+        vbase = where(t, g, vpage, vn);
+        if (FMT != kBf16) vex = *(const u32x4*)(c.ve + vbase);
 #pragma unroll
-        for (int dt = 0; dt < kDt; ++dt) vreg[dt] = *(const u32x4*)v_at(dt);
+        for (int dt = 0; dt < kDt; ++dt) vreg[dt] = __builtin_nontemporal_load((const u32x4*)v_at(dt));
+        vpage = page_in(t + 4, g);
     };
 
     f4_t o[kDt];
 #pragma unroll
     for (int dt = 0; dt < kDt; ++dt) o[dt] = f4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.0f;
+    u32x4 qf[kSteps];
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st)
+        qf[st] = ldg16(qp + (FMT == kBf16 ? 32 * st + 8 * g : 64 * (st >> 1) + 16 * g + 8 * (st & 1)));
     // scores of the loaded tile (raw), and the masks of a tile at an edge
     auto scores = [&](f4_t (&sc)[kKt]) {
 #pragma unroll
         for (int kt = 0; kt < kKt; ++kt) {
             sc[kt] = f4_t{0.f, 0.f, 0.f, 0.f};
-            const float ks = FMT == kBf16 ? 1.0f : exp_float((ke4[kt] >> (8 * rl)) & 0xFFu);
+            const float ks = FMT == kBf16 ? 1.0f : exp_float((kex[kt] >> (8 * rl)) & 0xFFu);
 #pragma unroll
             for (int st = 0; st < kSteps; ++st) {
                 u32x4 kf;
@@ -595,15 +661,19 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
     auto nf = [](uint32_t x) {
         return FMT == kBf16 ? nonfinite2(x) : ((x & 0x7F7F7F7Fu) + (kE == FP8_E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u;
     };
-    auto vfrag = [&](u32x4 v, int st) {  // values of the keys 8 st .. 8 st + 7 of this lane's group
+    auto vfrag = [&](u32x4 v, int st) {  // keys 8 st .. 8 st + 7 of this lane's group
         if (FMT == kBf16) return v;
         return cvt8b<kE>(v[2 * st & 3], v[(2 * st + 1) & 3], 1.0f);
     };
 
     bool hidden = false;  // infinities or NaN among the values of an edge
-    const int tend = rg.t1 * (kTile / kKeys), tfirst = rg.t0 * (kTile / kKeys) + w;
+    const int tend = te * (kTile / kKeys), tfirst = tb * (kTile / kKeys) + w;
     int t = tfirst;
     if (t < tend) {
+        if (tb > 0 || p.window > 0) {
+            kpage = page_in(t, rb);
+            vpage = page_in(t, g);
+        }
         load_k(t);
         load_v(t);
     }
@@ -616,27 +686,6 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
             const uint32_t bits = seen_bits(kb);
 #pragma unroll
             for (int i = 0; i < kG; ++i) sc[i >> 2][i & 3] = (bits >> i) & 1u ? sc[i >> 2][i & 3] : -INFINITY;
-            if (__any(vn < kG)) {  // slots that hold no token may hold NaN
-                uint32_t mk[4];
-                token_masks<kG / 4>(vn, mk);
-#pragma unroll
-                for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) vreg[dt][k] &= mk[k];
-            }
-            uint32_t any = 0;
-#pragma unroll
-            for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) any |= nf(vreg[dt][k]);
-            if (__any(any)) {  // their finite part here, what they add below
-                hidden = true;
-#pragma unroll
-                for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        vreg[dt][k] &= ~((nf(vreg[dt][k]) >> (FMT == kBf16 ? 15 : 7)) * (FMT == kBf16 ? 0xFFFFu : 0xFFu));
-            }
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -662,32 +711,45 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
                 pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][i], p.c2, moff));
                 l += pr[i];
                 // an exponent of a masked slot may be anything, its weight is 0
-                if (FMT != kBf16) pr[i] *= exp_float(min((ve4[kt] >> (8 * i)) & 0xFFu, 254u));
+                if (FMT != kBf16) pr[i] *= exp_float(min((vex[kt] >> (8 * i)) & 0xFFu, 254u));
             }
             pf[kt >> 1][2 * (kt & 1)] = pack_bf16x2(pr[0], pr[1]);
             pf[kt >> 1][2 * (kt & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
         }
+        if (!edge) {
 #pragma unroll
-        for (int st = 0; st < kPv; ++st)
+            for (int st = 0; st < kPv; ++st)
 #pragma unroll
-            for (int dt = 0; dt < kDt; ++dt) o[dt] = mfma_bf16(vfrag(vreg[dt], st), pf[st], o[dt]);
+                for (int dt = 0; dt < kDt; ++dt) o[dt] = mfma_bf16(vfrag(vreg[dt], st), pf[st], o[dt]);
+        } else {
+            uint32_t mk[4], any = 0;
+            token_masks<kG / 4>(vn, mk);  // slots that hold no token may hold NaN
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt) {
+                u32x4 v = vreg[dt];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t x = v[k] & mk[k], bad = nf(x);
+                    any |= bad;
+                    v[k] = x & ~((bad >> (FMT == kBf16 ? 15 : 7)) * (FMT == kBf16 ? 0xFFFFu : 0xFFu));
+                }
+                // the finite part here, what the rest adds below
+#pragma unroll
+                for (int st = 0; st < kPv; ++st) o[dt] = mfma_bf16(vfrag(v, st), pf[st], o[dt]);
+            }
+            hidden = hidden || __any(any);
+        }
         if (more) load_v(t + 4);
     };
-    // bf16 values are operands as they are loaded: there a tile at an edge takes
-    // code of its own, or the compiler copies the registers of every tile, and so
-    // waits for their loads early.  (FP8 codes pass through a conversion anyway;
-    // with two copies of that code they would not fit the registers.)
     for (; t < tend; t += 4) {
         const int kb = rg.start + kKeys * t;
-        if (FMT != kBf16) tile(kb, is_edge(kb));
-        else if (is_edge(kb)) tile(kb, std::true_type{});
-        else tile(kb, std::false_type{});
+        tile(kb, is_edge(kb));
     }
     if (hidden) {
 #pragma unroll 1
         for (t = tfirst; t < tend; t += 4) {
             const int kb = rg.start + kKeys * t;
-            vbase = where(t, g, vn);
+            vbase = where(t, g, page_in(t, g), vn);
             if (!is_edge(kb)) continue;
             const uint32_t bits = seen_bits(kb);
             uint32_t mk[4];
@@ -720,39 +782,60 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
         sl[w][r16] = l;
     }
     __syncthreads();
-    uint32_t mag = 0;
-    constexpr int kCh = DH / 8;
-    for (int i = tid; i < m1 * kCh; i += kT) {
-        const int row = i / kCh, ch = i % kCh;
-        float mm = -INFINITY;
+    const int row = tid / kCh, ch = tid % kCh;
+    const bool mine = row < m1;
+    float mm = -INFINITY, acc[8], ll = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+    if (mine) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) mm = fmaxf(mm, sm[k][row]);
-        float acc[8], ll = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const float f = sm[k][row] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sm[k][row] - mm) * p.c2);
-            if (f == 0.0f && sl[k][row] == 0.0f) continue;
-            ll += f * sl[k][row];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] += f * so[k][row][8 * ch + e];
-        }
-        const int64_t grow = sq.r0 + row / p.grp;
-        const int head = hk * p.grp + row % p.grp;
-        if (p.splits > 1) {
-            const int64_t at = ((int64_t)split * c.rows + grow) * p.nh + head;
-            if (ch == 0) p.part_ml[at] = make_float2(mm, ll);
-            float* d = p.part_o + at * DH + 8 * ch;
-            *(float4*)d = make_float4(acc[0], acc[1], acc[2], acc[3]);
-            *(float4*)(d + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
-        } else {
-            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-            const uint4 v = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
-                                       pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
-            mag = max(mag, put8(p, cast, bq, grow, (int64_t)head * DH + 8 * ch, v));
+            const float* x = &so[k][row][8 * ch];
+            add_part(acc, ll, make_float2(sm[k][row], sl[k][row]), mm, p.c2, *(const float4*)x, *(const float4*)(x + 4));
         }
     }
+    bool write = true;
+    if (rg.live > 1) {
+        // [part][item][row]: d_head outputs, (maximum, sum)
+        const int64_t step = (int64_t)items * kFew, at = (int64_t)item * kFew + row;
+        uint64_t* po = (uint64_t*)p.part_o + at * (DH / 2) + 4 * ch;
+        uint64_t* pm = (uint64_t*)p.part_ml + at;
+        if (mine) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put_far(po + part * step * (DH / 2) + e, acc[2 * e], acc[2 * e + 1]);
+            if (ch == 0) put_far(pm + part * step, mm, ll);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");  // they are where every XCD sees them
+        __syncthreads();
+        if (tid == 0) {
+            const int done = __hip_atomic_fetch_add(p.counts + item, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last = done == rg.live - 1;
+            if (last) __hip_atomic_store(p.counts + item, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        write = last;
+        if (write && mine) {
+            mm = -INFINITY;
+            ll = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+            for (int k = 0; k < rg.live; ++k) mm = fmaxf(mm, get_far(pm + k * step).x);
+#pragma unroll 2
+            for (int k = 0; k < rg.live; ++k) {
+                float2 x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = get_far(po + k * step * (DH / 2) + e);
+                add_part(acc, ll, get_far(pm + k * step), mm, p.c2, make_float4(x[0].x, x[0].y, x[1].x, x[1].y),
+                         make_float4(x[2].x, x[2].y, x[3].x, x[3].y));
+            }
+        }
+    }
+    uint32_t mag = 0;
+    if (write && mine)
+        mag = put8(p, cast, bq, sq.r0 + row / p.grp, (int64_t)(hk * p.grp + row % p.grp) * DH + 8 * ch,
+                   scaled8(acc, ll == 0.0f ? 0.0f : 1.0f / ll));
     if (p.q8) {
         const uint32_t bm = block_max(mag, redm);
         if (tid == 0) p.parts[blockIdx.x] = bm;
@@ -799,7 +882,7 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
     const bool cast = p.q8 && p.pred;
     const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
     const int m1 = min(m0 + kMany, mtot);
-    const Range rg = range_of(p, sq, min(m0, mtot), max(m1, 1), split, p.splits);
+    const Range rg = range_of(p, sq, min(m0, mtot), max(m1, 1), split, p.per);
     if (m0 >= mtot || (p.few_on && mtot <= kFew) || (split > 0 && rg.t0 >= rg.t1)) {
         if (p.q8 && tid == 0) p.parts[blockIdx.x] = 0u;
         return;
@@ -1094,9 +1177,9 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
     }
 }
 
-// ---- join of the key ranges of one (row, head) by DH / 8 lanes
+// ---- join of the key ranges of many_kernel's rows, one (row, head) by DH / 8 lanes
 template <int DH>
-__global__ __launch_bounds__(kT) void combine_kernel(AttnArgs p) {
+__global__ __launch_bounds__(kT) void many_join_kernel(AttnArgs p) {
     constexpr int kCh = DH / 8;
     __shared__ uint32_t redm[kT / 64];
     const CacheView& c = p.c;
@@ -1108,39 +1191,25 @@ __global__ __launch_bounds__(kT) void combine_kernel(AttnArgs p) {
     const int64_t r = item / p.nh;
     const int head = (int)(item % p.nh);
     uint32_t mag = 0;
-    // a workgroup's items can lie in two sequences or more: search for each row
+    // a workgroup's rows can lie in two sequences or more
     int s = wave_search(c.n_seqs, min(first / p.nh, c.rows - 1), [&](int i) { return row_at(c, i); });
     while (s + 1 < c.n_seqs && row_at(c, s + 1) <= r) ++s;
     const Seq sq = seq_of(c, s);
-    const int i = (int)(r - sq.r0);
-    if (r < c.rows && i >= 0 && i < min(sq.n, p.max_rows)) {
-        const int mtot = min(sq.n, p.max_rows) * p.grp;
-        const bool few = p.few_on && mtot <= kFew;
-        const int n = few ? p.few_splits : p.many_splits;
-        if (n > 1) {
-            const int mm = i * p.grp + head % p.grp, m0 = few ? 0 : mm / kMany * kMany;
-            const Range rg = range_of(p, sq, m0, few ? mtot : min(m0 + kMany, mtot), 0, n);
-            const int64_t step = c.rows * p.nh, at = r * p.nh + head;
-            float top = -INFINITY;
-            for (int k = 0; k < rg.live; ++k) top = fmaxf(top, p.part_ml[k * step + at].x);
-            float acc[8], ll = 0.0f;
+    const int i = (int)(r - sq.r0), mtot = min(sq.n, p.max_rows) * p.grp;
+    if (r < c.rows && i >= 0 && i * p.grp < mtot && !(p.few_on && mtot <= kFew)) {
+        const int m0 = (i * p.grp + head % p.grp) / kMany * kMany;
+        const Range rg = range_of(p, sq, m0, min(m0 + kMany, mtot), 0, p.per);
+        const int64_t step = c.rows * p.nh, at = r * p.nh + head;
+        float top = -INFINITY, acc[8], ll = 0.0f;
+        for (int k = 0; k < rg.live; ++k) top = fmaxf(top, p.part_ml[k * step + at].x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-            for (int k = 0; k < rg.live; ++k) {
-                const float2 ml = p.part_ml[k * step + at];
-                const float* d = p.part_o + (k * step + at) * DH + 8 * ch;
-                const float4 x = *(const float4*)d, y = *(const float4*)(d + 4);
-                if (ml.x == -INFINITY && ml.y == 0.0f) continue;
-                const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((ml.x - top) * p.c2);
-                ll += f * ml.y;
-                acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
-                acc[4] += f * y.x; acc[5] += f * y.y; acc[6] += f * y.z; acc[7] += f * y.w;
-            }
-            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-            const uint4 v = make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
-                                       pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
-            mag = put8(p, cast, bq, r, (int64_t)head * DH + 8 * ch, v);
+        for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+#pragma unroll 2
+        for (int k = 0; k < rg.live; ++k) {
+            const float* d = p.part_o + (k * step + at) * DH + 8 * ch;
+            add_part(acc, ll, p.part_ml[k * step + at], top, p.c2, *(const float4*)d, *(const float4*)(d + 4));
         }
+        mag = put8(p, cast, bq, r, (int64_t)head * DH + 8 * ch, scaled8(acc, ll == 0.0f ? 0.0f : 1.0f / ll));
     }
     if (p.q8) {
         const uint32_t bm = block_max(mag, redm);
@@ -1224,35 +1293,47 @@ int32_t launch_cache_read(const CacheView& c, int fmt, int d_head, uint16_t* k, 
 namespace {
 // How a call is split over workgroups, from its sizes alone.
 struct Plan {
-    bool few, many;            // which kernels run
-    int few_splits, many_splits;
-    int64_t few_wg, many_wg, join_wg;
-    int64_t parts, words, ws_bytes;
+    bool few, many;        // which kernels run
+    int few_parts, few_per;  // parts of an item, tiles of one, at most
+    int splits, per;       // many_kernel's key ranges, and tiles of each
+    int64_t few_wg, many_wg, many_join;
+    int64_t parts;
+    // offsets in the workspace, in bytes, behind the counts: words of the quantise, partials of either kernel
+    int64_t words, few_o, few_ml, many_o, many_ml, ws_bytes;
 };
 Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t max_rows, int64_t max_len) {
     Plan p;
     const int64_t grp = nh / nkv, cap = max_rows < rows ? max_rows : rows;
+    const int64_t tiles = (max_len + kTile - 1) / kTile;
     p.many = cap * grp > kFew;
     // sequences of one length have no single tokens among them
     p.few = !p.many || (grp <= kFew && n_seqs > 1 && rows < n_seqs * max_rows);
-    // Enough workgroups for two on each compute unit, each with at least 512
-    // keys of the longest sequence.
-    auto splits = [&](int64_t wg) {
-        const int64_t want = (kWant + wg - 1) / wg, most = (max_len + kLeast - 1) / kLeast;
-        const int64_t n = want < most ? want : most;
-        return (int)(n < 1 ? 1 : n);
+    // as many ranges as give `want` workgroups if all sequences were of the
+    // longest length, of at least `least` tiles
+    auto cut = [&](int64_t wg, int64_t want, int64_t least, int* n, int* per) {
+        const int64_t most = (want + wg - 1) / wg;
+        int64_t t = (tiles + most - 1) / most;
+        t = t < least ? least : t;
+        *per = (int)t;
+        *n = (int)((tiles + t - 1) / t);
+        if (*n < 1) *n = 1;
     };
-    const int64_t few = n_seqs * nkv, many = (rows * grp / kMany + n_seqs) * nkv;
-    p.few_splits = p.few ? splits(few) : 1;
-    p.many_splits = p.many ? splits(many) : 1;
-    p.few_wg = p.few ? few * p.few_splits : 0;
-    p.many_wg = p.many ? many * p.many_splits : 0;
-    const int most = p.few_splits > p.many_splits ? p.few_splits : p.many_splits;
-    const int64_t items = rows * nh, per = kT / (d_head / 8);
-    p.join_wg = most > 1 ? (items + per - 1) / per : 0;
-    p.parts = p.few_wg + p.many_wg + p.join_wg;
-    p.words = (1 + p.parts + 3) & ~(int64_t)3;
-    p.ws_bytes = 4 * p.words + (most > 1 ? most * items * (4 * (int64_t)d_head + 8) : 0);
+    const int64_t items = n_seqs * nkv, wg = (rows * grp / kMany + n_seqs) * nkv;
+    cut(items, items <= kCounts ? kFewWant : 1, kFewLeast, &p.few_parts, &p.few_per);
+    cut(wg, kManyWant, kManyLeast, &p.splits, &p.per);
+    if (!p.many) p.splits = 1;
+    if (!p.few) p.few_parts = 1;
+    p.few_wg = p.few ? items * p.few_parts : 0;
+    p.many_wg = p.many ? wg * p.splits : 0;
+    p.many_join = p.splits > 1 ? (rows * nh + kT / (d_head / 8) - 1) / (kT / (d_head / 8)) : 0;
+    p.parts = p.few_wg + p.many_wg + p.many_join;
+    const int64_t fs = p.few_parts > 1 ? p.few_parts * items * kFew : 0, ms = p.splits > 1 ? p.splits * rows * nh : 0;
+    p.words = kCounts * 4;
+    p.few_o = (p.words + (1 + p.parts) * 4 + 15) & ~(int64_t)15;
+    p.few_ml = p.few_o + fs * d_head * 4;
+    p.many_o = p.few_ml + fs * 8;
+    p.many_ml = p.many_o + ms * d_head * 4;
+    p.ws_bytes = p.many_ml + ms * 8;
     return p;
 }
 }  // namespace
@@ -1268,8 +1349,8 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
                                void* ws, hipStream_t s) {
     const bool quant = fq && fq->q;
     const Plan pl = plan_of(c.rows, nh, c.nkv, d_head, c.n_seqs, max_rows, (int64_t)c.max_pages << c.page_shift);
-    const int most = pl.few_splits > pl.many_splits ? pl.few_splits : pl.many_splits;
-    uint32_t* words = (uint32_t*)ws;
+    char* base = (char*)ws;
+    uint32_t* words = (uint32_t*)(base + pl.words);
     AttnArgs a;
     a.c = c;
     a.q = q;
@@ -1279,8 +1360,10 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
     a.max_rows = (int)(max_rows < c.rows ? max_rows : c.rows);
     a.window = (int)(window < ((int64_t)1 << 30) ? window : 0);  // beyond any position: none
     a.few_on = pl.few;
-    a.few_splits = pl.few_splits;
-    a.many_splits = pl.many_splits;
+    a.splits = pl.splits;
+    a.per = pl.per;
+    a.few_per = pl.few_per;
+    a.counts = (int32_t*)base;
     a.c2 = (float)(1.4426950408889634 / sqrt((double)d_head));
     a.o = o;
     a.ldo = ldo;
@@ -1289,24 +1372,21 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
     a.q8 = quant ? fq->q : nullptr;
     a.ldq8 = quant ? fq->ldq : 0;
     a.qfmt = quant ? fq->fmt : FP8_E4M3;
-    a.part_o = (float*)(words + pl.words);
-    a.part_ml = (float2*)(a.part_o + (int64_t)most * c.rows * nh * d_head);
+    a.parts = words + 1;
     with_cache(fmt, d_head, [&](auto F, auto D) {
         constexpr int kF = decltype(F)::value, kD = decltype(D)::value;
-        if (pl.many) {
-            a.splits = pl.many_splits;
-            a.parts = words + 1 + pl.few_wg;
-            hipLaunchKernelGGL((many_kernel<kF, kD>), dim3((unsigned)pl.many_wg), dim3(kT), 0, s, a);
-        }
-        if (pl.few) {
-            a.splits = pl.few_splits;
-            a.parts = words + 1;
-            hipLaunchKernelGGL((few_kernel<kF, kD>), dim3((unsigned)pl.few_wg), dim3(kT), 0, s, a);
-        }
-        if (pl.join_wg) {
-            a.parts = words + 1 + pl.few_wg + pl.many_wg;
-            hipLaunchKernelGGL((combine_kernel<kD>), dim3((unsigned)pl.join_wg), dim3(kT), 0, s, a);
-        }
+        auto go = [&](auto kernel, int64_t wg) {
+            if (wg == 0) return;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(kT), 0, s, a);
+            a.parts += wg;
+        };
+        a.part_o = (float*)(base + pl.many_o);
+        a.part_ml = (float2*)(base + pl.many_ml);
+        go(many_kernel<kF, kD>, pl.many_wg);
+        go(many_join_kernel<kD>, pl.many_join);
+        a.part_o = (float*)(base + pl.few_o);
+        a.part_ml = (float2*)(base + pl.few_ml);
+        go(few_kernel<kF, kD>, pl.few_wg);
     });
     int32_t st = hip_status();
     if (st == FP8_OK && quant) {

@@ -706,6 +706,9 @@ def _shaped(t: torch.Tensor, name: str, shape, dtype, device) -> torch.Tensor:
     return t
 
 
+CACHE_WS_COUNTS = 65536
+
+
 class KVCache:
     """Pages of keys and values (llama_cache): fmt E4M3 or E5M2 (codes with one
     exponent byte per token and head, value = code * 2^(exp - 127)) or
@@ -809,8 +812,12 @@ def llama_cache_attention_ws_bytes(rows: int, n_heads: int, cache: KVCache, seqs
 
 
 def cache_attention_workspace(rows: int, n_heads: int, cache: KVCache, seqs: CacheSeqs, max_rows: int) -> torch.Tensor:
-    return torch.empty(max(llama_cache_attention_ws_bytes(rows, n_heads, cache, seqs, max_rows), 16),
-                       dtype=torch.uint8, device=cache.device)
+    """Workspace of llama_cache_attention: its counters are zero, and left zero by
+    every completed call (one per stream of concurrent calls)."""
+    ws = torch.empty(max(llama_cache_attention_ws_bytes(rows, n_heads, cache, seqs, max_rows), CACHE_WS_COUNTS),
+                     dtype=torch.uint8, device=cache.device)
+    ws[:CACHE_WS_COUNTS].zero_()
+    return ws
 
 
 def llama_cache_attention(q, cache: KVCache, seqs: CacheSeqs, n_heads: int, max_rows: int, window: int = 0, o=None,
