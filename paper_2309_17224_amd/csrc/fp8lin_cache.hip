@@ -354,16 +354,20 @@ __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restr
 typedef float f16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kFew = 16;      // packed rows of few_kernel
+constexpr int kFewW = 4, kFewT = 64 * kFewW;  // its waves and threads
 constexpr int kMany = 128;    // packed rows of a workgroup of many_kernel
 constexpr int kTile = 64;     // keys of a tile
-#ifndef FW
-#define FW 1024
-#define FL 8
+#ifndef MW
 #define MW 512
 #define ML 8
 #endif
 constexpr int kManyWant = MW, kManyLeast = ML;
-constexpr int kFewWant = FW, kFewLeast = FL;
+constexpr int kCus = 256;          // compute units
+constexpr int kShares = 512;       // workgroups of few_kernel that run at once
+constexpr int kShareLeast = 8;     // tiles of a share at least
+constexpr int kFlatTiles = 64;     // of a share, if all sequences were of the longest length, for shares to be worth it
+constexpr int kFlatSeqs = 1024;    // sequences that a workgroup counts through
+constexpr int kFewPart = 4;        // tiles of a part of an item at least: one step a wave
 constexpr int kCounts = LLAMA_CACHE_WS_COUNTS / 4;  // counters at the start of the workspace: items that can be cut
 
 struct AttnArgs {
@@ -375,7 +379,7 @@ struct AttnArgs {
     int window;           // 0: none
     int few_on;           // few_kernel takes the sequences of up to kFew packed rows
     int splits, per;      // many_kernel's key ranges: how many at most, and tiles of each
-    int few_per;          // few_kernel: tiles of a part at most
+    int flat, few_parts;  // few_kernel: equal shares of all tiles; parts of an item
     int32_t* counts;      // and finished parts of each item
     float c2;             // log2(e) / sqrt(d_head)
     uint16_t* o;
@@ -387,7 +391,7 @@ struct AttnArgs {
     uint8_t* q8;
     int64_t ldq8;
     int qfmt;
-    // partials: output, (maximum, sum); few_kernel's [part][item][kFew], many_kernel's
+    // partials: output, (maximum, sum); few_kernel's [share][2][kFew], many_kernel's
     // [split][row][head]
     float* part_o;
     float2* part_ml;
@@ -523,7 +527,7 @@ __device__ __forceinline__ void add_part(float* acc, float& ll, float2 ml, float
 }
 
 // ---- up to 16 packed rows
-// Wave w takes the steps w, w + 4, ... of its workgroup's keys: steps of 64 keys in
+// Wave w takes the steps w, w + kFewW, ... of its workgroup's keys: steps of 64 keys in
 // FP8, 32 in bf16, 16 KB either way at d_head 128.  Of a step's four groups of G =
 // 16 (8) keys, lane (r, g) = (lane % 16, lane / 16) reads for key tile kt the bytes
 // 64 v + 16 g .. of key G (r / 4) + 4 kt + r % 4 (so that a load takes whole 64-byte
@@ -532,13 +536,83 @@ __device__ __forceinline__ void add_part(float* acc, float& ll, float2 ml, float
 // values for dimension 16 dt + r it reads as one vector.  Nothing moves between
 // lanes.  The cache is read once: its loads carry the non-temporal hint.
 //
-// An item, a (sequence, key/value head), of more than few_per tiles is cut into
-// equal parts, a workgroup each; the one that finishes last joins them.  The
-// partials pass through device-scope atomic stores and loads, which the L2s of
-// the XCDs do not hold back, and a count of the finished parts, which is zero
-// again when the call ends.
+// Work: without `flat` a workgroup takes one item, a (sequence, key/value head), or
+// where those are few one of few_parts equal parts of it.
+// With it, the tiles of all items in a row are cut into equal shares, one for each
+// workgroup: however ragged the lengths, every compute unit (whose loads run at
+// some 35 GB/s at most) has the same work.  An item that several shares cut is joined by
+// the one that finishes last.  The partials pass through device-scope atomic
+// stores and loads, which the L2s of the XCDs do not hold back, and a count of the
+// finished parts of the item, which is zero again when the call ends.
+struct FewWork {
+    int s, hk, nt;   // item, its tiles
+    int64_t at;      // its first tile among all
+    int per;         // tiles of a share
+};
+// Tiles of sequence s (0 if it is not few_kernel's, or sees no key).
+__device__ __forceinline__ int few_tiles(const AttnArgs& p, int s) {
+    const Seq sq = seq_of(p.c, s);
+    const int m1 = min(sq.n, p.max_rows) * p.grp;
+    return m1 < 1 || m1 > kFew ? 0 : range_of(p, sq, 0, m1, 0, 1).nt;
+}
+// The sequence of the k-th largest number of tiles, if there are up to 64;
+// sequence k otherwise.  Workgroups take the longest items first, and those of the
+// second one on a compute unit the shortest first, so that a long one has a short
+// one beside it.
+__device__ __forceinline__ int few_ranked(const AttnArgs& p, int k) {
+    const int lane = threadIdx.x & 63, ns = p.c.n_seqs;
+    if (ns > 64 || ns == 1) return k;
+    const int mine = lane < ns ? few_tiles(p, lane) : -1;
+    int rank = 0;
+    for (int j = 0; j < ns; ++j) {
+        const int x = __builtin_amdgcn_readlane(mine, j);
+        rank += x > mine || (x == mine && j < lane);
+    }
+    return __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(lane < ns && rank == k)) - 1);
+}
+// Tiles of a share, and the item that the first tile of one falls into (nt 0: none).
+__device__ __forceinline__ FewWork few_locate(const AttnArgs& p, int share, int shares) {
+    const int lane = threadIdx.x & 63, ns = p.c.n_seqs, nkv = p.c.nkv;
+    FewWork f = {0, 0, 0, 0, 0};
+    int64_t total = 0;
+    int mine = 0;  // tiles of this lane's sequence of the last 64 looked at
+    int upto = 0;  // and of those before it, itself included (below 2^31: 64 times 2^24)
+    auto look = [&](int s0) {
+        upto = mine = s0 + lane < ns ? few_tiles(p, s0 + lane) : 0;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int y = __shfl_up(upto, off, 64);
+            upto += lane >= off ? y : 0;
+        }
+    };
+    for (int s0 = 0; s0 < ns; s0 += 64) {
+        look(s0);
+        total += __builtin_amdgcn_readlane(upto, 63);
+    }
+    total *= nkv;
+    const int64_t per = (total + shares - 1) / shares;
+    f.per = (int)(per < kShareLeast ? kShareLeast : per);
+    const int64_t from = (int64_t)share * f.per;
+    int64_t before = 0;
+    for (int s0 = 0; s0 < ns && from < total; s0 += 64) {
+        if (ns > 64) look(s0);
+        const uint64_t beyond = __ballot((before + upto) * nkv > from);
+        if (beyond) {
+            const int k = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)beyond) - 1);
+            f.s = s0 + k;
+            f.nt = __builtin_amdgcn_readlane(mine, k);
+            const int64_t start = (before + __builtin_amdgcn_readlane(upto, k) - f.nt) * nkv;
+            f.hk = (int)((from - start) / f.nt);
+            f.at = start + (int64_t)f.hk * f.nt;
+            break;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return f;
+}
+
 template <int FMT, int DH>
-__global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
+__global__ __launch_bounds__(kFewT, 2) void few_kernel(AttnArgs p) {
     constexpr int kE = FMT == kBf16 ? 1 : FMT;
     constexpr int kSteps = DH / 32;                    // of the contraction over d_head
     constexpr int kKv = DH * kEsz<FMT> / 64;           // 16-byte vectors of a lane's keys
@@ -546,10 +620,10 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
     constexpr int kG = 16 / kEsz<FMT>, kKeys = 4 * kG; // keys of a lane group, of a step
     constexpr int kKt = kG / 4, kPv = kG / 8;          // key tiles, steps of P . V
     constexpr int kCh = DH / 8;
-    static_assert(kFew * kCh <= kT, "a thread for eight values of a row");
-    __shared__ float so[4][kFew][DH + 4];
-    __shared__ float sm[4][kFew], sl[4][kFew];
-    __shared__ uint32_t redm[kT / 64];
+    static_assert(kFew * kCh <= kFewT, "a thread for eight values of a row");
+    __shared__ float so[kFewW][kFew][DH + 4];
+    __shared__ float sm[kFewW][kFew], sl[kFewW][kFew];
+    __shared__ uint32_t redm[kFewW];
     __shared__ int last;
     const CacheView& c = p.c;
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
@@ -557,290 +631,366 @@ __global__ __launch_bounds__(kT, 2) void few_kernel(AttnArgs p) {
     // do not heed the lane mask, are then scalar
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rb = r16 >> 2, rl = r16 & 3;  // group and place of this lane's keys
-    // the first parts of all items first: every item has one
-    const int items = c.n_seqs * c.nkv, part = blockIdx.x / items, item = blockIdx.x % items;
-    const int hk = item % c.nkv, s = item / c.nkv;
-    // Pages of the first part's first step, before the lengths are there (used
-    // where they turn out to start at key 0).
-    int kpage = -1, vpage = -1;  // of the next step to load
-    if (part == 0 && c.max_pages > 0) {
-        const int32_t* row = c.pages + (int64_t)s * c.ld_pages;
-        kpage = row[min((kKeys * w + kG * rb) >> c.page_shift, c.max_pages - 1)];
-        vpage = row[min((kKeys * w + kG * g) >> c.page_shift, c.max_pages - 1)];
-    }
     const bool cast = p.q8 && p.pred;
     const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
-    const Seq sq = seq_of(c, s);
-    const int m1 = min(sq.n, p.max_rows) * p.grp;
-    const Range rg = range_of(p, sq, 0, max(m1, 1), 0, p.few_per);
-    const int share = rg.live > 1 ? (rg.nt + rg.live - 1) / rg.live : rg.nt;  // tiles of a part
-    const int tb = part * share, te = min(tb + share, rg.nt);
-    if (m1 < 1 || m1 > kFew || (part > 0 && tb >= te)) {
-        if (p.q8 && tid == 0) p.parts[blockIdx.x] = 0u;
-        return;
-    }
-    // this lane's query (rows past the last one repeat it, and are not stored)
-    const int mq = min(r16, m1 - 1), tok = mq / p.grp;
-    const int pos = sq.p0 + tok;
-    const uint16_t* qp = p.q + (sq.r0 + tok) * p.ldq + (int64_t)(hk * p.grp + mq % p.grp) * DH;
-    const int lo = p.window > 0 ? pos - p.window : -1;  // the last key before those that the row sees
-
-    u32x4 kreg[kKt][kKv], vreg[kDt];
-    u32x4 kex, vex;
-    int kn, vn;            // valid keys of the two groups (0 if the page is absent)
-    int64_t kbase, vbase;  // slots of their first keys
-    auto page_in = [&](int t, int grp) {
-        const int key = rg.start + kKeys * t + kG * grp;
-        const int i = min(key >> c.page_shift, c.max_pages - 1);  // in the table, where the key is not
-        return c.pages[(int64_t)s * c.ld_pages + i];
-    };
-    auto where = [&](int t, int grp, int page, int& n) {
-        const int key = rg.start + kKeys * t + kG * grp;
-        const bool here = page >= 0 && page < c.n_pages;
-        n = here ? max(min(rg.kend - key, kG), 0) : 0;
-        return slot_of(c, here ? page : 0, hk, key);
-    };
-    auto load_k = [&](int t) {
-        kbase = where(t, rb, kpage, kn);
-        if (FMT != kBf16) kex = *(const u32x4*)(c.ke + kbase);
-#pragma unroll
-        for (int kt = 0; kt < kKt; ++kt)
-#pragma unroll
-            for (int v = 0; v < kKv; ++v)
-                kreg[kt][v] = __builtin_nontemporal_load(
-                    (const u32x4*)(c.k + (kbase + 4 * kt + rl) * (DH * kEsz<FMT>) + 64 * v + 16 * g));
-        kpage = page_in(t + 4, rb);
-    };
-    auto v_at = [&](int dt) {
-        return c.v + ((vbase & ~(int64_t)(kBlk - 1)) * DH + (16 * dt + r16) * kBlk + (vbase & (kBlk - kG))) * kEsz<FMT>;
-    };
-    auto load_v = [&](int t) {
-        vbase = where(t, g, vpage, vn);
-        if (FMT != kBf16) vex = *(const u32x4*)(c.ve + vbase);
-#pragma unroll
-        for (int dt = 0; dt < kDt; ++dt) vreg[dt] = __builtin_nontemporal_load((const u32x4*)v_at(dt));
-        vpage = page_in(t + 4, g);
-    };
-
-    f4_t o[kDt];
-#pragma unroll
-    for (int dt = 0; dt < kDt; ++dt) o[dt] = f4_t{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.0f;
-    u32x4 qf[kSteps];
-#pragma unroll
-    for (int st = 0; st < kSteps; ++st)
-        qf[st] = ldg16(qp + (FMT == kBf16 ? 32 * st + 8 * g : 64 * (st >> 1) + 16 * g + 8 * (st & 1)));
-    // scores of the loaded tile (raw), and the masks of a tile at an edge
-    auto scores = [&](f4_t (&sc)[kKt]) {
-#pragma unroll
-        for (int kt = 0; kt < kKt; ++kt) {
-            sc[kt] = f4_t{0.f, 0.f, 0.f, 0.f};
-            const float ks = FMT == kBf16 ? 1.0f : exp_float((kex[kt] >> (8 * rl)) & 0xFFu);
-#pragma unroll
-            for (int st = 0; st < kSteps; ++st) {
-                u32x4 kf;
-                if (FMT == kBf16) kf = kreg[kt][st];
-                else kf = cvt8b<kE>(kreg[kt][st / 2][2 * (st & 1)], kreg[kt][st / 2][2 * (st & 1) + 1], ks);
-                sc[kt] = mfma_bf16(kf, qf[st], sc[kt]);
-            }
-        }
-    };
-    auto is_edge = [&](int kb) {
-        return kb + kKeys - 1 > rg.first || (p.window > 0 && kb <= rg.last - p.window) || __any(vn < kG);
-    };
-    // bit i: key i of this lane's group is seen by its row; keys lo + 1 .. lo +
-    // seen are, if the page is present
-    auto seen_bits = [&](int kb) {
-        const int seen = vn > 0 ? max(min(pos, rg.kend - 1) - lo, 0) : 0, from = kb + kG * g - lo - 1;
-        uint32_t bits = 0;
-#pragma unroll
-        for (int i = 0; i < kG; ++i) bits |= (unsigned)(from + i) < (unsigned)seen ? 1u << i : 0u;
-        return bits;
-    };
-    // a 1 in the top bit of each value that is not finite
-    auto nf = [](uint32_t x) {
-        return FMT == kBf16 ? nonfinite2(x) : ((x & 0x7F7F7F7Fu) + (kE == FP8_E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u;
-    };
-    auto vfrag = [&](u32x4 v, int st) {  // keys 8 st .. 8 st + 7 of this lane's group
-        if (FMT == kBf16) return v;
-        return cvt8b<kE>(v[2 * st & 3], v[(2 * st + 1) & 3], 1.0f);
-    };
-
-    bool hidden = false;  // infinities or NaN among the values of an edge
-    const int tend = te * (kTile / kKeys), tfirst = tb * (kTile / kKeys) + w;
-    int t = tfirst;
-    if (t < tend) {
-        if (tb > 0 || p.window > 0) {
-            kpage = page_in(t, rb);
-            vpage = page_in(t, g);
-        }
-        load_k(t);
-        load_v(t);
-    }
-    auto tile = [&](int kb, auto edge) {
-        const bool more = t + 4 < tend;  // its loads follow the last use of this tile's registers
-        f4_t sc[kKt];
-        scores(sc);
-        if (more) load_k(t + 4);
-        if (edge) {
-            const uint32_t bits = seen_bits(kb);
-#pragma unroll
-            for (int i = 0; i < kG; ++i) sc[i >> 2][i & 3] = (bits >> i) & 1u ? sc[i >> 2][i & 3] : -INFINITY;
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int kt = 0; kt < kKt; ++kt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kt][i]);
-        mx = quad_max(mx);
-        if (__any(mx > m)) {
-            const float mn = fmaxf(m, mx);
-            const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * p.c2);
-            m = mn;
-            l *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
-        }
-        const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
-        u32x4 pf[kPv];
-#pragma unroll
-        for (int kt = 0; kt < kKt; ++kt) {
-            float pr[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][i], p.c2, moff));
-                l += pr[i];
-                // an exponent of a masked slot may be anything, its weight is 0
-                if (FMT != kBf16) pr[i] *= exp_float(min((vex[kt] >> (8 * i)) & 0xFFu, 254u));
-            }
-            pf[kt >> 1][2 * (kt & 1)] = pack_bf16x2(pr[0], pr[1]);
-            pf[kt >> 1][2 * (kt & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
-        }
-        if (!edge) {
-#pragma unroll
-            for (int st = 0; st < kPv; ++st)
-#pragma unroll
-                for (int dt = 0; dt < kDt; ++dt) o[dt] = mfma_bf16(vfrag(vreg[dt], st), pf[st], o[dt]);
+    uint32_t mag = 0;
+    FewWork f;
+    const int items = c.n_seqs * c.nkv;
+    int part = 0;
+    int64_t at = 0, end = INT64_MAX;
+    int kpage = -1, vpage = -1;  // of the next step to load
+    bool any = true;
+    if (p.flat) {
+        f = few_locate(p, blockIdx.x, gridDim.x);
+        at = (int64_t)blockIdx.x * f.per;
+        end = at + f.per;
+        any = f.nt > 0;
+    } else {
+        int i = blockIdx.x;
+        if (p.few_parts > 1) {  // all run at once: in order
+            part = i / items;
+            i %= items;
+            f.s = i / c.nkv;
         } else {
-            uint32_t mk[4], any = 0;
-            token_masks<kG / 4>(vn, mk);  // slots that hold no token may hold NaN
-#pragma unroll
-            for (int dt = 0; dt < kDt; ++dt) {
-                u32x4 v = vreg[dt];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t x = v[k] & mk[k], bad = nf(x);
-                    any |= bad;
-                    v[k] = x & ~((bad >> (FMT == kBf16 ? 15 : 7)) * (FMT == kBf16 ? 0xFFFFu : 0xFFu));
-                }
-                // the finite part here, what the rest adds below
-#pragma unroll
-                for (int st = 0; st < kPv; ++st) o[dt] = mfma_bf16(vfrag(v, st), pf[st], o[dt]);
-            }
-            hidden = hidden || __any(any);
+            if (items > kCus && items <= 2 * kCus && i >= kCus) i = items - 1 - (i - kCus);
+            f.s = few_ranked(p, i / c.nkv);
         }
-        if (more) load_v(t + 4);
-    };
-    for (; t < tend; t += 4) {
-        const int kb = rg.start + kKeys * t;
-        tile(kb, is_edge(kb));
+        f.hk = i % c.nkv;
+        f.at = 0;
+        f.per = INT32_MAX;
+        // pages of the first step, before the lengths are there (used if the
+        // keys turn out to start at 0)
+        if (part == 0 && c.max_pages > 0) {
+            const int32_t* row = c.pages + (int64_t)f.s * c.ld_pages;
+            kpage = row[min((kKeys * w + kG * rb) >> c.page_shift, c.max_pages - 1)];
+            vpage = row[min((kKeys * w + kG * g) >> c.page_shift, c.max_pages - 1)];
+        }
     }
-    if (hidden) {
-#pragma unroll 1
-        for (t = tfirst; t < tend; t += 4) {
+    while (any) {
+        const int s = f.s, hk = f.hk;
+        const Seq sq = seq_of(c, s);
+        const int m1 = min(sq.n, p.max_rows) * p.grp;
+        if (m1 < 1 || m1 > kFew) break;
+        const Range rg = range_of(p, sq, 0, m1, 0, 1);
+        int tb, te, live = 1;  // this workgroup's tiles, parts of the item without `flat`
+        if (p.flat) {
+            tb = (int)(at - f.at);
+            te = (int)(end - f.at < rg.nt ? end - f.at : rg.nt);
+        } else {
+            live = max(min(p.few_parts, rg.nt / kFewPart), 1);
+            const int each = (rg.nt + live - 1) / live;
+            live = each > 0 ? (rg.nt + each - 1) / each : 1;
+            tb = min(part * each, rg.nt);
+            te = min(tb + each, rg.nt);
+            if (part >= live && part > 0) break;
+        }
+        // this lane's query (rows past the last one repeat it, and are not stored)
+        const int mq = min(r16, m1 - 1), tok = mq / p.grp;
+        const int pos = sq.p0 + tok;
+        const uint16_t* qp = p.q + (sq.r0 + tok) * p.ldq + (int64_t)(hk * p.grp + mq % p.grp) * DH;
+        const int lo = p.window > 0 ? pos - p.window : -1;  // the last key before those that the row sees
+
+        u32x4 kreg[kKt][kKv], vreg[kDt];
+        u32x4 kex, vex;
+        int kn, vn;            // valid keys of the two groups (0 if the page is absent)
+        int64_t kbase, vbase;  // slots of their first keys
+        auto page_in = [&](int t, int grp) {
+            const int key = rg.start + kKeys * t + kG * grp;
+            const int i = min(key >> c.page_shift, c.max_pages - 1);  // in the table, where the key is not
+            return c.pages[(int64_t)s * c.ld_pages + i];
+        };
+        auto where = [&](int t, int grp, int page, int& n) {
+            const int key = rg.start + kKeys * t + kG * grp;
+            const bool here = page >= 0 && page < c.n_pages;
+            n = here ? max(min(rg.kend - key, kG), 0) : 0;
+            return slot_of(c, here ? page : 0, hk, key);
+        };
+        auto load_k = [&](int t) {
+            kbase = where(t, rb, kpage, kn);
+            if (FMT != kBf16) kex = *(const u32x4*)(c.ke + kbase);
+#pragma unroll
+            for (int kt = 0; kt < kKt; ++kt)
+#pragma unroll
+                for (int v = 0; v < kKv; ++v)
+                    kreg[kt][v] = __builtin_nontemporal_load(
+                        (const u32x4*)(c.k + (kbase + 4 * kt + rl) * (DH * kEsz<FMT>) + 64 * v + 16 * g));
+            kpage = page_in(t + kFewW, rb);
+        };
+        auto v_at = [&](int dt) {
+            return c.v + ((vbase & ~(int64_t)(kBlk - 1)) * DH + (16 * dt + r16) * kBlk + (vbase & (kBlk - kG))) * kEsz<FMT>;
+        };
+        auto load_v = [&](int t) {
+            vbase = where(t, g, vpage, vn);
+            if (FMT != kBf16) vex = *(const u32x4*)(c.ve + vbase);
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt) vreg[dt] = __builtin_nontemporal_load((const u32x4*)v_at(dt));
+            vpage = page_in(t + kFewW, g);
+        };
+
+        f4_t o[kDt];
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt) o[dt] = f4_t{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.0f;
+        u32x4 qf[kSteps];
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st)
+            qf[st] = ldg16(qp + (FMT == kBf16 ? 32 * st + 8 * g : 64 * (st >> 1) + 16 * g + 8 * (st & 1)));
+        // scores of the loaded tile (raw), and the masks of a tile at an edge
+        auto scores = [&](f4_t (&sc)[kKt]) {
+#pragma unroll
+            for (int kt = 0; kt < kKt; ++kt) {
+                sc[kt] = f4_t{0.f, 0.f, 0.f, 0.f};
+                const float ks = FMT == kBf16 ? 1.0f : exp_float((kex[kt] >> (8 * rl)) & 0xFFu);
+#pragma unroll
+                for (int st = 0; st < kSteps; ++st) {
+                    u32x4 kf;
+                    if (FMT == kBf16) kf = kreg[kt][st];
+                    else kf = cvt8b<kE>(kreg[kt][st / 2][2 * (st & 1)], kreg[kt][st / 2][2 * (st & 1) + 1], ks);
+                    sc[kt] = mfma_bf16(kf, qf[st], sc[kt]);
+                }
+            }
+        };
+        auto is_edge = [&](int kb) {
+            return kb + kKeys - 1 > rg.first || (p.window > 0 && kb <= rg.last - p.window) || __any(vn < kG);
+        };
+        // bit i: key i of this lane's group is seen by its row; keys lo + 1 .. lo +
+        // seen are, if the page is present
+        auto seen_bits = [&](int kb) {
+            const int seen = vn > 0 ? max(min(pos, rg.kend - 1) - lo, 0) : 0, from = kb + kG * g - lo - 1;
+            uint32_t bits = 0;
+#pragma unroll
+            for (int i = 0; i < kG; ++i) bits |= (unsigned)(from + i) < (unsigned)seen ? 1u << i : 0u;
+            return bits;
+        };
+        // a 1 in the top bit of each value that is not finite
+        auto nf = [](uint32_t x) {
+            return FMT == kBf16 ? nonfinite2(x) : ((x & 0x7F7F7F7Fu) + (kE == FP8_E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u;
+        };
+        auto vfrag = [&](u32x4 v, int st) {  // keys 8 st .. 8 st + 7 of this lane's group
+            if (FMT == kBf16) return v;
+            return cvt8b<kE>(v[2 * st & 3], v[(2 * st + 1) & 3], 1.0f);
+        };
+
+        bool hidden = false;  // infinities or NaN among the values of an edge
+        const int tend = te * (kTile / kKeys), tfirst = tb * (kTile / kKeys) + w;
+        int t = tfirst;
+        if (t < tend) {
+            if (tb > 0 || p.flat || p.window > 0) {
+                kpage = page_in(t, rb);
+                vpage = page_in(t, g);
+            }
+            load_k(t);
+            load_v(t);
+        }
+        auto tile = [&](int kb, auto edge) {
+            const bool more = t + kFewW < tend;  // its loads follow the last use of this tile's registers
+            f4_t sc[kKt];
+            scores(sc);
+            if (more) load_k(t + kFewW);
+            if (edge) {
+                const uint32_t bits = seen_bits(kb);
+#pragma unroll
+                for (int i = 0; i < kG; ++i) sc[i >> 2][i & 3] = (bits >> i) & 1u ? sc[i >> 2][i & 3] : -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < kKt; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kt][i]);
+            mx = quad_max(mx);
+            if (__any(mx > m)) {
+                const float mn = fmaxf(m, mx);
+                const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * p.c2);
+                m = mn;
+                l *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
+            }
+            const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
+            u32x4 pf[kPv];
+#pragma unroll
+            for (int kt = 0; kt < kKt; ++kt) {
+                float pr[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][i], p.c2, moff));
+                    l += pr[i];
+                    // an exponent of a masked slot may be anything, its weight is 0
+                    if (FMT != kBf16) pr[i] *= exp_float(min((vex[kt] >> (8 * i)) & 0xFFu, 254u));
+                }
+                pf[kt >> 1][2 * (kt & 1)] = pack_bf16x2(pr[0], pr[1]);
+                pf[kt >> 1][2 * (kt & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
+            }
+            if (!edge) {
+#pragma unroll
+                for (int st = 0; st < kPv; ++st)
+#pragma unroll
+                    for (int dt = 0; dt < kDt; ++dt) o[dt] = mfma_bf16(vfrag(vreg[dt], st), pf[st], o[dt]);
+            } else {
+                uint32_t mk[4], any = 0;
+                token_masks<kG / 4>(vn, mk);  // slots that hold no token may hold NaN
+#pragma unroll
+                for (int dt = 0; dt < kDt; ++dt) {
+                    u32x4 v = vreg[dt];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t x = v[k] & mk[k], bad = nf(x);
+                        any |= bad;
+                        v[k] = x & ~((bad >> (FMT == kBf16 ? 15 : 7)) * (FMT == kBf16 ? 0xFFFFu : 0xFFu));
+                    }
+                    // the finite part here, what the rest adds below
+#pragma unroll
+                    for (int st = 0; st < kPv; ++st) o[dt] = mfma_bf16(vfrag(v, st), pf[st], o[dt]);
+                }
+                hidden = hidden || __any(any);
+            }
+            if (more) load_v(t + kFewW);
+        };
+        for (; t < tend; t += kFewW) {
             const int kb = rg.start + kKeys * t;
-            vbase = where(t, g, page_in(t, g), vn);
-            if (!is_edge(kb)) continue;
-            const uint32_t bits = seen_bits(kb);
-            uint32_t mk[4];
-            token_masks<kG / 4>(vn, mk);
+            tile(kb, is_edge(kb));
+        }
+        if (hidden) {
+#pragma unroll 1
+            for (t = tfirst; t < tend; t += kFewW) {
+                const int kb = rg.start + kKeys * t;
+                vbase = where(t, g, page_in(t, g), vn);
+                if (!is_edge(kb)) continue;
+                const uint32_t bits = seen_bits(kb);
+                uint32_t mk[4];
+                token_masks<kG / 4>(vn, mk);
 #pragma unroll
-            for (int dt = 0; dt < kDt; ++dt) {  // one operand at a time: few registers
-                u32x4 vv = *(const u32x4*)v_at(dt);
+                for (int dt = 0; dt < kDt; ++dt) {  // one operand at a time: few registers
+                    u32x4 vv = *(const u32x4*)v_at(dt);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) vv[k] &= mk[k];
+                    for (int k = 0; k < 4; ++k) vv[k] &= mk[k];
 #pragma unroll
-                for (int st = 0; st < kPv; ++st) {
-                    u32x4 up, down;
-                    split_nonfinite(vfrag(vv, st), up, down);
-                    const u32x4 wm = ones_where(bits >> (8 * st));
-                    const f4_t zero = {0.f, 0.f, 0.f, 0.f};
-                    const f4_t cu = mfma_bf16(up, wm, zero), cd = mfma_bf16(down, wm, zero);
+                    for (int st = 0; st < kPv; ++st) {
+                        u32x4 up, down;
+                        split_nonfinite(vfrag(vv, st), up, down);
+                        const u32x4 wm = ones_where(bits >> (8 * st));
+                        const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+                        const f4_t cu = mfma_bf16(up, wm, zero), cd = mfma_bf16(down, wm, zero);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[dt][i] = add_nonfinite(o[dt][i], cu[i], cd[i]);
+                        for (int i = 0; i < 4; ++i) o[dt][i] = add_nonfinite(o[dt][i], cu[i], cd[i]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
         }
-    }
-    l = quad_sum(l);
-    // join the four waves
+        l = quad_sum(l);
+        // join the waves
 #pragma unroll
-    for (int dt = 0; dt < kDt; ++dt) *(f4_t*)&so[w][r16][16 * dt + 4 * g] = o[dt];
-    if (g == 0) {
-        sm[w][r16] = m;
-        sl[w][r16] = l;
-    }
-    __syncthreads();
-    const int row = tid / kCh, ch = tid % kCh;
-    const bool mine = row < m1;
-    float mm = -INFINITY, acc[8], ll = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-    if (mine) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) mm = fmaxf(mm, sm[k][row]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float* x = &so[k][row][8 * ch];
-            add_part(acc, ll, make_float2(sm[k][row], sl[k][row]), mm, p.c2, *(const float4*)x, *(const float4*)(x + 4));
+        for (int dt = 0; dt < kDt; ++dt) *(f4_t*)&so[w][r16][16 * dt + 4 * g] = o[dt];
+        if (g == 0) {
+            sm[w][r16] = m;
+            sl[w][r16] = l;
         }
-    }
-    bool write = true;
-    if (rg.live > 1) {
-        // [part][item][row]: d_head outputs, (maximum, sum)
-        const int64_t step = (int64_t)items * kFew, at = (int64_t)item * kFew + row;
-        uint64_t* po = (uint64_t*)p.part_o + at * (DH / 2) + 4 * ch;
-        uint64_t* pm = (uint64_t*)p.part_ml + at;
+        __syncthreads();
+        const int row = tid / kCh, ch = tid % kCh;
+        const bool mine = row < m1;
+        float mm = -INFINITY, acc[8], ll = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
         if (mine) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) put_far(po + part * step * (DH / 2) + e, acc[2 * e], acc[2 * e + 1]);
-            if (ch == 0) put_far(pm + part * step, mm, ll);
-        }
-        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");  // they are where every XCD sees them
-        __syncthreads();
-        if (tid == 0) {
-            const int done = __hip_atomic_fetch_add(p.counts + item, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            last = done == rg.live - 1;
-            if (last) __hip_atomic_store(p.counts + item, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        write = last;
-        if (write && mine) {
-            mm = -INFINITY;
-            ll = 0.0f;
+            for (int k = 0; k < kFewW; ++k) mm = fmaxf(mm, sm[k][row]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-            for (int k = 0; k < rg.live; ++k) mm = fmaxf(mm, get_far(pm + k * step).x);
-#pragma unroll 2
-            for (int k = 0; k < rg.live; ++k) {
-                float2 x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = get_far(po + k * step * (DH / 2) + e);
-                add_part(acc, ll, get_far(pm + k * step), mm, p.c2, make_float4(x[0].x, x[0].y, x[1].x, x[1].y),
-                         make_float4(x[2].x, x[2].y, x[3].x, x[3].y));
+            for (int k = 0; k < kFewW; ++k) {
+                const float* x = &so[k][row][8 * ch];
+                add_part(acc, ll, make_float2(sm[k][row], sl[k][row]), mm, p.c2, *(const float4*)x, *(const float4*)(x + 4));
             }
         }
+        bool write = true;
+        if (tb > 0 || te < rg.nt) {
+            // d_head outputs and (maximum, sum) of kFew rows: without `flat` [part][item]; with it
+            // [share][2], the part of an item that starts in the share in 1, of one
+            // that started before in 0
+            const int64_t w0 = p.flat ? f.at / f.per : 0, w1 = p.flat ? (f.at + rg.nt - 1) / f.per : live - 1;
+            uint64_t* po = (uint64_t*)p.part_o + row * (DH / 2) + 4 * ch;
+            uint64_t* pm = (uint64_t*)p.part_ml + row;
+            auto slot = [&](int64_t k) {
+                return (p.flat ? 2 * k + (k == w0) : k * items + s * c.nkv + hk) * kFew;
+            };
+            const int64_t own = slot(p.flat ? blockIdx.x : part);
+            if (mine) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) put_far(po + own * (DH / 2) + e, acc[2 * e], acc[2 * e + 1]);
+                if (ch == 0) put_far(pm + own, mm, ll);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");  // they are where every XCD sees them
+            __syncthreads();
+            if (tid == 0) {
+                int32_t* count = p.counts + (int64_t)s * c.nkv + hk;
+                const int done = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                last = done == w1 - w0;
+                if (last) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            write = last;
+            if (write && mine) {
+                mm = -INFINITY;
+                ll = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+                // eight parts' loads at once: each takes a trip to memory.  (Those
+                // behind the last part read it again, with no weight.)
+                for (int64_t k0 = w0; k0 <= w1; k0 += 8) {
+                    float2 ml[8], x[8][4];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int64_t sl = slot(min(k0 + k, w1));
+                        ml[k] = get_far(pm + sl);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[k][e] = get_far(po + sl * (DH / 2) + e);
+                    }
+                    float top = mm;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (k0 + k > w1) ml[k] = make_float2(-INFINITY, 0.0f);
+                        top = fmaxf(top, ml[k].x);
+                    }
+                    const float f = mm == -INFINITY ? (top == -INFINITY ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f((mm - top) * p.c2);
+                    mm = top;
+                    if (ll != 0.0f) {
+                        ll *= f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) acc[e] *= f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        add_part(acc, ll, ml[k], mm, p.c2, make_float4(x[k][0].x, x[k][0].y, x[k][1].x, x[k][1].y),
+                                 make_float4(x[k][2].x, x[k][2].y, x[k][3].x, x[k][3].y));
+                }
+            }
+        }
+        if (write && mine)
+            mag = max(mag, put8(p, cast, bq, sq.r0 + row / p.grp, (int64_t)(hk * p.grp + row % p.grp) * DH + 8 * ch,
+                                scaled8(acc, ll == 0.0f ? 0.0f : 1.0f / ll)));
+        if (!p.flat) break;
+        at = f.at += rg.nt;
+        if (++f.hk == c.nkv) {  // the next sequence that has tiles
+            f.hk = 0;
+            f.nt = 0;
+            while (f.nt == 0 && ++f.s < c.n_seqs) f.nt = few_tiles(p, f.s);
+        }
+        any = f.nt > 0 && at < end;
+        __syncthreads();  // the next item writes to the shared memory
+        }
+        // items that see no key have no tiles: one share writes their zeros
+        if (p.flat)
+            for (int s = blockIdx.x; s < c.n_seqs; s += gridDim.x) {
+                const Seq sq = seq_of(c, s);
+                const int n = min(sq.n, p.max_rows), cols = p.nh * DH / 8;
+                if (n < 1 || n * p.grp > kFew || few_tiles(p, s) > 0) continue;
+                for (int i = tid; i < n * cols; i += kFewT)
+                    put8(p, cast, bq, sq.r0 + i / cols, 8 * (i % cols), make_uint4(0u, 0u, 0u, 0u));
+            }
+        if (p.q8) {
+            const uint32_t bm = block_max(mag, redm);
+            if (tid == 0) p.parts[blockIdx.x] = bm;
+        }
     }
-    uint32_t mag = 0;
-    if (write && mine)
-        mag = put8(p, cast, bq, sq.r0 + row / p.grp, (int64_t)(hk * p.grp + row % p.grp) * DH + 8 * ch,
-                   scaled8(acc, ll == 0.0f ? 0.0f : 1.0f / ll));
-    if (p.q8) {
-        const uint32_t bm = block_max(mag, redm);
-        if (tid == 0) p.parts[blockIdx.x] = bm;
-    }
-}
 
 // ---- tiles of 128 packed rows
 // Wave w owns packed rows 32 w .. 32 w + 31 of the tile, one per lane pair (the
@@ -1293,8 +1443,8 @@ int32_t launch_cache_read(const CacheView& c, int fmt, int d_head, uint16_t* k, 
 namespace {
 // How a call is split over workgroups, from its sizes alone.
 struct Plan {
-    bool few, many;        // which kernels run
-    int few_parts, few_per;  // parts of an item, tiles of one, at most
+    bool few, many, flat;  // which kernels run, and few_kernel in shares
+    int few_parts;         // or in parts of an item
     int splits, per;       // many_kernel's key ranges, and tiles of each
     int64_t few_wg, many_wg, many_join;
     int64_t parts;
@@ -1308,26 +1458,33 @@ Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t 
     p.many = cap * grp > kFew;
     // sequences of one length have no single tokens among them
     p.few = !p.many || (grp <= kFew && n_seqs > 1 && rows < n_seqs * max_rows);
-    // as many ranges as give `want` workgroups if all sequences were of the
-    // longest length, of at least `least` tiles
-    auto cut = [&](int64_t wg, int64_t want, int64_t least, int* n, int* per) {
-        const int64_t most = (want + wg - 1) / wg;
-        int64_t t = (tiles + most - 1) / most;
-        t = t < least ? least : t;
-        *per = (int)t;
-        *n = (int)((tiles + t - 1) / t);
-        if (*n < 1) *n = 1;
-    };
-    const int64_t items = n_seqs * nkv, wg = (rows * grp / kMany + n_seqs) * nkv;
-    cut(items, items <= kCounts ? kFewWant : 1, kFewLeast, &p.few_parts, &p.few_per);
-    cut(wg, kManyWant, kManyLeast, &p.splits, &p.per);
-    if (!p.many) p.splits = 1;
-    if (!p.few) p.few_parts = 1;
-    p.few_wg = p.few ? items * p.few_parts : 0;
+    const int64_t items = n_seqs * nkv;
+    // few_kernel.  Shares where a compute unit would have much to read and the
+    // items are few enough to be uneven (measured: 32 sequences of up to 16000
+    // tokens, 8 heads, 97 us against 126 with an item a workgroup; but 16 of up to 2500, 32 heads, 78
+    // against 34).  Parts where items would leave compute units idle: about
+    // sqrt(2 tiles) of them, since a part costs the join what half a tile costs
+    // its reader (one of 30000 tokens, 8 heads: 469 tiles, 29 parts 26 us, 64 parts 36).
+    p.flat = p.few && items <= kCounts && n_seqs <= kFlatSeqs && items < 8 * kCus && tiles >= kFlatTiles &&
+             items * tiles >= kShares * kFlatTiles;
+    p.few_parts = 1;
+    if (!p.flat && items < kCus) {
+        const int64_t room = 2 * kCus / items, most = tiles / kFewPart;
+        p.few_parts = (int)(room < most ? room : most);
+        while ((int64_t)p.few_parts * p.few_parts > 2 * tiles) --p.few_parts;
+        if (p.few_parts < 1) p.few_parts = 1;
+    }
+    p.few_wg = !p.few ? 0 : p.flat ? kShares : items * p.few_parts;
+    // many_kernel: as many ranges as give kManyWant workgroups if all sequences
+    // were of the longest length, of at least kManyLeast tiles
+    const int64_t wg = (rows * grp / kMany + n_seqs) * nkv, most = (kManyWant + wg - 1) / wg;
+    p.per = (int)((tiles + most - 1) / most < kManyLeast ? kManyLeast : (tiles + most - 1) / most);
+    p.splits = p.many ? (int)((tiles + p.per - 1) / p.per) : 1;
+    if (p.splits < 1) p.splits = 1;
     p.many_wg = p.many ? wg * p.splits : 0;
     p.many_join = p.splits > 1 ? (rows * nh + kT / (d_head / 8) - 1) / (kT / (d_head / 8)) : 0;
     p.parts = p.few_wg + p.many_wg + p.many_join;
-    const int64_t fs = p.few_parts > 1 ? p.few_parts * items * kFew : 0, ms = p.splits > 1 ? p.splits * rows * nh : 0;
+    const int64_t fs = p.flat ? 2 * kShares * kFew : p.few && p.few_parts > 1 ? p.few_wg * kFew : 0, ms = p.splits > 1 ? p.splits * rows * nh : 0;
     p.words = kCounts * 4;
     p.few_o = (p.words + (1 + p.parts) * 4 + 15) & ~(int64_t)15;
     p.few_ml = p.few_o + fs * d_head * 4;
@@ -1362,7 +1519,8 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
     a.few_on = pl.few;
     a.splits = pl.splits;
     a.per = pl.per;
-    a.few_per = pl.few_per;
+    a.flat = pl.flat;
+    a.few_parts = pl.few_parts;
     a.counts = (int32_t*)base;
     a.c2 = (float)(1.4426950408889634 / sqrt((double)d_head));
     a.o = o;
@@ -1375,9 +1533,9 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
     a.parts = words + 1;
     with_cache(fmt, d_head, [&](auto F, auto D) {
         constexpr int kF = decltype(F)::value, kD = decltype(D)::value;
-        auto go = [&](auto kernel, int64_t wg) {
+        auto go = [&](auto kernel, int64_t wg, int threads = kT) {
             if (wg == 0) return;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(kT), 0, s, a);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(threads), 0, s, a);
             a.parts += wg;
         };
         a.part_o = (float*)(base + pl.many_o);
@@ -1386,7 +1544,7 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
         go(many_join_kernel<kD>, pl.many_join);
         a.part_o = (float*)(base + pl.few_o);
         a.part_ml = (float2*)(base + pl.few_ml);
-        go(few_kernel<kF, kD>, pl.few_wg);
+        go(few_kernel<kF, kD>, pl.few_wg, kFewT);
     });
     int32_t st = hip_status();
     if (st == FP8_OK && quant) {
