@@ -17,6 +17,10 @@ namespace {
 constexpr int kT = 256;       // threads of every kernel here
 constexpr int kBlk = 16;      // tokens of a value block
 constexpr int kBf16 = LLAMA_CACHE_BF16;
+#ifndef BW
+#define BW 4096
+#endif
+constexpr int kBlockWgs = BW;  // workgroups of append and read that heads are grouped for
 
 template <int FMT> constexpr int kEsz = FMT == kBf16 ? 2 : 1;
 
@@ -120,128 +124,162 @@ __device__ __forceinline__ uint32_t codes4(const float* f, int b) {
     return w;
 }
 
-// One workgroup per block of 16 positions and group of heads: each lane holds
-// 8 + 8 values of one (token, head), elements 8 j .. of its two halves, which
-// are what the rotary embedding pairs.  Workgroups below gqk take query and key
-// heads, the others value heads, which they transpose through LDS.
+// A workgroup takes a block of 16 positions and a group of heads, as many (token,
+// head) at a time as it has lanes for (DH / 16 lanes each, 16 values a lane: all
+// tokens of two heads of 128 for a whole block, 32 heads for a single token), with
+// the next ones' loads under way.  Bound by memory once the
+// first loads (sequence, lengths, page, table) are there, which the many
+// workgroups hide from each other: with one pair of heads a workgroup, 2048
+// tokens of 80 heads took 19.8 us, with a group of them HERE.
 template <int FMT, int DH>
-__global__ __launch_bounds__(kT) void append_kernel(CacheView c, const uint16_t* __restrict__ qkv, int64_t ld, int nh,
-                                                    const float2* __restrict__ table, uint16_t* __restrict__ q,
-                                                    int64_t ldq, int gqk) {
-    constexpr int kLanes = DH / 16;                // lanes of one (token, head)
-    constexpr int kHeads = kT / (kBlk * kLanes);   // heads at a time
-    constexpr int kE = FMT == kBf16 ? 1 : FMT;     // a format for the code that bf16 does not run
-    __shared__ __attribute__((aligned(16))) uint8_t vt[kHeads * DH * kBlk * kEsz<FMT>];
-    Block b;
-    if (!block_of(c, blockIdx.x, &b)) return;
-    const int tid = threadIdx.x, j = tid % kLanes, t = (tid / kLanes) % kBlk, hs = tid / (kLanes * kBlk);
-    const int pos = b.b0 + t;
-    const bool live = t >= b.t0 && t < b.t1;
-    const int page = b.b0 < 0 ? -1 : page_of(c, b.s, b.b0);  // one page: page sizes are multiples of 16
-    const uint16_t* xr = qkv + (b.row + t) * ld;
-    if ((int)blockIdx.y < gqk) {
-        const int h = blockIdx.y * kHeads + hs;
-        if (!live || h >= nh + c.nkv) return;  // whole groups of kLanes lanes leave together
-        if (h < nh && !q) return;
-        const uint16_t* x = xr + (int64_t)h * DH + 8 * j;
-        const uint4 lo = ld16(x), hi = ld16(x + DH / 2);
-        const uint32_t aw[4] = {lo.x, lo.y, lo.z, lo.w}, bw[4] = {hi.x, hi.y, hi.z, hi.w};
-        float f0[8], f1[8];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            f0[2 * k] = lo_f(aw[k]);
-            f0[2 * k + 1] = hi_f(aw[k]);
-            f1[2 * k] = lo_f(bw[k]);
-            f1[2 * k + 1] = hi_f(bw[k]);
-        }
-        if (table && page >= 0) {  // absent positions are not in the table, and not stored
-            const float2* cs = table + (int64_t)pos * (DH / 2) + 8 * j;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float2 e = cs[k];
-                // In fp64, where the products are exact: a difference that
-                // cancels lands on the right side of the border between two
-                // codes.  The kernel waits for memory, not for this.
-                const double a = f0[k], d = f1[k];
-                f0[k] = (float)(a * e.x - d * e.y);
-                f1[k] = (float)(d * e.x + a * e.y);
-            }
-        }
-        if (h < nh) {
-            uint16_t* o = q + (b.row + t) * ldq + (int64_t)h * DH + 8 * j;
-            uint4 u = make_uint4(0u, 0u, 0u, 0u), w = u;
-            if (page >= 0) {
-                u = make_uint4(pack_bf16x2(f0[0], f0[1]), pack_bf16x2(f0[2], f0[3]), pack_bf16x2(f0[4], f0[5]), pack_bf16x2(f0[6], f0[7]));
-                w = make_uint4(pack_bf16x2(f1[0], f1[1]), pack_bf16x2(f1[2], f1[3]), pack_bf16x2(f1[4], f1[5]), pack_bf16x2(f1[6], f1[7]));
-            }
-            st16(o, u);
-            st16(o + DH / 2, w);
-            return;
-        }
-        if (page < 0) return;
-        const int64_t slot = slot_of(c, page, h - nh, pos);
-        if (FMT == kBf16) {
-            uint16_t* o = (uint16_t*)c.k + slot * DH + 8 * j;
-            st16(o, make_uint4(pack_bf16x2(f0[0], f0[1]), pack_bf16x2(f0[2], f0[3]), pack_bf16x2(f0[4], f0[5]), pack_bf16x2(f0[6], f0[7])));
-            st16(o + DH / 2, make_uint4(pack_bf16x2(f1[0], f1[1]), pack_bf16x2(f1[2], f1[3]), pack_bf16x2(f1[4], f1[5]), pack_bf16x2(f1[6], f1[7])));
-            return;
-        }
-        uint32_t mag = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) mag = max(mag, max(__float_as_uint(f0[k]) & 0x7FFFFFFFu, __float_as_uint(f1[k]) & 0x7FFFFFFFu));
+struct Append {
+    static constexpr int kLanes = DH / 16;                // lanes of one (token, head)
+    static constexpr int kUnits = kT / kLanes;            // (token, head) at a time
+    static constexpr int kE = FMT == kBf16 ? 1 : FMT;     // a format for the code that bf16 does not run
+
+    // Largest magnitude pattern over the lanes of a (token, head), as a bias.
+    static __device__ __forceinline__ int bias(uint32_t mag) {
 #pragma unroll
         for (int off = 1; off < kLanes; off <<= 1) mag = max(mag, (uint32_t)__shfl_xor((int)mag, off, 64));
-        const int bias = row_bias<kE>(mag);
-        uint8_t* o = c.k + slot * DH + 8 * j;
-        *(uint2*)o = make_uint2(codes4<kE>(f0, bias), codes4<kE>(f0 + 4, bias));
-        *(uint2*)(o + DH / 2) = make_uint2(codes4<kE>(f1, bias), codes4<kE>(f1 + 4, bias));
-        if (j == 0) c.ke[slot] = (uint8_t)(127 - bias);
+        return row_bias<kE>(mag);
+    }
+};
+
+__device__ __forceinline__ void halves(uint4 v, float* f) {  // eight bf16 -> fp32
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        f[2 * k] = lo_f(w[k]);
+        f[2 * k + 1] = hi_f(w[k]);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+__device__ __forceinline__ uint32_t mag_f(const float* f, int n, uint32_t m) {
+#pragma unroll
+    for (int k = 0; k < n; ++k) m = max(m, __float_as_uint(f[k]) & 0x7FFFFFFFu);
+    return m;
+}
+
+// Groups below gqk: heads_qk query and key heads each, others: heads_v value heads.
+template <int FMT, int DH>
+__global__ __launch_bounds__(kT) void append_kernel(CacheView c, const uint16_t* __restrict__ qkv, int64_t ld, int nh,
+                                                    const float2* __restrict__ table, uint16_t* q, int64_t ldq, int gqk,
+                                                    int heads_qk, int heads_v) {
+    using A = Append<FMT, DH>;
+    constexpr int kLanes = A::kLanes, kE = A::kE, kPair = A::kUnits / kBlk;  // heads of a whole block at a time
+    __shared__ __attribute__((aligned(16))) uint8_t vt[kPair * DH * kBlk * kEsz<FMT>];
+    Block b;
+    if (!block_of(c, blockIdx.x, &b)) return;
+    const int tid = threadIdx.x, j = tid % kLanes, unit = tid / kLanes, nt = b.t1 - b.t0;
+    const int per = A::kUnits / nt;  // heads at a time
+    const int hs = unit / nt, t = b.t0 + unit % nt, pos = b.b0 + t;
+    const int page = b.b0 < 0 ? -1 : page_of(c, b.s, b.b0);  // one page: page sizes are multiples of 16
+    const int64_t row = b.row + t;
+    if ((int)blockIdx.y < gqk) {
+        const int first = blockIdx.y * heads_qk + (q ? 0 : nh), end = min(first + heads_qk, nh + c.nkv);
+        if (hs >= per) return;  // lanes of one (token, head) stay together
+        const uint16_t* x = qkv + row * ld + 8 * j;  // elements 8 j .. of the two halves, which the rotation pairs
+        int h = first + hs;
+        if (h >= end) return;
+        uint4 lo = ld16(x + (int64_t)h * DH), hi = ld16(x + (int64_t)h * DH + DH / 2);
+        float2 cs[8];
+        const bool turn = table && page >= 0;  // absent positions are not in the table, and not stored
+        if (turn) {
+            const float4* tp = (const float4*)(table + (int64_t)pos * (DH / 2) + 8 * j);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float4 e = tp[k];
+                cs[2 * k] = make_float2(e.x, e.y);
+                cs[2 * k + 1] = make_float2(e.z, e.w);
+            }
+        }
+        for (; h < end; h += per) {
+            float f0[8], f1[8];
+            halves(lo, f0);
+            halves(hi, f1);
+            if (h + per < end) {
+                lo = ld16(x + (int64_t)(h + per) * DH);
+                hi = ld16(x + (int64_t)(h + per) * DH + DH / 2);
+            }
+            if (turn) {
+                // In fp64, where the products are exact: a difference that cancels
+                // lands on the right side of the border between two codes.
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const double u = f0[k], v = f1[k], co = cs[k].x, si = cs[k].y;
+                    f0[k] = (float)(u * co - v * si);
+                    f1[k] = (float)(v * co + u * si);
+                }
+            }
+            if (h < nh) {
+                uint16_t* o = q + row * ldq + (int64_t)h * DH + 8 * j;
+                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                st16(o, page >= 0 ? pack8(f0) : zero);
+                st16(o + DH / 2, page >= 0 ? pack8(f1) : zero);
+                continue;
+            }
+            if (page < 0) continue;
+            const int64_t slot = slot_of(c, page, h - nh, pos);
+            if (FMT == kBf16) {
+                uint16_t* o = (uint16_t*)c.k + slot * DH + 8 * j;
+                st16(o, pack8(f0));
+                st16(o + DH / 2, pack8(f1));
+                continue;
+            }
+            const int bias = A::bias(mag_f(f1, 8, mag_f(f0, 8, 0u)));
+            uint8_t* o = c.k + slot * DH + 8 * j;
+            *(uint2*)o = make_uint2(codes4<kE>(f0, bias), codes4<kE>(f0 + 4, bias));
+            *(uint2*)(o + DH / 2) = make_uint2(codes4<kE>(f1, bias), codes4<kE>(f1 + 4, bias));
+            if (j == 0) c.ke[slot] = (uint8_t)(127 - bias);
+        }
         return;
     }
-    // value heads: codes of the 16 tokens into LDS as [head][d][16], then out
-    // in the same order
+    // Value heads, 16 consecutive values a lane.  A whole block is transposed
+    // through LDS and leaves as 16-byte (bf16: 32-byte) rows of a dimension; of a
+    // part of a block, each value goes to its place, and the other tokens keep theirs.
     if (page < 0) return;
-    const int hv0 = (blockIdx.y - gqk) * kHeads, hv = hv0 + hs;
-    if (live && hv < c.nkv) {
-        const uint16_t* x = xr + (int64_t)(nh + c.nkv + hv) * DH + 16 * j;
-        const uint4 lo = ld16(x), hi = ld16(x + 8);
-        const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-        uint8_t* row = vt + (hs * DH + 16 * j) * kBlk * kEsz<FMT>;
-        if (FMT == kBf16) {
+    const int first = (blockIdx.y - gqk) * heads_v, end = min(first + heads_v, c.nkv);
+    const uint16_t* x = qkv + row * ld + (int64_t)(nh + c.nkv) * DH + 16 * j;
+    const bool whole = nt == kBlk;
+    for (int h0 = first; h0 < end; h0 += per) {
+        const int h = h0 + hs;
+        const bool live = hs < per && h < end;
+        if (live) {
+            const uint4 lo = ld16(x + (int64_t)h * DH), hi = ld16(x + (int64_t)h * DH + 8);
+            const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            const int64_t slot = slot_of(c, page, h, pos);
+            // the lane's first dimension of this token, in LDS or in the cache
+            uint8_t* dst = whole ? vt + ((hs * DH + 16 * j) * kBlk + t) * kEsz<FMT>
+                                 : c.v + ((slot - t) * DH + 16 * j * kBlk + t) * kEsz<FMT>;
+            if (FMT == kBf16) {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) ((uint16_t*)row)[k * kBlk + t] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
-        } else {
-            float f[16];
-            uint32_t mag = 0;
+                for (int k = 0; k < 16; ++k) ((uint16_t*)dst)[k * kBlk] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+            } else {
+                float f[16];
+                halves(lo, f);
+                halves(hi, f + 8);
+                const int bias = A::bias(mag_f(f, 16, 0u));
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                f[k] = k & 1 ? hi_f(w[k >> 1]) : lo_f(w[k >> 1]);
-                mag = max(mag, __float_as_uint(f[k]) & 0x7FFFFFFFu);
+                for (int k = 0; k < 16; k += 4) {
+                    const uint32_t cw = codes4<kE>(f + k, bias);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dst[(k + e) * kBlk] = (uint8_t)(cw >> (8 * e));
+                }
+                if (j == 0) c.ve[slot] = (uint8_t)(127 - bias);
             }
-#pragma unroll
-            for (int off = 1; off < kLanes; off <<= 1) mag = max(mag, (uint32_t)__shfl_xor((int)mag, off, 64));
-            const int bias = row_bias<kE>(mag);
-#pragma unroll
-            for (int k = 0; k < 16; k += 4) {
-                const uint32_t cw = codes4<kE>(f + k, bias);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) row[(k + e) * kBlk + t] = (uint8_t)(cw >> (8 * e));
-            }
-            if (j == 0) c.ve[slot_of(c, page, hv, pos)] = (uint8_t)(127 - bias);
         }
-    }
-    __syncthreads();
-    const int d = tid % DH, hd = tid / DH;  // one row of 16 tokens per thread: kHeads * DH = kT
-    if (hv0 + hd >= c.nkv) return;
-    const uint8_t* src = vt + tid * kBlk * kEsz<FMT>;
-    uint8_t* dst = c.v + (slot_of(c, page, hv0 + hd, b.b0) * DH + d * kBlk) * kEsz<FMT>;
-    if (b.t0 == 0 && b.t1 == kBlk) {
-        st16(dst, ld16(src));
-        if (FMT == kBf16) st16(dst + 16, ld16(src + 16));
-    } else {  // the other tokens of the block keep their values
-        for (int k = b.t0; k < b.t1; ++k) {
-            if (FMT == kBf16) ((uint16_t*)dst)[k] = ((const uint16_t*)src)[k];
-            else dst[k] = src[k];
+        if (whole) {
+            __syncthreads();
+            const int d = tid % DH, hd = h0 + tid / DH;  // one row of 16 tokens per thread
+            if (hd < end) {
+                const uint8_t* src = vt + tid * kBlk * kEsz<FMT>;
+                uint8_t* dst = c.v + (slot_of(c, page, hd, b.b0) * DH + d * kBlk) * kEsz<FMT>;
+                st16(dst, ld16(src));
+                if (FMT == kBf16) st16(dst + 16, ld16(src + 16));
+            }
+            __syncthreads();
         }
     }
 }
@@ -263,73 +301,92 @@ __device__ __forceinline__ void decode4(uint32_t w, float* f) {
 __device__ __forceinline__ float unscale_of(uint32_t e) { return ldexpf(e == 255u ? __builtin_nanf("") : 1.0f, (int)e - 127); }
 
 // ------------------------------------------------------------- read
-// The same blocks and head groups; blockIdx.y below gk reads keys (each lane 16
-// values of one token), the others values through the transpose.
+// The same blocks; groups of `heads` heads, keys below gk, then values.  A
+// workgroup reads whole blocks of as many heads as it has lanes for, the next
+// ones' loads under way: keys as they lie, values through a transpose in LDS.
 template <int FMT, int DH>
 __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restrict__ ko, int64_t ldk,
-                                                  uint16_t* __restrict__ vo, int64_t ldv, int gk) {
-    constexpr int kLanes = DH / 16, kHeads = kT / (kBlk * kLanes);
-    constexpr int kE = FMT == kBf16 ? 1 : FMT;
-    __shared__ __attribute__((aligned(16))) uint8_t vt[kHeads * DH * kBlk * kEsz<FMT>];
+                                                  uint16_t* __restrict__ vo, int64_t ldv, int gk, int heads) {
+    constexpr int kLanes = DH / 16, kPair = kT / (kBlk * kLanes);
+    constexpr int kE = FMT == kBf16 ? 1 : FMT, kV = kEsz<FMT>;  // vectors of a lane
+    __shared__ __attribute__((aligned(16))) uint8_t vt[kPair * DH * kBlk * kEsz<FMT>];
     Block b;
     if (!block_of(c, blockIdx.x, &b)) return;
     const bool keys = (int)blockIdx.y < gk;
-    const int h0 = (keys ? blockIdx.y : blockIdx.y - gk) * kHeads;
-    const int tid = threadIdx.x, j = tid % kLanes, t = (tid / kLanes) % kBlk, hs = tid / (kLanes * kBlk), h = h0 + hs;
+    const int first = (keys ? blockIdx.y : blockIdx.y - gk) * heads, end = min(first + heads, c.nkv);
+    const int tid = threadIdx.x, j = tid % kLanes, t = (tid / kLanes) % kBlk, hs = tid / (kLanes * kBlk);
     const int page = b.b0 < 0 ? -1 : page_of(c, b.s, b.b0);
-    const bool live = t >= b.t0 && t < b.t1 && h < c.nkv;
-    if (!keys && page >= 0) {
-        const int d = tid % DH, hd = tid / DH;
-        if (h0 + hd < c.nkv) {
-            const uint8_t* src = c.v + (slot_of(c, page, h0 + hd, b.b0) * DH + d * kBlk) * kEsz<FMT>;
-            uint8_t* dst = vt + tid * kBlk * kEsz<FMT>;
-            st16(dst, ld16(src));
-            if (FMT == kBf16) st16(dst + 16, ld16(src + 16));
-        }
+    const bool live = t >= b.t0 && t < b.t1;
+    uint16_t* out = (keys ? ko + (b.row + t) * ldk : vo + (b.row + t) * ldv) + 16 * j;
+    if (page < 0) {  // absent: zeros
+        for (int h = first + hs; h < end; h += kPair)
+            if (live) {
+                st16(out + (int64_t)h * DH, make_uint4(0u, 0u, 0u, 0u));
+                st16(out + (int64_t)h * DH + 8, make_uint4(0u, 0u, 0u, 0u));
+            }
+        return;
     }
-    __syncthreads();
-    if (!live) return;
-    uint16_t* o = (keys ? ko + (b.row + t) * ldk : vo + (b.row + t) * ldv) + (int64_t)h * DH + 16 * j;
-    uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-    if (page >= 0) {
-        const int64_t slot = slot_of(c, page, h, b.b0 + t);
-        const uint8_t* row = vt + (hs * DH + 16 * j) * kBlk * kEsz<FMT>;
+    // what this lane loads of a block: 16 dimensions of its token's key, or the 16
+    // tokens of dimension tid % DH of head tid / DH
+    const int ls = keys ? hs : tid / DH;
+    const int at = keys ? t * DH + 16 * j : (tid % DH) * kBlk;
+    const uint8_t* src = (keys ? c.k : c.v) + at * kEsz<FMT>;
+    const uint8_t* exps = keys ? c.ke : c.ve;
+    auto load = [&](int h0, uint4 (&v)[kV], uint32_t& e) {  // a head past the last one: the last one again
+        const int64_t slot = slot_of(c, page, min(h0 + ls, end - 1), b.b0);
+#pragma unroll
+        for (int k = 0; k < kV; ++k) v[k] = ld16(src + slot * DH * kEsz<FMT> + 16 * k);
+        if (FMT != kBf16) e = exps[slot_of(c, page, min(h0 + hs, end - 1), b.b0 + t)];
+    };
+    uint4 v[kV];
+    uint32_t e = 0;
+    load(first, v, e);
+    for (int h0 = first; h0 < end; h0 += kPair) {
+        uint4 x[kV];
+        const uint32_t ex = e;
+#pragma unroll
+        for (int k = 0; k < kV; ++k) x[k] = v[k];
+        if (h0 + kPair < end) load(h0 + kPair, v, e);
+        if (!keys) {
+#pragma unroll
+            for (int k = 0; k < kV; ++k) st16(vt + tid * kBlk * kEsz<FMT> + 16 * k, x[k]);
+            __syncthreads();
+            const uint8_t* col = vt + ((hs * DH + 16 * j) * kBlk + t) * kEsz<FMT>;
+            uint32_t w[4 * kV];
+            if (FMT == kBf16) {
+#pragma unroll
+                for (int k = 0; k < 4 * kV; ++k)
+                    w[k] = ((const uint16_t*)col)[2 * k * kBlk] | ((uint32_t)((const uint16_t*)col)[(2 * k + 1) * kBlk] << 16);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4 * kV; ++k)
+                    w[k] = col[4 * k * kBlk] | ((uint32_t)col[(4 * k + 1) * kBlk] << 8) |
+                           ((uint32_t)col[(4 * k + 2) * kBlk] << 16) | ((uint32_t)col[(4 * k + 3) * kBlk] << 24);
+            }
+#pragma unroll
+            for (int k = 0; k < kV; ++k) x[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+            __syncthreads();
+        }
+        const int h = h0 + hs;
+        if (!live || h >= end) continue;
+        uint4 o0, o1;
         if (FMT == kBf16) {
-            if (keys) {
-                const uint16_t* p = (const uint16_t*)c.k + slot * DH + 16 * j;
-                const uint4 a = ld16(p), e = ld16(p + 8);
-                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-                w[4] = e.x; w[5] = e.y; w[6] = e.z; w[7] = e.w;
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    w[k] = ((const uint16_t*)row)[2 * k * kBlk + t] | ((uint32_t)((const uint16_t*)row)[(2 * k + 1) * kBlk + t] << 16);
-            }
+            o0 = x[0];
+            o1 = x[kV - 1];
         } else {
-            uint32_t cw[4];
-            if (keys) {
-                const uint4 a = ld16(c.k + slot * DH + 16 * j);
-                cw[0] = a.x; cw[1] = a.y; cw[2] = a.z; cw[3] = a.w;
-            } else {
+            const float sc = unscale_of(ex);
+            const uint32_t cw[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
+            float f[16];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    cw[k] = 0;
+            for (int k = 0; k < 4; ++k) decode4<kE>(cw[k], f + 4 * k);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) cw[k] |= (uint32_t)row[(4 * k + e) * kBlk + t] << (8 * e);
-                }
-            }
-            const float sc = unscale_of(keys ? c.ke[slot] : c.ve[slot]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float f[4];
-                decode4<kE>(cw[k], f);
-                w[2 * k] = pack_bf16x2(f[0] * sc, f[1] * sc);
-                w[2 * k + 1] = pack_bf16x2(f[2] * sc, f[3] * sc);
-            }
+            for (int k = 0; k < 16; ++k) f[k] *= sc;
+            o0 = pack8(f);
+            o1 = pack8(f + 8);
         }
+        st16(out + (int64_t)h * DH, o0);
+        st16(out + (int64_t)h * DH + 8, o1);
     }
-    st16(o, make_uint4(w[0], w[1], w[2], w[3]));
-    st16(o + 8, make_uint4(w[4], w[5], w[6], w[7]));
 }
 
 // ------------------------------------------------------------- attention
@@ -1417,25 +1474,36 @@ void with_cache(int fmt, int d_head, Fn&& fn) {
 
 namespace fp8lin {
 
+// Heads of a group, so that about kBlockWgs workgroups run: a multiple of `per`, the
+// heads that a workgroup takes of a whole block at a time.
+static int group_heads(int64_t slots, int heads, int per) {
+    const int64_t groups = slots < kBlockWgs ? kBlockWgs / slots : 1;
+    const int64_t h = (heads + groups - 1) / groups;
+    return (int)((h + per - 1) / per * per);
+}
+
 int32_t launch_cache_append(const uint16_t* qkv, int64_t ld, int nh, const CacheView& c, int fmt, int d_head,
                             const float* table, uint16_t* q, int64_t ldq, hipStream_t s) {
-    const int per = kT / d_head;  // heads of one workgroup
-    const int gqk = (nh + c.nkv + per - 1) / per, gv = (c.nkv + per - 1) / per;
-    const dim3 grid((unsigned)block_slots(c.rows, c.n_seqs), (unsigned)(gqk + gv));
+    const int per = kT / d_head, qk = (q ? nh : 0) + c.nkv;
+    const int64_t slots = block_slots(c.rows, c.n_seqs);
+    const int hqk = group_heads(slots, qk + c.nkv, per), hv = hqk < c.nkv ? hqk : (c.nkv + per - 1) / per * per;
+    const int gqk = (qk + hqk - 1) / hqk, gv = (c.nkv + hv - 1) / hv;
+    const dim3 grid((unsigned)slots, (unsigned)(gqk + gv));
     with_cache(fmt, d_head, [&](auto F, auto D) {
         hipLaunchKernelGGL((append_kernel<decltype(F)::value, decltype(D)::value>), grid, dim3(kT), 0, s, c, qkv, ld, nh,
-                           (const float2*)table, q, ldq, gqk);
+                           (const float2*)table, q, ldq, gqk, hqk, hv);
     });
     return hip_status();
 }
 
 int32_t launch_cache_read(const CacheView& c, int fmt, int d_head, uint16_t* k, int64_t ldk, uint16_t* v, int64_t ldv,
                           hipStream_t s) {
-    const int per = kT / d_head, g = (c.nkv + per - 1) / per;
-    const dim3 grid((unsigned)block_slots(c.rows, c.n_seqs), (unsigned)((k ? g : 0) + (v ? g : 0)));
+    const int64_t slots = block_slots(c.rows, c.n_seqs);
+    const int h = group_heads(slots, 2 * c.nkv, kT / d_head), g = (c.nkv + h - 1) / h;
+    const dim3 grid((unsigned)slots, (unsigned)((k ? g : 0) + (v ? g : 0)));
     with_cache(fmt, d_head, [&](auto F, auto D) {
         hipLaunchKernelGGL((read_kernel<decltype(F)::value, decltype(D)::value>), grid, dim3(kT), 0, s, c, k, ldk, v, ldv,
-                           k ? g : 0);
+                           k ? g : 0, h);
     });
     return hip_status();
 }
