@@ -113,6 +113,10 @@ __device__ __forceinline__ int row_bias(uint32_t mag) {
     return min(bias_of<FMT>(mag, 0, &fl), 126);
 }
 
+// Place of row r (of 16 tokens) in the LDS copy of a value block: a row's space is
+// left out after every 16, so that lanes on rows 16 apart are on other banks.
+__host__ __device__ constexpr int vt_row(int r) { return r + (r >> 4); }
+
 // Four fp32 values -> four codes with bias b.
 template <int FMT>
 __device__ __forceinline__ uint32_t codes4(const float* f, int b) {
@@ -169,7 +173,7 @@ __global__ __launch_bounds__(kT) void append_kernel(CacheView c, const uint16_t*
                                                     int heads_qk, int heads_v) {
     using A = Append<FMT, DH>;
     constexpr int kLanes = A::kLanes, kE = A::kE, kPair = A::kUnits / kBlk;  // heads of a whole block at a time
-    __shared__ __attribute__((aligned(16))) uint8_t vt[kPair * DH * kBlk * kEsz<FMT>];
+    __shared__ __attribute__((aligned(16))) uint8_t vt[vt_row(kPair * DH) * kBlk * kEsz<FMT>];
     Block b;
     if (!block_of(c, blockIdx.x, &b)) return;
     const int tid = threadIdx.x, j = tid % kLanes, unit = tid / kLanes, nt = b.t1 - b.t0;
@@ -251,7 +255,7 @@ __global__ __launch_bounds__(kT) void append_kernel(CacheView c, const uint16_t*
             const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             const int64_t slot = slot_of(c, page, h, pos);
             // the lane's first dimension of this token, in LDS or in the cache
-            uint8_t* dst = whole ? vt + ((hs * DH + 16 * j) * kBlk + t) * kEsz<FMT>
+            uint8_t* dst = whole ? vt + (vt_row(hs * DH + 16 * j) * kBlk + t) * kEsz<FMT>
                                  : c.v + ((slot - t) * DH + 16 * j * kBlk + t) * kEsz<FMT>;
             if (FMT == kBf16) {
 #pragma unroll
@@ -274,7 +278,7 @@ __global__ __launch_bounds__(kT) void append_kernel(CacheView c, const uint16_t*
             __syncthreads();
             const int d = tid % DH, hd = h0 + tid / DH;  // one row of 16 tokens per thread
             if (hd < end) {
-                const uint8_t* src = vt + tid * kBlk * kEsz<FMT>;
+                const uint8_t* src = vt + vt_row(tid) * kBlk * kEsz<FMT>;
                 uint8_t* dst = c.v + (slot_of(c, page, hd, b.b0) * DH + d * kBlk) * kEsz<FMT>;
                 st16(dst, ld16(src));
                 if (FMT == kBf16) st16(dst + 16, ld16(src + 16));
@@ -309,7 +313,7 @@ __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restr
                                                   uint16_t* __restrict__ vo, int64_t ldv, int gk, int heads) {
     constexpr int kLanes = DH / 16, kPair = kT / (kBlk * kLanes);
     constexpr int kE = FMT == kBf16 ? 1 : FMT, kV = kEsz<FMT>;  // vectors of a lane
-    __shared__ __attribute__((aligned(16))) uint8_t vt[kPair * DH * kBlk * kEsz<FMT>];
+    __shared__ __attribute__((aligned(16))) uint8_t vt[vt_row(kPair * DH) * kBlk * kEsz<FMT>];
     Block b;
     if (!block_of(c, blockIdx.x, &b)) return;
     const bool keys = (int)blockIdx.y < gk;
@@ -349,9 +353,9 @@ __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restr
         if (h0 + kPair < end) load(h0 + kPair, v, e);
         if (!keys) {
 #pragma unroll
-            for (int k = 0; k < kV; ++k) st16(vt + tid * kBlk * kEsz<FMT> + 16 * k, x[k]);
+            for (int k = 0; k < kV; ++k) st16(vt + vt_row(tid) * kBlk * kEsz<FMT> + 16 * k, x[k]);
             __syncthreads();
-            const uint8_t* col = vt + ((hs * DH + 16 * j) * kBlk + t) * kEsz<FMT>;
+            const uint8_t* col = vt + (vt_row(hs * DH + 16 * j) * kBlk + t) * kEsz<FMT>;
             uint32_t w[4 * kV];
             if (FMT == kBf16) {
 #pragma unroll
@@ -384,8 +388,9 @@ __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restr
             o0 = pack8(f);
             o1 = pack8(f + 8);
         }
-        st16(out + (int64_t)h * DH, o0);
-        st16(out + (int64_t)h * DH + 8, o1);
+        // streaming stores: 25.0 -> 24.3 us for 16384 tokens of 8 heads
+        __builtin_nontemporal_store(u32x4{o0.x, o0.y, o0.z, o0.w}, (u32x4*)(out + (int64_t)h * DH));
+        __builtin_nontemporal_store(u32x4{o1.x, o1.y, o1.z, o1.w}, (u32x4*)(out + (int64_t)h * DH + 8));
     }
 }
 
