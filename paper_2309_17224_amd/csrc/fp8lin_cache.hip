@@ -1215,13 +1215,29 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
         __syncthreads();
         for (int t = rg.t0; t < rg.t1; ++t) {
             const int buf = (t - rg.t0) & 1;
-            // the next tile into the other buffer, which every wave has finished
-            // reading; after the last tile it is written once more for nothing
+            const uint8_t* Kl = lds + buf * 2 * kKb;
+            const uint8_t* Vl = Kl + kKb;
+            auto kfrag = [&](int ks, int kt) {
+                const int key = 32 * kt + l32;
+                return *(const u32x4*)(Kl + key * DH * 2 + (((2 * ks + h) ^ (key & kKmask)) << 4));
+            };
+            auto vfrag = [&](int dt, int b) {
+                const int dim = 32 * dt + l32;
+                return *(const u32x4*)(Vl + dim * (kTile * 2) + (((2 * b + h) ^ ((dim >> 1) & 7)) << 4));
+            };
+            // The first key operands are under way while the next tile goes into
+            // the other buffer, which every wave has finished reading (after the
+            // last tile it is written once more for nothing), the others while
+            // the first products run.
+            u32x4 kf[kSteps / 2][2];
+#pragma unroll
+            for (int ks = 0; ks < kSteps / 2; ++ks)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) kf[ks][kt] = kfrag(ks, kt);
+            __builtin_amdgcn_sched_barrier(0);
             store(buf ^ 1, finite);
             load(min(t + 2, rg.t1 - 1), page);
             page = page_at(min(t + 3, rg.t1 - 1));
-            const uint8_t* Kl = lds + buf * 2 * kKb;
-            const uint8_t* Vl = Kl + kKb;
             f16_t sc[2];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
@@ -1231,9 +1247,8 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
             for (int ks = 0; ks < kSteps; ++ks)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
-                    const int key = 32 * kt + l32;
-                    const u32x4 kf = *(const u32x4*)(Kl + key * DH * 2 + (((2 * ks + h) ^ (key & kKmask)) << 4));
-                    sc[kt] = mfma32(kf, qf[ks], sc[kt]);
+                    sc[kt] = mfma32(kf[ks % (kSteps / 2)][kt], qf[ks], sc[kt]);
+                    if (ks < kSteps / 2) kf[ks][kt] = kfrag(ks + kSteps / 2, kt);
                 }
             const int4 in4 = *(const int4*)info[buf];
             const int in[4] = {__builtin_amdgcn_readfirstlane(in4.x), __builtin_amdgcn_readfirstlane(in4.y),
@@ -1254,11 +1269,13 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
                     }
                 }
             }
-            auto vfrag = [&](int dt, int b) {
-                const int dim = 32 * dt + l32;
-                return *(const u32x4*)(Vl + dim * (kTile * 2) + (((2 * b + h) ^ ((dim >> 1) & 7)) << 4));
-            };
             if constexpr (finite) {
+                u32x4 vf[2][kDt];  // the first value operands, under way during the softmax
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int dt = 0; dt < kDt; ++dt) vf[b][dt] = vfrag(dt, b);
+                __builtin_amdgcn_sched_barrier(0);
                 float mx = -INFINITY;
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
@@ -1302,7 +1319,10 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
-                    for (int dt = 0; dt < kDt; ++dt) o[dt] = mfma32(vfrag(dt, b), pf[b], o[dt]);
+                    for (int dt = 0; dt < kDt; ++dt) {
+                        o[dt] = mfma32(vf[b & 1][dt], pf[b], o[dt]);
+                        if (b < 2) vf[b][dt] = vfrag(dt, b + 2);
+                    }
             } else {
                 // what infinities and NaN among the values add to the rows that see them
 #pragma unroll 1
