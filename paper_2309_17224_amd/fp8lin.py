@@ -732,7 +732,7 @@ class KVCache:
             self.v_exp = torch.empty(es, dtype=u8, device=dev) if v_exp is None else _shaped(v_exp, "v_exp", es, u8, dev)
         self._c = CacheStruct(_p(self.k), _p(self.v), _p(self.k_exp), _p(self.v_exp), n_pages, n_kv_heads, d_head,
                               page_size, self.fmt)
-        self._ref = ctypes.addressof(self._c)
+        self._ref, self._dev = ctypes.addressof(self._c), self.k.get_device()
 
 
 class CacheSeqs:
@@ -751,22 +751,33 @@ class CacheSeqs:
         self.cu_rows, self.kv_len, self.pages = cu_rows, kv_len, pages
         self.n_seqs, self.max_pages, self.device = n, pages.shape[1], kv_len.device
         self._c = SeqsStruct(_p(cu_rows), _p(kv_len), _p(pages), n, self.max_pages, _ld(pages))
-        self._ref = ctypes.addressof(self._c)
+        self._ref, self._dev = ctypes.addressof(self._c), kv_len.get_device()
 
 
-def _on_device(cache: KVCache, seqs: CacheSeqs, *tensors) -> None:
-    """Every tensor of a call sits on the current GPU (its stream runs the call)."""
-    dev = cache.device
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {dev}, which is not the current GPU")
-    if seqs.device != dev or any(t is not None and t.device != dev for t in tensors):
-        raise ValueError(f"every tensor of the call must be on {dev}")
+_BF16 = torch.bfloat16
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _cols(t: torch.Tensor, name: str, rows: int, cols: int) -> None:
-    _bf16(t, name)
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols:
-        raise ValueError(f"{name}: expected [{rows}, {cols}], got {tuple(t.shape)}")
+def _cache_device(cache: KVCache, seqs: CacheSeqs) -> None:
+    """The cache and the sequences are on the current GPU (its stream runs the call)."""
+    dev = cache._dev
+    if dev < 0 or seqs._dev != dev or _current() != dev:
+        raise ValueError(f"the cache is on {cache.device}, the sequences on {seqs.device}: "
+                         "both must be on the current GPU")
+
+
+def _mat(t: torch.Tensor, name: str, rows: int, cols: int, dev: int) -> int:
+    """Row stride of a bf16 tensor [rows or more, cols] with contiguous rows on GPU
+    dev.  (A call of these is a few microseconds of host work: one look at each
+    property.)"""
+    if t.dtype is not _BF16:
+        raise TypeError(f"{name}: expected bfloat16, got {t.dtype}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] < rows or shape[1] != cols or (stride[1] != 1 and cols > 1):
+        raise ValueError(f"{name}: expected [{rows}, {cols}] with contiguous rows, got {tuple(shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, the cache on GPU {dev}")
+    return stride[0] if shape[0] > 1 else max(cols, 1)
 
 
 def llama_cache_append(qkv, cache: KVCache, seqs: CacheSeqs, n_heads: int, table=None, q=None, stream=None):
@@ -774,16 +785,24 @@ def llama_cache_append(qkv, cache: KVCache, seqs: CacheSeqs, n_heads: int, table
     at least max_pages * page_size positions; None: no rotation) and write keys
     and values into the cache.  qkv: [rows, (n_heads + 2 n_kv_heads) d_head].
     q: [rows, n_heads d_head], may be a view of qkv's query columns.  Returns q."""
+    dev = cache._dev
     rows, dh = qkv.shape[0], cache.d_head
-    _cols(qkv, "qkv", rows, (n_heads + 2 * cache.n_kv_heads) * dh)
-    q = torch.empty((rows, n_heads * dh), dtype=torch.bfloat16, device=qkv.device) if q is None else q
-    _cols(q, "q", rows, n_heads * dh)
-    _on_device(cache, seqs, qkv, table, q)
-    if table is not None and (table.dtype != torch.float32 or not table.is_contiguous()):
-        raise TypeError("table: expected a contiguous float32 tensor")
-    st = lib().llama_cache_append(_p(qkv), rows, _ld(qkv), n_heads, cache._ref, seqs._ref, _p(table),
-                                  table.numel() // dh if table is not None else 0, _p(q), _ld(q), _stream(stream))
-    _check("llama_cache_append", st)
+    ld = _mat(qkv, "qkv", rows, (n_heads + 2 * cache.n_kv_heads) * dh, dev)
+    if q is None:
+        q = torch.empty((rows, n_heads * dh), dtype=_BF16, device=qkv.device)
+    ldq = _mat(q, "q", rows, n_heads * dh, dev)
+    tp, tn = None, 0
+    if table is not None:
+        if table.dtype is not torch.float32 or not table.is_contiguous():
+            raise TypeError("table: expected a contiguous float32 tensor")
+        if table.get_device() != dev:
+            raise ValueError(f"table: on {table.device}, the cache on GPU {dev}")
+        tp, tn = table.data_ptr(), table.numel() // dh
+    _cache_device(cache, seqs)
+    st = lib().llama_cache_append(qkv.data_ptr(), rows, ld, n_heads, cache._ref, seqs._ref, tp, tn, q.data_ptr(), ldq,
+                                  _stream(stream))
+    if st:
+        _check("llama_cache_append", st)
     return q
 
 
@@ -791,19 +810,18 @@ def llama_cache_read(cache: KVCache, seqs: CacheSeqs, rows: int, k=None, v=None,
                      stream=None):
     """Cached keys and values of the positions that the call's rows stand for, as
     bf16 [rows, n_kv_heads d_head].  Returns (k, v)."""
+    dev = cache._dev
     cols = cache.n_kv_heads * cache.d_head
-    bf = dict(dtype=torch.bfloat16, device=cache.device)
     if want_k and k is None:
-        k = torch.empty((rows, cols), **bf)
+        k = torch.empty((rows, cols), dtype=_BF16, device=cache.device)
     if want_v and v is None:
-        v = torch.empty((rows, cols), **bf)
-    for t, name in ((k, "k"), (v, "v")):
-        if t is not None:
-            _cols(t, name, rows, cols)
-    _on_device(cache, seqs, k, v)
-    st = lib().llama_cache_read(cache._ref, seqs._ref, rows, _p(k), _ld(k) if k is not None else 0, _p(v),
-                                _ld(v) if v is not None else 0, _stream(stream))
-    _check("llama_cache_read", st)
+        v = torch.empty((rows, cols), dtype=_BF16, device=cache.device)
+    ldk = _mat(k, "k", rows, cols, dev) if k is not None else 0
+    ldv = _mat(v, "v", rows, cols, dev) if v is not None else 0
+    _cache_device(cache, seqs)
+    st = lib().llama_cache_read(cache._ref, seqs._ref, rows, _p(k), ldk, _p(v), ldv, _stream(stream))
+    if st:
+        _check("llama_cache_read", st)
     return k, v
 
 
@@ -825,19 +843,27 @@ def llama_cache_attention(q, cache: KVCache, seqs: CacheSeqs, n_heads: int, max_
     """Causal grouped-query attention of the call's rows (q [rows, n_heads
     d_head]) over the cache, optionally with the fused quantise of o (its ws is
     this call's).  max_rows: at least the rows of every sequence.  Returns o."""
+    dev = cache._dev
     rows, cols = q.shape[0], n_heads * cache.d_head
-    _cols(q, "q", rows, cols)
-    o = torch.empty((rows, cols), dtype=torch.bfloat16, device=q.device) if o is None else o
-    _cols(o, "o", rows, cols)
+    ldq = _mat(q, "q", rows, cols, dev)
+    if o is None:
+        o = torch.empty((rows, cols), dtype=_BF16, device=q.device)
+    ldo = _mat(o, "o", rows, cols, dev)
+    quant = _NO_QUANT[:-2]
+    _cache_device(cache, seqs)
     if fq is not None:
-        ws = fq.ws
+        ws, quant = fq.ws, fq.args()[:-2]
         if fq.q.shape != (rows, cols) or fq.q.dtype != torch.uint8:
             raise ValueError(f"fq.q: expected uint8 [{rows}, {cols}]")
+        if any(t is not None and t.get_device() != dev for t in (fq.q, fq.bias, fq.bias_pred, fq.amax_bits, fq.flags)):
+            raise ValueError(f"fq: every tensor must be on GPU {dev}")
     elif ws is None:
         ws = cache_attention_workspace(rows, n_heads, cache, seqs, max_rows)
-    _on_device(cache, seqs, q, o, ws)
-    quant = fq.args()[:-2] if fq else _NO_QUANT[:-2]
-    st = lib().llama_cache_attention(_p(q), rows, _ld(q), n_heads, cache._ref, seqs._ref, max_rows, window, _p(o),
-                                     _ld(o), *quant, _p(ws), ws.numel() * ws.element_size(), _stream(stream))
-    _check("llama_cache_attention", st)
+    if ws.get_device() != dev:
+        raise ValueError(f"ws: on {ws.device}, the cache on GPU {dev}")
+    st = lib().llama_cache_attention(q.data_ptr(), rows, ldq, n_heads, cache._ref, seqs._ref, max_rows, window,
+                                     o.data_ptr(), ldo, *quant, ws.data_ptr(), ws.numel() * ws.element_size(),
+                                     _stream(stream))
+    if st:
+        _check("llama_cache_attention", st)
     return o
