@@ -1540,11 +1540,11 @@ struct Plan {
     int few_parts;         // or in parts of an item
     int splits, per;       // many_kernel's key ranges, and tiles of each
     int64_t few_wg, many_wg, many_join;
-    int64_t parts;
+    int64_t parts, room;   // workgroups that write outputs; at most, whatever the window
     // offsets in the workspace, in bytes, behind the counts: words of the quantise, partials of either kernel
     int64_t words, few_o, few_ml, many_o, many_ml, ws_bytes;
 };
-Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t max_rows, int64_t max_len) {
+Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t max_rows, int64_t max_len, int64_t window) {
     Plan p;
     const int64_t grp = nh / nkv, cap = max_rows < rows ? max_rows : rows;
     const int64_t tiles = (max_len + kTile - 1) / kTile;
@@ -1570,16 +1570,22 @@ Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t 
     p.few_wg = !p.few ? 0 : p.flat ? kShares : items * p.few_parts;
     // many_kernel: as many ranges as give kManyWant workgroups if all sequences
     // were of the longest length, of at least kManyLeast tiles
-    const int64_t wg = (rows * grp / kMany + n_seqs) * nkv, most = (kManyWant + wg - 1) / wg;
-    p.per = (int)((tiles + most - 1) / most < kManyLeast ? kManyLeast : (tiles + most - 1) / most);
-    p.splits = p.many ? (int)((tiles + p.per - 1) / p.per) : 1;
-    if (p.splits < 1) p.splits = 1;
+    const int64_t wg = (rows * grp / kMany + n_seqs) * nkv;
+    int64_t seen = tiles;  // of a tile of rows
+    if (window > 0 && (window + kMany / grp) / kTile + 2 < tiles) seen = (window + kMany / grp) / kTile + 2;
+    int64_t most = (kManyWant + wg - 1) / wg, least = tiles / kManyLeast;  // the workspace is for any window
+    most = most < least ? most : least;
+    most = most < 1 || !p.many ? 1 : most;
+    p.per = (int)((seen + most - 1) / most < kManyLeast ? kManyLeast : (seen + most - 1) / most);
+    p.splits = (int)((seen + p.per - 1) / p.per);
+    if (p.splits < 1 || !p.many) p.splits = 1;
     p.many_wg = p.many ? wg * p.splits : 0;
     p.many_join = p.splits > 1 ? (rows * nh + kT / (d_head / 8) - 1) / (kT / (d_head / 8)) : 0;
     p.parts = p.few_wg + p.many_wg + p.many_join;
-    const int64_t fs = p.flat ? 2 * kShares * kFew : p.few && p.few_parts > 1 ? p.few_wg * kFew : 0, ms = p.splits > 1 ? p.splits * rows * nh : 0;
+    p.room = p.few_wg + (p.many ? wg * most : 0) + (most > 1 ? (rows * nh + kT / (d_head / 8) - 1) / (kT / (d_head / 8)) : 0);
+    const int64_t fs = p.flat ? 2 * kShares * kFew : p.few && p.few_parts > 1 ? p.few_wg * kFew : 0, ms = most > 1 ? most * rows * nh : 0;
     p.words = kCounts * 4;
-    p.few_o = (p.words + (1 + p.parts) * 4 + 15) & ~(int64_t)15;
+    p.few_o = (p.words + (1 + p.room) * 4 + 15) & ~(int64_t)15;
     p.few_ml = p.few_o + fs * d_head * 4;
     p.many_o = p.few_ml + fs * 8;
     p.many_ml = p.many_o + ms * d_head * 4;
@@ -1590,15 +1596,15 @@ Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t 
 
 CacheAttnPlan cache_attn_plan(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t max_rows,
                               int64_t max_len) {
-    const Plan p = plan_of(rows, nh, nkv, d_head, n_seqs, max_rows, max_len);
-    return CacheAttnPlan{p.parts, p.ws_bytes};
+    const Plan p = plan_of(rows, nh, nkv, d_head, n_seqs, max_rows, max_len, 0);
+    return CacheAttnPlan{p.room, p.ws_bytes};
 }
 
 int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const CacheView& c, int fmt, int d_head,
                                int64_t max_rows, int64_t window, uint16_t* o, int64_t ldo, const FusedQuant* fq,
                                void* ws, hipStream_t s) {
     const bool quant = fq && fq->q;
-    const Plan pl = plan_of(c.rows, nh, c.nkv, d_head, c.n_seqs, max_rows, (int64_t)c.max_pages << c.page_shift);
+    const Plan pl = plan_of(c.rows, nh, c.nkv, d_head, c.n_seqs, max_rows, (int64_t)c.max_pages << c.page_shift, window);
     char* base = (char*)ws;
     uint32_t* words = (uint32_t*)(base + pl.words);
     AttnArgs a;
