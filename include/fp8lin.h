@@ -651,8 +651,8 @@ int32_t llama_cache_read(const llama_cache *cache, const llama_cache_seqs *seqs,
  *        joined.  Calls that may run at the same time need separate workspaces.
  * Softmax statistics and sums in fp32; the probabilities are rounded to bf16
  * for the product with the values, and o is rounded once.  The key ranges
- * depend on the sizes of the call alone (n_heads, rows, n_seqs, max_rows,
- * max_pages) and on a sequence's own length: a call gives the same bits every
+ * depend on the sizes of the call (n_heads, rows, n_seqs, max_rows, max_pages,
+ * window) and on the lengths, never on timing: a call gives the same bits every
  * time.
  */
 #define LLAMA_CACHE_WS_COUNTS 65536

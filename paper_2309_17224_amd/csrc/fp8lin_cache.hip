@@ -17,10 +17,10 @@ namespace {
 constexpr int kT = 256;       // threads of every kernel here
 constexpr int kBlk = 16;      // tokens of a value block
 constexpr int kBf16 = LLAMA_CACHE_BF16;
-#ifndef BW
-#define BW 4096
-#endif
-constexpr int kBlockWgs = BW;  // workgroups of append and read that heads are grouped for
+// Workgroups of append and read that heads are grouped for: 4096 (64 single tokens
+// of 80 heads 5.9 us, read of 2464 tokens of 2 x 32 heads 15.0; with 2048: 5.3 and 17.1, with
+// 8192: 8.3 and 14.3).
+constexpr int kBlockWgs = 4096;
 
 template <int FMT> constexpr int kEsz = FMT == kBf16 ? 2 : 1;
 
@@ -133,8 +133,8 @@ __device__ __forceinline__ uint32_t codes4(const float* f, int b) {
 // tokens of two heads of 128 for a whole block, 32 heads for a single token), with
 // the next ones' loads under way.  Bound by memory once the
 // first loads (sequence, lengths, page, table) are there, which the many
-// workgroups hide from each other: with one pair of heads a workgroup, 2048
-// tokens of 80 heads took 19.8 us, with a group of them HERE.
+// workgroups hide from each other.  Measured: 2048 tokens of 80 heads in 17.9 us
+// (80 MB at 4.5 TB/s), 64 single tokens in 5.9 us, one in 3.8 us.
 template <int FMT, int DH>
 struct Append {
     static constexpr int kLanes = DH / 16;                // lanes of one (token, head)
@@ -400,10 +400,10 @@ __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restr
 // kernels, both with the scores transposed (S^T = K . Q^T, then O^T += V^T . P^T),
 // so that the probabilities a lane holds are already the operand of the second
 // product:
-//   few_kernel   up to 16 packed rows (single tokens): each wave takes tiles of
+//   few_body   up to 16 packed rows (single tokens): each wave takes tiles of
 //                64 keys on its own, keys and values from memory straight into
 //                the operand registers; bound by reading the cache;
-//   many_kernel  tiles of 128 packed rows: keys and values through LDS, there in
+//   many_body  tiles of 128 packed rows: keys and values through LDS, there in
 //                bf16; bound by the matrix cores and the exponentials.
 // FP8 codes become bf16 exactly (v_cvt_scalef32_pk_bf16_*).  Both products run
 // on the bf16 matrix instructions: those of FP8 operands keep about 14 bits of
@@ -412,20 +412,20 @@ __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restr
 // conversion; a value's multiplies its probability, whose lanes are along keys.
 //
 // The key range of a tile of rows can be split over several workgroups, which
-// leave (maximum, sum, unnormalised output) in fp32 for combine_kernel.
+// leave (maximum, sum, unnormalised output) in fp32: few_body's are joined by the
+// workgroup that ends last, many_body's by many_join_kernel.
 typedef float f16_t __attribute__((ext_vector_type(16)));
 
-constexpr int kFew = 16;      // packed rows of few_kernel
+constexpr int kFew = 16;      // packed rows of few_body
 constexpr int kFewW = 4, kFewT = 64 * kFewW;  // its waves and threads
-constexpr int kMany = 128;    // packed rows of a workgroup of many_kernel
+constexpr int kMany = 128;    // packed rows of a workgroup of many_body
 constexpr int kTile = 64;     // keys of a tile
-#ifndef MW
-#define MW 512
-#define ML 8
-#endif
-constexpr int kManyWant = MW, kManyLeast = ML;
+// many_body: workgroups that key ranges are cut for (two on a compute unit: 512 tokens
+// over 8192 before them, 64 heads in groups of 8, take 201 us with 1024 and 188 with
+// 512), and tiles of a range at least.
+constexpr int kManyWant = 512, kManyLeast = 8;
 constexpr int kCus = 256;          // compute units
-constexpr int kShares = 512;       // workgroups of few_kernel that run at once
+constexpr int kShares = 512;       // workgroups of few_body that run at once
 constexpr int kShareLeast = 8;     // tiles of a share at least
 constexpr int kFlatTiles = 64;     // of a share, if all sequences were of the longest length, for shares to be worth it
 constexpr int kFlatSeqs = 1024;    // sequences that a workgroup counts through
@@ -439,9 +439,9 @@ struct AttnArgs {
     int nh, grp;
     int max_rows;
     int window;           // 0: none
-    int few_on;           // few_kernel takes the sequences of up to kFew packed rows
-    int splits, per;      // many_kernel's key ranges: how many at most, and tiles of each
-    int flat, few_parts;  // few_kernel: equal shares of all tiles; parts of an item
+    int few_on;           // few_body takes the sequences of up to kFew packed rows
+    int splits, per;      // many_body's key ranges: how many at most, and tiles of each
+    int flat, few_parts;  // few_body: equal shares of all tiles; parts of an item
     int32_t* counts;      // and finished parts of each item
     float c2;             // log2(e) / sqrt(d_head)
     uint16_t* o;
@@ -453,10 +453,11 @@ struct AttnArgs {
     uint8_t* q8;
     int64_t ldq8;
     int qfmt;
-    // partials: output, (maximum, sum); few_kernel's [share][2][kFew], many_kernel's
+    // partials: output, (maximum, sum); few_body's [share][2][kFew], many_body's
     // [split][row][head]
-    float* part_o;
-    float2* part_ml;
+    float *few_o, *many_o;
+    float2 *few_ml, *many_ml;
+    int many_wg;          // workgroups of many_body, before those of few_body
 };
 
 __device__ __forceinline__ f16_t mfma32(u32x4 a, u32x4 b, f16_t c) {
@@ -611,7 +612,7 @@ struct FewWork {
     int64_t at;      // its first tile among all
     int per;         // tiles of a share
 };
-// Tiles of sequence s (0 if it is not few_kernel's, or sees no key).
+// Tiles of sequence s (0 if it is not few_body's, or sees no key).
 __device__ __forceinline__ int few_tiles(const AttnArgs& p, int s) {
     const Seq sq = seq_of(p.c, s);
     const int m1 = min(sq.n, p.max_rows) * p.grp;
@@ -673,8 +674,15 @@ __device__ __forceinline__ FewWork few_locate(const AttnArgs& p, int share, int 
     return f;
 }
 
+template <int DH>
+struct FewLds {
+    float so[kFewW][kFew][DH + 4];
+    float sm[kFewW][kFew], sl[kFewW][kFew];
+    int last;
+};
+// Workgroup `wg` of `wgs`; returns the largest magnitude of what this thread wrote.
 template <int FMT, int DH>
-__global__ __launch_bounds__(kFewT, 2) void few_kernel(AttnArgs p) {
+__device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds, int wg, int wgs, bool cast, int bq) {
     constexpr int kE = FMT == kBf16 ? 1 : FMT;
     constexpr int kSteps = DH / 32;                    // of the contraction over d_head
     constexpr int kKv = DH * kEsz<FMT> / 64;           // 16-byte vectors of a lane's keys
@@ -683,18 +691,15 @@ __global__ __launch_bounds__(kFewT, 2) void few_kernel(AttnArgs p) {
     constexpr int kKt = kG / 4, kPv = kG / 8;          // key tiles, steps of P . V
     constexpr int kCh = DH / 8;
     static_assert(kFew * kCh <= kFewT, "a thread for eight values of a row");
-    __shared__ float so[kFewW][kFew][DH + 4];
-    __shared__ float sm[kFewW][kFew], sl[kFewW][kFew];
-    __shared__ uint32_t redm[kFewW];
-    __shared__ int last;
+    auto &so = lds.so;
+    auto &sm = lds.sm, &sl = lds.sl;
+    int& last = lds.last;
     const CacheView& c = p.c;
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
     // uniform to the compiler too: branches around matrix instructions, which
     // do not heed the lane mask, are then scalar
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rb = r16 >> 2, rl = r16 & 3;  // group and place of this lane's keys
-    const bool cast = p.q8 && p.pred;
-    const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
     uint32_t mag = 0;
     FewWork f;
     const int items = c.n_seqs * c.nkv;
@@ -703,12 +708,12 @@ __global__ __launch_bounds__(kFewT, 2) void few_kernel(AttnArgs p) {
     int kpage = -1, vpage = -1;  // of the next step to load
     bool any = true;
     if (p.flat) {
-        f = few_locate(p, blockIdx.x, gridDim.x);
-        at = (int64_t)blockIdx.x * f.per;
+        f = few_locate(p, wg, wgs);
+        at = (int64_t)wg * f.per;
         end = at + f.per;
         any = f.nt > 0;
     } else {
-        int i = blockIdx.x;
+        int i = wg;
         if (p.few_parts > 1) {  // all run at once: in order
             part = i / items;
             i %= items;
@@ -969,12 +974,12 @@ __global__ __launch_bounds__(kFewT, 2) void few_kernel(AttnArgs p) {
             // [share][2], the part of an item that starts in the share in 1, of one
             // that started before in 0
             const int64_t w0 = p.flat ? f.at / f.per : 0, w1 = p.flat ? (f.at + rg.nt - 1) / f.per : live - 1;
-            uint64_t* po = (uint64_t*)p.part_o + row * (DH / 2) + 4 * ch;
-            uint64_t* pm = (uint64_t*)p.part_ml + row;
+            uint64_t* po = (uint64_t*)p.few_o + row * (DH / 2) + 4 * ch;
+            uint64_t* pm = (uint64_t*)p.few_ml + row;
             auto slot = [&](int64_t k) {
                 return (p.flat ? 2 * k + (k == w0) : k * items + s * c.nkv + hk) * kFew;
             };
-            const int64_t own = slot(p.flat ? blockIdx.x : part);
+            const int64_t own = slot(p.flat ? wg : part);
             if (mine) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) put_far(po + own * (DH / 2) + e, acc[2 * e], acc[2 * e + 1]);
@@ -1038,21 +1043,18 @@ __global__ __launch_bounds__(kFewT, 2) void few_kernel(AttnArgs p) {
         }
         any = f.nt > 0 && at < end;
         __syncthreads();  // the next item writes to the shared memory
-        }
-        // items that see no key have no tiles: one share writes their zeros
-        if (p.flat)
-            for (int s = blockIdx.x; s < c.n_seqs; s += gridDim.x) {
-                const Seq sq = seq_of(c, s);
-                const int n = min(sq.n, p.max_rows), cols = p.nh * DH / 8;
-                if (n < 1 || n * p.grp > kFew || few_tiles(p, s) > 0) continue;
-                for (int i = tid; i < n * cols; i += kFewT)
-                    put8(p, cast, bq, sq.r0 + i / cols, 8 * (i % cols), make_uint4(0u, 0u, 0u, 0u));
-            }
-        if (p.q8) {
-            const uint32_t bm = block_max(mag, redm);
-            if (tid == 0) p.parts[blockIdx.x] = bm;
-        }
     }
+    // items that see no key have no tiles: one share writes their zeros
+    if (p.flat)
+        for (int s = wg; s < c.n_seqs; s += wgs) {
+            const Seq sq = seq_of(c, s);
+            const int n = min(sq.n, p.max_rows), cols = p.nh * DH / 8;
+            if (n < 1 || n * p.grp > kFew || few_tiles(p, s) > 0) continue;
+            for (int i = tid; i < n * cols; i += kFewT)
+                put8(p, cast, bq, sq.r0 + i / cols, 8 * (i % cols), make_uint4(0u, 0u, 0u, 0u));
+        }
+    return mag;
+}
 
 // ---- tiles of 128 packed rows
 // Wave w owns packed rows 32 w .. 32 w + 31 of the tile, one per lane pair (the
@@ -1064,8 +1066,16 @@ __global__ __launch_bounds__(kFewT, 2) void few_kernel(AttnArgs p) {
 //      8-11, 4-7, 12-15 that the scores' registers have; chunk c at
 //      c ^ (d / 2 mod 8).  Any 16 rows of one chunk then cover the 64 banks.
 // Score register i of lane (q, h) is key 8 (i / 4) + 4 h + i % 4 of 32.
+template <int DH>
+struct ManyLds {
+    uint8_t __attribute__((aligned(16))) kv[4 * kTile * DH * 2];  // K0 V0 K1 V1; output staging
+    float __attribute__((aligned(16))) vsc[2][kTile];             // 2^(exp - 127) of the values
+    int __attribute__((aligned(16))) info[2][4];                  // valid keys of a block
+    int hidden;                                                   // values were left to the second sweep
+};
+// Workgroup `wg` of `wgs`; returns the largest magnitude of what this thread wrote.
 template <int FMT, int DH>
-__global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
+__device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& shared, int wg, int wgs, bool cast, int bq) {
     constexpr int kE = FMT == kBf16 ? 1 : FMT;
     constexpr int kSteps = DH / 16;                       // of the contraction over d_head
     constexpr int kDt = DH / 32;                          // tiles of dimensions
@@ -1074,31 +1084,26 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
     constexpr int kKv = DH * kEsz<FMT> / 64;              // 16-byte vectors of keys a lane brings in
     constexpr int kVd = DH / 64;                          // dimensions whose values it brings in
     constexpr int kVv = kEsz<FMT>;                        // vectors of each
-    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kKb];  // K0 V0 K1 V1; output staging
-    __shared__ __attribute__((aligned(16))) float vsc[2][kTile];   // 2^(exp - 127) of the values
-    __shared__ __attribute__((aligned(16))) int info[2][4];        // valid keys of a block
-    __shared__ int hidden;                                         // values were left to the second sweep
-    __shared__ uint32_t redm[kT / 64];
+    auto& lds = shared.kv;
+    auto& vsc = shared.vsc;
+    auto& info = shared.info;
+    int& hidden = shared.hidden;
     const CacheView& c = p.c;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, h = lane >> 5;
-    const int hk = blockIdx.x % c.nkv;
-    int rest = blockIdx.x / c.nkv;
+    const int hk = wg % c.nkv;
+    int rest = wg / c.nkv;
     const int split = rest % p.splits;
-    rest = (int)(gridDim.x / (c.nkv * p.splits)) - 1 - rest / p.splits;  // the last rows, with the longest ranges, first
+    rest = wgs / (c.nkv * p.splits) - 1 - rest / p.splits;  // the last rows, with the longest ranges, first
     // tile slots: as many for each sequence as cu_rows[s + 1] / kMany + 1 - cu_rows[s] / kMany in packed rows
     const int s = wave_search(c.n_seqs, rest, [&](int i) { return row_at(c, i) * p.grp / kMany + i; });
     const Seq sq = seq_of(c, s);
     const int m0 = (int)(rest - (sq.r0 * p.grp / kMany + s)) * kMany;
     const int mtot = min(sq.n, p.max_rows) * p.grp;
-    const bool cast = p.q8 && p.pred;
-    const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
     const int m1 = min(m0 + kMany, mtot);
     const Range rg = range_of(p, sq, min(m0, mtot), max(m1, 1), split, p.per);
-    if (m0 >= mtot || (p.few_on && mtot <= kFew) || (split > 0 && rg.t0 >= rg.t1)) {
-        if (p.q8 && tid == 0) p.parts[blockIdx.x] = 0u;
-        return;
-    }
+    if (m0 >= mtot || (p.few_on && mtot <= kFew) || (split > 0 && rg.t0 >= rg.t1))
+        return 0u;
     const int mq = min(m0 + 32 * w + l32, m1 - 1), tok = mq / p.grp;
     const int pos = sq.p0 + tok;
     const uint16_t* qp = p.q + (sq.r0 + tok) * p.ldq + (int64_t)(hk * p.grp + mq % p.grp) * DH;
@@ -1372,16 +1377,15 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
     if (p.splits > 1) {
         if (m0 + 32 * w + l32 < m1) {
             const int64_t at = ((int64_t)split * c.rows + sq.r0 + tok) * p.nh + hk * p.grp + mq % p.grp;
-            if (h == 0) p.part_ml[at] = make_float2(m, l);
+            if (h == 0) p.many_ml[at] = make_float2(m, l);
 #pragma unroll
             for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
                 for (int q4 = 0; q4 < 4; ++q4)
-                    *(float4*)(p.part_o + at * DH + 32 * dt + 8 * q4 + 4 * h) =
+                    *(float4*)(p.many_o + at * DH + 32 * dt + 8 * q4 + 4 * h) =
                         make_float4(o[dt][4 * q4], o[dt][4 * q4 + 1], o[dt][4 * q4 + 2], o[dt][4 * q4 + 3]);
         }
-        if (p.q8 && tid == 0) p.parts[blockIdx.x] = 0u;
-        return;
+        return 0u;
     }
     // rows of this head's d_head values through LDS (16-byte chunk c of row r at c ^ r)
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -1403,13 +1407,38 @@ __global__ __launch_bounds__(kT, 2) void many_kernel(AttnArgs p) {
         const uint4 v = *(const uint4*)(lds + row * DH * 2 + ((ch ^ (row & kKmask)) << 4));
         mag = max(mag, put8(p, cast, bq, sq.r0 + mm / p.grp, (int64_t)(hk * p.grp + mm % p.grp) * DH + 8 * ch, v));
     }
+    return mag;
+}
+
+// The kernels.  Both in one launch where a call may have sequences of either kind:
+// the latency of the one is then under the work of the other.
+template <int FMT, int DH, bool MANY, bool FEW>
+__global__ __launch_bounds__(kT, 2) void attn_kernel(AttnArgs p) {
+    static_assert(kFewT == kT, "one launch for both");
+    __shared__ union Lds {
+        __device__ Lds() {}
+        ManyLds<MANY ? DH : 0> many;
+        FewLds<FEW ? DH : 0> few;
+    } lds;
+    __shared__ uint32_t redm[kT / 64];
+    const bool cast = p.q8 && p.pred;
+    const int bq = p.q8 ? fused_bias(p.pred, p.used) : 0;
+    const int wg = blockIdx.x;
+    uint32_t mag = 0;
+    if constexpr (MANY) {
+        if (!FEW || wg < p.many_wg) mag = many_body<FMT, DH>(p, lds.many, wg, p.many_wg, cast, bq);
+    }
+    if constexpr (FEW) {
+        const int before = MANY ? p.many_wg : 0;
+        if (wg >= before) mag = few_body<FMT, DH>(p, lds.few, wg - before, gridDim.x - before, cast, bq);
+    }
     if (p.q8) {
         const uint32_t bm = block_max(mag, redm);
-        if (tid == 0) p.parts[blockIdx.x] = bm;
+        if (threadIdx.x == 0) p.parts[wg] = bm;
     }
 }
 
-// ---- join of the key ranges of many_kernel's rows, one (row, head) by DH / 8 lanes
+// ---- join of the key ranges of many_body's rows, one (row, head) by DH / 8 lanes
 template <int DH>
 __global__ __launch_bounds__(kT) void many_join_kernel(AttnArgs p) {
     constexpr int kCh = DH / 8;
@@ -1433,13 +1462,13 @@ __global__ __launch_bounds__(kT) void many_join_kernel(AttnArgs p) {
         const Range rg = range_of(p, sq, m0, min(m0 + kMany, mtot), 0, p.per);
         const int64_t step = c.rows * p.nh, at = r * p.nh + head;
         float top = -INFINITY, acc[8], ll = 0.0f;
-        for (int k = 0; k < rg.live; ++k) top = fmaxf(top, p.part_ml[k * step + at].x);
+        for (int k = 0; k < rg.live; ++k) top = fmaxf(top, p.many_ml[k * step + at].x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
 #pragma unroll 2
         for (int k = 0; k < rg.live; ++k) {
-            const float* d = p.part_o + (k * step + at) * DH + 8 * ch;
-            add_part(acc, ll, p.part_ml[k * step + at], top, p.c2, *(const float4*)d, *(const float4*)(d + 4));
+            const float* d = p.many_o + (k * step + at) * DH + 8 * ch;
+            add_part(acc, ll, p.many_ml[k * step + at], top, p.c2, *(const float4*)d, *(const float4*)(d + 4));
         }
         mag = put8(p, cast, bq, r, (int64_t)head * DH + 8 * ch, scaled8(acc, ll == 0.0f ? 0.0f : 1.0f / ll));
     }
@@ -1536,9 +1565,9 @@ int32_t launch_cache_read(const CacheView& c, int fmt, int d_head, uint16_t* k, 
 namespace {
 // How a call is split over workgroups, from its sizes alone.
 struct Plan {
-    bool few, many, flat;  // which kernels run, and few_kernel in shares
+    bool few, many, flat;  // which kernels run, and few_body in shares
     int few_parts;         // or in parts of an item
-    int splits, per;       // many_kernel's key ranges, and tiles of each
+    int splits, per;       // many_body's key ranges, and tiles of each
     int64_t few_wg, many_wg, many_join;
     int64_t parts, room;   // workgroups that write outputs; at most, whatever the window
     // offsets in the workspace, in bytes, behind the counts: words of the quantise, partials of either kernel
@@ -1550,9 +1579,9 @@ Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t 
     const int64_t tiles = (max_len + kTile - 1) / kTile;
     p.many = cap * grp > kFew;
     // sequences of one length have no single tokens among them
-    p.few = !p.many || (grp <= kFew && n_seqs > 1 && rows < n_seqs * max_rows);
+    p.few = !p.many || (grp <= kFew && n_seqs > 1 && rows < n_seqs * cap);
     const int64_t items = n_seqs * nkv;
-    // few_kernel.  Shares where a compute unit would have much to read and the
+    // few_body.  Shares where a compute unit would have much to read and the
     // items are few enough to be uneven (measured: 32 sequences of up to 16000
     // tokens, 8 heads, 97 us against 126 with an item a workgroup; but 16 of up to 2500, 32 heads, 78
     // against 34).  Parts where items would leave compute units idle: about
@@ -1568,7 +1597,7 @@ Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t 
         if (p.few_parts < 1) p.few_parts = 1;
     }
     p.few_wg = !p.few ? 0 : p.flat ? kShares : items * p.few_parts;
-    // many_kernel: as many ranges as give kManyWant workgroups if all sequences
+    // many_body: as many ranges as give kManyWant workgroups if all sequences
     // were of the longest length, of at least kManyLeast tiles
     const int64_t wg = (rows * grp / kMany + n_seqs) * nkv;
     int64_t seen = tiles;  // of a tile of rows
@@ -1604,6 +1633,7 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
                                int64_t max_rows, int64_t window, uint16_t* o, int64_t ldo, const FusedQuant* fq,
                                void* ws, hipStream_t s) {
     const bool quant = fq && fq->q;
+    if (window >= (int64_t)1 << 30) window = 0;  // beyond any position: none
     const Plan pl = plan_of(c.rows, nh, c.nkv, d_head, c.n_seqs, max_rows, (int64_t)c.max_pages << c.page_shift, window);
     char* base = (char*)ws;
     uint32_t* words = (uint32_t*)(base + pl.words);
@@ -1614,7 +1644,7 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
     a.nh = nh;
     a.grp = nh / c.nkv;
     a.max_rows = (int)(max_rows < c.rows ? max_rows : c.rows);
-    a.window = (int)(window < ((int64_t)1 << 30) ? window : 0);  // beyond any position: none
+    a.window = (int)window;
     a.few_on = pl.few;
     a.splits = pl.splits;
     a.per = pl.per;
@@ -1630,20 +1660,22 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
     a.ldq8 = quant ? fq->ldq : 0;
     a.qfmt = quant ? fq->fmt : FP8_E4M3;
     a.parts = words + 1;
+    a.few_o = (float*)(base + pl.few_o);
+    a.few_ml = (float2*)(base + pl.few_ml);
+    a.many_o = (float*)(base + pl.many_o);
+    a.many_ml = (float2*)(base + pl.many_ml);
+    a.many_wg = (int)pl.many_wg;
     with_cache(fmt, d_head, [&](auto F, auto D) {
         constexpr int kF = decltype(F)::value, kD = decltype(D)::value;
-        auto go = [&](auto kernel, int64_t wg, int threads = kT) {
+        auto go = [&](auto kernel, int64_t wg) {
             if (wg == 0) return;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(threads), 0, s, a);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(kT), 0, s, a);
             a.parts += wg;
         };
-        a.part_o = (float*)(base + pl.many_o);
-        a.part_ml = (float2*)(base + pl.many_ml);
-        go(many_kernel<kF, kD>, pl.many_wg);
+        if (pl.many && pl.few) go(attn_kernel<kF, kD, true, true>, pl.many_wg + pl.few_wg);
+        else if (pl.many) go(attn_kernel<kF, kD, true, false>, pl.many_wg);
+        else go(attn_kernel<kF, kD, false, true>, pl.few_wg);
         go(many_join_kernel<kD>, pl.many_join);
-        a.part_o = (float*)(base + pl.few_o);
-        a.part_ml = (float2*)(base + pl.few_ml);
-        go(few_kernel<kF, kD>, pl.few_wg, kFewT);
     });
     int32_t st = hip_status();
     if (st == FP8_OK && quant) {

@@ -203,11 +203,10 @@ int32_t launch_cache_append(const uint16_t* qkv, int64_t ld, int nh, const Cache
                             const float* table, uint16_t* q, int64_t ldq, hipStream_t s);
 int32_t launch_cache_read(const CacheView& c, int fmt, int d_head, uint16_t* k, int64_t ldk, uint16_t* v, int64_t ldv,
                           hipStream_t s);
-// Sizes of an attention call: workspace bytes for the partial results, and
-// the workgroups that write outputs (maxima of a fused quantise).
+// Sizes of an attention call, for any window.
 struct CacheAttnPlan {
-    int64_t parts;       // workgroups that write the output
-    int64_t ws_bytes;    // everything: 1 + parts words, then the partials
+    int64_t parts;       // workgroups that may write outputs, at most
+    int64_t ws_bytes;    // counts, words of a fused quantise (1 + parts), partial results
 };
 CacheAttnPlan cache_attn_plan(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t max_rows,
                               int64_t max_len);
