@@ -117,15 +117,14 @@ def read(cache, cu, kv_len, pages, rows):
 
 
 def attention(q, cache, cu, kv_len, pages, n_heads, max_rows=None, window=0):
-    """q bf16 patterns [rows, n_heads D].  Returns fp64 (o, a, t, u), [rows, n_heads
-    D] the first two, [rows, n_heads] the others: the attention, the
-    softmax-weighted mean of |v|, and over the keys a row sees the largest
-    sum_d |q_d k_d| / sqrt(D) and max_d |q_d| sum_d |k_d| / sqrt(D) (what the
-    roundings of the probabilities, scores and queries scale with)."""
+    """q bf16 patterns [rows, n_heads D].  Returns fp64 (o, a, t), [rows, n_heads D]
+    the first two, [rows, n_heads] the last: the attention, the softmax-weighted
+    mean of |v|, and over the keys a row sees the largest sum_d |q_d k_d| /
+    sqrt(D) (what the roundings of the probabilities and scores scale with)."""
     nk, d = cache.heads, cache.d_head
     grp = n_heads // nk
     o = np.zeros((q.shape[0], n_heads, d))
-    mean, top, most = np.zeros_like(o), np.zeros(o.shape[:2]), np.zeros(o.shape[:2])
+    mean, top = np.zeros_like(o), np.zeros(o.shape[:2])
     for s in range(len(kv_len)):
         n = int(cu[s + 1]) - int(cu[s])
         if n == 0:
@@ -153,5 +152,4 @@ def attention(q, cache, cu, kv_len, pages, n_heads, max_rows=None, window=0):
                 sl = slice(hk * grp, (hk + 1) * grp)
                 o[r, sl], mean[r, sl] = p @ v, p @ np.abs(v)
                 top[r, sl] = (np.abs(qv[hk]) @ np.abs(k).T).max(axis=1) / np.sqrt(d)
-                most[r, sl] = np.abs(qv[hk]).max(axis=1) * np.abs(k).sum(axis=1).max() / np.sqrt(d)
-    return o.reshape(q.shape), mean.reshape(q.shape), top, most
+    return o.reshape(q.shape), mean.reshape(q.shape), top

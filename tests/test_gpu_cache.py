@@ -5,16 +5,13 @@ Bars, from the arithmetic:
     there), rounded to fp32; bias, codes and exponents are integer work, and
     the bf16 roundings of the queries, keys and values are from that fp32 value.
   * read: bit for bit (codes times a power of two).
-  * attention, per element, with A the softmax-weighted mean of |v|, T the
-    largest sum_d |q_d k_d| / sqrt(d) of the row's keys, and U the largest
-    max|q| sum_d |k_d| / sqrt(d):
+  * attention, per element, with A the softmax-weighted mean of |v| and T the
+    largest sum_d |q_d k_d| / sqrt(d) of the row's keys:
       scores: an fp32 sum of d products is off by at most d 2^-24 T; the scaled
       score is rounded once more, and so is its difference to the maximum
-      (4 2^-24 T together).  Queries over FP8 keys are split into a sum of two
-      E4M3 rows scaled to the row's largest value, which leaves at most 2^-22 of
-      that value of an element: 2^-22 U.  ds = (d + 4) 2^-24 T + 2^-22 U is the
-      error of a score; a probability is off by the factor exp(2 ds) at most, as
-      is their sum: 4 ds A in the result (first order; 8 ds A for the rest);
+      (4 2^-24 T together).  ds = (d + 4) 2^-24 T is the error of a score; a
+      probability is off by the factor exp(2 ds) at most, as is their sum: 4 ds A
+      in the result (first order; 8 ds A for the rest);
       probabilities: rounded to bf16, 2^-8 A; their fp32 sums over n keys:
       n 2^-24 A each, and exp2's own error (2^-22) twice;
       the result rounded to bf16: 2^-8 of its value.
@@ -176,23 +173,23 @@ def test_read_one_output(gpu):
 
 
 # ------------------------------------------------------------------ attention
-def bound(c, want, mean, top, most):
+def bound(c, want, mean, top):
     """Largest allowed difference of each element (see the module's docstring)."""
     n, d = max(int(c.kv_len.max()), 1), c.d_head
-    ds = np.repeat((d + 4) * 2.0 ** -24 * top + 2.0 ** -22 * most, d, axis=1)
+    ds = np.repeat((d + 4) * 2.0 ** -24 * top, d, axis=1)
     off = (8 * ds + 2.0 ** -8 + 2 * n * 2.0 ** -24 + 2.0 ** -20) * mean
     return off + 2.0 ** -8 * (np.abs(want) + off) + 1e-30
 
 
 def check(c, q, o, window=0, max_rows=None, what=""):
-    want, mean, top, most = C.attention(q, c.host, c.cu, c.kv_len, c.pages, c.heads, max_rows, window)
+    want, mean, top = C.attention(q, c.host, c.cu, c.kv_len, c.pages, c.heads, max_rows, window)
     got = D.bf16_to_f64(np_bits(o))
     live = np.zeros(c.rows, dtype=bool)
     for s in range(len(c.kv_len)):
         n = int(c.cu[s + 1] - c.cu[s])
         live[c.cu[s]:c.cu[s] + (n if max_rows is None else min(n, max_rows))] = True
     assert (np_bits(o)[~live] == SENTINEL).all()
-    err, lim = np.abs(got - want)[live], bound(c, want, mean, top, most)[live]
+    err, lim = np.abs(got - want)[live], bound(c, want, mean, top)[live]
     worst = float((err / lim).max()) if err.size else 0.0
     den = np.linalg.norm(want[live])
     print(f"{what} worst {worst:.3f} of the bound, rel {np.linalg.norm((got - want)[live]) / max(den, 1e-30):.2e}", flush=True)

@@ -43,9 +43,9 @@ def test_prefill_through_a_bf16_cache_equals_the_decoder_oracle():
     same = q == rot[:, :heads * d]
     assert same.mean() > 0.999       # the table is rounded to fp32
     k, v = C.read(c.host, c.cu, c.kv_len, c.pages, n)
-    o, mean, top, most = C.attention(q, c.host, c.cu, c.kv_len, c.pages, heads)
+    o, mean, top = C.attention(q, c.host, c.cu, c.kv_len, c.pages, heads)
     assert np.array_equal(D.round_bf16(o), D.attention(q, k, v, n, heads, nk, d))
-    assert np.all(np.abs(o) <= mean + 1e-12) and np.all(top > 0) and np.all(most >= top)
+    assert np.all(np.abs(o) <= mean + 1e-12) and np.all(top > 0)
 
 
 def test_a_chunk_sees_what_the_whole_sees():
