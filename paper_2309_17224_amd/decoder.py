@@ -26,6 +26,9 @@ per sequence of the call ("sequence": the per-data-sample activation biases of
 the paper's inference, App. D): then each glue kernel writes its bf16 output
 only, fp8_quantise_segments gives every sequence its own Eq. 3 bias and codes,
 and fp8_linear_fwd_rows unscales each output row by its sequence's bias.
+
+CachedDecoderLayer is the layer over a paged key/value cache (chunked prefill
+and token-by-token decode of several sequences).
 """
 from __future__ import annotations
 
@@ -236,3 +239,81 @@ class DecoderLayer:
         for n, a in (("xn", self.xn), ("att", self.att), ("hn", self.hn), ("act", self.act)):
             b[n] = a.seg_bias.cpu().tolist() if self.bias_per == "sequence" else int(a.bias.item())
         return b
+
+
+class CachedDecoderLayer(DecoderLayer):
+    """The layer over a paged key/value cache: token-by-token and chunked
+    inference of several sequences.  A call takes cfg.rows rows; set_sequences
+    says whose they are (cfg.seq_len does not matter), so prefill chunks, single tokens and
+    padding rows behind the last sequence may share one call and one captured
+    graph.  In place of RoPE and the attention within the call's rows:
+
+      K, V of the rows -> cache, Q rotated     (llama_cache_append)
+      att = causal GQA attention(Q, cache)     -> E4 codes, bias   (fused quantise)
+
+    kv_fmt: E4M3 or E5M2 (one Eq. 3 bias per token and head) or CACHE_BF16.
+    cache: a KVCache to use (shared pages), or None for one of n_pages pages of
+    page_size tokens.  max_rows: the most rows of one sequence in a call."""
+
+    def __init__(self, cfg: LayerConfig, weights: dict, device, n_seqs: int, max_pages: int, page_size: int = 64,
+                 n_pages: int | None = None, kv_fmt: int = F.E4M3, max_rows: int | None = None, window: int = 0,
+                 cache: F.KVCache | None = None):
+        dev = torch.device(device)
+        n_pages = n_seqs * max_pages if n_pages is None else n_pages
+        self.cache = F.KVCache(n_pages, cfg.n_kv_heads, cfg.d_head, page_size, kv_fmt, dev) if cache is None else cache
+        if (self.cache.n_kv_heads, self.cache.d_head) != (cfg.n_kv_heads, cfg.d_head):
+            raise ValueError(f"cache of {self.cache.n_kv_heads} heads of {self.cache.d_head}, layer of {cfg.n_kv_heads} of {cfg.d_head}")
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.seqs = F.CacheSeqs(torch.zeros(n_seqs + 1, **i32), torch.zeros(n_seqs, **i32),
+                                torch.full((n_seqs, max_pages), -1, **i32))
+        self.max_rows = cfg.rows if max_rows is None else max_rows
+        self.window = window
+        super().__init__(cfg, weights, device)
+        self.table = F.llama_rope_table(max_pages * self.cache.page_size, cfg.d_head, ROPE_THETA, device=dev)
+        self.att.ws = F.cache_attention_workspace(cfg.rows, cfg.n_heads, self.cache, self.seqs, self.max_rows)
+        self.att.x.zero_()
+        self.att.q.zero_()
+
+    def set_sequences(self, rows, kv_len, pages=None):
+        """rows: rows of each sequence in the next call, in order; kv_len: its
+        tokens in the cache, those included; pages: [n_seqs, <= max_pages] page
+        numbers (-1: absent), or None to keep them.  Copies into the device
+        tensors that a captured graph reads; sequences left out have no rows.
+        Rows behind the last sequence are padding: the layer computes them too
+        (each bias is of all rows of a call), from zeros that this puts there."""
+        n = self.seqs.n_seqs
+        if len(rows) != len(kv_len) or len(rows) > n:
+            raise ValueError(f"up to {n} sequences, as many rows as lengths")
+        if any(r < 0 or r > self.max_rows for r in rows) or sum(rows) > self.cfg.rows:
+            raise ValueError(f"rows: 0 to {self.max_rows} of a sequence, {self.cfg.rows} in all")
+        if any(k < r or k > self.seqs.max_pages * self.cache.page_size for r, k in zip(rows, kv_len)):
+            raise ValueError("kv_len: at least the sequence's rows, at most what its pages hold")
+        if pages is not None and (len(pages) > n or any(len(row) > self.seqs.max_pages for row in pages)):
+            raise ValueError(f"pages: up to {self.seqs.max_pages} of each of {n} sequences")
+        rows, kv_len = list(rows) + [0] * (n - len(rows)), list(kv_len) + [0] * (n - len(kv_len))
+        cu = [0]
+        for r in rows:
+            cu.append(cu[-1] + r)
+        self.seqs.cu_rows.copy_(torch.tensor(cu, dtype=torch.int32))
+        self.seqs.kv_len.copy_(torch.tensor(kv_len, dtype=torch.int32))
+        if pages is not None:
+            t = torch.full((n, self.seqs.max_pages), -1, dtype=torch.int32)
+            for s, row in enumerate(pages):
+                t[s, :len(row)] = torch.as_tensor(row, dtype=torch.int32)
+            self.seqs.pages.copy_(t)
+        if cu[-1] < self.cfg.rows:
+            for x in (self.H, self.att.x, self.att.q):
+                x[cu[-1]:].zero_()
+
+    def _build(self):
+        c = self.cfg
+        R = c.rows
+        q = self.qkv[:, :self.dq]
+        calls = super()._build()
+        at = [label for label, _, _, _ in calls].index("rope")
+        calls[at] = ("rope+cache append", "glue", 2 * R * (2 * self.dq + 2 * self.dkv) + 2 * R * self.dkv,
+                     lambda: F.llama_cache_append(self.qkv, self.cache, self.seqs, c.n_heads, table=self.table, q=q))
+        calls[at + 1] = ("cache attention+quantise", "attention", 0,  # its work follows the sequences' lengths
+                         lambda: F.llama_cache_attention(q, self.cache, self.seqs, c.n_heads, self.max_rows,
+                                                         window=self.window, o=self.att.x, fq=self.att.fq()))
+        return calls
