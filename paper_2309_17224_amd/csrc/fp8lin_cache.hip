@@ -1102,7 +1102,8 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
     const int mtot = min(sq.n, p.max_rows) * p.grp;
     const int m1 = min(m0 + kMany, mtot);
     const Range rg = range_of(p, sq, min(m0, mtot), max(m1, 1), split, p.per);
-    if (m0 >= mtot || (p.few_on && mtot <= kFew) || (split > 0 && rg.t0 >= rg.t1))
+    // (below 0 only where cu_rows does not start with 0)
+    if (m0 < 0 || m0 >= mtot || (p.few_on && mtot <= kFew) || (split > 0 && rg.t0 >= rg.t1))
         return 0u;
     const int mq = min(m0 + 32 * w + l32, m1 - 1), tok = mq / p.grp;
     const int pos = sq.p0 + tok;

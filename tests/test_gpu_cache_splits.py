@@ -12,9 +12,10 @@ import torch
 
 from cache_cases import SENTINEL, Case, blank, rand_bits, strided
 from oracle import cache as C
+from oracle import decoder as D
 from paper_2309_17224_amd import fp8lin as F
 from parity_util import np_bits
-from test_gpu_cache import check, say
+from test_gpu_cache import bound, check, say
 
 pytestmark = pytest.mark.gpu
 
@@ -234,6 +235,27 @@ def test_inconsistent_rows_stay_inside(gpu):
         assert len(free) == 5
         for n, t in before.items():
             assert torch.equal(getattr(cache, n)[free], t[free]), n
+
+
+def test_first_sequence_behind_row_0(gpu):
+    """Rows before cu_rows[0] belong to no sequence: they are left, those behind are right."""
+    say("rows before the first sequence")
+    c = Case(64, 4, 2, 128, E4, 64, [700, 130, 1], [700, 300, 65])
+    q = rand_bits(c.rng, (c.rows, 512))
+    cache, seqs = c.device(gpu)
+    seqs = F.CacheSeqs(seqs.cu_rows[1:], seqs.kv_len[1:], seqs.pages[1:])
+    o = blank(c.rows, 512, gpu)
+    F.llama_cache_attention(strided(q, gpu, 0), cache, seqs, 4, 700, o=o)
+    k, v = blank(c.rows, 256, gpu), blank(c.rows, 256, gpu)
+    F.llama_cache_read(cache, seqs, c.rows, k=k, v=v)
+    torch.cuda.synchronize()
+    for t in (o, k, v):
+        assert (np_bits(t)[:700] == SENTINEL).all()
+    want, mean, top = C.attention(q, c.host, c.cu[1:], c.kv_len[1:], c.pages[1:], 4)
+    err = np.abs(D.bf16_to_f64(np_bits(o)) - want)
+    assert (err <= bound(c, want, mean, top))[700:].all()
+    wk, wv = C.read(c.host, c.cu[1:], c.kv_len[1:], c.pages[1:], c.rows)
+    assert np.array_equal(np_bits(k)[700:], wk[700:]) and np.array_equal(np_bits(v)[700:], wv[700:])
 
 
 def test_append_without_queries(gpu):
