@@ -690,6 +690,7 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
     constexpr int kG = 16 / kEsz<FMT>, kKeys = 4 * kG; // keys of a lane group, of a step
     constexpr int kKt = kG / 4, kPv = kG / 8;          // key tiles, steps of P . V
     constexpr int kCh = DH / 8;
+    constexpr int kJoin = 8;                           // parts that are read at once
     static_assert(kFew * kCh <= kFewT, "a thread for eight values of a row");
     auto &so = lds.so;
     auto &sm = lds.sm, &sl = lds.sl;
@@ -873,14 +874,15 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
 #pragma unroll
                 for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
             }
-            const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
+            const float moff = m == -INFINITY ? 0.0f : m;
             u32x4 pf[kPv];
 #pragma unroll
             for (int kt = 0; kt < kKt; ++kt) {
                 float pr[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][i], p.c2, moff));
+                    // the difference first: its product with c2 is never above 0, however large the scores
+                    pr[i] = __builtin_amdgcn_exp2f((sc[kt][i] - moff) * p.c2);
                     l += pr[i];
                     // an exponent of a masked slot may be anything, its weight is 0
                     if (FMT != kBf16) pr[i] *= exp_float(min((vex[kt] >> (8 * i)) & 0xFFu, 254u));
@@ -1000,12 +1002,12 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
                 ll = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-                // eight parts' loads at once: each takes a trip to memory.  (Those
+                // several parts' loads at once: each takes a trip to memory.  (Those
                 // behind the last part read it again, with no weight.)
-                for (int64_t k0 = w0; k0 <= w1; k0 += 8) {
-                    float2 ml[8], x[8][4];
+                for (int64_t k0 = w0; k0 <= w1; k0 += kJoin) {
+                    float2 ml[kJoin], x[kJoin][4];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
+                    for (int k = 0; k < kJoin; ++k) {
                         const int64_t sl = slot(min(k0 + k, w1));
                         ml[k] = get_far(pm + sl);
 #pragma unroll
@@ -1013,7 +1015,7 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
                     }
                     float top = mm;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
+                    for (int k = 0; k < kJoin; ++k) {
                         if (k0 + k > w1) ml[k] = make_float2(-INFINITY, 0.0f);
                         top = fmaxf(top, ml[k].x);
                     }
@@ -1025,7 +1027,7 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
                         for (int e = 0; e < 8; ++e) acc[e] *= f;
                     }
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
+                    for (int k = 0; k < kJoin; ++k)
                         add_part(acc, ll, ml[k], mm, p.c2, make_float4(x[k][0].x, x[k][0].y, x[k][1].x, x[k][1].y),
                                  make_float4(x[k][2].x, x[k][2].y, x[k][3].x, x[k][3].y));
                 }
@@ -1071,7 +1073,7 @@ struct ManyLds {
     uint8_t __attribute__((aligned(16))) kv[4 * kTile * DH * 2];  // K0 V0 K1 V1; output staging
     float __attribute__((aligned(16))) vsc[2][kTile];             // 2^(exp - 127) of the values
     int __attribute__((aligned(16))) info[2][4];                  // valid keys of a block
-    int hidden;                                                   // values were left to the second sweep
+    int hidden;                                                   // sums came out nonfinite
 };
 // Workgroup `wg` of `wgs`; returns the largest magnitude of what this thread wrote.
 template <int FMT, int DH>
@@ -1084,6 +1086,7 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
     constexpr int kKv = DH * kEsz<FMT> / 64;              // 16-byte vectors of keys a lane brings in
     constexpr int kVd = DH / 64;                          // dimensions whose values it brings in
     constexpr int kVv = kEsz<FMT>;                        // vectors of each
+    enum { kAll, kFinite, kRest };                        // sweeps over the keys: of all values, or in two
     auto& lds = shared.kv;
     auto& vsc = shared.vsc;
     auto& info = shared.info;
@@ -1140,8 +1143,8 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
             ve = c.ve[slot + (lane & 15)];
         }
     };
-    // finite: without infinities and NaN among the values
-    auto store = [&](int buf, auto finite) {
+    // mode kFinite: infinities and NaN among the values left out
+    auto store = [&](int buf, auto mode) {
         uint8_t* Kl = lds + buf * 2 * kKb;
         uint8_t* Vl = Kl + kKb;
         const int key = kBlk * w + (lane >> 2);
@@ -1162,26 +1165,18 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
 #pragma unroll
                 for (int k = 0; k < 4 * kVv; ++k) vraw[d][k / 4][k % 4] &= mk[k];
         }
-        if constexpr (finite) {
-            // a 1 in the top bit of each value that is not
+        if constexpr (mode == kFinite) {
+            // a 1 in the top bit of each value that is not finite
             auto nf = [](uint32_t x) {
                 return FMT == kBf16 ? nonfinite2(x) : ((x & 0x7F7F7F7Fu) + (kE == FP8_E5M2 ? 0x04040404u : 0x01010101u)) & 0x80808080u;
             };
-            uint32_t any = 0;
 #pragma unroll
             for (int d = 0; d < kVd; ++d)
 #pragma unroll
-                for (int k = 0; k < 4 * kVv; ++k) any |= nf(vraw[d][k / 4][k % 4]);
-            if (__builtin_expect(__any(any), 0)) {
-                hidden = 1;
-#pragma unroll
-                for (int d = 0; d < kVd; ++d)
-#pragma unroll
-                    for (int k = 0; k < 4 * kVv; ++k) {
-                        const uint32_t x = vraw[d][k / 4][k % 4];
-                        vraw[d][k / 4][k % 4] = x & ~((nf(x) >> (FMT == kBf16 ? 15 : 7)) * (FMT == kBf16 ? 0xFFFFu : 0xFFu));
-                    }
-            }
+                for (int k = 0; k < 4 * kVv; ++k) {
+                    const uint32_t x = vraw[d][k / 4][k % 4];
+                    vraw[d][k / 4][k % 4] = x & ~((nf(x) >> (FMT == kBf16 ? 15 : 7)) * (FMT == kBf16 ? 0xFFFFu : 0xFFu));
+                }
         }
 #pragma unroll
         for (int d = 0; d < kVd; ++d) {
@@ -1204,18 +1199,24 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
     };
 
     f16_t o[kDt];
+    float m, l;
+    auto start = [&]() {
+        m = -INFINITY;
+        l = 0.0f;
 #pragma unroll
-    for (int dt = 0; dt < kDt; ++dt)
+        for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
-    float m = -INFINITY, l = 0.0f;
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+    };
+    start();
     const float lazy = 8.0f / p.c2;
+    bool apart = false;  // this row takes differences of scores first
 
-    auto sweep = [&](auto finite) {
+    auto sweep = [&](auto mode) {
         int page = page_at(rg.t0);
         load(rg.t0, page);
         page = page_at(min(rg.t0 + 1, rg.t1 - 1));
-        store(0, finite);
+        store(0, mode);
         load(min(rg.t0 + 1, rg.t1 - 1), page);
         page = page_at(min(rg.t0 + 2, rg.t1 - 1));
         __syncthreads();
@@ -1241,7 +1242,7 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) kf[ks][kt] = kfrag(ks, kt);
             __builtin_amdgcn_sched_barrier(0);
-            store(buf ^ 1, finite);
+            store(buf ^ 1, mode);
             load(min(t + 2, rg.t1 - 1), page);
             page = page_at(min(t + 3, rg.t1 - 1));
             f16_t sc[2];
@@ -1275,7 +1276,7 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
                     }
                 }
             }
-            if constexpr (finite) {
+            if constexpr (mode != kRest) {
                 u32x4 vf[2][kDt];  // the first value operands, under way during the softmax
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
@@ -1302,7 +1303,7 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
 #pragma unroll
                     for (int dt = 0; dt < kDt; ++dt) o[dt] *= alpha;
                 }
-                const float moff = m == -INFINITY ? 0.0f : -m * p.c2;
+                const float mref = m == -INFINITY ? 0.0f : m, moff = -mref * p.c2;
                 u32x4 pf[4];
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
@@ -1311,7 +1312,8 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
                         float pr[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            pr[i] = __builtin_amdgcn_exp2f(fmaf(sc[kt][4 * q4 + i], p.c2, moff));
+                            const float s = sc[kt][4 * q4 + i];
+                            pr[i] = __builtin_amdgcn_exp2f(mode == kFinite && apart ? (s - mref) * p.c2 : fmaf(s, p.c2, moff));
                             l += pr[i];
                         }
                         if (FMT != kBf16) {
@@ -1365,11 +1367,33 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
     };
     if (rg.t0 < rg.t1) {
         if (tid == 0) hidden = 0;
+        // An infinity or NaN among the values makes sums of every row nonfinite, of
+        // those that do not see it too (0 * NaN).  The loop does not look for them
+        // (which cost 2 % of the call); where a sum comes out nonfinite, two others do
+        // it again: one with the finite values, one that adds what the rest gives
+        // to the rows that see it.  Scores beyond 2^30 do the same to their own row:
+        // their product with c2 is rounded by more than an exponent holds.  Such rows
+        // take the difference first, in one sweep more.
+        auto nonfinite = [&]() {  // any of this lane's sums
+            bool bad = !(l < INFINITY);
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) bad |= !(fabsf(o[dt][i]) < INFINITY);
+            return bad;
+        };
+        sweep(IC<kAll>{});
+        if (__any(nonfinite())) hidden = 1;
         __syncthreads();
-        sweep(IC<1>{});
-        // The loop above has no branch for infinities and NaN among the values:
-        // a second one, if there were any, adds what they give.
-        if (hidden) sweep(IC<0>{});
+        if (hidden) {
+            for (int again = 0; again < 2; ++again) {
+                start();
+                sweep(IC<kFinite>{});
+                const int bad = nonfinite();
+                apart = bad || __shfl_xor(bad, 32, 64);  // the lanes of a row alike
+            }
+            sweep(IC<kRest>{});
+        }
     }
     {
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
@@ -1413,8 +1437,14 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
 
 // The kernels.  Both in one launch where a call may have sequences of either kind:
 // the latency of the one is then under the work of the other.
+// Waves a SIMD: three where many_body's registers suffice (40 sequences of 128 rows
+// over 960 keys, 12 heads of 64, E4M3: 44 us, with two 60).  With few_body beside it three
+// are slower where single tokens have most of the keys (24 sequences over 2500,
+// five of 200 rows, bf16: 66 us against 54), faster where few have (35 against 39).
+template <int DH, bool MANY, bool FEW>
+constexpr int kWaves = DH == 64 && MANY && !FEW ? 3 : 2;
 template <int FMT, int DH, bool MANY, bool FEW>
-__global__ __launch_bounds__(kT, 2) void attn_kernel(AttnArgs p) {
+__global__ __launch_bounds__(kT, (kWaves<DH, MANY, FEW>)) void attn_kernel(AttnArgs p) {
     static_assert(kFewT == kT, "one launch for both");
     __shared__ union Lds {
         __device__ Lds() {}

@@ -276,3 +276,28 @@ def test_append_without_queries(gpu):
         for n in ("k", "v", "k_exp", "v_exp"):
             t = getattr(a, n)
             assert t is None or torch.equal(t.view(torch.uint8), getattr(b, n).view(torch.uint8)), n
+
+
+@pytest.mark.parametrize("fmt,new,total", [(E4, [1, 1], [900, 70]), (BF, [1], [3000]), (E4, [90], [400]),
+                                           (BF, [130, 1], [500, 300]), (E4, [200], [2000])])
+def test_scores_beyond_what_their_exponents_hold(gpu, fmt, new, total):
+    """Scores of 2^40 to 2^43, exact in fp32: the largest one takes all, ties share."""
+    say("large scores", fmt, new, total)
+    c = Case(65, 4, 2, 128, fmt, 64, new, total)
+    h = c.host
+    if fmt == BF:
+        h.k[...] = 0
+        h.k[..., 0] = C.round_bf16(c.rng.integers(1, 8, h.k[..., 0].shape).astype(np.float64))
+    else:
+        h.k[...] = 0
+        h.k[..., 0] = c.rng.integers(0x38, 0x50, h.k[..., 0].shape)      # 1 to 7.5
+        h.k_exp[...] = 127
+    q = np.zeros((c.rows, 512), dtype=np.uint16)
+    q[:, ::128] = C.round_bf16(np.full((c.rows, 4), 2.0 ** 40))
+    cache, seqs = c.device(gpu)
+    o = F.llama_cache_attention(strided(q, gpu, 0), cache, seqs, 4, c.max_rows)
+    torch.cuda.synchronize()
+    want, mean, _ = C.attention(q, h, c.cu, c.kv_len, c.pages, 4)
+    # the weights are 1 and 0: sums of the winners in fp32, one rounding; two for P = 1 (exact)
+    lim = 2.0 ** -8 * np.abs(want) + (2.0 ** -7 + max(total) * 2.0 ** -23) * mean
+    assert (np.abs(D.bf16_to_f64(np_bits(o)) - want) <= lim).all()
