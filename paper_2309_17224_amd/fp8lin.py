@@ -841,8 +841,9 @@ def cache_attention_workspace(rows: int, n_heads: int, cache: KVCache, seqs: Cac
 def llama_cache_attention(q, cache: KVCache, seqs: CacheSeqs, n_heads: int, max_rows: int, window: int = 0, o=None,
                           fq: FusedQuant | None = None, ws=None, stream=None):
     """Causal grouped-query attention of the call's rows (q [rows, n_heads
-    d_head]) over the cache, optionally with the fused quantise of o (its ws is
-    this call's).  max_rows: at least the rows of every sequence.  Returns o."""
+    d_head]) over the cache, optionally with the fused quantise of o (its ws, a
+    cache_attention_workspace, is then the call's; without
+    either one is made for the call, on the current stream only).  max_rows: at least the rows of every sequence.  Returns o."""
     dev = cache._dev
     rows, cols = q.shape[0], n_heads * cache.d_head
     ldq = _mat(q, "q", rows, cols, dev)
@@ -853,11 +854,13 @@ def llama_cache_attention(q, cache: KVCache, seqs: CacheSeqs, n_heads: int, max_
     _cache_device(cache, seqs)
     if fq is not None:
         ws, quant = fq.ws, fq.args()[:-2]
-        if fq.q.shape != (rows, cols) or fq.q.dtype != torch.uint8:
-            raise ValueError(f"fq.q: expected uint8 [{rows}, {cols}]")
+        if fq.q.shape != (rows, cols) or fq.q.dtype != torch.uint8 or fq.q.stride(1) != 1:
+            raise ValueError(f"fq.q: expected uint8 [{rows}, {cols}] with contiguous rows")
         if any(t is not None and t.get_device() != dev for t in (fq.q, fq.bias, fq.bias_pred, fq.amax_bits, fq.flags)):
             raise ValueError(f"fq: every tensor must be on GPU {dev}")
     elif ws is None:
+        if stream is not None:  # its zeros are written on the current stream, and its memory is that one's
+            raise ValueError("ws: a call on a stream of the caller's needs a workspace")
         ws = cache_attention_workspace(rows, n_heads, cache, seqs, max_rows)
     if ws.get_device() != dev:
         raise ValueError(f"ws: on {ws.device}, the cache on GPU {dev}")

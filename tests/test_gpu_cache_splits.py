@@ -258,6 +258,26 @@ def test_first_sequence_behind_row_0(gpu):
     assert np.array_equal(np_bits(k)[700:], wk[700:]) and np.array_equal(np_bits(v)[700:], wv[700:])
 
 
+def test_another_stream_needs_a_workspace(gpu):
+    say("another stream")
+    c = Case(66, 8, 2, 128, E4, 16, [1, 30], [900, 200])
+    cache, seqs = c.device(gpu)
+    q = strided(rand_bits(c.rng, (c.rows, 1024)), gpu, 0)
+    want = F.llama_cache_attention(q, cache, seqs, 8, 30)
+    ws, o = F.cache_attention_workspace(c.rows, 8, cache, seqs, 30), torch.zeros_like(q)
+    st = torch.cuda.Stream()
+    with pytest.raises(ValueError):
+        F.llama_cache_attention(q, cache, seqs, 8, 30, o=o, stream=st)
+    torch.cuda.synchronize()
+    F.llama_cache_attention(q, cache, seqs, 8, 30, o=o, ws=ws, stream=st)
+    st.synchronize()
+    assert torch.equal(o, want)
+    with torch.cuda.stream(st):
+        o2 = F.llama_cache_attention(q, cache, seqs, 8, 30)
+    st.synchronize()
+    assert torch.equal(o2, want)
+
+
 def test_append_without_queries(gpu):
     """The C call with q NULL writes the same cache."""
     say("append without queries")
