@@ -321,3 +321,29 @@ def test_scores_beyond_what_their_exponents_hold(gpu, fmt, new, total):
     # the weights are 1 and 0: sums of the winners in fp32, one rounding; two for P = 1 (exact)
     lim = 2.0 ** -8 * np.abs(want) + (2.0 ** -7 + max(total) * 2.0 ** -23) * mean
     assert (np.abs(D.bf16_to_f64(np_bits(o)) - want) <= lim).all()
+
+
+@pytest.mark.parametrize("fmt", [E4, BF])
+def test_cache_beyond_32_bit_offsets(gpu, fmt):
+    """Pages at the ends of a cache of 5.2 (bf16: 10.5) GB for keys and for values: the
+    bits of a small cache."""
+    say("large cache", fmt)
+    n_pages, kv, page = 80000, 8, 64
+    big, small = F.KVCache(n_pages, kv, 128, page, fmt, gpu), F.KVCache(8, kv, 128, page, fmt, gpu)
+    far = torch.tensor([[n_pages - 1, 0, 65536, -1], [32768, n_pages - 2, 40001, 1]], dtype=torch.int32, device=gpu)
+    near = torch.tensor([[0, 1, 2, -1], [3, 4, 5, 6]], dtype=torch.int32, device=gpu)
+    table = F.llama_rope_table(4 * page, 128, device=gpu)
+    outs = []
+    for cache, pages in ((big, far), (small, near)):
+        rng = np.random.default_rng(67)
+        got = []
+        for new, total in (([150, 200], [150, 200]), ([1, 1], [151, 201]), ([1, 40], [152, 241])):
+            cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device=gpu)
+            seqs = F.CacheSeqs(cu, torch.tensor(total, dtype=torch.int32, device=gpu), pages)
+            x = strided(rand_bits(rng, (sum(new), 24 * 128)), gpu, 0)
+            q = F.llama_cache_append(x, cache, seqs, 8, table=table)
+            got += [q, F.llama_cache_attention(q, cache, seqs, 8, max(new)), *F.llama_cache_read(cache, seqs, sum(new))]
+        outs.append(got)
+    torch.cuda.synchronize()
+    for a, b in zip(*outs):
+        assert torch.isfinite(a.float()).all() and torch.equal(a, b)
