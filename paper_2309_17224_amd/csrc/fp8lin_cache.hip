@@ -1074,9 +1074,9 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
 //
 // Bound by what two waves a SIMD overlap of 32 matrix instructions (a third of the
 // time), 291 vector instructions (as long) and 51 of LDS (as long) a tile, at d_head
-// 128 in E4M3: 512 tokens over 8192 before them, 64 heads on 8, in 177 us (800
-// TFLOP/s; a library product of 8192^3 runs at 1190), 2 x 2048 tokens of 32 heads in
-// bf16 in 105 (655).  Measured and left: software pipelining within a wave (spills at
+// 128 in E4M3: 512 tokens over 8192 before them, 64 heads on 8, in 177 to 182 us
+// (800 to 780 TFLOP/s; a library product of 8192^3 runs at 1190), 2 x 2048 tokens of 32
+// heads in bf16 in 105 to 107 (650).  Measured and left: software pipelining within a wave (spills at
 // 128; 122 us against 128 at 64), matrix instructions on FP8 operands (see above).
 template <int DH>
 struct ManyLds {
