@@ -424,6 +424,7 @@ constexpr int kTile = 64;     // keys of a tile
 // over 8192 before them, 64 heads in groups of 8, take 201 us with 1024 and 188 with
 // 512), and tiles of a range at least.
 constexpr int kManyWant = 512, kManyLeast = 8;
+constexpr float kLargeScore = 16384.0f;  // many_body: of a maximum times log2(e) / sqrt(d_head), beyond which differences come first
 constexpr int kCus = 256;          // compute units
 constexpr int kShares = 512;       // workgroups of few_body that run at once
 constexpr int kShareLeast = 8;     // tiles of a share at least
@@ -1379,11 +1380,16 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
         if (tid == 0) hidden = 0;
         // An infinity or NaN among the values makes sums of every row nonfinite, of
         // those that do not see it too (0 * NaN).  The loop does not look for them
-        // (which cost 2 % of the call); where a sum comes out nonfinite, two others do
-        // it again: one with the finite values, one that adds what the rest gives
-        // to the rows that see it.  Scores beyond 2^30 do the same to their own row:
-        // their product with c2 is rounded by more than an exponent holds.  Such rows
-        // take the difference first, in one sweep more.
+        // (which cost 2 % of the call); where a sum comes out nonfinite, others do
+        // it again: two with the finite values, one that adds what the rest gives
+        // to the rows that see it.  Large scores need them too: the product of the
+        // maximum with c2 is rounded, by up to 2^-24 of itself, and the row's weights
+        // before and after a new maximum are off by as many powers of two: to zeros,
+        // to infinities, or in between.  Rows whose product ends above 2^14 take the
+        // difference first.  (Below, the rounding is 2^-11, a fraction of that of the
+        // probabilities.  A maximum that was above 2^15 on the way and is not at the end
+        // left weights of 0, infinities or NaN behind; rows where the latter stay
+        // nonfinite take the difference in the second sweep.)
         auto nonfinite = [&]() {  // any of this lane's sums
             bool bad = !(l < INFINITY);
 #pragma unroll
@@ -1393,14 +1399,15 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
             return bad;
         };
         sweep(IC<kAll>{});
-        if (__any(nonfinite())) hidden = 1;
+        apart = m != -INFINITY && fabsf(m) * p.c2 > kLargeScore;
+        if (__any(nonfinite() || apart)) hidden = 1;
         __syncthreads();
         if (hidden) {
             for (int again = 0; again < 2; ++again) {
                 start();
                 sweep(IC<kFinite>{});
                 const int bad = nonfinite();
-                apart = bad || __shfl_xor(bad, 32, 64);  // the lanes of a row alike
+                apart = apart || bad || __shfl_xor(bad, 32, 64);  // the lanes of a row alike
             }
             sweep(IC<kRest>{});
         }
