@@ -561,7 +561,8 @@ int32_t llama_residual_add(const void *a, const void *b, void *out, int64_t n, v
  *          blocks of 16 tokens, the tokens innermost (the order in which the
  *          product of probabilities and values reads them)
  *   k_exp, v_exp: [n_pages, n_kv_heads, page_size] bytes, 127 - b for a bias b
- *          (clamped to b <= 126): value = code * 2^(exp - 127).  NULL for bf16.
+ *          (clamped to b <= 126): value = code * 2^(exp - 127).  An append writes
+ *          1 to 247; 255 counts as 254.  NULL for bf16.
  * fmt: FP8_E4M3, FP8_E5M2 or LLAMA_CACHE_BF16.  (The paper's (a) formats are
  * FP8_ENOTSUP: the matrix cores do not read them.)  d_head 64 or 128
  * (FP8_ENOTSUP otherwise).  page_size: a power of two, 16 to 1024.

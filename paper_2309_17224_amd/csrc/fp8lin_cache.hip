@@ -301,8 +301,11 @@ __device__ __forceinline__ void decode4(uint32_t w, float* f) {
     f[2] = decode<FMT, 2>(w);
     f[3] = decode<FMT, 3>(w);
 }
-// 2^(e - 127) of an exponent byte (0: 2^-127, 255: NaN).
-__device__ __forceinline__ float unscale_of(uint32_t e) { return ldexpf(e == 255u ? __builtin_nanf("") : 1.0f, (int)e - 127); }
+// 2^(e - 127) of an exponent byte (0: 2^-127; 255 counts as 254, so that the weight 0 of
+// a token that a row does not see stays 0).
+__device__ __forceinline__ float exp_float(uint32_t e) {
+    return __uint_as_float(min(max(e << 23, 0x00400000u), 0x7F000000u));
+}
 
 // ------------------------------------------------------------- read
 // The same blocks; groups of `heads` heads, keys below gk, then values.  A
@@ -378,7 +381,7 @@ __global__ __launch_bounds__(kT) void read_kernel(CacheView c, uint16_t* __restr
             o0 = x[0];
             o1 = x[kV - 1];
         } else {
-            const float sc = unscale_of(ex);
+            const float sc = exp_float(ex);
             const uint32_t cw[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
             float f[16];
 #pragma unroll
@@ -478,7 +481,6 @@ __device__ __forceinline__ u32x4 cvt8b(uint32_t w0, uint32_t w1, float scale) {
     return u32x4{cvt2b<FMT, false>(w0, scale), cvt2b<FMT, true>(w0, scale), cvt2b<FMT, false>(w1, scale),
                  cvt2b<FMT, true>(w1, scale)};
 }
-__device__ __forceinline__ float exp_float(uint32_t e) { return __uint_as_float(e << 23); }
 
 // Key range of the packed rows m0 .. m1 - 1 of a sequence, as tiles of 64 keys
 // from a multiple of 64 on, and the `per` tiles of it that a split takes.
@@ -888,8 +890,7 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
                     // the difference first: its product with c2 is never above 0, however large the scores
                     pr[i] = __builtin_amdgcn_exp2f((sc[kt][i] - moff) * p.c2);
                     l += pr[i];
-                    // an exponent of a masked slot may be anything, its weight is 0
-                    if (FMT != kBf16) pr[i] *= exp_float(min((vex[kt] >> (8 * i)) & 0xFFu, 254u));
+                    if (FMT != kBf16) pr[i] *= exp_float((vex[kt] >> (8 * i)) & 0xFFu);
                 }
                 pf[kt >> 1][2 * (kt & 1)] = pack_bf16x2(pr[0], pr[1]);
                 pf[kt >> 1][2 * (kt & 1) + 1] = pack_bf16x2(pr[2], pr[3]);
