@@ -645,9 +645,11 @@ int32_t llama_cache_read(const llama_cache *cache, const llama_cache_seqs *seqs,
  * fmt .. ldq8: fused quantise of o as in llama_attention (q8 == NULL: none); its
  *        amax is over the rows of sequences only.
  * ws:    workspace of llama_cache_attention_ws_bytes(...) bytes, 16-byte aligned,
- *        whose first LLAMA_CACHE_WS_COUNTS bytes must hold zeros before the first
- *        call; every call that returns FP8_OK and runs to completion leaves them
- *        zero again (calls of other sizes may use it too).  The rest is scratch: it
+ *        whose first LLAMA_CACHE_WS_COUNTS bytes (counters) must hold zeros where q8 is
+ *        NULL; every call that returns FP8_OK and runs to completion leaves zeros there
+ *        (calls of other sizes may use it too), other entry points do not.  With q8 the
+ *        call clears the counters that it needs, so that a workspace which other fused
+ *        calls use will do.  The rest is scratch: it
  *        holds the partial results of key ranges that are computed apart and then
  *        joined.  Calls that may run at the same time need separate workspaces.
  * Softmax statistics and sums in fp32; the probabilities are rounded to bf16

@@ -1453,6 +1453,14 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
     return mag;
 }
 
+// The counts of a call with the fused quantise, whose workspace other fused calls may have
+// written (a launch of 1.6 us, only where items are cut: a count that does not start
+// from zero never says which part is the last, and the item's rows stay unwritten).
+__global__ __launch_bounds__(kT) void clear_kernel(int32_t* counts, int n) {
+    const int i = blockIdx.x * kT + threadIdx.x;
+    if (i < n) counts[i] = 0;
+}
+
 // The kernels.  Both in one launch where a call may have sequences of either kind:
 // the latency of the one is then under the work of the other.
 // Waves a SIMD: three where many_body's registers suffice (40 sequences of 128 rows
@@ -1732,6 +1740,10 @@ int32_t launch_cache_attention(const uint16_t* q, int64_t ldq, int nh, const Cac
     a.many_o = (float*)(base + pl.many_o);
     a.many_ml = (float2*)(base + pl.many_ml);
     a.many_wg = (int)pl.many_wg;
+    if (quant && pl.few && (pl.flat || pl.few_parts > 1)) {
+        const int n = c.n_seqs * c.nkv;
+        hipLaunchKernelGGL(clear_kernel, dim3((unsigned)((n + kT - 1) / kT)), dim3(kT), 0, s, a.counts, n);
+    }
     with_cache(fmt, d_head, [&](auto F, auto D) {
         constexpr int kF = decltype(F)::value, kD = decltype(D)::value;
         auto go = [&](auto kernel, int64_t wg) {

@@ -831,7 +831,8 @@ def llama_cache_attention_ws_bytes(rows: int, n_heads: int, cache: KVCache, seqs
 
 def cache_attention_workspace(rows: int, n_heads: int, cache: KVCache, seqs: CacheSeqs, max_rows: int) -> torch.Tensor:
     """Workspace of llama_cache_attention: its counters are zero, and left zero by
-    every completed call (one per stream of concurrent calls)."""
+    every completed call of it; other calls must not write it, unless it is only
+    used with a fused quantise (one per stream of concurrent calls)."""
     ws = torch.empty(max(llama_cache_attention_ws_bytes(rows, n_heads, cache, seqs, max_rows), CACHE_WS_COUNTS),
                      dtype=torch.uint8, device=cache.device)
     ws[:CACHE_WS_COUNTS].zero_()
@@ -841,9 +842,10 @@ def cache_attention_workspace(rows: int, n_heads: int, cache: KVCache, seqs: Cac
 def llama_cache_attention(q, cache: KVCache, seqs: CacheSeqs, n_heads: int, max_rows: int, window: int = 0, o=None,
                           fq: FusedQuant | None = None, ws=None, stream=None):
     """Causal grouped-query attention of the call's rows (q [rows, n_heads
-    d_head]) over the cache, optionally with the fused quantise of o (its ws, a
-    cache_attention_workspace, is then the call's; without
-    either one is made for the call, on the current stream only).  max_rows: at least the rows of every sequence.  Returns o."""
+    d_head]) over the cache, optionally with the fused quantise of o (its ws, of
+    llama_cache_attention_ws_bytes and shared with other fused calls if wanted, is
+    then the call's; without either one is made for the call, on the current stream
+    only).  max_rows: at least the rows of every sequence.  Returns o."""
     dev = cache._dev
     rows, cols = q.shape[0], n_heads * cache.d_head
     ldq = _mat(q, "q", rows, cols, dev)

@@ -1,0 +1,74 @@
+"""The cache attention's fused quantise with the workspace of other fused calls, and outputs
+that the binding makes on a stream of the caller's."""
+import numpy as np
+import pytest
+import torch
+
+from cache_cases import Case, blank, rand_bits, strided
+from paper_2309_17224_amd import fp8lin as F
+from parity_util import np_bits
+from test_gpu_cache import say
+
+pytestmark = pytest.mark.gpu
+
+
+#       heads kv page capacity new total; the counters that it uses are cleared
+CUT = [(8, 1, 64, 500, [1], [9001]),                                       # parts of an item
+       (16, 8, 1024, 48, [1] * 6, [1, 3000, 64, 0, 777, 900]),             # shares
+       (16, 4, 512, 40, [1] * 30 + [50], [20 * i + 1 for i in range(30)] + [400]),   # shares beside a chunk
+       (8, 8, 32, None, [1] * 40, [30] * 40)]                              # neither
+
+
+@pytest.mark.parametrize("heads,kv,page,capacity,new,total", CUT)
+def test_workspace_of_another_fused_call(gpu, heads, kv, page, capacity, new, total):
+    """A FusedQuant whose workspace RMSNorm or anything else has written: the same outputs,
+    again and again, and in a captured graph."""
+    say("workspace of another call", heads, kv, page, capacity, new[:3], total[:3])
+    c = Case(91, heads, kv, 128, F.E4M3, page, new, total, capacity=capacity)
+    cols, cut = heads * 128, capacity is not None
+    q = strided(rand_bits(c.rng, (c.rows, cols)), gpu, 0)
+    cache, seqs = c.device(gpu)
+    want = F.llama_cache_attention(q, cache, seqs, heads, c.max_rows)
+    rq, _, rb, ra, rf = F.fp8_quantise(want, F.E4M3)
+    size = max(F.llama_cache_attention_ws_bytes(c.rows, heads, cache, seqs, c.max_rows), F.llama_rmsnorm_ws_bytes(1000))
+    ws = torch.empty((size,), dtype=torch.uint8, device=gpu)
+    x, gain = torch.randn((1000, 512), device=gpu).to(torch.bfloat16), torch.ones(512, device=gpu).to(torch.bfloat16)
+    nq, ns = torch.empty((1000, 512), dtype=torch.uint8, device=gpu), torch.zeros(3, dtype=torch.int32, device=gpu)
+
+    def norm():
+        F.llama_rmsnorm_quantise(x, gain, fq=F.FusedQuant(nq, ns[0:1], ws, amax_bits=ns[1:2], flags=ns[2:3]))
+
+    q8, s = torch.empty((c.rows, cols), dtype=torch.uint8, device=gpu), torch.zeros(3, dtype=torch.int32, device=gpu)
+    o = blank(c.rows, cols, gpu)
+    fq = F.FusedQuant(q8, s[0:1], ws, amax_bits=s[1:2], flags=s[2:3])
+
+    def attend():
+        F.llama_cache_attention(q, cache, seqs, heads, c.max_rows, o=o, fq=fq)
+
+    def expect():
+        torch.cuda.synchronize()
+        assert torch.equal(o.view(torch.int16), want.view(torch.int16)) and torch.equal(q8, rq)
+        assert s.cpu().tolist() == [int(rb.item()), int(ra.item()), int(rf.item())]
+        assert not cut or not ws[:4 * len(new) * kv].count_nonzero()
+        o.fill_(7.0)
+        q8.fill_(0x55)
+        s.fill_(77)
+
+    norm()
+    attend()
+    expect()
+    for byte in (0xFF, 0x7F, 0x01):
+        ws.fill_(byte)
+        attend()
+        expect()
+        attend()
+        expect()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        norm()
+        attend()
+    for byte in (0xFF, 0x00, 0x01, 0x80):
+        ws.fill_(byte)
+        g.replay()
+        expect()
+    assert np.isfinite(np_bits(want).astype(np.float64)).all()
