@@ -709,12 +709,32 @@ def _shaped(t: torch.Tensor, name: str, shape, dtype, device) -> torch.Tensor:
 CACHE_WS_COUNTS = 65536
 
 
-class KVCache:
+class _Described:
+    """An object whose C struct (address in _ref) holds the pointers and sizes of its
+    attributes: those cannot be set to others, which the struct would not follow."""
+    _fixed = frozenset()
+
+    def __setattr__(self, name, value):
+        if name in self._fixed and "_ref" in self.__dict__ and value is not self.__dict__.get(name):  # += sets the same one
+            raise AttributeError(f"{type(self).__name__}.{name} cannot be replaced: copy into the tensor "
+                                 f"(.copy_()), or make another {type(self).__name__}")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        if name in self._fixed:
+            raise AttributeError(f"{type(self).__name__}.{name} cannot be deleted")
+        object.__delattr__(self, name)
+
+
+class KVCache(_Described):
     """Pages of keys and values (llama_cache): fmt E4M3 or E5M2 (codes with one
     exponent byte per token and head, value = code * 2^(exp - 127)) or
     CACHE_BF16.  k [n_pages, n_kv_heads, page_size, d_head], v [n_pages,
     n_kv_heads, page_size / 16, d_head, 16], k_exp and v_exp [n_pages,
-    n_kv_heads, page_size]; buffers that are not given are allocated, empty."""
+    n_kv_heads, page_size]; buffers that are not given are allocated, empty.  The
+    tensors' contents may change, the attributes are those of the construction."""
+    _fixed = frozenset(("k", "v", "k_exp", "v_exp", "n_pages", "n_kv_heads", "d_head", "page_size", "fmt", "device",
+                        "_c", "_ref", "_dev"))
 
     def __init__(self, n_pages: int, n_kv_heads: int, d_head: int, page_size: int, fmt: int, device, k=None, v=None,
                  k_exp=None, v_exp=None):
@@ -732,13 +752,16 @@ class KVCache:
             self.v_exp = torch.empty(es, dtype=u8, device=dev) if v_exp is None else _shaped(v_exp, "v_exp", es, u8, dev)
         self._c = CacheStruct(_p(self.k), _p(self.v), _p(self.k_exp), _p(self.v_exp), n_pages, n_kv_heads, d_head,
                               page_size, self.fmt)
-        self._ref, self._dev = ctypes.addressof(self._c), self.k.get_device()
+        self._dev = self.k.get_device()
+        self._ref = ctypes.addressof(self._c)
 
 
-class CacheSeqs:
+class CacheSeqs(_Described):
     """The sequences of a call (llama_cache_seqs), int32 device tensors: cu_rows
     [n + 1], kv_len [n] (tokens cached, the call's own included), pages [n,
-    max_pages].  Their contents may change between calls."""
+    max_pages].  Their contents may change between calls (cu_rows.copy_(...)), the
+    attributes are those of the construction."""
+    _fixed = frozenset(("cu_rows", "kv_len", "pages", "n_seqs", "max_pages", "device", "_c", "_ref", "_dev"))
 
     def __init__(self, cu_rows: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor):
         n = kv_len.numel()
@@ -751,7 +774,8 @@ class CacheSeqs:
         self.cu_rows, self.kv_len, self.pages = cu_rows, kv_len, pages
         self.n_seqs, self.max_pages, self.device = n, pages.shape[1], kv_len.device
         self._c = SeqsStruct(_p(cu_rows), _p(kv_len), _p(pages), n, self.max_pages, _ld(pages))
-        self._ref, self._dev = ctypes.addressof(self._c), kv_len.get_device()
+        self._dev = kv_len.get_device()
+        self._ref = ctypes.addressof(self._c)
 
 
 _BF16 = torch.bfloat16
