@@ -804,6 +804,14 @@ def _mat(t: torch.Tensor, name: str, rows: int, cols: int, dev: int) -> int:
     return stride[0] if shape[0] > 1 else max(cols, 1)
 
 
+def _new(rows: int, cols: int, device, stream) -> torch.Tensor:
+    """bf16 output [rows, cols] of a call, of the memory of the stream that writes it."""
+    if stream is None:
+        return torch.empty((rows, cols), dtype=_BF16, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty((rows, cols), dtype=_BF16, device=device)
+
+
 def llama_cache_append(qkv, cache: KVCache, seqs: CacheSeqs, n_heads: int, table=None, q=None, stream=None):
     """Rotate the queries and keys of the call's rows (table: llama_rope_table of
     at least max_pages * page_size positions; None: no rotation) and write keys
@@ -813,7 +821,7 @@ def llama_cache_append(qkv, cache: KVCache, seqs: CacheSeqs, n_heads: int, table
     rows, dh = qkv.shape[0], cache.d_head
     ld = _mat(qkv, "qkv", rows, (n_heads + 2 * cache.n_kv_heads) * dh, dev)
     if q is None:
-        q = torch.empty((rows, n_heads * dh), dtype=_BF16, device=qkv.device)
+        q = _new(rows, n_heads * dh, qkv.device, stream)
     ldq = _mat(q, "q", rows, n_heads * dh, dev)
     tp, tn = None, 0
     if table is not None:
@@ -837,9 +845,9 @@ def llama_cache_read(cache: KVCache, seqs: CacheSeqs, rows: int, k=None, v=None,
     dev = cache._dev
     cols = cache.n_kv_heads * cache.d_head
     if want_k and k is None:
-        k = torch.empty((rows, cols), dtype=_BF16, device=cache.device)
+        k = _new(rows, cols, cache.device, stream)
     if want_v and v is None:
-        v = torch.empty((rows, cols), dtype=_BF16, device=cache.device)
+        v = _new(rows, cols, cache.device, stream)
     ldk = _mat(k, "k", rows, cols, dev) if k is not None else 0
     ldv = _mat(v, "v", rows, cols, dev) if v is not None else 0
     _cache_device(cache, seqs)
@@ -874,7 +882,7 @@ def llama_cache_attention(q, cache: KVCache, seqs: CacheSeqs, n_heads: int, max_
     rows, cols = q.shape[0], n_heads * cache.d_head
     ldq = _mat(q, "q", rows, cols, dev)
     if o is None:
-        o = torch.empty((rows, cols), dtype=_BF16, device=q.device)
+        o = _new(rows, cols, q.device, stream)
     ldo = _mat(o, "o", rows, cols, dev)
     quant = _NO_QUANT[:-2]
     _cache_device(cache, seqs)

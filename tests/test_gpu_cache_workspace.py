@@ -72,3 +72,30 @@ def test_workspace_of_another_fused_call(gpu, heads, kv, page, capacity, new, to
         g.replay()
         expect()
     assert np.isfinite(np_bits(want).astype(np.float64)).all()
+
+
+def test_outputs_made_on_the_callers_stream(gpu):
+    """Outputs that a call on a stream makes are of that stream's memory, not of the current
+    one's, whose freed blocks may be in use by its pending work; their values are right."""
+    say("outputs on a stream")
+    c = Case(92, 8, 2, 128, F.E4M3, 16, [1, 30], [900, 200])
+    cache, seqs = c.device(gpu)
+    x = strided(rand_bits(c.rng, (c.rows, 12 * 128)), gpu, 0)
+    q = F.llama_cache_append(x, cache, seqs, 8)
+    want = [q, *F.llama_cache_read(cache, seqs, c.rows), F.llama_cache_attention(q, cache, seqs, 8, 30)]
+    ws = F.cache_attention_workspace(c.rows, 8, cache, seqs, 30)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    spare = [torch.empty_like(w) for w in want for _ in range(3)]      # freed blocks of their sizes on the current stream
+    torch.cuda.synchronize()
+    del spare
+    q2 = F.llama_cache_append(x, cache, seqs, 8, stream=st)
+    got = [q2, *F.llama_cache_read(cache, seqs, c.rows, stream=st),
+           F.llama_cache_attention(q2, cache, seqs, 8, 30, ws=ws, stream=st)]
+    st.synchronize()
+    segments = torch.cuda.memory_snapshot()
+    for t, w in zip(got, want):
+        at = t.data_ptr()
+        home = [g for g in segments if g["address"] <= at < g["address"] + g["total_size"]]
+        assert len(home) == 1 and home[0]["stream"] == st.cuda_stream
+        assert torch.equal(t, w)
