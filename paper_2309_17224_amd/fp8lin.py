@@ -898,6 +898,8 @@ def llama_cache_attention(q, cache: KVCache, seqs: CacheSeqs, n_heads: int, max_
         ws = cache_attention_workspace(rows, n_heads, cache, seqs, max_rows)
     if ws.get_device() != dev:
         raise ValueError(f"ws: on {ws.device}, the cache on GPU {dev}")
+    if not ws.is_contiguous():  # an expanded one is shorter than its elements
+        raise ValueError("ws: expected a contiguous tensor")
     st = lib().llama_cache_attention(q.data_ptr(), rows, ldq, n_heads, cache._ref, seqs._ref, max_rows, window,
                                      o.data_ptr(), ldo, *quant, ws.data_ptr(), ws.numel() * ws.element_size(),
                                      _stream(stream))

@@ -99,3 +99,17 @@ def test_outputs_made_on_the_callers_stream(gpu):
         home = [g for g in segments if g["address"] <= at < g["address"] + g["total_size"]]
         assert len(home) == 1 and home[0]["stream"] == st.cuda_stream
         assert torch.equal(t, w)
+
+
+def test_workspace_of_fewer_bytes_than_elements(gpu):
+    """An expanded tensor is refused, as the call's workspace and as a fused quantise's."""
+    say("expanded workspace")
+    c = Case(93, 8, 2, 128, F.E4M3, 16, [1], [40])
+    cache, seqs = c.device(gpu)
+    q = strided(rand_bits(c.rng, (1, 1024)), gpu, 0)
+    size = F.llama_cache_attention_ws_bytes(1, 8, cache, seqs, 1)
+    q8, s = torch.empty((1, 1024), dtype=torch.uint8, device=gpu), torch.zeros(1, dtype=torch.int32, device=gpu)
+    for ws in (torch.zeros(1, dtype=torch.uint8, device=gpu).expand(size), torch.zeros(2 * size, dtype=torch.uint8, device=gpu)[::2]):
+        for kw in (dict(ws=ws), dict(fq=F.FusedQuant(q8, s, ws))):
+            with pytest.raises(ValueError, match="contiguous"):
+                F.llama_cache_attention(q, cache, seqs, 8, 1, **kw)
