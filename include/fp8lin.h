@@ -585,8 +585,8 @@ int32_t llama_residual_add(const void *a, const void *b, void *out, int64_t n, v
  * a page number outside [0, n_pages) is a page that is absent, and so is every
  * position below 0 or from max_pages * page_size on.  Tokens at absent places
  * are not stored, read back as zeros, and are seen by no query.
- * Sequences may share pages that none of them writes.  Two rows of one call
- * that write the same slot leave either's codes there.
+ * Sequences may share pages that none of them writes.  Where two rows of one call
+ * write the same slot, its codes and exponents are a mixture of theirs.
  */
 #define LLAMA_CACHE_BF16 16
 typedef struct llama_cache {
@@ -645,18 +645,22 @@ int32_t llama_cache_read(const llama_cache *cache, const llama_cache_seqs *seqs,
  * fmt .. ldq8: fused quantise of o as in llama_attention (q8 == NULL: none); its
  *        amax is over the rows of sequences only.
  * ws:    workspace of llama_cache_attention_ws_bytes(...) bytes, 16-byte aligned,
- *        whose first LLAMA_CACHE_WS_COUNTS bytes (counters) must hold zeros where q8 is
- *        NULL; every call that returns FP8_OK and runs to completion leaves zeros there
- *        (calls of other sizes may use it too), other entry points do not.  With q8 the
- *        call clears the counters that it needs, so that a workspace which other fused
- *        calls use will do.  The rest is scratch: it
- *        holds the partial results of key ranges that are computed apart and then
- *        joined.  Calls that may run at the same time need separate workspaces.
- * Softmax statistics and sums in fp32; the probabilities are rounded to bf16
- * for the product with the values, and o is rounded once.  The key ranges
- * depend on the sizes of the call (n_heads, rows, n_seqs, max_rows, max_pages,
- * window) and on the lengths, never on timing: a call gives the same bits every
- * time.
+ *        whose first LLAMA_CACHE_WS_COUNTS bytes (counters) must hold zeros where q8
+ *        is NULL; every call that returns FP8_OK and runs to completion leaves zeros
+ *        there (calls of other sizes may use it too), other entry points do not.  With
+ *        q8 the call clears the counters that it needs, so that a workspace which other
+ *        fused calls use will do.  The rest is scratch: it holds the partial results of
+ *        key ranges that are computed apart and then joined.  Calls that may run at the
+ *        same time need separate workspaces.
+ * Softmax statistics and sums in fp32; the probabilities (in FP8 times the
+ * value's 2^(exp - 127)) are rounded to bf16 for the product with the values, and o
+ * is rounded once.  Scores may be of any size, as long as q . k is finite in fp32.
+ * The sums are of up to 2^8 times the values and are divided at the end: those of a
+ * row that sees n keys are finite where n |v|, in FP8 n max_num 2^(exp - 127), is
+ * below 2^120; what is rounded to bf16 below 2^-126 is off by up to 2^-134 (times the
+ * value, in FP8 its code).  The key ranges depend on the sizes of the call (n_heads,
+ * rows, n_seqs, max_rows, max_pages, window) and on the lengths, never on timing: a
+ * call gives the same bits every time.
  */
 #define LLAMA_CACHE_WS_COUNTS 65536
 size_t llama_cache_attention_ws_bytes(int64_t rows, int32_t n_heads, const llama_cache *cache,

@@ -1,5 +1,6 @@
 """Exponent bytes that no append writes: 255 counts as 254 in every call, and where a row
-does not see its token it does not reach the row; 0 is 2^-127."""
+does not see its token it does not reach the row; 0 is 2^-127.  And values at both ends of
+the range that the attention takes."""
 import numpy as np
 import pytest
 import torch
@@ -9,11 +10,11 @@ from oracle import cache as C
 from oracle import decoder as D
 from paper_2309_17224_amd import fp8lin as F
 from parity_util import np_bits
-from test_gpu_cache import check, say
+from test_gpu_cache import bound, check, say
 
 pytestmark = pytest.mark.gpu
 
-E4, E5 = F.E4M3, F.E5M2
+E4, E5, BF = F.E4M3, F.E5M2, F.CACHE_BF16
 
 #       new total at window: rows at the token's place or behind it, and within the window, see it
 TOKENS = [([40], [150], 140, 0), ([5], [100], 97, 0), ([70], [500], 400, 65), ([5], [300], 232, 65),
@@ -102,3 +103,39 @@ def test_exponent_0(gpu, fmt, heads):
     o = D.bf16_to_f64(np_bits(F.llama_cache_attention(strided(q, gpu, 0), cache, seqs, heads, 1)))
     want = np.repeat(c.host.value(c.pages[0, 0], 0)[1], heads // 2, axis=0).reshape(1, -1)
     assert np.array_equal(o, want)
+
+
+@pytest.mark.parametrize("new,total,at,window", TOKENS)
+@pytest.mark.parametrize("fmt", [E4, E5, BF])
+@pytest.mark.parametrize("large", [True, False])
+def test_range_of_values(gpu, large, fmt, new, total, at, window):
+    """The largest values whose sums are stated to be finite, of one sign, and small
+    exponents: within the bound, there with 2^-134 of the largest code for each key."""
+    say("range of values", large, fmt, new, total, window)
+    c = Case(85, 4, 2, 128, fmt, 16, new, total)
+    n = max(total)
+    if fmt == BF:       # scaled by a power of two
+        e = 120 - int(np.ceil(np.log2(n))) if large else -120
+        v = np.abs(c.rng.standard_normal(c.host.v.shape)) if large else c.rng.standard_normal(c.host.v.shape)
+        v = np.clip(v / 4, -0.996, 0.996)
+        c.host.v[...] = C.round_bf16(np.ldexp(v, e))
+        code = 2.0 ** e
+    else:
+        top = 8.81 if fmt == E4 else 15.81                 # log2 of the largest code, rounded up
+        e = int(np.ceil(120 - np.log2(n) - top)) - 1 if large else -113
+        c.host.v_exp[...] = c.rng.integers(e + 125, e + 128, c.host.v_exp.shape)
+        if large:
+            c.host.v[...] &= 0x7F
+        code = 2.0 ** top
+        assert not large or n * 2.0 ** (top + e) < 2.0 ** 120
+    q = rand_bits(c.rng, (c.rows, 512), 2.0)
+    cache, seqs = c.device(gpu)
+    o = F.llama_cache_attention(strided(q, gpu, 0), cache, seqs, 4, c.max_rows, window=window)
+    want, mean, top = C.attention(q, c.host, c.cu, c.kv_len, c.pages, 4, window=window)
+    got = D.bf16_to_f64(np_bits(o))
+    tiny = 0.0 if large else n * 2.0 ** -134 * code + 2.0 ** -134      # the output below bf16's normal range
+    scale = 2.0 ** (-100 if large else 100)                # bound's own floor is for ordinary values
+    lim = bound(c, want * scale, mean * scale, top) / scale + 1.02 * tiny
+    assert np.isfinite(got).all()
+    print("worst %.3f of the bound" % (np.abs(got - want) / lim).max(), flush=True)
+    assert (np.abs(got - want) <= lim).all()
