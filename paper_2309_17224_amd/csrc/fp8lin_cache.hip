@@ -167,8 +167,9 @@ __device__ __forceinline__ uint32_t mag_f(const float* f, int n, uint32_t m) {
 }
 
 // Groups below gqk: heads_qk query and key heads each, others: heads_v value heads.
+// q may be qkv's query columns: a lane writes there what it has read before.
 template <int FMT, int DH>
-__global__ __launch_bounds__(kT) void append_kernel(CacheView c, const uint16_t* __restrict__ qkv, int64_t ld, int nh,
+__global__ __launch_bounds__(kT) void append_kernel(CacheView c, const uint16_t* qkv, int64_t ld, int nh,
                                                     const float2* __restrict__ table, uint16_t* q, int64_t ldq, int gqk,
                                                     int heads_qk, int heads_v) {
     using A = Append<FMT, DH>;
@@ -766,21 +767,23 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
 
         u32x4 kreg[kKt][kKv], vreg[kDt];
         u32x4 kex, vex;
-        int kn, vn;            // valid keys of the two groups (0 if the page is absent)
-        int64_t kbase, vbase;  // slots of their first keys
+        int64_t kbase, vbase;  // slots of the first keys of the two groups
+        int vn;                // valid keys of the values' one (0 if the page is absent)
         auto page_in = [&](int t, int grp) {
             const int key = rg.start + kKeys * t + kG * grp;
             const int i = min(key >> c.page_shift, c.max_pages - 1);  // in the table, where the key is not
             return c.pages[(int64_t)s * c.ld_pages + i];
         };
-        auto where = [&](int t, int grp, int page, int& n) {
-            const int key = rg.start + kKeys * t + kG * grp;
-            const bool here = page >= 0 && page < c.n_pages;
-            n = here ? max(min(rg.kend - key, kG), 0) : 0;
-            return slot_of(c, here ? page : 0, hk, key);
+        auto here = [&](int page) { return page >= 0 && page < c.n_pages; };
+        auto where = [&](int t, int grp, int page) {
+            return slot_of(c, here(page) ? page : 0, hk, rg.start + kKeys * t + kG * grp);
+        };
+        auto values_at = [&](int t, int page) {
+            vbase = where(t, g, page);
+            vn = here(page) ? max(min(rg.kend - (rg.start + kKeys * t + kG * g), kG), 0) : 0;
         };
         auto load_k = [&](int t) {
-            kbase = where(t, rb, kpage, kn);
+            kbase = where(t, rb, kpage);
             if (FMT != kBf16) kex = *(const u32x4*)(c.ke + kbase);
 #pragma unroll
             for (int kt = 0; kt < kKt; ++kt)
@@ -794,7 +797,7 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
             return c.v + ((vbase & ~(int64_t)(kBlk - 1)) * DH + (16 * dt + r16) * kBlk + (vbase & (kBlk - kG))) * kEsz<FMT>;
         };
         auto load_v = [&](int t) {
-            vbase = where(t, g, vpage, vn);
+            values_at(t, vpage);
             if (FMT != kBf16) vex = *(const u32x4*)(c.ve + vbase);
 #pragma unroll
             for (int dt = 0; dt < kDt; ++dt) vreg[dt] = __builtin_nontemporal_load((const u32x4*)v_at(dt));
@@ -928,7 +931,7 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
 #pragma unroll 1
             for (t = tfirst; t < tend; t += kFewW) {
                 const int kb = rg.start + kKeys * t;
-                vbase = where(t, g, page_in(t, g), vn);
+                values_at(t, page_in(t, g));
                 if (!is_edge(kb)) continue;
                 const uint32_t bits = seen_bits(kb);
                 uint32_t mk[4];
