@@ -602,8 +602,8 @@ __device__ __forceinline__ void add_part(float* acc, float& ll, float2 ml, float
 // of the rows, the scores that lane (q, g) gets are of the keys G g + 4 kt + i, whose
 // values for dimension 16 dt + r it reads as one vector.  Nothing moves between
 // lanes.  The cache is read once: its loads carry the non-temporal hint.  Bound by
-// memory: 32 sequences of up to 16000 tokens, 64 heads on 8, in 95 us (5.2 TB/s; 6.0 to
-// 6.4 where the lengths are equal, a plain sum over as much memory 6.0), 16 of up to 2500
+// memory: 32 sequences of up to 16000 tokens, 64 heads on 8, in 95 us (5.2 TB/s; 16 to 64
+// of 8000 to 16000 each 5.9 to 6.5, a plain sum over 1 GiB 6.0), 16 of up to 2500
 // with 32 heads of their own in 32 us; one token over 300 in 7.5, mostly its loads in turn.
 //
 // Work: without `flat` a workgroup takes one item, a (sequence, key/value head), or
@@ -1079,9 +1079,10 @@ __device__ __forceinline__ uint32_t few_body(const AttnArgs& p, FewLds<DH>& lds,
 //
 // Bound by what two waves a SIMD overlap of 32 matrix instructions (a third of the
 // time), 291 vector instructions (as long) and 51 of LDS (as long) a tile, at d_head
-// 128 in E4M3: 512 tokens over 8192 before them, 64 heads on 8, in 177 to 182 us
-// (800 to 780 TFLOP/s; a library product of 8192^3 runs at 1190), 2 x 2048 tokens of 32
-// heads in bf16 in 105 to 107 (650).  Measured and left: software pipelining within a wave (spills at
+// 128 in E4M3: 512 tokens over 8192 before them, 64 heads on 8, in 176 to 182 us
+// (805 to 780 TFLOP/s; a library product of 8192^3 runs at 1190), 2 x 2048 tokens of 32
+// heads in bf16 in 104 to 109 (660 to 630; the attention within a call, which has whole
+// sequences and no pages, takes 81).  Measured and left: software pipelining within a wave (spills at
 // 128; 122 us against 128 at 64), matrix instructions on FP8 operands (see above).
 template <int DH>
 struct ManyLds {
@@ -1393,7 +1394,7 @@ __device__ __forceinline__ uint32_t many_body(const AttnArgs& p, ManyLds<DH>& sh
         // difference first.  (Below, the rounding is 2^-11, a fraction of that of the
         // probabilities.  A maximum that was above 2^15 on the way and is not at the end
         // left weights of 0, infinities or NaN behind; rows where the latter stay
-        // nonfinite take the difference in the second sweep.)
+        // nonfinite take the difference in the second sweep.)  Four sweeps in place of one.
         auto nonfinite = [&]() {  // any of this lane's sums
             bool bad = !(l < INFINITY);
 #pragma unroll
@@ -1661,8 +1662,9 @@ Plan plan_of(int64_t rows, int nh, int nkv, int d_head, int64_t n_seqs, int64_t 
     const int64_t items = n_seqs * nkv;
     // few_body.  Shares where a compute unit would have much to read and the
     // items are few enough to be uneven (measured: 32 sequences of up to 16000
-    // tokens, 8 heads, 97 us against 126 with an item a workgroup; but 16 of up to 2500, 32 heads, 78
-    // against 34).  Parts where items would leave compute units idle: about
+    // tokens, 8 heads, 97 us against 126 with an item a workgroup; but 16 of up to 2500, 32 heads, 81
+    // against 32).  Lengths are on the device: the rule goes by the table's, and those 16
+    // take shares too where it holds 4096 positions.  Parts where items would leave compute units idle: about
     // sqrt(2 tiles) of them, since a part costs the join what half a tile costs
     // its reader (one of 30000 tokens, 8 heads: 469 tiles, 29 parts 26 us, 64 parts 36).
     p.flat = p.few && items <= kCounts && n_seqs <= kFlatSeqs && items < 8 * kCus && tiles >= kFlatTiles &&

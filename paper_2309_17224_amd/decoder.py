@@ -253,7 +253,8 @@ class CachedDecoderLayer(DecoderLayer):
 
     kv_fmt: E4M3 or E5M2 (one Eq. 3 bias per token and head) or CACHE_BF16.
     cache: a KVCache to use (shared pages), or None for one of n_pages pages of
-    page_size tokens.  max_rows: the most rows of one sequence in a call."""
+    page_size tokens.  max_rows: the most rows of one sequence in a call.  The
+    activation biases are of all rows of a call (DecoderLayer's bias_per="tensor")."""
 
     def __init__(self, cfg: LayerConfig, weights: dict, device, n_seqs: int, max_pages: int, page_size: int = 64,
                  n_pages: int | None = None, kv_fmt: int = F.E4M3, max_rows: int | None = None, window: int = 0,
