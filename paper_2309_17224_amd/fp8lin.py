@@ -864,7 +864,8 @@ def llama_cache_attention_ws_bytes(rows: int, n_heads: int, cache: KVCache, seqs
 def cache_attention_workspace(rows: int, n_heads: int, cache: KVCache, seqs: CacheSeqs, max_rows: int) -> torch.Tensor:
     """Workspace of llama_cache_attention: its counters are zero, and left zero by
     every completed call of it; other calls must not write it, unless it is only
-    used with a fused quantise (one per stream of concurrent calls)."""
+    used with a fused quantise (one per stream of concurrent calls).  The zeros are
+    written on the current stream: a first call on another one has to wait for it."""
     ws = torch.empty(max(llama_cache_attention_ws_bytes(rows, n_heads, cache, seqs, max_rows), CACHE_WS_COUNTS),
                      dtype=torch.uint8, device=cache.device)
     ws[:CACHE_WS_COUNTS].zero_()
