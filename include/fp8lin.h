@@ -84,6 +84,14 @@ extern "C" {
 #define FP8_FLAG_ZERO 2u
 #define FP8_FLAG_SATURATED 4u  /* fp8_quantise_delayed: the codes of this call clipped */
 
+/* Activations of the feed-forward calls: x; max(x, 0); x Phi(x); x (1 + tanh(sqrt(2/pi)
+ * (x + 0.044715 x^3))) / 2; x / (1 + exp(-x)). */
+#define FP8_ACT_NONE 0
+#define FP8_ACT_RELU 1
+#define FP8_ACT_GELU 2
+#define FP8_ACT_GELU_TANH 3
+#define FP8_ACT_SILU 4
+
 /* Largest accepted |margin|. */
 #define FP8_MAX_MARGIN 65536
 
@@ -544,6 +552,153 @@ int32_t llama_swiglu_quantise(const void *gu, int64_t ldgu, int64_t rows, int64_
  * multiple of 8); out may be a or b.  Exact rounding of the sum.
  */
 int32_t llama_residual_add(const void *a, const void *b, void *out, int64_t n, void *stream);
+
+/*
+ * ---- the feed-forward block: what lies around its FP8 linears --------------
+ * Training needs the layers between the FP8 linears forward and backward: the
+ * GPT models (Table 1) have LayerNorm, biases, GELU and residual sums, Llama 2 a
+ * gated pair of projections (SwiGLU).  The matmuls below do in their epilogue what
+ * follows the product (or, backward, what follows the grad-input product on its
+ * way to the linear before); fp32 arithmetic throughout, every output rounded once.
+ * Tensors are row-major with row strides (ld*, in elements) of any length from
+ * the row's on and start on their element size; FP8 operands are as in
+ * fp8_linear_fwd and fp8_linear_bwd_dx (dense, 16-byte aligned).  Outputs must not
+ * overlap inputs unless stated.
+ *
+ * fp8_out_quantise -- codes of a call's output (a host struct of device pointers,
+ * read before the call returns; NULL: none): the same bits as fp8_quantise of it.
+ * fmt .. flags: as fp8_quantise.  q: out, codes, row stride ldq.  qT: out, optional,
+ * the transposed codes, row stride ldqT.  ws: workspace of the call's size, 4-byte
+ * aligned; scratch, distinct for calls that may run at the same time.
+ * An empty output has amax 0, bias 0 and FP8_FLAG_ZERO.
+ */
+typedef struct fp8_out_quantise {
+    int32_t fmt, margin;
+    const int32_t *bias_pred;
+    int32_t *bias;
+    uint32_t *amax_bits, *flags;
+    uint8_t *q;
+    int64_t ldq;
+    uint8_t *qT;
+    int64_t ldqT;
+    void *ws;
+    size_t ws_bytes;
+} fp8_out_quantise;
+
+/*
+ * fp8_linear_fwd_act -- forward FP8 matmul with bias, activation and residual sum:
+ *   z = 2^-(bx + bw) X8 W8 + bias;  y = round(act(z) + res)
+ * x8, bx, w8t, bw: as fp8_linear_fwd.
+ * bias:  optional, [N] of type bias_dt.  act: FP8_ACT_*.
+ * res:   optional, [M, N] of y's type; may be y itself (ldres = ldy).
+ * z:     out, optional, bf16 [M, N]: the values before the activation, rounded, for
+ *        fp8_linear_bwd_dx_act.
+ * y:     out, [M, N], y_dt = FP8_DT_BF16 or FP8_DT_F32.
+ * quant: optional, codes of y; its ws of fp8_linear_quantise_ws_bytes(M, N) bytes.
+ * K == 0: z = bias.  M == 0 or N == 0: no output.
+ */
+int32_t fp8_linear_fwd_act(const uint8_t *x8, const int32_t *bx, const uint8_t *w8t, const int32_t *bw,
+                           const void *bias, int32_t bias_dt, int32_t act, const void *res, int64_t ldres, void *z,
+                           int64_t ldz, void *y, int32_t y_dt, int64_t ldy, int64_t M, int64_t N, int64_t K,
+                           const fp8_out_quantise *quant, void *stream);
+
+/*
+ * fp8_linear_fwd_glu -- both projections of a gated feed-forward block, the
+ * activation and the product in one matmul:
+ *   (g | u) = 2^-(bx + bw) X8 (Wg | Wu) + bias;  a = round(act(g) u)
+ * x8, bx: [M, K] codes.  w8t, bw: [2 N, K] E4M3 codes, the gate's N rows first, as
+ *         the transposed cast of a fused gate+up weight [K, 2 N].
+ * bias:   optional, [2 N].  act: FP8_ACT_* (Llama 2: FP8_ACT_SILU).
+ * gu:     out, optional, bf16 [M, 2 N]: g and u, rounded, for fp8_linear_bwd_dx_glu
+ *         (a is of the unrounded ones).
+ * a:      out, bf16 [M, N].  quant: codes of a, ws of fp8_linear_quantise_ws_bytes(M, N).
+ * N is at most 2^30 - 16 (FP8_ENOTSUP beyond).
+ */
+int32_t fp8_linear_fwd_glu(const uint8_t *x8, const int32_t *bx, const uint8_t *w8t, const int32_t *bw,
+                           const void *bias, int32_t bias_dt, int32_t act, void *gu, int64_t ldgu, void *a, int64_t lda,
+                           int64_t M, int64_t N, int64_t K, const fp8_out_quantise *quant, void *stream);
+
+/*
+ * fp8_linear_bwd_dx_act -- grad-input FP8 matmul of a linear whose input was
+ * act(z), down to the gradient of z:
+ *   t = 2^-(bg + bw) dY8 W8^T;  dz = round(t act'(z));  db = sum over rows of t act'(z)
+ * dy8, bg, w8, bw: as fp8_linear_bwd_dx (dY8 [M, N], W8 [K, N]).
+ * z:     bf16 [M, K] (fp8_linear_fwd_act of the linear before).
+ * dz:    out, bf16 [M, K]; may be z itself (lddz = ldz).
+ * db:    out, optional, [K] of type db_dt: the gradient of that linear's bias, summed
+ *        in fp32 in an order that the sizes alone set, rounded once.
+ * quant: optional, codes of dz; its ws of fp8_linear_quantise_ws_bytes(M, K) bytes.
+ * ws:    with db, workspace of gpt_bias_grad_ws_bytes(M, K) bytes, 4-byte aligned;
+ *        scratch, distinct for calls that may run at the same time.
+ * N == 0: t = 0.  M == 0: db = 0.
+ * The slope of FP8_ACT_RELU at 0 is 0.
+ */
+size_t gpt_bias_grad_ws_bytes(int64_t rows, int64_t cols);
+int32_t fp8_linear_bwd_dx_act(const uint8_t *dy8, const int32_t *bg, const uint8_t *w8, const int32_t *bw,
+                              const void *z, int64_t ldz, int32_t act, void *dz, int64_t lddz, void *db, int32_t db_dt,
+                              int64_t M, int64_t N, int64_t K, const fp8_out_quantise *quant, void *ws, size_t ws_bytes,
+                              void *stream);
+
+/*
+ * fp8_linear_bwd_dx_glu -- grad-input FP8 matmul of the down projection, down to the
+ * gradients of the gate's and the up projection's outputs:
+ *   t = 2^-(bg + bw) dY8 W8^T;  dg = round(t u act'(g));  du = round(t act(g))
+ * dy8, bg, w8, bw: dY8 [M, N], W8 [K, N] (the down projection's codes).
+ * gu:    bf16 [M, 2 K] (fp8_linear_fwd_glu).
+ * dgu:   out, bf16 [M, 2 K], dg first; may be gu itself (lddgu = ldgu).
+ * db:    out, optional, [2 K]: the sums over rows, as in fp8_linear_bwd_dx_act.
+ * quant: codes of dgu, ws of fp8_linear_quantise_ws_bytes(M, 2 K).
+ * ws:    with db, gpt_bias_grad_ws_bytes(M, 2 K) bytes.
+ * K is at most 2^30 - 16 (FP8_ENOTSUP beyond).
+ */
+int32_t fp8_linear_bwd_dx_glu(const uint8_t *dy8, const int32_t *bg, const uint8_t *w8, const int32_t *bw,
+                              const void *gu, int64_t ldgu, int32_t act, void *dgu, int64_t lddgu, void *db,
+                              int32_t db_dt, int64_t M, int64_t N, int64_t K, const fp8_out_quantise *quant, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/*
+ * gpt_bias_grad -- db = sum over the rows of dy [rows, cols] (type dt, row stride
+ * lddy), the gradient of a bias: fp32 sums in an order that the sizes alone set,
+ * rounded once to db_dt.  rows == 0 gives zeros.
+ * ws: gpt_bias_grad_ws_bytes(rows, cols) bytes, 4-byte aligned; scratch.
+ */
+int32_t gpt_bias_grad(const void *dy, int32_t dt, int64_t rows, int64_t cols, int64_t lddy, void *db, int32_t db_dt,
+                      void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * gpt_layernorm_quantise -- LayerNorm of each row, optionally of a residual sum:
+ *   h = x (res == NULL) or round(x + res);
+ *   y = round((h - mean) rstd g + b),  rstd = 1 / sqrt(mean_j (h_j - mean)^2 + eps)
+ * x, res, h, y: [rows, cols] of type dt (bf16 or fp32); g, b: [cols] of type g_dt,
+ * b optional.  h: out, optional (the new residual stream).
+ * mean, rstd: out, optional, fp32 [rows], for gpt_layernorm_bwd.
+ * quant: optional, codes of y (bf16 only, without qT: FP8_ENOTSUP otherwise); its ws
+ *        of gpt_layernorm_ws_bytes(rows) bytes.
+ * eps >= 0.  Statistics in fp32, the variance of the centred values.
+ */
+size_t gpt_layernorm_ws_bytes(int64_t rows);
+int32_t gpt_layernorm_quantise(const void *x, int64_t ldx, const void *res, int64_t ldr, int32_t dt, const void *g,
+                               const void *b, int32_t g_dt, int64_t rows, int64_t cols, float eps, void *h, int64_t ldh,
+                               void *y, int64_t ldy, float *mean, float *rstd, const fp8_out_quantise *quant,
+                               void *stream);
+
+/*
+ * gpt_layernorm_bwd -- its gradients: with xh = (h - mean) rstd and w = dy g,
+ *   dx = round(rstd (w - mean_j w_j - xh mean_j (w_j xh_j)) + dres)
+ *   dg = sum over rows of dy xh;  db = sum over rows of dy
+ * dy, h, dres, dx: [rows, cols] of type dt; h: the normalised sum (x itself without a
+ * residual).  dres: optional, the gradient that reaches h past the norm; dx is then
+ * that of the residual stream.
+ * dg, db: out, optional, fp32 [cols], summed in an order that the sizes alone set.
+ * ws: with dg or db, gpt_layernorm_bwd_ws_bytes(rows, cols) bytes, 4-byte aligned;
+ *     scratch, distinct for calls that may run at the same time.
+ * rows == 0: dg = db = 0.
+ */
+size_t gpt_layernorm_bwd_ws_bytes(int64_t rows, int64_t cols);
+int32_t gpt_layernorm_bwd(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dres, int64_t lddr,
+                          int32_t dt, const void *g, int32_t g_dt, const float *mean, const float *rstd, int64_t rows,
+                          int64_t cols, void *dx, int64_t lddx, float *dg, float *db, void *ws, size_t ws_bytes,
+                          void *stream);
 
 /*
  * ---- paged key/value cache of the decoder layer --------------------------

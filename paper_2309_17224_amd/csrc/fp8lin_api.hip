@@ -575,6 +575,193 @@ int32_t llama_residual_add(const void* a, const void* b, void* out, int64_t n, v
     return launch_residual_add((const uint16_t*)a, (const uint16_t*)b, (uint16_t*)out, n, as_stream(stream));
 }
 
+// ---- the feed-forward block
+}  // extern "C"
+
+namespace {
+bool act_ok(int32_t a) { return a >= FP8_ACT_NONE && a <= FP8_ACT_SILU; }
+bool sizes_ok(int64_t m, int64_t n, int64_t k) {
+    return m >= 0 && n >= 0 && k >= 0 && m <= kMaxDim && n <= kMaxDim && k <= kMaxDim;
+}
+// A tensor of `cols` columns and element size `size`.
+bool rows_at(const void* p, int64_t ld, int64_t cols, int size) { return p && aligned(p, size) && ld >= cols; }
+
+// Arguments of an output's quantise (null: none).  need: bytes of its workspace.
+int32_t out_quant_checks(const fp8_out_quantise* t, int64_t rows, int64_t cols, size_t need) {
+    if (!t) return FP8_OK;
+    if (!fmt_ok(t->fmt) || t->margin < -FP8_MAX_MARGIN || t->margin > FP8_MAX_MARGIN) return FP8_EINVAL;
+    if (!t->bias || !aligned(t->bias, 4) || (t->bias_pred && !aligned(t->bias_pred, 4))) return FP8_EINVAL;
+    if ((t->amax_bits && !aligned(t->amax_bits, 4)) || (t->flags && !aligned(t->flags, 4))) return FP8_EINVAL;
+    if (rows == 0 || cols == 0) return FP8_OK;
+    if (!t->q || t->ldq < cols || (t->qT && t->ldqT < rows)) return FP8_EINVAL;
+    if (!t->ws || !aligned(t->ws, 4) || t->ws_bytes < need) return FP8_EINVAL;
+    return FP8_OK;
+}
+
+int32_t out_quant_empty(const fp8_out_quantise* t, void* stream) {
+    if (!t) return FP8_OK;
+    return launch_scale_bias(nullptr, FP8_DT_BF16, 0, t->fmt, t->margin, t->bias, t->amax_bits, t->flags, nullptr,
+                             as_stream(stream));
+}
+
+// The checks that the four matmuls share, then the call.  e: everything but the
+// workspace's sums; out_cols: columns of the output; db: the column sums, or null.
+int32_t epilogue_mm(int mode, Epi& e, int64_t out_cols, void* db, int32_t db_dt, const fp8_out_quantise* quant, void* ws,
+                    size_t ws_bytes, void* stream) {
+    if (!sizes_ok(e.M, e.N, e.K) || !act_ok(e.act) || !dt_ok(e.out_dt)) return FP8_EINVAL;
+    const bool empty = e.M == 0 || e.N == 0;
+    const int32_t st = out_quant_checks(quant, e.M, out_cols, quant ? fp8_linear_quantise_ws_bytes(e.M, out_cols) : 0);
+    if (st != FP8_OK) return st;
+    if (db && (!dt_ok(db_dt) || !aligned(db, esize(db_dt)))) return FP8_EINVAL;
+    if (!empty) {
+        if (!e.ba || !e.bb || !aligned(e.ba, 4) || !aligned(e.bb, 4)) return FP8_EINVAL;
+        if ((e.K > 0 && (!e.A || !e.B)) || !operands_ok(e.A, e.B, e.K)) return FP8_EINVAL;
+        const int64_t wide = mode == kEpiGlu ? 2 * e.N : out_cols;  // columns of what is kept or read back
+        if (!rows_at(e.out, e.ldo, out_cols, esize(e.out_dt))) return FP8_EINVAL;
+        if (e.bias && (!dt_ok(e.bias_dt) || !aligned(e.bias, esize(e.bias_dt)))) return FP8_EINVAL;
+        if (e.res && !rows_at(e.res, e.ldres, out_cols, esize(e.out_dt))) return FP8_EINVAL;
+        if (e.keep && !rows_at(e.keep, e.ldkeep, wide, 2)) return FP8_EINVAL;
+        if ((mode == kEpiActBwd || mode == kEpiGluBwd) && !rows_at(e.z, e.ldz, wide, 2)) return FP8_EINVAL;
+        if (db && (!ws || !aligned(ws, 4) || ws_bytes < gpt_bias_grad_ws_bytes(e.M, out_cols))) return FP8_EINVAL;
+        const bool pair = mode == kEpiGlu || mode == kEpiGluBwd;
+        if (e.M > INT32_MAX || e.N > (pair ? ((int64_t)1 << 30) - 16 : INT32_MAX)) return FP8_ENOTSUP;
+    }
+    if (empty) {
+        const int32_t qst = out_quant_empty(quant, stream);
+        if (qst != FP8_OK || !db || out_cols == 0) return qst;
+        return launch_sums_finish(nullptr, 0, out_cols, db, out_cols, nullptr, db_dt, as_stream(stream));
+    }
+    e.sums = db ? (float*)ws : nullptr;
+    e.sum_cols = out_cols;
+    int32_t lst = launch_epilogue_mm(mode, e, as_stream(stream));
+    if (lst == FP8_OK && db)
+        lst = launch_sums_finish((const float*)ws, epi_sum_rows(mode, e.M, e.N, e.K), out_cols, db, out_cols, nullptr, db_dt,
+                                 as_stream(stream));
+    if (lst != FP8_OK || !quant) return lst;
+    return launch_quantise(e.out, e.out_dt, e.M, out_cols, e.ldo, quant->fmt, quant->margin, quant->bias_pred, quant->bias,
+                           quant->amax_bits, quant->flags, quant->q, quant->ldq, quant->qT, quant->ldqT,
+                           (uint32_t*)quant->ws, as_stream(stream));
+}
+}  // namespace
+
+extern "C" {
+
+int32_t fp8_linear_fwd_act(const uint8_t* x8, const int32_t* bx, const uint8_t* w8t, const int32_t* bw, const void* bias,
+                           int32_t bias_dt, int32_t act, const void* res, int64_t ldres, void* z, int64_t ldz, void* y,
+                           int32_t y_dt, int64_t ldy, int64_t M, int64_t N, int64_t K, const fp8_out_quantise* quant,
+                           void* stream) {
+    Epi e{};
+    e.A = x8, e.B = w8t, e.ba = bx, e.bb = bw, e.M = M, e.N = N, e.K = K, e.act = act, e.out_dt = y_dt;
+    e.bias = bias, e.bias_dt = bias_dt, e.res = res, e.ldres = ldres, e.keep = (uint16_t*)z, e.ldkeep = ldz;
+    e.out = y, e.ldo = ldy;
+    return epilogue_mm(kEpiAct, e, N, nullptr, 0, quant, nullptr, 0, stream);
+}
+
+int32_t fp8_linear_fwd_glu(const uint8_t* x8, const int32_t* bx, const uint8_t* w8t, const int32_t* bw, const void* bias,
+                           int32_t bias_dt, int32_t act, void* gu, int64_t ldgu, void* a, int64_t lda, int64_t M, int64_t N,
+                           int64_t K, const fp8_out_quantise* quant, void* stream) {
+    Epi e{};
+    e.A = x8, e.B = w8t, e.ba = bx, e.bb = bw, e.M = M, e.N = N, e.K = K, e.act = act, e.out_dt = FP8_DT_BF16;
+    e.bias = bias, e.bias_dt = bias_dt, e.keep = (uint16_t*)gu, e.ldkeep = ldgu, e.out = a, e.ldo = lda;
+    return epilogue_mm(kEpiGlu, e, N, nullptr, 0, quant, nullptr, 0, stream);
+}
+
+int32_t fp8_linear_bwd_dx_act(const uint8_t* dy8, const int32_t* bg, const uint8_t* w8, const int32_t* bw, const void* z,
+                              int64_t ldz, int32_t act, void* dz, int64_t lddz, void* db, int32_t db_dt, int64_t M,
+                              int64_t N, int64_t K, const fp8_out_quantise* quant, void* ws, size_t ws_bytes,
+                              void* stream) {
+    // t [M, K] = dY8 [M, N] . W8 [K, N]^T: contraction over N.
+    Epi e{};
+    e.A = dy8, e.B = w8, e.ba = bg, e.bb = bw, e.M = M, e.N = K, e.K = N, e.act = act, e.out_dt = FP8_DT_BF16;
+    e.z = (const uint16_t*)z, e.ldz = ldz, e.out = dz, e.ldo = lddz;
+    return epilogue_mm(kEpiActBwd, e, K, db, db_dt, quant, ws, ws_bytes, stream);
+}
+
+int32_t fp8_linear_bwd_dx_glu(const uint8_t* dy8, const int32_t* bg, const uint8_t* w8, const int32_t* bw, const void* gu,
+                              int64_t ldgu, int32_t act, void* dgu, int64_t lddgu, void* db, int32_t db_dt, int64_t M,
+                              int64_t N, int64_t K, const fp8_out_quantise* quant, void* ws, size_t ws_bytes,
+                              void* stream) {
+    Epi e{};
+    e.A = dy8, e.B = w8, e.ba = bg, e.bb = bw, e.M = M, e.N = K, e.K = N, e.act = act, e.out_dt = FP8_DT_BF16;
+    e.z = (const uint16_t*)gu, e.ldz = ldgu, e.out = dgu, e.ldo = lddgu;
+    return epilogue_mm(kEpiGluBwd, e, 2 * K, db, db_dt, quant, ws, ws_bytes, stream);
+}
+
+size_t gpt_bias_grad_ws_bytes(int64_t rows, int64_t cols) {
+    if (rows <= 0 || cols <= 0 || rows > kMaxDim || cols > 2 * kMaxDim) return 0;
+    // a matmul's epilogue writes a row of sums for every 16 to 64 rows of its tiles
+    const int64_t n = (rows + 15) / 16 + 3, own = colsum_rows(rows, cols);
+    return (size_t)(n > own ? n : own) * (size_t)cols * sizeof(float);
+}
+
+int32_t gpt_bias_grad(const void* dy, int32_t dt, int64_t rows, int64_t cols, int64_t lddy, void* db, int32_t db_dt,
+                      void* ws, size_t ws_bytes, void* stream) {
+    if (!sizes_ok(rows, cols, 0) || !dt_ok(dt) || !dt_ok(db_dt)) return FP8_EINVAL;
+    if (cols == 0) return FP8_OK;
+    if (!db || !aligned(db, esize(db_dt))) return FP8_EINVAL;
+    if (rows == 0) return launch_sums_finish(nullptr, 0, cols, db, cols, nullptr, db_dt, as_stream(stream));
+    if (!rows_at(dy, lddy, cols, esize(dt))) return FP8_EINVAL;
+    if (!ws || !aligned(ws, 4) || ws_bytes < gpt_bias_grad_ws_bytes(rows, cols)) return FP8_EINVAL;
+    if (cols > INT32_MAX) return FP8_ENOTSUP;
+    return launch_colsum(dy, dt, rows, cols, lddy, db, db_dt, (float*)ws, as_stream(stream));
+}
+
+size_t gpt_layernorm_ws_bytes(int64_t rows) {
+    if (rows <= 0 || rows > kMaxDim) return 0;
+    return (size_t)(1 + rows) * sizeof(uint32_t);
+}
+
+int32_t gpt_layernorm_quantise(const void* x, int64_t ldx, const void* res, int64_t ldr, int32_t dt, const void* g,
+                               const void* b, int32_t g_dt, int64_t rows, int64_t cols, float eps, void* h, int64_t ldh,
+                               void* y, int64_t ldy, float* mean, float* rstd, const fp8_out_quantise* quant,
+                               void* stream) {
+    if (!sizes_ok(rows, cols, 0) || !dt_ok(dt) || !dt_ok(g_dt) || !(eps >= 0.0f) || eps > 3.0e38f) return FP8_EINVAL;
+    const int32_t st = out_quant_checks(quant, rows, cols, quant ? gpt_layernorm_ws_bytes(rows) : 0);
+    if (st != FP8_OK) return st;
+    if (rows == 0 || cols == 0) return out_quant_empty(quant, stream);
+    const int size = esize(dt);
+    if (!rows_at(x, ldx, cols, size) || !rows_at(y, ldy, cols, size) || !g || !aligned(g, esize(g_dt))) return FP8_EINVAL;
+    if ((b && !aligned(b, esize(g_dt))) || (res && !rows_at(res, ldr, cols, size)) || (h && !rows_at(h, ldh, cols, size)))
+        return FP8_EINVAL;
+    if ((mean && !aligned(mean, 4)) || (rstd && !aligned(rstd, 4))) return FP8_EINVAL;
+    if (quant && (dt != FP8_DT_BF16 || quant->qT)) return FP8_ENOTSUP;
+    if (rows > INT32_MAX || cols > INT32_MAX) return FP8_ENOTSUP;
+    NormArgs a{};
+    a.rows = rows, a.cols = cols, a.ldx = ldx, a.ldr = ldr, a.ldh = ldh, a.ldy = ldy, a.dt = dt, a.g_dt = g_dt;
+    a.eps = eps, a.x = x, a.res = res, a.g = g, a.b = b, a.h = h, a.y = y, a.mean = mean, a.rstd = rstd;
+    FusedQuant fq{};
+    if (quant)
+        fq = FusedQuant{quant->fmt, quant->margin, quant->bias_pred, quant->bias, quant->amax_bits, quant->flags, quant->q,
+                        quant->ldq, (uint32_t*)quant->ws};
+    return launch_layernorm(a, quant ? &fq : nullptr, as_stream(stream));
+}
+
+size_t gpt_layernorm_bwd_ws_bytes(int64_t rows, int64_t cols) {
+    if (rows <= 0 || cols <= 0 || rows > kMaxDim || cols > kMaxDim) return 0;
+    return (size_t)norm_sum_rows(rows, cols) * 2 * (size_t)cols * sizeof(float);
+}
+
+int32_t gpt_layernorm_bwd(const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* dres, int64_t lddr,
+                          int32_t dt, const void* g, int32_t g_dt, const float* mean, const float* rstd, int64_t rows,
+                          int64_t cols, void* dx, int64_t lddx, float* dg, float* db, void* ws, size_t ws_bytes,
+                          void* stream) {
+    if (!sizes_ok(rows, cols, 0) || !dt_ok(dt) || !dt_ok(g_dt)) return FP8_EINVAL;
+    if ((dg && !aligned(dg, 4)) || (db && !aligned(db, 4))) return FP8_EINVAL;
+    if (cols == 0) return FP8_OK;
+    if (rows == 0)
+        return dg || db ? launch_sums_finish(nullptr, 0, 2 * cols, dg, cols, db, FP8_DT_F32, as_stream(stream)) : FP8_OK;
+    const int size = esize(dt);
+    if (!rows_at(dy, lddy, cols, size) || !rows_at(h, ldh, cols, size) || !rows_at(dx, lddx, cols, size)) return FP8_EINVAL;
+    if ((dres && !rows_at(dres, lddr, cols, size)) || !g || !aligned(g, esize(g_dt))) return FP8_EINVAL;
+    if (!mean || !rstd || !aligned(mean, 4) || !aligned(rstd, 4)) return FP8_EINVAL;
+    if ((dg || db) && (!ws || !aligned(ws, 4) || ws_bytes < gpt_layernorm_bwd_ws_bytes(rows, cols))) return FP8_EINVAL;
+    if (rows > INT32_MAX || cols > INT32_MAX) return FP8_ENOTSUP;
+    NormArgs a{};
+    a.rows = rows, a.cols = cols, a.ldx = ldh, a.ldy = lddx, a.lddy = lddy, a.lddr = lddr, a.dt = dt, a.g_dt = g_dt;
+    a.x = h, a.g = g, a.y = dx, a.mean = (float*)mean, a.rstd = (float*)rstd, a.dy = dy, a.dres = dres;
+    return launch_layernorm_bwd(a, dg, db, (float*)ws, as_stream(stream));
+}
+
 // ---- paged key/value cache
 }  // extern "C"
 

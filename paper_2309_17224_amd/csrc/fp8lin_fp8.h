@@ -274,6 +274,12 @@ __device__ __forceinline__ uint4 ld16_any(const void* p) {
 __device__ __forceinline__ void st8_any(void* p, uint32_t a, uint32_t b) { *(u32x2_any*)p = u32x2_any{a, b}; }
 __device__ __forceinline__ void st16_any(void* p, uint4 v) { *(u32x4_any*)p = u32x4_any{v.x, v.y, v.z, v.w}; }
 
+// 16-byte store with the non-temporal hint: outputs are not read again by the
+// kernel and should not displace cached operands.
+__device__ __forceinline__ void st_stream(void* p, uint4 v) {
+    __builtin_nontemporal_store(u32x4_any{v.x, v.y, v.z, v.w}, (u32x4_any*)p);
+}
+
 // v moved down by sh bits (0 <= sh <= 128), zeros from above.
 __device__ __forceinline__ uint4 shr128(uint4 v, int sh) {
     const uint64_t lo = v.x | ((uint64_t)v.y << 32), hi = v.z | ((uint64_t)v.w << 32);

@@ -46,16 +46,12 @@
 // K not a multiple of 128, or K >= 2^22: fp8lin_gemm_ragged.hip.
 #include <algorithm>
 
-#include "fp8lin_mm.h"
+#include "fp8lin_mm_256.h"
 
 namespace fp8lin {
 namespace {
 
 // ------------------------------------------------------------ main kernel
-constexpr int kBM = 256, kBN = 256, kBK = 128;
-constexpr int kMainThreads = 512;      // 8 waves: two groups of four
-constexpr int kTileBytes = kBM * kBK;  // one operand tile, 32 KiB
-
 __device__ __forceinline__ int bq_used(const int32_t* pred) { return clamp_bias(*pred); }
 
 // Epilogue staging rows (bytes): 32 output rows of a wave per pass; the
@@ -64,10 +60,8 @@ constexpr int kEpRowBf16 = 128 * 2 + 16, kEpRowF32 = 128 * 4 + 16;
 constexpr int kEpBf16Bytes = 8 * 32 * kEpRowBf16, kEpF32Bytes = 8 * 32 * kEpRowF32;
 constexpr int kCodesOff = kEpBf16Bytes;
 constexpr int kEpBytes = kCodesOff + kBM * kBN > kEpF32Bytes ? kCodesOff + kBM * kBN : kEpF32Bytes;
-// Main loop: two A stages and three B stages (B tiles are copied two steps
-// ahead, see gemm_tile); the epilogue reuses the space, and the workgroup's
-// amax words sit in its last 64 bytes, past every epilogue staging area.
-constexpr int kSmemBytes = 2 * kTileBytes + 3 * kBN * kBK;
+// The epilogue reuses the main loop's space, and the workgroup's amax words sit
+// in its last 64 bytes, past every epilogue staging area.
 constexpr int kWmxOff = kSmemBytes - 64;
 static_assert(kEpBytes <= kWmxOff && kSmemBytes <= 160 * 1024, "LDS budget");
 static_assert(kCodesOff % 16 == 0, "codes staging alignment");
@@ -99,10 +93,7 @@ __device__ __forceinline__ void gemm_tile(
     static_assert(QF < 0 || OUT_DT == FP8_DT_BF16, "fused quantise is for bf16 outputs");
     static_assert(QF < 0 || TN == 256, "fused quantise stages whole 256 x 256 tiles");
     static_assert(TN % 64 == 0 && TN >= 64 && TN <= 256, "tile width");
-    constexpr int kNbw = TN / 32;                  // 16-column blocks per wave, B copies per loader wave
-    constexpr int kBStage = TN * kBK;              // one B tile in LDS
-    constexpr int kNf = 4 + kNbw;                  // fragment pieces a wave reads per step
-    constexpr int kNc = 8 + kNbw;                  // copies a loader wave issues per stage
+    constexpr int kNbw = TN / 32;  // 16-column blocks per wave
 
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     // group (0: waves 0-3, 1: waves 4-7) and quadrant; wave-uniform
@@ -111,145 +102,11 @@ __device__ __forceinline__ void gemm_tile(
     tile_of(bid, nb, tiles_m, tiles_n, tm, tn);
     const int m0 = tm * kBM, n0 = col0 + tn * TN;
 
-    // Loader (group 0): wave sq fills rows [64 sq, 64 sq + 64) of the A tile
-    // and [TN/4 sq, TN/4 (sq + 1)) of the B tile, 8 rows per copy (voff[0..7]
-    // for A, voff[8..] for B); lane -> row r = (first row) + 8 i + lane / 8 and
-    // physical chunk lane % 8, which holds logical chunk (lane % 8) ^
-    // chunk_swz(r).  Rows past the matrix edge re-read the last row (their
-    // outputs are not stored).  Offsets are relative to the tile's first row,
-    // so they fit 32 bits for K < 2^22.
-    const int lrow = lane >> 3;
-    uint32_t voff[kNc];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = sq * 64 + i * 8 + lrow;
-        voff[i] = (uint32_t)((min(m0 + r, M - 1) - m0) * K + ((lane & 7) ^ chunk_swz(r)) * 16);
-    }
-#pragma unroll
-    for (int i = 0; i < kNbw; ++i) {
-        const int r = sq * (TN / 4) + i * 8 + lrow;
-        voff[8 + i] = (uint32_t)((min(n0 + r, N - 1) - n0) * K + ((lane & 7) ^ chunk_swz(r)) * 16);
-    }
-    const uint8_t* baseA = A + (int64_t)m0 * K;
-    const uint8_t* baseB = B + (int64_t)n0 * K;
-    // LDS addresses of this wave's first loader rows (wave-uniform); copy d
-    // < 8 fills A row group d, copy d >= 8 B row group d - 8.
-    // LDS: A stages 0 and 1 at s * kTileBytes, B stages 0, 1 and 2 after them.
-    const uint32_t lds_a = __builtin_amdgcn_readfirstlane(lds_addr(smem) + sq * 64 * kBK);
-    const uint32_t lds_b = __builtin_amdgcn_readfirstlane(lds_addr(smem) + 2 * kTileBytes + sq * (TN / 4) * kBK);
-    auto dma = [&](int d, int stage, int k0) {  // stage: of A for d < 8, of B for d >= 8
-        lds_dma16_s((d >= 8 ? baseB : baseA) + k0, voff[d],
-                    d >= 8 ? lds_b + (d - 8) * 8 * kBK + stage * kBStage : lds_a + d * 8 * kBK + stage * kTileBytes);
-    };
-
     // this wave's sub-tile: rows [wr0, wr0 + 64), columns [wc0, wc0 + TN/2) of the tile
     const int wr0 = (sq >> 1) * 128 + g * 64, wc0 = (sq & 1) * (TN / 2);
     const int frow = lane & 15, fg = lane >> 4;
-    // byte offsets (within a 16-row block) of this lane's two fragment pieces
-    const int fo0 = frow * kBK + (((2 * fg) ^ chunk_swz(frow)) << 4);
-    const int fo1 = frow * kBK + (((2 * fg + 1) ^ chunk_swz(frow)) << 4);
-
     v4f acc[4][kNbw];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < kNbw; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-
-    // Ping-pong pipeline.  Phases are separated by workgroup barriers; in
-    // every phase one group issues MFMAs and the other loads:
-    //   phase 1:        group 0 loads fragments of step 0
-    //   phase 2k + 2:   group 0 MFMAs of step k,   group 1 loads step k
-    //   phase 2k + 3:   group 0 loads step k + 1,  group 1 MFMAs of step k
-    // A load phase reads all kNf fragment pieces of the wave's next step and
-    // waits for them before the barrier.  A tile k sits in A stage k % 2, B
-    // tile k in B stage k % 3.  Group 0 copies A tile k + 1 in its load phase
-    // of step k (after both groups have read A tile k - 1 from that stage) and
-    // waits for the copies at the end of its next MFMA phase.  Group 1 copies
-    // B tile k + 2 in its load phase of step k (B tile k - 1 has been read by
-    // then) and, before that phase's barrier, waits for B tile k + 1 — issued
-    // one load phase earlier — but not for the copies it has just issued.
-    // Steps 0 and 1 are copied before phase 1.  Every wave passes 2 nk + 1
-    // barriers (group 1 passes one before its first load phase and none after
-    // its last MFMA phase), so the groups stay in step.
-    const int nk = K / kBK;
-    if (nk > 0) {
-        if (g == 0) {
-#pragma unroll
-            for (int d = 0; d < 8; ++d) dma(d, 0, 0);
-            if (nk > 1) {
-#pragma unroll
-                for (int d = 0; d < 8; ++d) dma(d, 1, kBK);
-                wait_vmcnt<8>();
-            } else {
-                wait_vmcnt<0>();
-            }
-        } else {
-#pragma unroll
-            for (int d = 8; d < kNc; ++d) dma(d, 0, 0);
-            if (nk > 1) {
-#pragma unroll
-                for (int d = 8; d < kNc; ++d) dma(d, 1, kBK);
-                wait_vmcnt<kNbw>();
-            } else {
-                wait_vmcnt<0>();
-            }
-        }
-        ws_barrier();
-        if (g == 1) ws_barrier();
-    }
-    v8i af[4], bf[kNbw];
-    int bs = 0;  // k % 3: the B stage of step k
-    for (int kt = 0; kt < nk; ++kt) {
-        const uint8_t* sa = smem + (kt & 1) * kTileBytes + wr0 * kBK;
-        const uint8_t* sb = smem + 2 * kTileBytes + bs * kBStage + wc0 * kBK;
-        if (g == 0 && kt >= 1 && kt + 1 < nk) {
-            // A tile of step kt + 1, the copies spread over the fragment reads
-            const int st = (kt + 1) & 1, k1 = (kt + 1) * kBK;
-#pragma unroll
-            for (int q = 0; q < kNf; ++q) {
-                if (q < 4) af[q] = ld_frag(sa + q * 16 * kBK, fo0, fo1);
-                else bf[q - 4] = ld_frag(sb + (q - 4) * 16 * kBK, fo0, fo1);
-                if (q < 8) dma(q, st, k1);
-            }
-#pragma unroll
-            for (int d = kNf; d < 8; ++d) dma(d, st, k1);
-        } else if (g == 1 && kt + 2 < nk) {
-            // B tile of step kt + 2 into the stage B tile kt - 1 used
-            const int st = bs == 0 ? 2 : bs - 1, k2 = (kt + 2) * kBK;
-#pragma unroll
-            for (int q = 0; q < kNf; ++q) {
-                if (q < 4) af[q] = ld_frag(sa + q * 16 * kBK, fo0, fo1);
-                else bf[q - 4] = ld_frag(sb + (q - 4) * 16 * kBK, fo0, fo1);
-                if (q < kNbw) dma(8 + q, st, k2);
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < kNf; ++q) {
-                if (q < 4) af[q] = ld_frag(sa + q * 16 * kBK, fo0, fo1);
-                else bf[q - 4] = ld_frag(sb + (q - 4) * 16 * kBK, fo0, fo1);
-            }
-        }
-        if (g == 1) {  // B tile kt + 1 has landed (the copies just issued need not have)
-            if (kt + 2 < nk) wait_vmcnt<kNbw>();
-            else wait_vmcnt<0>();
-        }
-        bs = bs == 2 ? 0 : bs + 1;
-        wait_lgkmcnt0();
-        ws_barrier();
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < kNbw; ++j) {
-                acc[i][j] = mfma16<FB, FA>(bf[j], af[i], acc[i][j]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        if (g == 0) {
-            wait_vmcnt<0>();
-            ws_barrier();
-        } else if (kt + 1 < nk) {
-            ws_barrier();
-        }
-    }
+    mm256_loop<FA, FB, TN, false>(smem, A, B, M, N, K, m0, n0, acc);
 
     // Epilogue: y = 2^-(ba + bb) acc (exact ldexp), rounded once to the output
     // type, staged through LDS 32 rows at a time per wave so that every global
@@ -430,7 +287,7 @@ __device__ __forceinline__ void gemm_tile(
 // The 256-row kernel.  Workgroups below g1 take 256 x 256 tiles (tiles_m x
 // tiles_n of them); with TN2 > 0 the rest take tiles TN2 wide over the
 // columns after them (tiles_m x tiles_n2), a last round of narrower tiles
-// instead of a partial round of full ones (see narrow_split).  g1 is a whole
+// instead of a partial round of full ones (see mm256_split).  g1 is a whole
 // number of rounds of 8 workgroups per XCD, so both parts keep their XCD
 // layout.
 template <int FA, int FB, int OUT_DT, bool AMAX, int QF = -1, int TN2 = 0>
@@ -479,40 +336,6 @@ __global__ void bias_finish_kernel(uint32_t* amax_out, BiasOut bo) {
 // take it.  The 256 x 256 tiles are few or finish apart.
 constexpr int64_t kFoldInLaunch = 256;
 
-// Columns of 256-wide tiles taken in whole rounds of kRound workgroups, and
-// the rest in one round of narrower tiles: with all 256-wide, a last partial
-// round costs as much as a full one.  E.g. 4096 x 11008 (16 x 43 tiles):
-// two rounds over the first 8192 columns, then 240 tiles 192 wide (0.75 of
-// the work each) over the last 2816.  Every output is still computed by one
-// workgroup over the whole K in the same order, so the bits do not change.
-// ndp: 256-wide tile columns; tw, tn2: width and count of the narrow ones
-// (tw = 0: no narrow launch).
-void narrow_split(int tiles_m, int tiles_n, int64_t N, int& ndp, int& tw, int& tn2) {
-    ndp = tiles_n;
-    tw = 0;
-    tn2 = 0;
-    const int64_t T = (int64_t)tiles_m * tiles_n;
-    if (T % kRound == 0 || tiles_m > kRound) return;
-    int gcd = kRound, b = tiles_m;
-    while (b) {
-        const int t = gcd % b;
-        gcd = b;
-        b = t;
-    }
-    const int step = kRound / gcd;  // tile columns per whole number of rounds
-    const int c = tiles_n / step * step;
-    const int64_t nrem = N - (int64_t)c * kBN;
-    for (int w : {64, 128, 192}) {
-        const int64_t strips = (nrem + w - 1) / w;
-        if (tiles_m * strips <= kRound) {
-            ndp = c;
-            tw = w;
-            tn2 = (int)strips;
-            return;
-        }
-    }
-}
-
 // Estimated time (us) of gemm_nt_256: a fit to its times at 33 to 2048 rows
 // and weights 512 to 57344 wide, on codes of normal data, weights in cache and
 // not (4 % off on average).  Per k-step: a part for each round of 256-wide
@@ -523,7 +346,7 @@ void narrow_split(int tiles_m, int tiles_n, int64_t N, int& ndp, int& tw, int& t
 double main_us(int64_t M, int64_t N, int64_t K) {
     const int64_t tiles_m = (M + kBM - 1) / kBM, tiles_n = (N + kBN - 1) / kBN;
     int ndp, tw, tn2;
-    narrow_split((int)tiles_m, (int)tiles_n, N, ndp, tw, tn2);
+    mm256_split((int)tiles_m, (int)tiles_n, N, ndp, tw, tn2);
     const double part = (double)(tiles_m * tn2) / kRound;
     const double weight = (double)N * (double)K, panels = (double)std::min<int64_t>(M, 8 * kBM) * (double)K + weight / 8;
     const double step = 1.24 * (double)((tiles_m * ndp + kRound - 1) / kRound) +
@@ -542,7 +365,7 @@ void launch_t(const MmRoute& r, const uint8_t* A, const int32_t* ba, const uint8
     } else {
         const int tiles_m = (int)((M + kBM - 1) / kBM), tiles_n = (int)((N + kBN - 1) / kBN);
         int ndp, tw, tn2;
-        narrow_split(tiles_m, tiles_n, N, ndp, tw, tn2);
+        mm256_split(tiles_m, tiles_n, N, ndp, tw, tn2);
         const int g1 = tiles_m * ndp, grid = g1 + tiles_m * tn2;
 #define FP8LIN_GEMM256(TW)                                                                                         \
     hipLaunchKernelGGL((gemm_nt_256<FA, FB, OUT_DT, AMAX, -1, TW>), dim3(grid), dim3(kMainThreads), 0, s, A, B, ba, \
@@ -602,6 +425,40 @@ void fused_fmt(int qfmt, const uint8_t* A, const int32_t* ba, const uint8_t* B, 
 
 }  // namespace
 
+// Columns of 256-wide tiles taken in whole rounds of kRound workgroups, and
+// the rest in one round of narrower tiles: with all 256-wide, a last partial
+// round costs as much as a full one.  E.g. 4096 x 11008 (16 x 43 tiles):
+// two rounds over the first 8192 columns, then 240 tiles 192 wide (0.75 of
+// the work each) over the last 2816.  Every output is still computed by one
+// workgroup over the whole K in the same order, so the bits do not change.
+// ndp: 256-wide tile columns; tw, tn2: width and count of the narrow ones
+// (tw = 0: no narrow launch).
+void mm256_split(int tiles_m, int tiles_n, int64_t N, int& ndp, int& tw, int& tn2) {
+    ndp = tiles_n;
+    tw = 0;
+    tn2 = 0;
+    const int64_t T = (int64_t)tiles_m * tiles_n;
+    if (T % kRound == 0 || tiles_m > kRound) return;
+    int gcd = kRound, b = tiles_m;
+    while (b) {
+        const int t = gcd % b;
+        gcd = b;
+        b = t;
+    }
+    const int step = kRound / gcd;  // tile columns per whole number of rounds
+    const int c = tiles_n / step * step;
+    const int64_t nrem = N - (int64_t)c * kBN;
+    for (int w : {64, 128, 192}) {
+        const int64_t strips = (nrem + w - 1) / w;
+        if (tiles_m * strips <= kRound) {
+            ndp = c;
+            tw = w;
+            tn2 = (int)strips;
+            return;
+        }
+    }
+}
+
 // The LDS-staged kernels need K a multiple of 128 and 32-bit offsets within a
 // tile.  The small tiles (fp8lin_gemm_stream.hip) take up to 32 rows always,
 // and beyond that where they are estimated to be faster: of 700 measured
@@ -610,10 +467,10 @@ void fused_fmt(int qfmt, const uint8_t* A, const int32_t* ba, const uint8_t* B, 
 // the best on average: 512 x 8192 x 8192 45.5 against 48.3 us, 1024 x 768 x 768
 // 6.0 against 7.8, 64 x 4096 x 11008 16.8 against 55.8; 1024 x 4096 x 4096 27.8
 // against 26.4 and 100 x 22016 x 4096 32.8 against 26.1, so those go there.
-MmRoute mm_route(int64_t M, int64_t N, int64_t K, bool with_amax) {
+MmRoute mm_route(int64_t M, int64_t N, int64_t K, bool with_amax, bool even) {
     if (K % kBK != 0 || K >= (1 << 22)) return {kMmRagged, 0, 0};
     MmRoute r{kMmStream, 0, 0};
-    const double us = stream_tile(M, N, K, with_amax, &r.mb, &r.nb);
+    const double us = stream_tile(M, N, K, with_amax, &r.mb, &r.nb, even);
     if (M <= 32) return r;
     const int64_t tiles = ((M + kBM - 1) / kBM) * ((N + kBN - 1) / kBN);
     if (tiles <= 16 * kRound && us < main_us(M, N, K)) return r;

@@ -10,44 +10,17 @@
 // 16-byte chunks XOR-swizzled as in the aligned kernels.  The last k-step's
 // bytes past the row end are zero in LDS, so they add nothing.  The k order
 // inside the sums is that of the 256 x 256 kernel with a zero-padded K.
-#include "fp8lin_mm.h"
+#include "fp8lin_mm_ragged.h"
 
 namespace fp8lin {
 namespace {
-
-constexpr int kRk = 128;  // bytes of k per step
-
-// Bytes [k, k + 16) of a row of K bytes, zero from K on; reads only bytes of
-// the row.  With K >= 16 one load ending at the row's end, moved down.
-__device__ __forceinline__ uint4 ld16_tail(const uint8_t* row, int64_t k, int64_t K) {
-    if (K < 16) {  // one or two loads that overlap: sixteen guarded bytes took 1.7 us
-        if (k > 0) return make_uint4(0u, 0u, 0u, 0u);
-        if (K >= 8) {
-            const u32x2_any lo = *(const u32x2_any*)row, hi = *(const u32x2_any*)(row + K - 8);
-            const uint64_t h = (hi.x | ((uint64_t)hi.y << 32)) >> 8 >> (8 * (15 - K));
-            return make_uint4(lo.x, lo.y, (uint32_t)h, (uint32_t)(h >> 32));
-        }
-        if (K >= 4) {
-            const uint32_t lo = *(const u32_any*)row, hi = *(const u32_any*)(row + K - 4);
-            return make_uint4(lo, hi >> 8 >> (8 * (7 - K)), 0u, 0u);
-        }
-        const uint32_t b0 = row[0], b1 = row[min((int64_t)1, K - 1)], b2 = row[K - 1];
-        return make_uint4(b0 | (K > 1 ? b1 << 8 : 0u) | (K > 2 ? b2 << 16 : 0u), 0u, 0u, 0u);
-    }
-    const int64_t at = min(k, K - 16);
-    const int sh = (int)min(k - at, (int64_t)16) * 8;  // bits to drop
-    return shr128(ld16_any(row + at), sh);
-}
 
 // One BM x BN output tile per workgroup, WT x WT per wave.
 template <int FA, int FB, int BM, int BN, int WT>
 __global__ __launch_bounds__((BM / WT) * (BN / WT) * 64) void gemm_nt_ragged(MmArgs p, int tiles_m, int tiles_n) {
     constexpr int kNt = (BM / WT) * (BN / WT) * 64, kWaves = kNt / 64;
-    constexpr int kRows = BM + BN, kStage = kRows * kRk;
-    constexpr int kRpi = kNt / 8;            // rows per load of the workgroup (8 lanes a row)
-    constexpr int kNc = kRows / kRpi;        // loads per thread and step
-    constexpr int kB = WT / 16;              // 16-row blocks of a wave's sub-tile
-    static_assert(kRows % kRpi == 0 && BM % kRpi == 0, "loader rows");
+    constexpr int kStage = (BM + BN) * kRk;
+    constexpr int kB = WT / 16;  // 16-row blocks of a wave's sub-tile
     // epilogue staging: 32 output rows of a wave at a time
     constexpr int kEpRow = WT * 4 + 16, kEpWave = 32 * kEpRow;
     constexpr int kSmem = 2 * kStage > kWaves * kEpWave ? 2 * kStage : kWaves * kEpWave;
@@ -59,81 +32,10 @@ __global__ __launch_bounds__((BM / WT) * (BN / WT) * 64) void gemm_nt_ragged(MmA
     const int64_t M = p.M, N = p.N, K = p.K;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
 
-    // loader: chunk tid % 8 of rows tid / 8 + i kRpi of the tile (A rows, then
-    // B rows); rows past the matrix edge read the last row (not stored)
-    const int lc = tid & 7, lr = tid >> 3;
-    const uint8_t* row[kNc];
-    uint32_t dst[kNc];
-#pragma unroll
-    for (int i = 0; i < kNc; ++i) {
-        const int r = lr + i * kRpi;
-        row[i] = i * kRpi < BM ? p.A + min(m0 + r, M - 1) * K : p.B + min(n0 + r - BM, N - 1) * K;
-        dst[i] = r * kRk + ((lc ^ chunk_swz(r)) << 4);
-    }
-    const int nk = (int)((K + kRk - 1) / kRk);
-    uint4 rg[kNc];
-    auto load = [&](int kt) {
-        const int64_t k = (int64_t)kt * kRk + lc * 16;
-        if ((int64_t)(kt + 1) * kRk <= K) {
-#pragma unroll
-            for (int i = 0; i < kNc; ++i) rg[i] = ld16_any(row[i] + k);
-        } else if (K % 16 == 0) {  // whole chunks, nothing to shift (1024 x 8 x 64: 4.6 us with)
-#pragma unroll
-            for (int i = 0; i < kNc; ++i) {
-                const uint4 v = ld16_any(row[i] + min(k, K - 16));
-                rg[i] = k < K ? v : make_uint4(0u, 0u, 0u, 0u);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kNc; ++i) rg[i] = ld16_tail(row[i], k, K);
-        }
-    };
-    auto store = [&](int kt) {
-        uint8_t* d = smem + (kt & 1) * kStage;
-#pragma unroll
-        for (int i = 0; i < kNc; ++i) *(uint4*)(d + dst[i]) = rg[i];
-    };
-
     const int wr0 = (w / (BN / WT)) * WT, wc0 = (w % (BN / WT)) * WT;
     const int frow = lane & 15, fg = lane >> 4;
-    const int fo0 = frow * kRk + (((2 * fg) ^ chunk_swz(frow)) << 4);
-    const int fo1 = frow * kRk + (((2 * fg + 1) ^ chunk_swz(frow)) << 4);
     v4f acc[kB][kB];
-#pragma unroll
-    for (int i = 0; i < kB; ++i)
-#pragma unroll
-        for (int j = 0; j < kB; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-
-    if (nk > 0) {
-        load(0);
-        store(0);
-        if (nk > 1) load(1);
-    }
-    wait_lgkmcnt0();
-    ws_barrier();
-    // step kt: write step kt + 1 (loaded during step kt - 1) into the other
-    // stage, which every wave finished reading before the last barrier, issue
-    // the loads of step kt + 2, multiply step kt
-    for (int kt = 0; kt < nk; ++kt) {
-        if (kt + 1 < nk) {
-            store(kt + 1);
-            if (kt + 2 < nk) load(kt + 2);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        const uint8_t* sa = smem + (kt & 1) * kStage + wr0 * kRk;
-        const uint8_t* sb = smem + (kt & 1) * kStage + (BM + wc0) * kRk;
-        v8i af[kB], bf[kB];
-#pragma unroll
-        for (int i = 0; i < kB; ++i) af[i] = ld_frag(sa + i * 16 * kRk, fo0, fo1);
-#pragma unroll
-        for (int j = 0; j < kB; ++j) bf[j] = ld_frag(sb + j * 16 * kRk, fo0, fo1);
-#pragma unroll
-        for (int i = 0; i < kB; ++i)
-#pragma unroll
-            for (int j = 0; j < kB; ++j) acc[i][j] = mfma16<FB, FA>(bf[j], af[i], acc[i][j]);
-        wait_lgkmcnt0();
-        ws_barrier();
-    }
+    ragged_loop<FA, FB, BM, BN, WT, false>(smem, p.A, p.B, M, N, K, m0, n0, acc);
 
     // Epilogue: unscale, round once, stage 32 rows of the wave at a time in
     // LDS (its own region) and store 16-byte pieces of whole row runs.

@@ -22,31 +22,17 @@
 //    result does not depend on timing.
 //  * 16-byte chunk c of LDS row r is stored at chunk c ^ (r % 16): the lanes
 //    of every ds_read_b128 phase (see fp8lin_gemm.hip) hit distinct banks.
-#include "fp8lin_mm.h"
+#include "fp8lin_mm_stream.h"
 
 namespace fp8lin {
 namespace {
 
-constexpr int kSlBuf = 3;
-
-// Waves 0-3 multiply; with more than 16 rows of A waves 4-7 copy, otherwise
-// the multiplying waves copy too (see the main loop).
-constexpr bool copy_waves(int mb) { return mb > 1; }
-constexpr int stream_threads(int mb) { return copy_waves(mb) ? 512 : 256; }
-constexpr int stream_kc(int mb, int nb) { return mb + nb <= 6 ? 512 : mb + nb <= 12 ? 256 : 128; }
-
 template <int FA, int FB, int MB, int NB>
 __global__ __launch_bounds__(stream_threads(MB)) void gemm_nt_stream(MmArgs p, int tiles_m, int nt) {
-    constexpr int kRowsB = 16 * NB, kRows = 16 * (MB + NB);
-    constexpr int kKC = stream_kc(MB, NB);
-    constexpr int kStage = kRows * kKC, kCpr = kKC / 16, kRpi = 64 / kCpr;  // chunks per row, rows per copy
-    constexpr int kNiw = kRows / kRpi / 4;                                  // copies per wave and stage
-    constexpr int kSlots = kKC / 128;
-    constexpr int kWn = kSlots == 4 ? 1 : 2, kWm = kSlots == 1 ? 2 : 1;  // waves over the tile's columns, rows
-    constexpr int kNbw = NB / kWn, kMbw = MB / kWm;
-    static_assert(kRows % (4 * kRpi) == 0 && NB % kWn == 0 && MB % kWm == 0, "tile split");
-    static_assert(kSlBuf * kStage <= 160 * 1024 && (kSlots == 1 || kSlots * MB * NB * 1024 <= kSlBuf * kStage), "LDS budget");
-    __shared__ __attribute__((aligned(1024))) uint8_t sm[kSlBuf * kStage];
+    using T = StreamTile<MB, NB>;
+    constexpr int kRowsB = 16 * NB, kSlots = T::kSlots, kNbw = T::kNbw, kMbw = T::kMbw;
+    static_assert(kSlots == 1 || kSlots * MB * NB * 1024 <= kSlBuf * T::kStage, "LDS budget");
+    __shared__ __attribute__((aligned(1024))) uint8_t sm[kSlBuf * T::kStage];
     __shared__ uint32_t wmx[8];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int M = (int)p.M, N = (int)p.N, K = (int)p.K;
@@ -56,109 +42,11 @@ __global__ __launch_bounds__(stream_threads(MB)) void gemm_nt_stream(MmArgs p, i
     int tm = tile % tiles_m, tn = tile / tiles_m;
     if (kSlots == 1) tile_of(blockIdx.x, gridDim.x, tiles_m, (N + kRowsB - 1) / kRowsB, tm, tn);
     const int m0 = tm * (16 * MB), n0 = tn * kRowsB;
-    // 16-byte chunk c of LDS row r is stored at chunk c ^ swz(r)
-    auto swz = [](int r) { return kKC == 128 ? chunk_swz(r) : r & 15; };
-
-    // copy t of this wave: LDS rows kRpi d .. (d = kNiw w + t), B rows first;
-    // rows past the matrix edge read the last row (their outputs are not stored)
-    const int lrow = lane / kCpr, lchunk = lane % kCpr;
-    uint32_t voff[kNiw];
-#pragma unroll
-    for (int t = 0; t < kNiw; ++t) {
-        const int r = ((w & 3) * kNiw + t) * kRpi + lrow;
-        const int src = r < kRowsB ? min(n0 + r, N - 1) - n0 : min(m0 + r - kRowsB, M - 1) - m0;
-        voff[t] = (uint32_t)(src * K + ((lchunk ^ swz(r)) << 4));
-    }
-    const uint8_t* baseA = p.A + (int64_t)m0 * K;
-    const uint8_t* baseB = p.B + (int64_t)n0 * K;
-    const uint32_t lds0 = lds_addr(sm);
-    const int nst = (K + kKC - 1) / kKC;
-    auto issue = [&](int st) {
-        const int buf = st % kSlBuf, end = K - st * kKC - 16;  // offset of the row's last chunk
-        const bool part = end + 16 < kKC;
-#pragma unroll
-        for (int t = 0; t < kNiw; ++t) {
-            const int d = (w & 3) * kNiw + t;
-            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + buf * kStage + d * 1024);
-            uint32_t v = voff[t];
-            if (part) {  // chunks past the row end re-read its last one (never multiplied)
-                const int c = (lchunk ^ swz(d * kRpi + lrow)) << 4;
-                v -= (uint32_t)max(0, c - end);
-            }
-            if (d * kRpi >= kRowsB) lds_dma16_s(baseA + (int64_t)st * kKC, v, dst);
-            else if (nt) lds_dma16_nt(baseB + (int64_t)st * kKC, v, dst);
-            else lds_dma16_s(baseB + (int64_t)st * kKC, v, dst);
-        }
-    };
-
     const int frow = lane & 15, fg = lane >> 4;
     const int slot = w % kSlots, part = (w & 3) / kSlots;
-    const int nb0 = part % kWn * kNbw, mb0 = part / kWn * kMbw;  // this wave's blocks of the tile
-    const int fo0 = frow * kKC + (((slot * 8 + 2 * fg) ^ swz(frow)) << 4);
-    const int fo1 = frow * kKC + (((slot * 8 + 2 * fg + 1) ^ swz(frow)) << 4);
+    const int nb0 = part % T::kWn * kNbw, mb0 = part / T::kWn * kMbw;  // this wave's blocks of the tile
     v4f acc[kMbw][kNbw];
-#pragma unroll
-    for (int i = 0; i < kMbw; ++i)
-#pragma unroll
-        for (int j = 0; j < kNbw; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    auto multiply = [&](int st) {
-        if (st * kKC + slot * 128 >= K) return;
-        const uint8_t* sb = sm + (st % kSlBuf) * kStage + nb0 * 16 * kKC;
-        const uint8_t* sa = sm + (st % kSlBuf) * kStage + (kRowsB + mb0 * 16) * kKC;
-        v8i bf[kNbw];
-#pragma unroll
-        for (int j = 0; j < kNbw; ++j) bf[j] = ld_frag(sb + j * 16 * kKC, fo0, fo1);
-#pragma unroll
-        for (int i = 0; i < kMbw; ++i) {
-            const v8i af = ld_frag(sa + i * 16 * kKC, fo0, fo1);
-#pragma unroll
-            for (int j = 0; j < kNbw; ++j) acc[i][j] = mfma16<FB, FA>(bf[j], af, acc[i][j]);
-        }
-        wait_lgkmcnt0();  // the next barrier frees this buffer
-    };
-    // wait until stage st has landed, stages up to `issued` being on their way
-    auto landed = [&](int st, int issued) {
-        if (st < issued) wait_vmcnt<kNiw>();
-        else wait_vmcnt<0>();
-    };
-    if (copy_waves(MB)) {
-        // Between barriers st and st + 1 the multiplying waves take stage st
-        // and the copying waves issue stage st + 2 into the buffer of stage
-        // st - 1 and wait for stage st + 1: an issue that stalls for room
-        // among the outstanding fills stalls no multiplication (100 x 12288 x
-        // 4096: 23.6 -> 18.0 us, 512 x 8192 x 8192: 93 -> 61 us).
-        if (w >= 4) {
-            if (nst > 0) issue(0);
-            if (nst > 1) issue(1);
-            landed(0, nst - 1);
-            ws_barrier();
-            for (int st = 0; st < nst; ++st) {
-                if (st + 2 < nst) issue(st + 2);
-                landed(st + 1, nst - 1);
-                ws_barrier();
-            }
-        } else {
-            ws_barrier();
-            for (int st = 0; st < nst; ++st) {
-                multiply(st);
-                ws_barrier();
-            }
-        }
-    } else {
-        // Few MFMAs per stage: copying waves of their own gain nothing and
-        // cost 1-5 % of a stream from HBM (16 x 57344 x 8192: 74.8 against
-        // 79.1 us).
-        if (nst > 0) issue(0);
-        if (nst > 1) issue(1);
-        for (int st = 0; st < nst; ++st) {
-            landed(st, nst - 1);
-            ws_barrier();
-            // the buffer of stage st - 1, which every wave has finished reading
-            if (st + 2 < nst) issue(st + 2);
-            multiply(st);
-        }
-        ws_barrier();
-    }
+    stream_loop<FA, FB, MB, NB, false>(sm, p.A, p.B, M, N, K, m0, n0, nt, acc);
     uint32_t mx = 0;
     const int bb = *p.bb;
     auto put = [&](int mb, int nb, v4f sum) {
@@ -210,14 +98,6 @@ void launch_one(const MmArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((gemm_nt_stream<FA, FB, MB, NB>), dim3((unsigned)(tm * tn)), dim3(stream_threads(MB)), 0, s, a, tm,
                        tm == 1);
 }
-
-// Tile shapes (16-row blocks of A and of B) the kernel is built for: those the
-// rule below chooses somewhere for 1 to 2048 rows and weights of 128 to 57344
-// ((1, 4), (4, 2) and (8, 4) only for calls that take the amax).
-#define FP8LIN_STREAM_TILES(X)                                                                             \
-    X(1, 1) X(1, 2) X(1, 3) X(1, 4) X(1, 5) X(1, 6) X(1, 8) X(2, 1) X(2, 2) X(2, 3) X(2, 4) X(2, 6) X(2, 8)  \
-    X(3, 1) X(3, 2) X(3, 3) X(3, 4) X(3, 6) X(3, 8) X(4, 2) X(4, 4) X(4, 6) X(4, 8) X(5, 2) X(5, 4) X(5, 6) \
-    X(6, 4) X(6, 6) X(8, 4) X(8, 8) X(10, 6)
 
 template <int FA, int FB>
 void launch_t(int mb, int nb, const MmArgs& a, hipStream_t s) {
@@ -287,11 +167,11 @@ constexpr double kFoldUs = 0.009;
 // depend on whether its amax is asked for, the best one with the folds counted
 // (256 x 768 x 768 with its amax: 14.4 us in the 768 workgroups that are best
 // without, 8.1 in 96; in gemm_nt_256 10.2).
-double stream_tile(int64_t M, int64_t N, int64_t K, bool with_amax, int* mb, int* nb) {
+double stream_tile(int64_t M, int64_t N, int64_t K, bool with_amax, int* mb, int* nb, bool even) {
     double best = 0;
     int kc = 0;
 #define FP8LIN_STREAM_COST(MB, NB)                                                                             \
-    if (16 * (MB - 1) < M || MB == 1)                                                                          \
+    if ((16 * (MB - 1) < M || MB == 1) && (NB % 2 == 0 || !even))                                              \
         if (const double t = stream_us<MB, NB>(M, N, K); best == 0 || t < best) {                              \
             best = t;                                                                                          \
             *mb = MB;                                                                                          \

@@ -114,7 +114,8 @@ void launch_gemm_ragged(int fa, int fb, const MmArgs& a, hipStream_t s);
 // multiple of 128, 16-byte aligned operands).  stream_tile: its best tile,
 // and the estimated time in us without the amax.  stream_tile_at: the tiles
 // the kernel is built for, i = 0, 1, ...; false past the last one.
-double stream_tile(int64_t M, int64_t N, int64_t K, bool with_amax, int* mb, int* nb);
+// even: of the tiles with an even number of 16-column blocks.
+double stream_tile(int64_t M, int64_t N, int64_t K, bool with_amax, int* mb, int* nb, bool even);
 int64_t stream_workgroups(int64_t M, int64_t N, int mb, int nb);
 bool stream_tile_at(int i, int* mb, int* nb);
 void launch_gemm_stream(int fa, int fb, int mb, int nb, const MmArgs& a, hipStream_t s);
@@ -126,7 +127,9 @@ enum MmKernel { kMmRagged = 0, kMmStream = 1, kMm256 = 2 };
 struct MmRoute {
     int kernel, mb, nb;
 };
-MmRoute mm_route(int64_t M, int64_t N, int64_t K, bool with_amax);
+MmRoute mm_route(int64_t M, int64_t N, int64_t K, bool with_amax, bool even = false);
+// The 256-row kernel's columns in tiles of 256 and in a last round of narrower ones.
+void mm256_split(int tiles_m, int tiles_n, int64_t N, int& ndp, int& tw, int& tn2);
 
 // C[m, n] = 2^-(*ba + *bb) * sum_k A[m, k] * B[n, k]; A [M, K] (format fa),
 // B [N, K] (format fb), both dense and, if K > 0, starting on 16-byte
@@ -157,6 +160,52 @@ int32_t launch_gemm_nt_bias(const uint8_t* A, int fa, const int32_t* ba, const u
                             const int32_t* bb, void* C, int out_dt, int64_t M, int64_t N, int64_t K, int bfmt,
                             int32_t margin, int32_t* bias, uint32_t* amax_bits, uint32_t* flags, uint32_t* ws,
                             hipStream_t s, int ba_rows = 0, const MmRoute* route = nullptr);
+
+// ---- matmuls of a feed-forward block (fp8lin_ffn.hip, fp8lin_ffn_small.hip)
+// What the epilogue does (see there), and its operands; A [M, K] (E4M3 forward,
+// E5M2 backward) and B [N, K] E4M3 (kEpiGlu: two of them, one after the other)
+// as in launch_gemm_nt.  Row strides in elements; arguments checked.
+enum EpiMode { kEpiAct = 0, kEpiGlu = 1, kEpiActBwd = 2, kEpiGluBwd = 3 };
+struct Epi {
+    const uint8_t *A, *B;
+    const int32_t *ba, *bb;
+    int64_t M, N, K;             // N: output columns (of one projection)
+    int act, out_dt, bias_dt;
+    const void *bias, *res;      // forward, may be null: [N] ([2 N]); [M, N] of type out_dt
+    uint16_t* keep;              // forward, may be null: values before the activation, [M, N] ([M, 2 N])
+    const uint16_t* z;           // backward: those values
+    void* out;                   // [M, N]; kEpiGluBwd [M, 2 N]
+    int64_t ldres, ldkeep, ldz, ldo;
+    float* sums;                 // backward, may be null: column sums of groups of rows, [epi_sum_rows, sum_cols]
+    int64_t sum_cols;
+};
+MmRoute epi_route(int mode, int64_t M, int64_t N, int64_t K);
+int64_t epi_sum_rows(int mode, int64_t M, int64_t N, int64_t K);
+int32_t launch_epilogue_mm(int mode, const Epi& e, hipStream_t s);
+void launch_ffn_small(int mode, int mb, int nb, const Epi& e, hipStream_t s);
+// out0[c] (c < n0) and out1[c - n0] = sum over the rows of part [rows, cols] fp32,
+// of type dt; either may be null.
+int32_t launch_sums_finish(const float* part, int64_t rows, int64_t cols, void* out0, int64_t n0, void* out1, int dt,
+                           hipStream_t s);
+
+// ---- layer norm (fp8lin_norm.hip); arguments checked
+struct NormArgs {
+    int64_t rows, cols, ldx, ldr, ldh, ldy, lddy, lddr;
+    int dt, g_dt;                  // of x, res, h, y (dy, dres, dx); of g and b
+    float eps;
+    const void *x, *res, *g, *b;   // res, b may be null
+    void *h, *y;                   // h may be null; y: the backward's dx
+    float *mean, *rstd;            // written by the forward (may be null), read by the backward
+    const void *dy, *dres;         // backward; dres may be null
+};
+int32_t launch_layernorm(const NormArgs& a, const struct FusedQuant* fq, hipStream_t s);
+// dx, and dg, db (either may be null) through part [norm_sum_rows, 2 cols].
+int64_t norm_sum_rows(int64_t rows, int64_t cols);
+int32_t launch_layernorm_bwd(const NormArgs& a, float* dg, float* db, float* part, hipStream_t s);
+// Column sums of x [rows, cols] through part [colsum_rows, cols].
+int64_t colsum_rows(int64_t rows, int64_t cols);
+int32_t launch_colsum(const void* x, int dt, int64_t rows, int64_t cols, int64_t ldx, void* out, int out_dt, float* part,
+                      hipStream_t s);
 
 // ---- decoder-layer glue (fp8lin_decoder.hip)
 // The FP8-AMAX quantise fused into a glue kernel's bf16 output: codes cast

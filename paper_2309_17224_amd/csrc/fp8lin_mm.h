@@ -68,6 +68,10 @@ __device__ __forceinline__ v8i ld_frag(const uint8_t* p, int fo0, int fo1) {
 // is one-to-one, so the 16 lanes hit 16 distinct bank groups.
 __device__ __forceinline__ int chunk_swz(int r) { return ((r >> 1) & 1) | (((r >> 2) & 1) << 2); }
 
+// Two matrices multiplied as a pair: a tile's rows are blocks of 16 rows from
+// them in turn; row of its matrix (from the tile's first) that tile row r is.
+__device__ __forceinline__ int pair_row(int r) { return (r >> 5) * 16 + (r & 15); }
+
 // Contiguous tile ranges per XCD, then grouped row-major order inside.
 __device__ __forceinline__ void tile_of(int b, int nb, int tiles_m, int tiles_n, int& tm, int& tn) {
     const int x = b & 7, l = b >> 3;
@@ -81,12 +85,6 @@ __device__ __forceinline__ void tile_of(int b, int nb, int tiles_m, int tiles_n,
     const int r = t - gid * group;
     tm = first + r % gm;
     tn = r / gm;
-}
-
-// 16-byte store with the non-temporal hint: outputs are not read again by the
-// kernel and should not displace cached operands.
-__device__ __forceinline__ void st_stream(void* p, uint4 v) {
-    __builtin_nontemporal_store(u32x4_any{v.x, v.y, v.z, v.w}, (u32x4_any*)p);
 }
 
 // Store 4 consecutive outputs of row m starting at column n (unscaled by

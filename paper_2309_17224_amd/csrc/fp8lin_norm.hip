@@ -1,0 +1,426 @@
+// Layer norm of the GPT models (Table 1), forward and backward, and the column
+// sums that a bias gradient is, for gfx950.
+//
+//   h = x (+ res), rounded; y = (h - mean) rstd g + b, rstd = 1 / sqrt(var + eps)
+//   dx = rstd (w - mean_j w - xh mean_j (w xh)) (+ dres), w = dy g, xh = (h - mean) rstd
+//   dg = sum over rows of dy xh, db = sum over rows of dy
+//
+// Everything is bound by memory: h and dy are read once where a row fits the
+// registers of its threads, statistics are fp32 and of the centred values (the
+// mean is taken first), and each output is rounded once.
+#include <algorithm>
+
+#include "fp8lin_glue.h"
+#include "fp8lin_vals.h"
+
+namespace fp8lin {
+namespace {
+
+// Threads that share a row, and eights of columns each of them holds.
+constexpr int kNormBlock = 256;
+
+// Sum over the T threads of a row, the same in all of them; red: a slot for
+// every wave of the block, free again after the next barrier.
+template <int T>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+    v = wave_sum(v);
+    if (T == 64) return v;
+    const int w = threadIdx.x >> 6;
+    __syncthreads();  // earlier sums have been read
+    if ((threadIdx.x & 63) == 0) red[w] = v;
+    __syncthreads();
+    constexpr int kW = T / 64;
+    const float* p = red + w / kW * kW;
+    float s[kW];
+#pragma unroll
+    for (int i = 0; i < kW; ++i) s[i] = p[i];
+#pragma unroll
+    for (int d = 1; d < kW; d *= 2)
+#pragma unroll
+        for (int i = 0; i + d < kW; i += 2 * d) s[i] += s[i + d];
+    return s[0];
+}
+
+// One value of v rounded to type DT.
+template <int DT>
+__device__ __forceinline__ float rounded(float v) {
+    return DT == FP8_DT_BF16 ? __uint_as_float(pack_bf16x2(v, 0.0f) << 16) : v;
+}
+
+// ------------------------------------------------------------- forward
+template <int DT, int T, int CH, int FMT>
+__global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const int32_t* __restrict__ pred,
+                                                               int32_t* __restrict__ used, uint32_t* __restrict__ parts,
+                                                               uint8_t* __restrict__ q, int64_t ldq) {
+    constexpr bool kQuant = FMT >= 0;
+    __shared__ float red[kNormBlock / 64];
+    __shared__ uint32_t redm[kNormBlock / 64];
+    const int tid = threadIdx.x % T;
+    const int64_t r = (int64_t)blockIdx.x * (kNormBlock / T) + threadIdx.x / T;
+    const bool live = r < a.rows;
+    const int64_t row = live ? r : a.rows - 1, cols = a.cols;
+    const bool in_regs = cols <= (int64_t)8 * T * CH;
+    float h[CH][8];
+    auto load = [&](int64_t c, float (&v)[8]) {
+        const int nv = (int)min((int64_t)8, cols - c);
+        ld_vals<8>(a.x, row * a.ldx + c, DT, nv, v);
+        if (a.res) {
+            float w[8];
+            ld_vals<8>(a.res, row * a.ldr + c, DT, nv, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = rounded<DT>(v[i] + w[i]);
+        }
+    };
+    float sum = 0.0f;
+    if (in_regs) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int64_t c = (int64_t)8 * (tid + T * k);
+            if (c < cols) {
+                load(c, h[k]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[k][i] = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += h[k][i];
+    } else {
+        for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
+            float v[8];
+            load(c, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+    }
+    const float mean = row_sum<T>(sum, red) / (float)cols;
+    float ss = 0.0f;
+    auto centred = [&](int64_t c, const float (&v)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = c + i < cols ? v[i] - mean : 0.0f;
+            ss = fmaf(d, d, ss);
+        }
+    };
+    if (in_regs) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) centred((int64_t)8 * (tid + T * k), h[k]);
+    } else {
+        for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
+            float v[8];
+            load(c, v);
+            centred(c, v);
+        }
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<T>(ss, red) / (float)cols + a.eps);
+    if (live && tid == 0) {
+        if (a.mean) a.mean[r] = mean;
+        if (a.rstd) a.rstd[r] = rstd;
+    }
+    const bool cast = kQuant && pred;
+    const int bq = kQuant ? fused_bias(pred, used) : 0;
+    uint32_t mag = 0;
+    auto store = [&](int64_t c, const float (&v)[8]) {
+        if (!live || c >= cols) return;
+        const int nv = (int)min((int64_t)8, cols - c);
+        if (a.h) st_vals<8>(a.h, r * a.ldh + c, DT, nv, v);
+        float g[8], b[8] = {}, y[8];
+        ld_vals<8>(a.g, c, a.g_dt, nv, g);
+        if (a.b) ld_vals<8>(a.b, c, a.g_dt, nv, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = fmaf((v[i] - mean) * rstd, g[i], b[i]);
+        st_vals<8>(a.y, r * a.ldy + c, DT, nv, y);
+        if (kQuant) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = i < nv ? y[i] : 0.0f;
+            const uint4 w = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
+                                       pack_bf16x2(y[6], y[7]));
+            mag = max(mag, mag8(w));
+            if (cast) {
+                const uint2 c8 = codes8<FMT < 0 ? 0 : FMT>(w, bq);
+                uint8_t* p = q + r * ldq + c;
+                if (nv == 8) st8_any(p, c8.x, c8.y);
+                else
+                    for (int i = 0; i < nv; ++i) p[i] = (uint8_t)((i < 4 ? c8.x : c8.y) >> (8 * (i & 3)));
+            }
+        }
+    };
+    if (in_regs) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) store((int64_t)8 * (tid + T * k), h[k]);
+    } else {
+        for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
+            float v[8];
+            load(c, v);
+            store(c, v);
+        }
+    }
+    if (kQuant) {
+        const uint32_t bm = block_max(mag, redm);
+        if (threadIdx.x == 0) parts[blockIdx.x] = bm;
+    }
+}
+
+// ------------------------------------------------------------- backward
+// A row's threads hold its columns and, of every row they take, add their part
+// of the column sums: one row of part for each group of T threads.  CH == 0: rows
+// too wide for that, read twice, and the column sums are colsum_kernel's.
+template <int DT, int T, int CH>
+__global__ __launch_bounds__(T < kNormBlock ? kNormBlock : T) void layernorm_bwd_kernel(NormArgs a, float* __restrict__ part) {
+    constexpr int kBlock = T < kNormBlock ? kNormBlock : T, kCh = CH > 0 ? CH : 1;
+    __shared__ float red[2 * (kBlock / 64)];
+    const int tid = threadIdx.x % T;
+    const int64_t slot = (int64_t)blockIdx.x * (kBlock / T) + threadIdx.x / T, slots = (int64_t)gridDim.x * (kBlock / T);
+    const int64_t cols = a.cols;
+    const float inv = 1.0f / (float)cols;
+    float g[kCh][8], sg[kCh][8], sb[kCh][8];
+#pragma unroll
+    for (int k = 0; k < kCh; ++k) {
+        const int64_t c = (int64_t)8 * (tid + T * k);
+        const int nv = (int)max((int64_t)0, min((int64_t)8, cols - c));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sg[k][i] = sb[k][i] = g[k][i] = 0.0f;
+        if (CH > 0 && nv > 0) ld_vals<8>(a.g, c, a.g_dt, nv, g[k]);
+    }
+    // every thread of a block takes the same number of turns (the sums are the block's)
+    const int64_t turns = (a.rows - (int64_t)blockIdx.x * (kBlock / T) + slots - 1) / slots;
+    for (int64_t turn = 0; turn < turns; ++turn) {
+        const int64_t r = slot + turn * slots;
+        const bool live = r < a.rows;
+        const int64_t row = live ? r : a.rows - 1;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float xh[kCh][8], dy[kCh][8], c1 = 0.0f, c2 = 0.0f;
+        auto load = [&](int64_t c, float (&x)[8], float (&d)[8]) {
+            const int nv = (int)min((int64_t)8, cols - c);
+            ld_vals<8>(a.x, row * a.ldx + c, DT, nv, x);
+            ld_vals<8>(a.dy, row * a.lddy + c, DT, nv, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean) * rstd;
+        };
+        auto finish = [&](int64_t c, const float (&x)[8], const float (&d)[8], const float (&gg)[8]) {
+            if (!live || c >= cols) return;
+            const int nv = (int)min((int64_t)8, cols - c);
+            float y[8], w[8];
+            if (a.dres) ld_vals<8>(a.dres, r * a.lddr + c, DT, nv, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                y[i] = rstd * (d[i] * gg[i] - c1 - x[i] * c2);
+                if (a.dres) y[i] += w[i];
+            }
+            st_vals<8>(a.y, r * a.ldy + c, DT, nv, y);
+        };
+        if (CH > 0) {
+#pragma unroll
+            for (int k = 0; k < kCh; ++k) {
+                const int64_t c = (int64_t)8 * (tid + T * k);
+                if (c < cols) {
+                    load(c, xh[k], dy[k]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) xh[k][i] = dy[k][i] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kCh; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float w = dy[k][i] * g[k][i];
+                    c1 += w;
+                    c2 = fmaf(w, xh[k][i], c2);
+                    if (live) {
+                        sg[k][i] = fmaf(dy[k][i], xh[k][i], sg[k][i]);
+                        sb[k][i] += dy[k][i];
+                    }
+                }
+        } else {
+            for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
+                const int nv = (int)min((int64_t)8, cols - c);
+                float gg[8];
+                load(c, xh[0], dy[0]);
+                ld_vals<8>(a.g, c, a.g_dt, nv, gg);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float w = i < nv ? dy[0][i] * gg[i] : 0.0f;
+                    c1 += w;
+                    c2 = fmaf(w, xh[0][i], c2);
+                }
+            }
+        }
+        c1 = row_sum<T>(c1, red) * inv;
+        c2 = row_sum<T>(c2, red + kBlock / 64) * inv;
+        if (CH > 0) {
+#pragma unroll
+            for (int k = 0; k < kCh; ++k) finish((int64_t)8 * (tid + T * k), xh[k], dy[k], g[k]);
+        } else {
+            for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
+                float gg[8];
+                load(c, xh[0], dy[0]);
+                ld_vals<8>(a.g, c, a.g_dt, (int)min((int64_t)8, cols - c), gg);
+                finish(c, xh[0], dy[0], gg);
+            }
+        }
+    }
+    if (CH > 0 && part) {
+        float* p = part + slot * 2 * cols;
+#pragma unroll
+        for (int k = 0; k < kCh; ++k) {
+            const int64_t c = (int64_t)8 * (tid + T * k);
+            const int nv = (int)max((int64_t)0, min((int64_t)8, cols - c));
+            st_vals<8>(p, c, FP8_DT_F32, nv, sg[k]);
+            st_vals<8>(p, cols + c, FP8_DT_F32, nv, sb[k]);
+        }
+    }
+}
+
+// ------------------------------------------------------------- column sums
+// A workgroup sums 512 columns over every gridDim.y-th group of kSumRows rows,
+// a wave each fourth row; its waves' sums are added in order: one row of part for
+// each blockIdx.y.  NORM: the layer norm's two sums instead, of dy xh into
+// columns [0, cols) and dy into [cols, 2 cols).
+constexpr int kSumRows = 64;
+template <int DT, bool NORM>
+__global__ __launch_bounds__(256) void colsum_kernel(NormArgs a, float* __restrict__ part) {
+    constexpr int kNs = NORM ? 2 : 1;
+    __shared__ float red[kNs][4][512];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 512 + 8 * lane;
+    const int nv = (int)max((int64_t)0, min((int64_t)8, a.cols - c));
+    float s[kNs][8] = {};
+    if (nv > 0) {
+        for (int64_t r0 = (int64_t)blockIdx.y * kSumRows; r0 < a.rows; r0 += (int64_t)gridDim.y * kSumRows) {
+            const int64_t end = min(r0 + kSumRows, a.rows);
+#pragma unroll 4
+            for (int64_t r = r0 + w; r < end; r += 4) {
+                float d[8], x[8];
+                ld_vals<8>(a.dy, r * a.lddy + c, DT, nv, d);
+                if (NORM) {
+                    ld_vals<8>(a.x, r * a.ldx + c, DT, nv, x);
+                    const float mean = a.mean[r], rstd = a.rstd[r];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[0][i] = fmaf(d[i], (x[i] - mean) * rstd, s[0][i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[kNs - 1][i] += d[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kNs; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) red[k][w][8 * lane + i] = s[k][i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 512; i += 256) {
+        const int64_t col = (int64_t)blockIdx.x * 512 + i;
+        if (col >= a.cols) break;
+#pragma unroll
+        for (int k = 0; k < kNs; ++k)
+            part[(int64_t)blockIdx.y * kNs * a.cols + k * a.cols + col] =
+                (red[k][0][i] + red[k][1][i]) + (red[k][2][i] + red[k][3][i]);
+    }
+}
+
+// ------------------------------------------------------------- host side
+constexpr int64_t kNormWidest = 16384;  // columns a row's threads hold in the backward pass
+constexpr int64_t kSumGroups = 256;     // rows of partial column sums, at most
+
+// Threads of a row in the backward pass: 8 columns each, 16 beyond 8192.
+int bwd_threads(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024; }
+
+int64_t bwd_blocks(int64_t rows, int64_t cols) {
+    const int t = bwd_threads(cols), per = t < kNormBlock ? kNormBlock / t : 1;
+    return std::min<int64_t>((rows + per - 1) / per, 256);
+}
+
+}  // namespace
+
+int64_t colsum_rows(int64_t rows, int64_t cols) {
+    (void)cols;
+    return std::max<int64_t>(1, std::min<int64_t>((rows + kSumRows - 1) / kSumRows, kSumGroups));
+}
+
+int64_t norm_sum_rows(int64_t rows, int64_t cols) {
+    if (cols > kNormWidest) return colsum_rows(rows, cols);
+    const int t = bwd_threads(cols);
+    return bwd_blocks(rows, cols) * (t < kNormBlock ? kNormBlock / t : 1);
+}
+
+int32_t launch_layernorm(const NormArgs& a, const FusedQuant* fq, hipStream_t s) {
+    const bool quant = fq && fq->q;
+    int grid = 0;
+    auto go = [&](auto D, auto Tt, auto C, auto Fm) {
+        constexpr int kT = decltype(Tt)::value;
+        grid = (int)((a.rows + kNormBlock / kT - 1) / (kNormBlock / kT));
+        hipLaunchKernelGGL((layernorm_kernel<decltype(D)::value, kT, decltype(C)::value, decltype(Fm)::value>), dim3(grid),
+                           dim3(kNormBlock), 0, s, a, quant ? fq->pred : nullptr, quant ? (int32_t*)fq->ws : nullptr,
+                           quant ? fq->ws + 1 : nullptr, quant ? fq->q : nullptr, quant ? fq->ldq : (int64_t)0);
+    };
+    auto size = [&](auto D, auto Fm) {
+        if (a.cols <= 512) go(D, IC<64>{}, IC<1>{}, Fm);
+        else if (a.cols <= 1024) go(D, IC<64>{}, IC<2>{}, Fm);
+        else if (a.cols <= 4096) go(D, IC<256>{}, IC<2>{}, Fm);
+        else if (a.cols <= 8192) go(D, IC<256>{}, IC<4>{}, Fm);
+        else go(D, IC<256>{}, IC<8>{}, Fm);
+    };
+    if (a.dt == FP8_DT_F32) size(IC<FP8_DT_F32>{}, IC<-1>{});
+    else if (!quant) size(IC<FP8_DT_BF16>{}, IC<-1>{});
+    else with_fmt(fq->fmt, [&](auto Fm) { size(IC<FP8_DT_BF16>{}, Fm); });
+    const int32_t st = hip_status();
+    if (st != FP8_OK || !quant) return st;
+    return launch_quant_check(a.y, FP8_DT_BF16, a.rows, a.cols, a.ldy, fq->fmt, fq->margin, fq->ws + 1, grid,
+                              (const int32_t*)fq->ws, fq->bias, fq->amax_bits, fq->flags, fq->q, fq->ldq, nullptr, 0, s);
+}
+
+int32_t launch_layernorm_bwd(const NormArgs& a, float* dg, float* db, float* part, hipStream_t s) {
+    const int64_t sums = norm_sum_rows(a.rows, a.cols);
+    const bool want = dg || db;
+    auto go = [&](auto D, auto Tt, auto C) {
+        constexpr int kT = decltype(Tt)::value;
+        const int64_t blocks = decltype(C)::value == 0 ? std::min<int64_t>(a.rows, 2048) : bwd_blocks(a.rows, a.cols);
+        hipLaunchKernelGGL((layernorm_bwd_kernel<decltype(D)::value, kT, decltype(C)::value>), dim3((unsigned)blocks),
+                           dim3(kT < kNormBlock ? kNormBlock : kT), 0, s, a, want ? part : nullptr);
+    };
+    auto size = [&](auto D) {
+        switch (bwd_threads(a.cols)) {
+            case 64: go(D, IC<64>{}, IC<1>{}); break;
+            case 128: go(D, IC<128>{}, IC<1>{}); break;
+            case 256: go(D, IC<256>{}, IC<1>{}); break;
+            case 512: go(D, IC<512>{}, IC<1>{}); break;
+            default:
+                if (a.cols <= 8192) go(D, IC<1024>{}, IC<1>{});
+                else if (a.cols <= kNormWidest) go(D, IC<1024>{}, IC<2>{});
+                else go(D, IC<1024>{}, IC<0>{});
+        }
+    };
+    if (a.dt == FP8_DT_BF16) size(IC<FP8_DT_BF16>{});
+    else size(IC<FP8_DT_F32>{});
+    int32_t st = hip_status();
+    if (st != FP8_OK || !want) return st;
+    if (a.cols > kNormWidest) {
+        const dim3 grid((unsigned)((a.cols + 511) / 512), (unsigned)sums);
+        if (a.dt == FP8_DT_BF16) hipLaunchKernelGGL((colsum_kernel<FP8_DT_BF16, true>), grid, dim3(256), 0, s, a, part);
+        else hipLaunchKernelGGL((colsum_kernel<FP8_DT_F32, true>), grid, dim3(256), 0, s, a, part);
+        st = hip_status();
+        if (st != FP8_OK) return st;
+    }
+    return launch_sums_finish(part, sums, 2 * a.cols, dg, a.cols, db, FP8_DT_F32, s);
+}
+
+int32_t launch_colsum(const void* x, int dt, int64_t rows, int64_t cols, int64_t ldx, void* out, int out_dt, float* part,
+                      hipStream_t s) {
+    NormArgs a{};
+    a.rows = rows;
+    a.cols = cols;
+    a.dy = x;
+    a.lddy = ldx;
+    const int64_t sums = colsum_rows(rows, cols);
+    const dim3 grid((unsigned)((cols + 511) / 512), (unsigned)sums);
+    if (dt == FP8_DT_BF16) hipLaunchKernelGGL((colsum_kernel<FP8_DT_BF16, false>), grid, dim3(256), 0, s, a, part);
+    else hipLaunchKernelGGL((colsum_kernel<FP8_DT_F32, false>), grid, dim3(256), 0, s, a, part);
+    const int32_t st = hip_status();
+    if (st != FP8_OK) return st;
+    return launch_sums_finish(part, sums, cols, out, cols, nullptr, out_dt, s);
+}
+
+}  // namespace fp8lin

@@ -22,6 +22,7 @@ CACHE_BF16 = 16     # format of an unquantised key/value cache
 E4_A, E5_A = 2, 3   # the paper's formats (Table 7 rows "(a)"); bias and cast calls only
 DT_BF16, DT_F32 = 0, 1
 FLAG_NONFINITE, FLAG_ZERO, FLAG_SATURATED = 1, 2, 4
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 OK, EINVAL, ENOTSUP, EHIP = 0, 1, 2, 3
 
 # Every symbol declared in include/fp8lin.h.
@@ -38,6 +39,9 @@ EXPORTS = (
     "llama_rmsnorm_ws_bytes", "llama_rmsnorm_quantise", "llama_rope_table", "llama_rope",
     "llama_attention_ws_bytes", "llama_attention", "llama_swiglu_ws_bytes", "llama_swiglu_quantise",
     "llama_residual_add",
+    "fp8_linear_fwd_act", "fp8_linear_fwd_glu", "fp8_linear_bwd_dx_act", "fp8_linear_bwd_dx_glu",
+    "gpt_bias_grad_ws_bytes", "gpt_bias_grad", "gpt_layernorm_ws_bytes", "gpt_layernorm_quantise",
+    "gpt_layernorm_bwd_ws_bytes", "gpt_layernorm_bwd",
     "llama_cache_append", "llama_cache_read", "llama_cache_attention_ws_bytes", "llama_cache_attention",
 )
 
@@ -136,6 +140,29 @@ def lib() -> ctypes.CDLL:
                                             sz, vp]
         L.llama_residual_add.restype = i32
         L.llama_residual_add.argtypes = [vp, vp, vp, i64, vp]
+        L.fp8_linear_fwd_act.restype = i32
+        L.fp8_linear_fwd_act.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, i64, vp, i64, vp, i32, i64, i64, i64, i64,
+                                         vp, vp]
+        L.fp8_linear_fwd_glu.restype = i32
+        L.fp8_linear_fwd_glu.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, i64, vp, i64, i64, i64, i64, vp, vp]
+        for name in ("fp8_linear_bwd_dx_act", "fp8_linear_bwd_dx_glu"):
+            f = getattr(L, name)
+            f.restype = i32
+            f.argtypes = [vp, vp, vp, vp, vp, i64, i32, vp, i64, vp, i32, i64, i64, i64, vp, vp, sz, vp]
+        for name in ("gpt_bias_grad_ws_bytes", "gpt_layernorm_bwd_ws_bytes"):
+            f = getattr(L, name)
+            f.restype = sz
+            f.argtypes = [i64, i64]
+        L.gpt_bias_grad.restype = i32
+        L.gpt_bias_grad.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, sz, vp]
+        L.gpt_layernorm_ws_bytes.restype = sz
+        L.gpt_layernorm_ws_bytes.argtypes = [i64]
+        L.gpt_layernorm_quantise.restype = i32
+        L.gpt_layernorm_quantise.argtypes = [vp, i64, vp, i64, i32, vp, vp, i32, i64, i64, f32, vp, i64, vp, i64, vp, vp,
+                                             vp, vp]
+        L.gpt_layernorm_bwd.restype = i32
+        L.gpt_layernorm_bwd.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, i32, vp, vp, i64, i64, vp, i64, vp, vp, vp,
+                                        sz, vp]
         L.llama_cache_append.restype = i32
         L.llama_cache_append.argtypes = [vp, i64, i64, i32, vp, vp, vp, i64, vp, i64, vp]
         L.llama_cache_read.restype = i32
@@ -171,6 +198,10 @@ def _stream(stream=None):
     if _raw_stream is not None:
         return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
+
+
+_BF16 = torch.bfloat16
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _dt(t: torch.Tensor) -> int:
@@ -587,12 +618,13 @@ class FusedQuant:
     """Arguments of a quantise fused into a glue call: codes q [rows, cols]
     (uint8), the format and margin, an optional predicted bias, and one-element
     int32 device tensors for the bias, amax bits and flags; ws is the op's
-    workspace (uint8 tensor)."""
+    workspace (uint8 tensor).  qT: the transposed codes [cols, rows], for the
+    calls that write them (the matmuls of the feed-forward block)."""
 
-    def __init__(self, q, bias, ws, fmt=E4M3, margin=0, bias_pred=None, amax_bits=None, flags=None):
+    def __init__(self, q, bias, ws, fmt=E4M3, margin=0, bias_pred=None, amax_bits=None, flags=None, qT=None):
         self.q, self.bias, self.ws = q, bias, ws
         self.fmt, self.margin, self.bias_pred = fmt, margin, bias_pred
-        self.amax_bits, self.flags = amax_bits, flags
+        self.amax_bits, self.flags, self.qT = amax_bits, flags, qT
 
     def args(self):
         return (self.fmt, self.margin, _p(self.bias_pred), _p(self.bias), _p(self.amax_bits), _p(self.flags),
@@ -680,6 +712,278 @@ def llama_residual_add(a, b, out=None, stream=None):
     st = lib().llama_residual_add(_p(a), _p(b), _p(out), a.numel(), _stream(stream))
     _check("llama_residual_add", st)
     return out
+
+
+# ------------------------------------------------------------------ the feed-forward block
+class OutQuantise(ctypes.Structure):
+    """fp8_out_quantise of the C header."""
+    _fields_ = [("fmt", ctypes.c_int32), ("margin", ctypes.c_int32), ("bias_pred", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("amax_bits", ctypes.c_void_p), ("flags", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("qT", ctypes.c_void_p), ("ldqT", ctypes.c_int64),
+                ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t)]
+
+
+def _gpu(t: torch.Tensor, name: str) -> int:
+    """The GPU of a call's first operand: the current one, whose stream runs the call."""
+    dev = t.get_device()
+    if dev < 0 or _current() != dev:
+        raise ValueError(f"{name}: on {t.device}, which is not the current GPU")
+    return dev
+
+
+def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dev: int, dtype=_BF16) -> int:
+    """Row stride of a tensor [rows, cols] of one or of several types, with contiguous rows, on GPU dev."""
+    if t.dtype is not dtype and (not isinstance(dtype, tuple) or t.dtype not in dtype):
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols or (cols > 1 and stride[1] != 1):
+        raise ValueError(f"{name}: expected [{rows}, {cols}] with contiguous rows, got {tuple(shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, the call on GPU {dev}")
+    if rows > 1 and stride[0] < cols:  # an expanded tensor's rows lie on each other
+        raise ValueError(f"{name}: rows {stride[0]} elements apart, {cols} long")
+    return stride[0] if rows > 1 else max(cols, 1)
+
+
+def _vec(t: torch.Tensor, name: str, n: int, dev: int, dtypes) -> int:
+    """Address of a contiguous vector of n elements (any shape) of one of the types on GPU dev."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: expected one of {dtypes}, got {t.dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(t.shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, the call on GPU {dev}")
+    return t.data_ptr()
+
+
+_FLOATS = (torch.bfloat16, torch.float32)
+_INT = (torch.int32,)
+_U8 = (torch.uint8,)
+
+
+def _made(shape, dtype, device, stream) -> torch.Tensor:
+    """A tensor of the memory of the stream that a call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _scratch(ws, nbytes: int, dev: int, device, stream):
+    """Address and bytes of a workspace; made for the call where none is given."""
+    if ws is None:
+        ws = _made(max(nbytes, 4), torch.uint8, device, stream)
+    elif ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"ws: expected a contiguous tensor on GPU {dev}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _out_quantise(fq: FusedQuant | None, rows: int, cols: int, dev: int):
+    """fp8_out_quantise of a FusedQuant (kept alive by the caller until the call has returned)."""
+    if fq is None:
+        return None
+    ldq = _rows(fq.q, "fq.q", rows, cols, dev, torch.uint8)
+    qT, ldqT = None, 0
+    if fq.qT is not None:
+        qT, ldqT = fq.qT.data_ptr(), _rows(fq.qT, "fq.qT", cols, rows, dev, torch.uint8)
+    one = [None if t is None else _vec(t, "fq's bias, prediction, amax and flags", 1, dev, _INT)
+           for t in (fq.bias_pred, fq.bias, fq.amax_bits, fq.flags)]
+    ws, nws = _scratch(fq.ws, 0, dev, None, None)
+    return OutQuantise(fq.fmt, fq.margin, *one, fq.q.data_ptr(), ldq, qT, ldqT, ws, nws)
+
+
+def _ref(quant):
+    return None if quant is None else ctypes.addressof(quant)
+
+
+def _operands(a8, ba, b8, bb, names):
+    """Checks of a matmul's operands [M, K] and [N, K]: M, N, K and the GPU."""
+    dev = _gpu(a8, names[0])
+    if a8.dim() != 2 or b8.dim() != 2 or a8.shape[1] != b8.shape[1]:
+        raise ValueError(f"{names[0]}, {names[2]}: expected [M, K] and [N, K], got {tuple(a8.shape)} and {tuple(b8.shape)}")
+    M, K = a8.shape
+    N = b8.shape[0]
+    return (_vec(a8, names[0], M * K, dev, _U8), _vec(ba, names[1], 1, dev, _INT), _vec(b8, names[2], N * K, dev, _U8),
+            _vec(bb, names[3], 1, dev, _INT)), M, N, K, dev
+
+
+_FWD_NAMES = ("x8", "bx", "w8t", "bw")
+_BWD_NAMES = ("dy8", "bg", "w8", "bw")
+
+
+def fp8_linear_quantise_ws_bytes(rows: int, cols: int) -> int:
+    return int(lib().fp8_linear_quantise_ws_bytes(int(rows), int(cols)))
+
+
+def fp8_linear_fwd_act(x8, bx, w8t, bw, act: int = ACT_NONE, bias=None, res=None, z=None, out_dt: int = DT_BF16, y=None,
+                       fq: FusedQuant | None = None, stream=None):
+    """y = act(z) + res, z = 2^-(bx+bw) X8 [M,K] . W8T [N,K]^T + bias, in one matmul.
+    bias: [N], bf16 or fp32.  res: [M, N] of y's type (may be y).  z: bf16 [M, N], written
+    for fp8_linear_bwd_dx_act.  fq: codes of y (ws of fp8_linear_quantise_ws_bytes(M, N)
+    bytes).  Returns y."""
+    ops, M, N, K, dev = _operands(x8, bx, w8t, bw, _FWD_NAMES)
+    if y is None:
+        y = _made((M, N), torch.bfloat16 if out_dt == DT_BF16 else torch.float32, x8.device, stream)
+    ldy = _rows(y, "y", M, N, dev, _FLOATS)
+    b, b_dt = (None, 0) if bias is None else (_vec(bias, "bias", N, dev, _FLOATS), _dt(bias))
+    ldr = 0 if res is None else _rows(res, "res", M, N, dev, y.dtype)
+    ldz = 0 if z is None else _rows(z, "z", M, N, dev)
+    quant = _out_quantise(fq, M, N, dev)
+    st = lib().fp8_linear_fwd_act(*ops, b, b_dt, act, _p(res), ldr, _p(z), ldz, y.data_ptr(), _dt(y), ldy, M, N, K,
+                                  _ref(quant), _stream(stream))
+    if st:
+        _check("fp8_linear_fwd_act", st)
+    return y
+
+
+def fp8_linear_fwd_glu(x8, bx, w8t, bw, act: int = ACT_SILU, bias=None, gu=None, a=None, fq: FusedQuant | None = None,
+                       stream=None):
+    """a = act(g) * u, (g | u) = 2^-(bx+bw) X8 [M,K] . W8T [2N,K]^T + bias (gate rows of W8T
+    first), in one matmul.  bias: [2 N].  gu: bf16 [M, 2 N], written for
+    fp8_linear_bwd_dx_glu.  fq: codes of a [M, N].  Returns a."""
+    ops, M, N2, K, dev = _operands(x8, bx, w8t, bw, _FWD_NAMES)
+    if N2 % 2:
+        raise ValueError(f"w8t: expected as many gate rows as up rows, got {N2} rows")
+    N = N2 // 2
+    if a is None:
+        a = _made((M, N), torch.bfloat16, x8.device, stream)
+    lda = _rows(a, "a", M, N, dev)
+    b, b_dt = (None, 0) if bias is None else (_vec(bias, "bias", N2, dev, _FLOATS), _dt(bias))
+    ldgu = 0 if gu is None else _rows(gu, "gu", M, N2, dev)
+    quant = _out_quantise(fq, M, N, dev)
+    st = lib().fp8_linear_fwd_glu(*ops, b, b_dt, act, _p(gu), ldgu, a.data_ptr(), lda, M, N, K, _ref(quant),
+                                  _stream(stream))
+    if st:
+        _check("fp8_linear_fwd_glu", st)
+    return a
+
+
+def gpt_bias_grad_ws_bytes(rows: int, cols: int) -> int:
+    return int(lib().gpt_bias_grad_ws_bytes(int(rows), int(cols)))
+
+
+def bias_grad_workspace(rows: int, cols: int, device) -> torch.Tensor:
+    """Workspace of gpt_bias_grad, and of the backward matmuls' bias gradients
+    (rows and columns of their output)."""
+    return torch.empty(max(gpt_bias_grad_ws_bytes(rows, cols), 4), dtype=torch.uint8, device=device)
+
+
+def _linear_bwd(name, dy8, bg, w8, bw, saved, saved_name, act, out, out_name, wide, db, fq, ws, stream):
+    ops, M, K, N, dev = _operands(dy8, bg, w8, bw, _BWD_NAMES)  # [M, N] and [K, N]
+    cols = wide * K
+    lds = _rows(saved, saved_name, M, cols, dev)
+    if out is None:
+        out = _made((M, cols), torch.bfloat16, dy8.device, stream)
+    ldo = _rows(out, out_name, M, cols, dev)
+    quant = _out_quantise(fq, M, cols, dev)
+    d, d_dt, w = None, 0, (None, 0)
+    if db is not None:
+        d, d_dt = _vec(db, "db", cols, dev, _FLOATS), _dt(db)
+        w = _scratch(ws, gpt_bias_grad_ws_bytes(M, cols) if ws is None else 0, dev, dy8.device, stream)
+    st = getattr(lib(), name)(*ops, saved.data_ptr(), lds, act, out.data_ptr(), ldo, d, d_dt, M, N, K, _ref(quant), *w,
+                              _stream(stream))
+    if st:
+        _check(name, st)
+    return out
+
+
+def fp8_linear_bwd_dx_act(dy8, bg, w8, bw, z, act: int, dz=None, db=None, fq: FusedQuant | None = None, ws=None,
+                          stream=None):
+    """dz = t act'(z), t = 2^-(bg+bw) dY8 [M,N] . W8 [K,N]^T: the gradient that reaches the
+    linear before, whose output before its activation was z [M, K].  db: its bias gradient
+    [K] (bf16 or fp32), the sum of t act'(z) over rows, with ws of gpt_bias_grad_ws_bytes(M,
+    K) bytes.  fq: codes of dz.  dz may be z.  Returns dz."""
+    return _linear_bwd("fp8_linear_bwd_dx_act", dy8, bg, w8, bw, z, "z", act, dz, "dz", 1, db, fq, ws, stream)
+
+
+def fp8_linear_bwd_dx_glu(dy8, bg, w8, bw, gu, act: int = ACT_SILU, dgu=None, db=None, fq: FusedQuant | None = None,
+                          ws=None, stream=None):
+    """dg = t u act'(g) and du = t act(g), t = 2^-(bg+bw) dY8 [M,N] . W8 [K,N]^T: the gradients
+    of the gate's and the up projection's outputs gu [M, 2 K], side by side.  db: their sums
+    over rows [2 K].  fq: codes of dgu.  dgu may be gu.  Returns dgu."""
+    return _linear_bwd("fp8_linear_bwd_dx_glu", dy8, bg, w8, bw, gu, "gu", act, dgu, "dgu", 2, db, fq, ws, stream)
+
+
+def gpt_bias_grad(dy, db=None, ws=None, stream=None):
+    """Sum over the rows of dy [rows, cols] (bf16 or fp32).  db: [cols], bf16 or fp32 (fp32
+    where it is made here).  Returns db."""
+    dev = _gpu(dy, "dy")
+    rows, cols = dy.shape
+    ld = _rows(dy, "dy", rows, cols, dev, _FLOATS)
+    if db is None:
+        db = _made((cols,), torch.float32, dy.device, stream)
+    d = _vec(db, "db", cols, dev, _FLOATS)
+    w = _scratch(ws, gpt_bias_grad_ws_bytes(rows, cols) if ws is None else 0, dev, dy.device, stream)
+    st = lib().gpt_bias_grad(dy.data_ptr(), _dt(dy), rows, cols, ld, d, _dt(db), *w, _stream(stream))
+    if st:
+        _check("gpt_bias_grad", st)
+    return db
+
+
+def gpt_layernorm_ws_bytes(rows: int) -> int:
+    return int(lib().gpt_layernorm_ws_bytes(int(rows)))
+
+
+def gpt_layernorm_quantise(x, g, b=None, eps=1e-5, res=None, h=None, y=None, mean=None, rstd=None,
+                           fq: FusedQuant | None = None, stream=None):
+    """y = LayerNorm(h) * g + b, h = x [+ res] (bf16 or fp32; g and b of one type).  h, mean,
+    rstd: written where given (mean and rstd fp32 [rows], for gpt_layernorm_bwd).  fq: codes
+    of a bf16 y, ws of gpt_layernorm_ws_bytes(rows) bytes, no qT.  Returns y."""
+    dev = _gpu(x, "x")
+    rows, cols = x.shape
+    ldx = _rows(x, "x", rows, cols, dev, _FLOATS)
+    if y is None:
+        y = _made((rows, cols), x.dtype, x.device, stream)
+    ldy = _rows(y, "y", rows, cols, dev, x.dtype)
+    ldr = 0 if res is None else _rows(res, "res", rows, cols, dev, x.dtype)
+    ldh = 0 if h is None else _rows(h, "h", rows, cols, dev, x.dtype)
+    gp = _vec(g, "g", cols, dev, _FLOATS)
+    bp = None if b is None else _vec(b, "b", cols, dev, (g.dtype,))
+    stats = [None if t is None else _vec(t, "mean, rstd", rows, dev, (torch.float32,)) for t in (mean, rstd)]
+    quant = _out_quantise(fq, rows, cols, dev)
+    st = lib().gpt_layernorm_quantise(x.data_ptr(), ldx, _p(res), ldr, _dt(x), gp, bp, _dt(g), rows, cols, float(eps),
+                                      _p(h), ldh, y.data_ptr(), ldy, *stats, _ref(quant), _stream(stream))
+    if st:
+        _check("gpt_layernorm_quantise", st)
+    return y
+
+
+def gpt_layernorm_bwd_ws_bytes(rows: int, cols: int) -> int:
+    return int(lib().gpt_layernorm_bwd_ws_bytes(int(rows), int(cols)))
+
+
+def layernorm_bwd_workspace(rows: int, cols: int, device) -> torch.Tensor:
+    return torch.empty(max(gpt_layernorm_bwd_ws_bytes(rows, cols), 4), dtype=torch.uint8, device=device)
+
+
+def gpt_layernorm_bwd(dy, h, g, mean, rstd, dres=None, dx=None, dg=None, db=None, want_params=True, ws=None, stream=None):
+    """Gradients of gpt_layernorm_quantise: dx (with dres, the gradient that reaches h past the
+    norm, added), dg and db (fp32 [cols]; made here with want_params).  h: what was
+    normalised.  Returns (dx, dg, db)."""
+    dev = _gpu(dy, "dy")
+    rows, cols = dy.shape
+    dt = dy.dtype
+    lddy = _rows(dy, "dy", rows, cols, dev, _FLOATS)
+    ldh = _rows(h, "h", rows, cols, dev, dt)
+    lddr = 0 if dres is None else _rows(dres, "dres", rows, cols, dev, dt)
+    if dx is None:
+        dx = _made((rows, cols), dt, dy.device, stream)
+    lddx = _rows(dx, "dx", rows, cols, dev, dt)
+    if want_params:
+        dg = _made((cols,), torch.float32, dy.device, stream) if dg is None else dg
+        db = _made((cols,), torch.float32, dy.device, stream) if db is None else db
+    f32 = (torch.float32,)
+    sums = [None if t is None else _vec(t, "dg, db", cols, dev, f32) for t in (dg, db)]
+    w = (None, 0)
+    if dg is not None or db is not None:
+        w = _scratch(ws, gpt_layernorm_bwd_ws_bytes(rows, cols) if ws is None else 0, dev, dy.device, stream)
+    st = lib().gpt_layernorm_bwd(dy.data_ptr(), lddy, h.data_ptr(), ldh, _p(dres), lddr, _dt(dy),
+                                 _vec(g, "g", cols, dev, _FLOATS), _dt(g), _vec(mean, "mean", rows, dev, f32),
+                                 _vec(rstd, "rstd", rows, dev, f32), rows, cols, dx.data_ptr(), lddx, *sums, *w,
+                                 _stream(stream))
+    if st:
+        _check("gpt_layernorm_bwd", st)
+    return dx, dg, db
 
 
 # ------------------------------------------------------------------ paged key/value cache
@@ -776,10 +1080,6 @@ class CacheSeqs(_Described):
         self._c = SeqsStruct(_p(cu_rows), _p(kv_len), _p(pages), n, self.max_pages, _ld(pages))
         self._dev = kv_len.get_device()
         self._ref = ctypes.addressof(self._c)
-
-
-_BF16 = torch.bfloat16
-_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _cache_device(cache: KVCache, seqs: CacheSeqs) -> None:
