@@ -879,6 +879,15 @@ int32_t fp8lin_mm_route(int64_t M, int64_t N, int64_t K, int32_t with_amax, int3
     return r.kernel;
 }
 
+// The same of a feed-forward matmul (EpiMode) with output [M, N] (of one
+// projection) and contraction K.
+int32_t fp8lin_epi_route(int32_t mode, int64_t M, int64_t N, int64_t K, int32_t* mb, int32_t* nb) {
+    const MmRoute r = epi_route(mode, M, N, K);
+    *mb = r.mb;
+    *nb = r.nb;
+    return r.kernel;
+}
+
 // Tile i of the small-tile kernel; 0 past the last one.
 int32_t fp8lin_mm_tile(int32_t i, int32_t* mb, int32_t* nb) { return stream_tile_at(i, mb, nb) ? 1 : 0; }
 

@@ -27,76 +27,16 @@
 namespace fp8lin {
 namespace {
 
-template <int FA, int FB, int MB, int NB>
-__global__ __launch_bounds__(stream_threads(MB)) void gemm_nt_stream(MmArgs p, int tiles_m, int nt) {
-    using T = StreamTile<MB, NB>;
-    constexpr int kRowsB = 16 * NB, kSlots = T::kSlots, kNbw = T::kNbw, kMbw = T::kMbw;
-    static_assert(kSlots == 1 || kSlots * MB * NB * 1024 <= kSlBuf * T::kStage, "LDS budget");
-    __shared__ __attribute__((aligned(1024))) uint8_t sm[kSlBuf * T::kStage];
-    __shared__ uint32_t wmx[8];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int M = (int)p.M, N = (int)p.N, K = (int)p.K;
-    // consecutive tiles of one XCD share their B rows
-    const int x = blockIdx.x & 7, per = gridDim.x >> 3, rem = gridDim.x & 7;
-    const int tile = x * per + min(x, rem) + (blockIdx.x >> 3);
-    int tm = tile % tiles_m, tn = tile / tiles_m;
-    if (kSlots == 1) tile_of(blockIdx.x, gridDim.x, tiles_m, (N + kRowsB - 1) / kRowsB, tm, tn);
-    const int m0 = tm * (16 * MB), n0 = tn * kRowsB;
-    const int frow = lane & 15, fg = lane >> 4;
-    const int slot = w % kSlots, part = (w & 3) / kSlots;
-    const int nb0 = part % T::kWn * kNbw, mb0 = part / T::kWn * kMbw;  // this wave's blocks of the tile
-    v4f acc[kMbw][kNbw];
-    stream_loop<FA, FB, MB, NB, false>(sm, p.A, p.B, M, N, K, m0, n0, nt, acc);
-    uint32_t mx = 0;
-    const int bb = *p.bb;
-    auto put = [&](int mb, int nb, v4f sum) {
-        const int64_t m = m0 + mb * 16 + frow, n = n0 + nb * 16 + fg * 4;
-        if (n >= N) return;
-        const int sh = row_shift(p.ba, p.ba_rows, bb, m, M);
-        mx = max(mx, p.out_dt == FP8_DT_BF16 ? store4<FP8_DT_BF16>(p.C, N, m, n, M, N, sum, sh)
-                                             : store4<FP8_DT_F32>(p.C, N, m, n, M, N, sum, sh));
-    };
-    if (kSlots == 1) {
-        if (w < 4) {
-#pragma unroll
-            for (int i = 0; i < kMbw; ++i)
-#pragma unroll
-                for (int j = 0; j < kNbw; ++j) put(mb0 + i, nb0 + j, acc[i][j]);
-        }
-    } else {
-        v4f* red = (v4f*)sm;  // [slot][16-row block][16-column block][lane]
-        if (w < 4) {
-#pragma unroll
-            for (int i = 0; i < kMbw; ++i)
-#pragma unroll
-                for (int j = 0; j < kNbw; ++j) red[((slot * MB + i) * NB + nb0 + j) * 64 + lane] = acc[i][j];
-        }
-        __syncthreads();
-        for (int b = w; b < MB * NB; b += stream_threads(MB) / 64) {
-            v4f sum = red[b * 64 + lane];
-#pragma unroll
-            for (int s = 1; s < kSlots; ++s) sum += red[(s * MB * NB + b) * 64 + lane];
-            put(b / NB, b % NB, sum);
-        }
-    }
-    if (p.with_amax) {
-        const uint32_t wv = wave_max_u32(mx);
-        if (lane == 0) wmx[w] = wv;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            uint32_t b = 0;
-#pragma unroll
-            for (int v = 0; v < stream_threads(MB) / 64; ++v) b = max(b, wmx[v]);
-            fold_amax(canon_amax(b), p.amax, p.bo);
-        }
-    }
-}
+struct Plain {
+    using Args = MmArgs;
+    static constexpr bool kPlain = true, kPair = false;
+};
 
 template <int FA, int FB, int MB, int NB>
 void launch_one(const MmArgs& a, hipStream_t s) {
     const int tm = (int)((a.M + 16 * MB - 1) / (16 * MB)), tn = (int)((a.N + 16 * NB - 1) / (16 * NB));
-    hipLaunchKernelGGL((gemm_nt_stream<FA, FB, MB, NB>), dim3((unsigned)(tm * tn)), dim3(stream_threads(MB)), 0, s, a, tm,
-                       tm == 1);
+    hipLaunchKernelGGL((gemm_nt_stream<FA, FB, MB, NB, Plain>), dim3((unsigned)(tm * tn)), dim3(stream_threads(MB)), 0, s,
+                       a, tm, tn, tm == 1);
 }
 
 template <int FA, int FB>

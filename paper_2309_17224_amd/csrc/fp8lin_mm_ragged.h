@@ -37,8 +37,8 @@ __device__ __forceinline__ uint4 ld16_tail(const uint8_t* row, int64_t k, int64_
 // WT, laid out as in mm256_loop.  smem: 2 (BM + BN) kRk bytes of LDS, which every
 // wave has finished reading on return.  PAIR: as in mm256_loop.
 template <int FA, int FB, int BM, int BN, int WT, bool PAIR>
-__device__ __forceinline__ void ragged_loop(uint8_t* __restrict__ smem, const uint8_t* __restrict__ A,
-                                            const uint8_t* __restrict__ B, int64_t M, int64_t N, int64_t K, int64_t m0,
+__device__ __forceinline__ void ragged_loop(uint8_t* smem, const uint8_t* A,
+                                            const uint8_t* B, int64_t M, int64_t N, int64_t K, int64_t m0,
                                             int64_t n0, v4f (&acc)[WT / 16][WT / 16]) {
     constexpr int kNt = (BM / WT) * (BN / WT) * 64;
     constexpr int kRows = BM + BN, kStage = kRows * kRk;

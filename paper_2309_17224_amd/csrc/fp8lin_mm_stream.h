@@ -1,7 +1,5 @@
-// The main loop of the small-tile matmul kernels (described in
-// fp8lin_gemm_stream.hip): one tile of 16 MB x 16 NB outputs of A [M, K] . B [N,
-// K]^T, K a multiple of 128, into the accumulators of a workgroup's first four
-// waves, which still hold partial sums over k.  Internal, not part of the ABI.
+// The small-tile matmul kernel (described in fp8lin_gemm_stream.hip), with the plain
+// epilogue or another.  Internal, not part of the ABI.
 #pragma once
 
 #include "fp8lin_mm.h"
@@ -25,33 +23,33 @@ constexpr int stream_kc(int mb, int nb) { return mb + nb <= 6 ? 512 : mb + nb <=
     X(3, 1) X(3, 2) X(3, 3) X(3, 4) X(3, 6) X(3, 8) X(4, 2) X(4, 4) X(4, 6) X(4, 8) X(5, 2) X(5, 4) X(5, 6) \
     X(6, 4) X(6, 6) X(8, 4) X(8, 8) X(10, 6)
 
-template <int MB, int NB>
-struct StreamTile {
-    static constexpr int kRowsB = 16 * NB, kRows = 16 * (MB + NB);
-    static constexpr int kKC = stream_kc(MB, NB);
-    static constexpr int kStage = kRows * kKC, kCpr = kKC / 16, kRpi = 64 / kCpr;  // chunks per row, rows per copy
-    static constexpr int kNiw = kRows / kRpi / 4;                                  // copies per wave and stage
-    static constexpr int kSlots = kKC / 128;                                       // slices of a stage's k
-    static constexpr int kWn = kSlots == 4 ? 1 : 2, kWm = kSlots == 1 ? 2 : 1;     // waves over the tile's columns, rows
-    static constexpr int kNbw = NB / kWn, kMbw = MB / kWm;
+// One tile of 16 MB x 16 NB outputs.  E: what becomes of the sums.  E::kPlain: as
+// MmArgs says (gemm_nt_stream's own epilogue); otherwise E::finish gets them in LDS, as
+// [slot][16-row block][16-column block][lane] partial sums over k, which it adds
+// over the slots.  E::kPair: B is two matrices of N rows each, one after the other,
+// and a tile takes blocks of 16 rows from them in turn, from row n0 / 2 on (NB even).
+template <int FA, int FB, int MB, int NB, class E>
+__global__ __launch_bounds__(stream_threads(MB)) void gemm_nt_stream(typename E::Args p, int tiles_m, int tiles_n, int nt) {
+    constexpr bool kPair = E::kPair;
+    constexpr int kRowsB = 16 * NB, kRows = 16 * (MB + NB);
+    constexpr int kKC = stream_kc(MB, NB);
+    constexpr int kStage = kRows * kKC, kCpr = kKC / 16, kRpi = 64 / kCpr;  // chunks per row, rows per copy
+    constexpr int kNiw = kRows / kRpi / 4;                                  // copies per wave and stage
+    constexpr int kSlots = kKC / 128;
+    constexpr int kWn = kSlots == 4 ? 1 : 2, kWm = kSlots == 1 ? 2 : 1;  // waves over the tile's columns, rows
+    constexpr int kNbw = NB / kWn, kMbw = MB / kWm;
     static_assert(kRows % (4 * kRpi) == 0 && NB % kWn == 0 && MB % kWm == 0, "tile split");
-    static_assert(kSlBuf * kStage <= 160 * 1024, "LDS budget");
-};
-
-// Tile rows m0 .. of A and n0 .. of B; wave w < 4 gets the k slice slot = w %
-// kSlots of kMbw x kNbw blocks of 16 x 16: rows from block part / kWn * kMbw,
-// columns from part % kWn * kNbw on (part = w / kSlots), laid out as in
-// mm256_loop.  nt: B's rows are read by no other workgroup.  sm: kSlBuf * kStage
-// bytes of LDS, which every wave has finished reading on return.
-// PAIR: as in mm256_loop (NB even).
-template <int FA, int FB, int MB, int NB, bool PAIR>
-__device__ __forceinline__ void stream_loop(uint8_t* __restrict__ sm, const uint8_t* __restrict__ A,
-                                            const uint8_t* __restrict__ B, int M, int N, int K, int m0, int n0, int nt,
-                                            v4f (&acc)[StreamTile<MB, NB>::kMbw][StreamTile<MB, NB>::kNbw]) {
-    using T = StreamTile<MB, NB>;
-    constexpr int kRowsB = T::kRowsB, kKC = T::kKC, kStage = T::kStage, kCpr = T::kCpr, kRpi = T::kRpi, kNiw = T::kNiw;
-    constexpr int kSlots = T::kSlots, kWn = T::kWn, kNbw = T::kNbw, kMbw = T::kMbw;
+    static_assert(kSlBuf * kStage <= 160 * 1024 && (kSlots == 1 || kSlots * MB * NB * 1024 <= kSlBuf * kStage), "LDS budget");
+    __shared__ __attribute__((aligned(1024))) uint8_t sm[kSlBuf * kStage];
+    __shared__ uint32_t wmx[8];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int M = (int)p.M, N = (int)p.N, K = (int)p.K;
+    // consecutive tiles of one XCD share their B rows
+    const int x = blockIdx.x & 7, per = gridDim.x >> 3, rem = gridDim.x & 7;
+    const int tile = x * per + min(x, rem) + (blockIdx.x >> 3);
+    int tm = tile % tiles_m, tn = tile / tiles_m;
+    if (kSlots == 1) tile_of(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
+    const int m0 = tm * (16 * MB), n0 = tn * kRowsB;
     // 16-byte chunk c of LDS row r is stored at chunk c ^ swz(r)
     auto swz = [](int r) { return kKC == 128 ? chunk_swz(r) : r & 15; };
 
@@ -63,12 +61,12 @@ __device__ __forceinline__ void stream_loop(uint8_t* __restrict__ sm, const uint
     for (int t = 0; t < kNiw; ++t) {
         const int r = ((w & 3) * kNiw + t) * kRpi + lrow;
         const int src = r >= kRowsB ? min(m0 + r - kRowsB, M - 1) - m0
-                        : PAIR      ? min(n0 / 2 + pair_row(r), N - 1) - n0 / 2
+                        : kPair     ? min(n0 / 2 + pair_row(r), N - 1) - n0 / 2
                                     : min(n0 + r, N - 1) - n0;
         voff[t] = (uint32_t)(src * K + ((lchunk ^ swz(r)) << 4));
     }
-    const uint8_t* baseA = A + (int64_t)m0 * K;
-    const uint8_t* baseB = B + (int64_t)(PAIR ? n0 / 2 : n0) * K;
+    const uint8_t* baseA = p.A + (int64_t)m0 * K;
+    const uint8_t* baseB = p.B + (int64_t)(kPair ? n0 / 2 : n0) * K;
     const uint32_t lds0 = lds_addr(sm);
     const int nst = (K + kKC - 1) / kKC;
     auto issue = [&](int st) {
@@ -84,7 +82,7 @@ __device__ __forceinline__ void stream_loop(uint8_t* __restrict__ sm, const uint
                 v -= (uint32_t)max(0, c - end);
             }
             // a copy's rows lie in one block of 16: which of the pair is wave-uniform
-            const uint8_t* b = baseB + (PAIR && ((d * kRpi >> 4) & 1) ? (int64_t)N * K : 0);
+            const uint8_t* b = baseB + (kPair && ((d * kRpi >> 4) & 1) ? (int64_t)N * K : 0);
             if (d * kRpi >= kRowsB) lds_dma16_s(baseA + (int64_t)st * kKC, v, dst);
             else if (nt) lds_dma16_nt(b + (int64_t)st * kKC, v, dst);
             else lds_dma16_s(b + (int64_t)st * kKC, v, dst);
@@ -96,6 +94,7 @@ __device__ __forceinline__ void stream_loop(uint8_t* __restrict__ sm, const uint
     const int nb0 = part % kWn * kNbw, mb0 = part / kWn * kMbw;  // this wave's blocks of the tile
     const int fo0 = frow * kKC + (((slot * 8 + 2 * fg) ^ swz(frow)) << 4);
     const int fo1 = frow * kKC + (((slot * 8 + 2 * fg + 1) ^ swz(frow)) << 4);
+    v4f acc[kMbw][kNbw];
 #pragma unroll
     for (int i = 0; i < kMbw; ++i)
 #pragma unroll
@@ -157,6 +156,63 @@ __device__ __forceinline__ void stream_loop(uint8_t* __restrict__ sm, const uint
             multiply(st);
         }
         ws_barrier();
+    }
+    if constexpr (!E::kPlain) {
+        // each block's partial sums to the wave that takes it
+        v4f* red = (v4f*)sm;  // [slot][16-row block][16-column block][lane]
+        static_assert(kSlots * MB * NB * 1024 <= kSlBuf * kStage && (!kPair || NB % 2 == 0), "LDS budget");
+        if (w < 4) {
+#pragma unroll
+            for (int i = 0; i < kMbw; ++i)
+#pragma unroll
+                for (int j = 0; j < kNbw; ++j) red[((slot * MB + mb0 + i) * NB + nb0 + j) * 64 + lane] = acc[i][j];
+        }
+        __syncthreads();
+        E::template finish<MB, NB, kSlots>(p, red, m0, n0);
+    } else {
+        uint32_t mx = 0;
+        const int bb = *p.bb;
+        auto put = [&](int mb, int nb, v4f sum) {
+            const int64_t m = m0 + mb * 16 + frow, n = n0 + nb * 16 + fg * 4;
+            if (n >= N) return;
+            const int sh = row_shift(p.ba, p.ba_rows, bb, m, M);
+            mx = max(mx, p.out_dt == FP8_DT_BF16 ? store4<FP8_DT_BF16>(p.C, N, m, n, M, N, sum, sh)
+                                                 : store4<FP8_DT_F32>(p.C, N, m, n, M, N, sum, sh));
+        };
+        if (kSlots == 1) {
+            if (w < 4) {
+#pragma unroll
+                for (int i = 0; i < kMbw; ++i)
+#pragma unroll
+                    for (int j = 0; j < kNbw; ++j) put(mb0 + i, nb0 + j, acc[i][j]);
+            }
+        } else {
+            v4f* red = (v4f*)sm;  // [slot][16-row block][16-column block][lane]
+            if (w < 4) {
+#pragma unroll
+                for (int i = 0; i < kMbw; ++i)
+#pragma unroll
+                    for (int j = 0; j < kNbw; ++j) red[((slot * MB + i) * NB + nb0 + j) * 64 + lane] = acc[i][j];
+            }
+            __syncthreads();
+            for (int b = w; b < MB * NB; b += stream_threads(MB) / 64) {
+                v4f sum = red[b * 64 + lane];
+#pragma unroll
+                for (int s = 1; s < kSlots; ++s) sum += red[(s * MB * NB + b) * 64 + lane];
+                put(b / NB, b % NB, sum);
+            }
+        }
+        if (p.with_amax) {
+            const uint32_t wv = wave_max_u32(mx);
+            if (lane == 0) wmx[w] = wv;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                uint32_t b = 0;
+#pragma unroll
+                for (int v = 0; v < stream_threads(MB) / 64; ++v) b = max(b, wmx[v]);
+                fold_amax(canon_amax(b), p.amax, p.bo);
+            }
+        }
     }
 }
 

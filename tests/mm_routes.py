@@ -18,6 +18,7 @@ def _lib():
         build.build()
     L = F.lib()
     L.fp8lin_mm_route.argtypes = [_i64, _i64, _i64, _i32, _vp, _vp]
+    L.fp8lin_epi_route.argtypes = [_i32, _i64, _i64, _i64, _vp, _vp]
     L.fp8lin_mm_tile.argtypes = [_i32, _vp, _vp]
     L.fp8lin_mm_forced.argtypes = [_i32, _i32, _i32, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _i64, _i64, _i64, _i32,
                                    _i32, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
@@ -30,6 +31,13 @@ def route(M: int, N: int, K: int, with_amax: bool = False):
     mb, nb = _i32(), _i32()
     kernel = _lib().fp8lin_mm_route(M, N, K, int(with_amax), ctypes.byref(mb), ctypes.byref(nb))
     return kernel, mb.value, nb.value
+
+
+def epilogue(mode: int, M: int, N: int, K: int):
+    """route of a feed-forward matmul: mode 0 fwd_act, 1 fwd_glu, 2 bwd_dx_act, 3 bwd_dx_glu; M
+    rows, N columns of the output (of one projection), contraction K."""
+    mb, nb = _i32(), _i32()
+    return _lib().fp8lin_epi_route(mode, M, N, K, ctypes.byref(mb), ctypes.byref(nb)), mb.value, nb.value
 
 
 def kernel(M: int, N: int, K: int) -> int:

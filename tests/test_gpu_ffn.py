@@ -1,0 +1,420 @@
+"""The feed-forward matmuls (fp8_linear_fwd_act, fp8_linear_fwd_glu and their
+backward forms) against the oracle in fp64.
+
+Two bars.  On small integers every product and sum is exact in the matrix core's
+fp32, and so is what follows it (no activation, or ReLU): outputs, kept values and
+bias gradients are then equal to the oracle's, rounded once, bit for bit, on
+shapes that take each kernel, with odd sizes, strides and alignments.  On
+method-shaped data the matrix core's sum of K products is off by at most 2^-11
+sum_k |a_k b_k| (the bar of the plain matmuls), which the activation passes on with
+its largest slope; then the fp32 arithmetic of the epilogue (2^-18 relative: the
+scaled error function's fit is within 5e-7, an exponential of -x^2/2 at |x| <= 6
+within 18 log2(e) 2^-24 = 1.6e-6, a few products) and 1e-9 where the tail of an
+activation is below that; then half a step of the output's type.
+"""
+import numpy as np
+import pytest
+import torch
+
+import mm_routes as R
+from oracle import ffn as O
+from paper_2309_17224_amd import fp8lin as F
+
+pytestmark = pytest.mark.gpu
+
+E4, E5 = torch.float8_e4m3fn, torch.float8_e5m2
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+ACT = {name: i for i, name in enumerate(O.ACTS)}
+SMALL = [(1, 16, 128), (1, 37, 256), (16, 200, 384), (1, 4100, 128), (1, 16390, 128), (17, 2050, 1024), (1100, 260, 128),
+         (256, 769, 2048), (33, 8200, 128), (500, 770, 128), (100, 8201, 256), (800, 769, 512), (600, 4090, 8192),
+         (512, 4096, 8192)]
+ANY_K = [(1, 1, 1), (5, 19, 17), (64, 64, 64), (130, 70, 200), (1030, 4097, 130)]
+WIDE = [(700, 4099, 128), (2049, 2100, 128), (515, 8200, 256)]
+SHAPES = SMALL + ANY_K + WIDE
+
+
+def test_shapes_take_every_kernel():
+    """In all four forms: small tiles of each split of k, any K in both tile sizes, 256-row tiles."""
+    for mode in range(4):
+        assert [R.epilogue(mode, *s)[0] for s in ANY_K] == [R.RAGGED] * len(ANY_K)
+        assert [R.epilogue(mode, *s)[0] for s in WIDE] == [R.MAIN] * len(WIDE)
+        tiles = {t[1:] for t in (R.epilogue(mode, *s) for s in SMALL) if t[0] == R.STREAM}
+        assert len(tiles) >= 8 and {R.stage(*t) for t in tiles} == {512, 256, 128}, tiles
+        assert mode != 1 or all(nb % 2 == 0 for _, nb in tiles)
+
+
+def codes(gen, rows, cols, kind, gpu, ints):
+    """Codes on the GPU and their values; ints: whole numbers from -2 to 2."""
+    if ints:
+        v = torch.randint(-2, 3, (rows, cols), generator=gen).float()
+    else:
+        v = torch.randn(rows, cols, generator=gen) * (16 if kind is E4 else 64)
+    q = v.to(kind)
+    return q.view(torch.uint8).to(gpu), q.double().numpy()
+
+
+def word(v, gpu):
+    return torch.tensor([v], dtype=torch.int32, device=gpu)
+
+
+def ints(gen, rows, cols, lo=-3, hi=4):
+    return torch.randint(lo, hi, (rows, cols), generator=gen).to(torch.bfloat16)
+
+
+class Strided:
+    """[rows, cols] inside a larger buffer: rows `pad` elements apart, `off` from its start; the rest holds a mark."""
+
+    def __init__(self, rows, cols, dtype, gpu, pad=0, off=0, value=None):
+        self.mark = 77
+        self.buf = torch.full((off + rows * (cols + pad) + 3,), self.mark, dtype=dtype, device=gpu)
+        self.t = self.buf[off:off + rows * (cols + pad)].view(rows, cols + pad)[:, :cols] if rows * (cols + pad) else \
+            torch.empty((rows, cols), dtype=dtype, device=gpu)
+        if value is not None:
+            self.t.copy_(value)
+
+    def untouched(self):
+        seen = torch.zeros_like(self.buf, dtype=torch.bool)
+        rows, cols = self.t.shape
+        at = self.t.storage_offset()
+        seen[at:at + rows * self.t.stride(0)].view(rows, self.t.stride(0))[:, :cols] = True
+        return bool((self.buf[~seen] == self.mark).all())
+
+
+def want_bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16)  # whole numbers below 2^24: one rounding
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("act,dt,pad,off", [("none", torch.bfloat16, 0, 0), ("relu", torch.float32, 3, 1), ("relu", torch.bfloat16, 5, 3)])
+def test_forward_exact(gpu, shape, act, dt, pad, off):
+    M, N, K = shape
+    gen = torch.Generator().manual_seed(M + 3 * N + 7 * K + len(act))
+    x8, x = codes(gen, M, K, E4, gpu, True)
+    w8, w = codes(gen, N, K, E4, gpu, True)
+    bias, res = ints(gen, 1, N), ints(gen, M, N, -9, 10)
+    s = 1                                              # 2^-(bx + bw), whole numbers stay whole
+    b = bias[0].to(gpu) if off != 1 else bias[0].float().to(gpu)
+    y = Strided(M, N, dt, gpu, pad, off)
+    z = Strided(M, N, torch.bfloat16, gpu, pad, off)
+    r = Strided(M, N, dt, gpu, pad + 1, off, res.to(gpu))
+    F.fp8_linear_fwd_act(x8, word(3, gpu), w8, word(-3 - s, gpu), ACT[act], bias=b, res=r.t, z=z.t, y=y.t)
+    zr, yr = O.linear_act(x * 2 ** s, w, bias.double().numpy(), act, res.double().numpy())
+    assert torch.equal(z.t.cpu(), want_bf16(zr))
+    assert torch.equal(y.t.cpu(), torch.from_numpy(yr).to(dt))
+    assert y.untouched() and z.untouched()
+    # alone: no bias, residual or kept values, and in place on the residual
+    y2 = F.fp8_linear_fwd_act(x8, word(0, gpu), w8, word(0, gpu), ACT[act], out_dt=F._dt(y.t))
+    assert torch.equal(y2.cpu(), torch.from_numpy(O.linear_act(x, w, None, act, None)[1]).to(dt))
+    F.fp8_linear_fwd_act(x8, word(0, gpu), w8, word(-s, gpu), ACT[act], bias=b, res=r.t, y=r.t)
+    assert torch.equal(r.t.cpu(), torch.from_numpy(yr).to(dt)) and r.untouched()
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("act,pad,off,keep", [("none", 0, 0, False), ("relu", 3, 1, True)])
+def test_glu_forward_exact(gpu, shape, act, pad, off, keep):
+    M, N, K = shape
+    gen = torch.Generator().manual_seed(M + 3 * N + 7 * K)
+    x8, x = codes(gen, M, K, E4, gpu, True)
+    w8, w = codes(gen, 2 * N, K, E4, gpu, True)
+    bias = ints(gen, 1, 2 * N)
+    a = Strided(M, N, torch.bfloat16, gpu, pad, off)
+    gu = Strided(M, 2 * N, torch.bfloat16, gpu, pad, off)
+    F.fp8_linear_fwd_glu(x8, word(0, gpu), w8, word(0, gpu), ACT[act], bias=bias[0].to(gpu) if keep else None,
+                         gu=gu.t if keep else None, a=a.t)
+    gur, ar = O.linear_glu(x, w, bias.double().numpy() if keep else None, act)
+    assert np.abs(ar).max() < 2 ** 24
+    assert torch.equal(a.t.cpu(), want_bf16(ar)) and a.untouched()
+    if keep:
+        assert torch.equal(gu.t.cpu(), want_bf16(gur)) and gu.untouched()
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("act,dt,pad,off", [("none", torch.float32, 0, 0), ("relu", torch.bfloat16, 3, 1)])
+def test_backward_exact(gpu, shape, act, dt, pad, off):
+    M, K, N = shape  # the output is [M, K], the contraction N
+    gen = torch.Generator().manual_seed(M + 3 * N + 7 * K)
+    dy8, dy = codes(gen, M, N, E5, gpu, True)
+    w8, w = codes(gen, K, N, E4, gpu, True)
+    zb = ints(gen, M, K)
+    z = Strided(M, K, torch.bfloat16, gpu, pad, off, zb.to(gpu))
+    dz = Strided(M, K, torch.bfloat16, gpu, pad, off)
+    db = torch.empty(K, dtype=dt, device=gpu)
+    F.fp8_linear_bwd_dx_act(dy8, word(5, gpu), w8, word(-5, gpu), z.t, ACT[act], dz=dz.t, db=db)
+    ref = O.linear_act_bwd(dy, w, zb.double().numpy(), act)
+    assert np.abs(ref).sum(axis=0).max() < 2 ** 24     # every partial sum of a column is exact
+    assert torch.equal(dz.t.cpu(), want_bf16(ref)) and dz.untouched()
+    assert torch.equal(db.cpu(), torch.from_numpy(ref.sum(axis=0)).to(dt))
+    F.fp8_linear_bwd_dx_act(dy8, word(0, gpu), w8, word(0, gpu), z.t, ACT[act], dz=z.t)  # in place, no sums
+    assert torch.equal(z.t.cpu(), want_bf16(ref)) and z.untouched()
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("act,dt,pad,off", [("none", torch.float32, 0, 0), ("relu", torch.bfloat16, 3, 1)])
+def test_glu_backward_exact(gpu, shape, act, dt, pad, off):
+    M, K, N = shape
+    gen = torch.Generator().manual_seed(M + 3 * N + 7 * K)
+    dy8, dy = codes(gen, M, N, E5, gpu, True)
+    w8, w = codes(gen, K, N, E4, gpu, True)
+    gub = ints(gen, M, 2 * K)
+    gu = Strided(M, 2 * K, torch.bfloat16, gpu, pad, off, gub.to(gpu))
+    dgu = Strided(M, 2 * K, torch.bfloat16, gpu, pad, off)
+    db = torch.empty(2 * K, dtype=dt, device=gpu)
+    F.fp8_linear_bwd_dx_glu(dy8, word(0, gpu), w8, word(0, gpu), gu.t, ACT[act], dgu=dgu.t, db=db)
+    ref = O.linear_glu_bwd(dy, w, gub.double().numpy(), act)
+    assert np.abs(ref).sum(axis=0).max() < 2 ** 24
+    assert torch.equal(dgu.t.cpu(), want_bf16(ref)) and dgu.untouched()
+    assert torch.equal(db.cpu(), torch.from_numpy(ref.sum(axis=0)).to(dt))
+    F.fp8_linear_bwd_dx_glu(dy8, word(0, gpu), w8, word(0, gpu), gu.t, ACT[act], dgu=gu.t)
+    assert torch.equal(gu.t.cpu(), want_bf16(ref)) and gu.untouched()
+
+
+# ------------------------------------------------------------------ method-shaped data
+DATA = [(1, 40, 256), (37, 200, 384), (130, 70, 200), (700, 4099, 128)]
+
+
+def sums_bound(a, b, s):
+    """The matrix core's error: 2^-11 of the sum of the products' magnitudes."""
+    return 2.0 ** -11 * s * (np.abs(a) @ np.abs(b).T)
+
+
+def close(got, ref, err, dt):
+    """|got - ref| <= err, and half a step of dt."""
+    g = got.double().cpu().numpy()
+    bound = err + HALF[dt] * (np.abs(ref) + err) + 2.0 ** -126
+    worst = np.max((np.abs(g - ref) - bound) / (bound + 1e-300)) if g.size else -1
+    assert worst <= 0, f"beyond the bound by {worst:.3g} of it"
+
+
+@pytest.mark.parametrize("shape", DATA, ids=str)
+@pytest.mark.parametrize("act", O.ACTS)
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_forward(gpu, shape, act, dt):
+    M, N, K = shape
+    gen = torch.Generator().manual_seed(11 + M)
+    x8, x = codes(gen, M, K, E4, gpu, False)
+    w8, w = codes(gen, N, K, E4, gpu, False)
+    s = 2.0 ** -12 if K == 128 else 2.0 ** -13
+    bias, res = torch.randn(N, generator=gen), torch.randn(M, N, generator=gen).to(dt)
+    z = torch.empty((M, N), dtype=torch.bfloat16, device=gpu)
+    y = F.fp8_linear_fwd_act(x8, word(7, gpu), w8, word(int(-np.log2(s)) - 7, gpu), ACT[act], bias=bias.to(gpu), res=res.to(gpu), z=z,
+                             out_dt=F.DT_F32 if dt is torch.float32 else F.DT_BF16)
+    zr, yr = O.linear_act(x * s, w, bias.double().numpy(), act, res.double().numpy())
+    e = sums_bound(x, w, s) + 2.0 ** -23 * np.abs(zr)
+    close(z, zr, e, torch.bfloat16)
+    f = O.act(zr, act)
+    close(y, yr, O.SLOPE_MAX[act] * e + 2.0 ** -18 * np.abs(f) + 1e-9 + 2.0 ** -24 * np.abs(yr), dt)
+
+
+@pytest.mark.parametrize("shape", DATA, ids=str)
+@pytest.mark.parametrize("act", O.ACTS)
+def test_glu_forward(gpu, shape, act):
+    M, N, K = shape
+    gen = torch.Generator().manual_seed(12 + M)
+    x8, x = codes(gen, M, K, E4, gpu, False)
+    w8, w = codes(gen, 2 * N, K, E4, gpu, False)
+    s = 2.0 ** -12 if K == 128 else 2.0 ** -13
+    bias = torch.randn(2 * N, generator=gen).to(torch.bfloat16)
+    gu = torch.empty((M, 2 * N), dtype=torch.bfloat16, device=gpu)
+    a = F.fp8_linear_fwd_glu(x8, word(0, gpu), w8, word(int(-np.log2(s)), gpu), ACT[act], bias=bias.to(gpu), gu=gu)
+    gur, ar = O.linear_glu(x * s, w, bias.double().numpy(), act)
+    e = sums_bound(x, w, s) + 2.0 ** -23 * np.abs(gur)
+    close(gu, gur, e, torch.bfloat16)
+    g, u = gur[:, :N], gur[:, N:]
+    eg, eu = O.SLOPE_MAX[act] * e[:, :N] + 2.0 ** -18 * np.abs(O.act(g, act)) + 1e-9, e[:, N:]
+    close(a, ar, eg * np.abs(u) + eu * np.abs(O.act(g, act)) + eg * eu + 2.0 ** -24 * np.abs(ar), torch.bfloat16)
+
+
+@pytest.mark.parametrize("shape", DATA, ids=str)
+@pytest.mark.parametrize("act", O.ACTS)
+@pytest.mark.parametrize("gated", [False, True], ids=["act", "glu"])
+def test_backward(gpu, shape, act, gated):
+    M, K, N = shape
+    gen = torch.Generator().manual_seed(13 + M)
+    dy8, dy = codes(gen, M, N, E5, gpu, False)
+    w8, w = codes(gen, K, N, E4, gpu, False)
+    s = 2.0 ** -16
+    cols = 2 * K if gated else K
+    z = (1.5 * torch.randn(M, cols, generator=gen)).to(torch.bfloat16)
+    db = torch.empty(cols, dtype=torch.float32, device=gpu)
+    call = F.fp8_linear_bwd_dx_glu if gated else F.fp8_linear_bwd_dx_act
+    dz = call(dy8, word(9, gpu), w8, word(7, gpu), z.to(gpu), ACT[act], db=db)
+    zv = z.double().numpy()
+    ref = (O.linear_glu_bwd if gated else O.linear_act_bwd)(dy * s, w, zv, act)
+    e, t = sums_bound(dy, w, s), np.abs(dy * s @ w.T)
+    d = np.abs(O.slope(zv[:, :K], act))
+    if gated:
+        u, f = np.abs(zv[:, K:]), np.abs(O.act(zv[:, :K], act))
+        err = np.concatenate([e * d * u + 2.0 ** -18 * t * u, e * f + t * (2.0 ** -18 * f + 1e-9)], axis=1)
+    else:
+        err = e * d + 2.0 ** -18 * t
+    close(dz, ref, err, torch.bfloat16)
+    # the sums: the terms' errors, and fp32 additions, each at most half a step of the sum of magnitudes
+    close(db, ref.sum(axis=0), err.sum(axis=0) + M * 2.0 ** -24 * (np.abs(ref) + err).sum(axis=0), torch.float32)
+
+
+@pytest.mark.parametrize("act", O.ACTS)
+def test_far_values_and_nonfinite(gpu, act):
+    """Values far out keep their limits: act(-inf) = 0, act(inf) = inf, slopes 0 and 1; NaN stays."""
+    z = torch.tensor([[-float("inf"), -3e38, -1e4, -200.0, -30.0, 30.0, 1e4, 3e38, float("inf"), float("nan"), 0.0, -0.0]])
+    n = z.shape[1]
+    one = torch.ones((1, 16), device=gpu).to(E4).view(torch.uint8)
+    zero = torch.zeros((n, 16), dtype=torch.uint8, device=gpu)
+    y = F.fp8_linear_fwd_act(one, word(0, gpu), zero, word(0, gpu), ACT[act], bias=z[0].to(gpu), out_dt=F.DT_F32)[0].cpu()
+    if act != "none":
+        assert y[0] == 0 and y[1] == 0 and y[2] == 0 and y[3] == 0 and abs(y[4]) < 1e-10
+    else:
+        assert torch.equal(y[:9], z[0, :9])
+    assert y[5] == 30 and y[6] == 1e4 and y[8] == float("inf") and torch.isnan(y[9]) and y[10] == 0 and y[11] == 0
+    ones = torch.ones((n, 16), device=gpu).to(E4).view(torch.uint8)
+    dy = torch.ones((1, 16), device=gpu).to(E5).view(torch.uint8)
+    d = F.fp8_linear_bwd_dx_act(dy, word(0, gpu), ones, word(4, gpu), z.to(torch.bfloat16).to(gpu), ACT[act])[0].float().cpu()
+    assert torch.equal(d[5:9], torch.ones(4)) and (torch.isnan(d[9]) or act == "none")
+    assert d[10] == (0 if act == "relu" else 1 if act == "none" else 0.5)
+    assert torch.equal(d[:5], torch.ones(5) if act == "none" else torch.zeros(5)) or (act == "silu" and d[4].abs() < 1e-10)
+
+
+# ------------------------------------------------------------------ codes of the outputs
+PREDS = [None, 0, 1, -2, "alias"]
+
+
+def quantised(out, fmt, margin):
+    return F.fp8_quantise(out, fmt, margin, want_qT=True)
+
+
+@pytest.mark.parametrize("shape", [(16, 1024, 256), (130, 70, 200), (700, 4099, 128), (2048, 4096, 256), (300, 520, 128)], ids=str)
+@pytest.mark.parametrize("kind", ["act", "glu", "act_bwd", "glu_bwd"])
+@pytest.mark.parametrize("pred", PREDS)
+def test_codes_are_those_of_the_output(gpu, shape, kind, pred):
+    M, N, K = shape
+    gen = torch.Generator().manual_seed(17 + M)
+    fwd, wide = kind in ("act", "glu"), 2 if kind == "glu" else 1
+    x8, _ = codes(gen, M, K, E4 if fwd else E5, gpu, False)
+    w8, _ = codes(gen, wide * N, K, E4, gpu, False)
+    cols = 2 * N if kind == "glu_bwd" else N
+    fmt, margin = {"act": (F.E4M3, 0), "glu": (F.E5M2, 1), "act_bwd": (F.E5M2, 0), "glu_bwd": (F.E4_A, -1)}[kind]
+    z = torch.randn(M, cols, generator=gen).to(torch.bfloat16).to(gpu)
+    args = (x8, word(6, gpu), w8, word(6, gpu))
+    res = z if kind == "act" else None
+
+    def call(fq, out=None):
+        if kind == "act":
+            return F.fp8_linear_fwd_act(*args, F.ACT_GELU, res=res, y=out, fq=fq)
+        if kind == "glu":
+            return F.fp8_linear_fwd_glu(*args, a=out, fq=fq)
+        if kind == "act_bwd":
+            return F.fp8_linear_bwd_dx_act(*args, z, F.ACT_GELU_TANH, dz=out, fq=fq)
+        return F.fp8_linear_bwd_dx_glu(*args, z, dgu=out, fq=fq)
+
+    alone = call(None)
+    q, qT, bias, amax, flags = quantised(alone, fmt, margin)
+    i32 = lambda: torch.full((1,), -99, dtype=torch.int32, device=gpu)  # noqa: E731
+    b = i32()
+    p = None if pred is None else b if pred == "alias" else word(int(bias) + pred, gpu)
+    if pred == "alias":
+        b.fill_(int(bias) - 2)
+    qs, qTs = Strided(M, cols, torch.uint8, gpu, 3, 1), Strided(cols, M, torch.uint8, gpu, 5, 2)
+    ws = torch.empty(max(F.fp8_linear_quantise_ws_bytes(M, cols), 4), dtype=torch.uint8, device=gpu)
+    out = Strided(M, cols, torch.bfloat16, gpu, 2, 1)
+    fq = F.FusedQuant(qs.t, b, ws, fmt, margin, bias_pred=p, amax_bits=i32(), flags=i32(), qT=qTs.t)
+    call(fq, out.t)
+    assert torch.equal(out.t, alone) and out.untouched()
+    assert (int(b), int(fq.amax_bits), int(fq.flags)) == (int(bias), int(amax), int(flags))
+    assert torch.equal(qs.t, q) and qs.untouched()
+    assert torch.equal(qTs.t, qT) and qTs.untouched()
+    fq2 = F.FusedQuant(torch.empty_like(q), b, ws, fmt, margin, bias_pred=p)   # codes alone, dense
+    call(fq2)
+    assert torch.equal(fq2.q, q) and int(b) == int(bias)
+
+
+def test_codes_of_fp32_and_nonfinite_outputs(gpu):
+    gen = torch.Generator().manual_seed(3)
+    x8, _ = codes(gen, 33, 256, E4, gpu, False)
+    w8, _ = codes(gen, 48, 256, E4, gpu, False)
+    res = torch.randn(33, 48, generator=gen).to(gpu)
+    for bad in (None, float("nan"), float("inf")):
+        if bad is not None:
+            res[5, 7] = bad
+        b, fl = word(3, gpu), word(0, gpu)
+        ws = torch.empty(F.fp8_linear_quantise_ws_bytes(33, 48), dtype=torch.uint8, device=gpu)
+        for dt in (torch.float32, torch.bfloat16):
+            fq = F.FusedQuant(torch.empty((33, 48), dtype=torch.uint8, device=gpu), b, ws, F.E4M3, 0, bias_pred=b, flags=fl)
+            y = F.fp8_linear_fwd_act(x8, word(5, gpu), w8, word(7, gpu), F.ACT_NONE, res=res.to(dt), out_dt=F.DT_F32 if dt is torch.float32 else F.DT_BF16, fq=fq)
+            q, _, bias, _, flags = F.fp8_quantise(y, F.E4M3)
+            assert torch.equal(fq.q, q) and int(b) == int(bias) and int(fl) == int(flags) == (0 if bad is None else F.FLAG_NONFINITE)
+
+
+# ------------------------------------------------------------------ edges
+def test_no_contraction_and_empty(gpu):
+    bias = torch.randn(24, device=gpu)
+    empty8 = lambda r: torch.empty((r, 0), dtype=torch.uint8, device=gpu)  # noqa: E731
+    z = word(0, gpu)
+    y = F.fp8_linear_fwd_act(empty8(5), z, empty8(24), z, F.ACT_RELU, bias=bias, out_dt=F.DT_F32)
+    assert torch.equal(y, bias.clamp(min=0).expand(5, 24))
+    a = F.fp8_linear_fwd_glu(empty8(5), z, empty8(24), z, F.ACT_NONE, bias=bias)
+    assert torch.equal(a, (bias[:12] * bias[12:]).to(torch.bfloat16).expand(5, 12))
+    db = torch.full((24,), 7.0, device=gpu)
+    F.fp8_linear_bwd_dx_act(empty8(5), z, empty8(24), z, torch.ones((5, 24), dtype=torch.bfloat16, device=gpu), F.ACT_GELU, db=db)
+    assert torch.equal(db, torch.zeros_like(db))
+    # no rows: sums and codes' bias are those of nothing
+    db.fill_(7)
+    b, fl = word(9, gpu), word(9, gpu)
+    fq = F.FusedQuant(torch.empty((0, 24), dtype=torch.uint8, device=gpu), b, torch.empty(4, dtype=torch.uint8, device=gpu),
+                      F.E5M2, 0, bias_pred=b, flags=fl)
+    w8 = torch.zeros((24, 16), dtype=torch.uint8, device=gpu)
+    F.fp8_linear_bwd_dx_act(torch.empty((0, 16), dtype=torch.uint8, device=gpu), z, w8, z,
+                            torch.empty((0, 24), dtype=torch.bfloat16, device=gpu), F.ACT_GELU, db=db, fq=fq)
+    assert torch.equal(db, torch.zeros_like(db)) and int(b) == 0 and int(fl) == F.FLAG_ZERO
+
+
+def test_same_bits_every_time_and_on_another_stream(gpu):
+    """Two calls on two streams at once, with workspaces of their own, give the first call's bits."""
+    gen = torch.Generator().manual_seed(5)
+    for M, K, N in ((260, 1100, 256), (2048, 4096, 256)):
+        dy8, _ = codes(gen, M, N, E5, gpu, False)
+        w8, _ = codes(gen, K, N, E4, gpu, False)
+        gu = torch.randn(M, 2 * K, generator=gen).to(torch.bfloat16).to(gpu)
+        one = word(6, gpu)
+        db = torch.empty(2 * K, device=gpu)
+        dgu = F.fp8_linear_bwd_dx_glu(dy8, one, w8, one, gu, db=db)
+        torch.cuda.synchronize()
+        runs = []
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        for s in streams:
+            d = torch.empty(2 * K, device=gpu)
+            s.wait_stream(torch.cuda.current_stream())
+            runs.append((F.fp8_linear_bwd_dx_glu(dy8, one, w8, one, gu, db=d, stream=s), d))
+        torch.cuda.synchronize()
+        for got, d in runs:
+            assert torch.equal(got, dgu) and torch.equal(d, db)
+
+
+def test_binding_refuses(gpu):
+    u8 = lambda *s: torch.zeros(s, dtype=torch.uint8, device=gpu)  # noqa: E731
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device=gpu)  # noqa: E731
+    i = word(0, gpu)
+    x, w = u8(4, 32), u8(8, 32)
+    bad = [
+        (ValueError, lambda: F.fp8_linear_fwd_act(x, i, u8(8, 31), i)),
+        (ValueError, lambda: F.fp8_linear_fwd_act(x.t().contiguous().t(), i, w, i)),
+        (TypeError, lambda: F.fp8_linear_fwd_act(x.to(torch.int8), i, w, i)),
+        (TypeError, lambda: F.fp8_linear_fwd_act(x, i.float(), w, i)),
+        (ValueError, lambda: F.fp8_linear_fwd_act(x, i, w, i, bias=bf(7))),
+        (TypeError, lambda: F.fp8_linear_fwd_act(x, i, w, i, res=bf(4, 8).float())),
+        (ValueError, lambda: F.fp8_linear_fwd_act(x, i, w, i, res=bf(1, 8).expand(4, 8))),
+        (ValueError, lambda: F.fp8_linear_fwd_act(x, i, w, i, z=bf(4, 9))),
+        (ValueError, lambda: F.fp8_linear_fwd_act(x, i, w, i, y=bf(5, 8))),
+        (ValueError, lambda: F.fp8_linear_fwd_act(x, i, w, i, bias=torch.zeros(8))),
+        (F.Fp8Error, lambda: F.fp8_linear_fwd_act(x, i, w, i, act=7)),
+        (ValueError, lambda: F.fp8_linear_fwd_glu(x, i, u8(7, 32), i)),
+        (ValueError, lambda: F.fp8_linear_fwd_glu(x, i, w, i, gu=bf(4, 4))),
+        (TypeError, lambda: F.fp8_linear_bwd_dx_act(x, i, w, i, bf(4, 8).float(), F.ACT_GELU)),
+        (ValueError, lambda: F.fp8_linear_bwd_dx_act(x, i, w, i, bf(4, 7), F.ACT_GELU)),
+        (ValueError, lambda: F.fp8_linear_bwd_dx_act(x, i, w, i, bf(4, 8), F.ACT_GELU, db=bf(9))),
+        (F.Fp8Error, lambda: F.fp8_linear_bwd_dx_act(x, i, w, i, bf(4, 8), F.ACT_GELU, db=bf(8), ws=u8(4))),
+        (ValueError, lambda: F.fp8_linear_bwd_dx_glu(x, i, w, i, bf(4, 8))),
+        (ValueError, lambda: F.gpt_bias_grad(bf(4, 8), db=bf(7))),
+        (ValueError, lambda: F.gpt_bias_grad(bf(8, 4).t())),
+    ]
+    for error, fn in bad:
+        with pytest.raises(error):
+            fn()
