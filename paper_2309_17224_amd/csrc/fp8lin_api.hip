@@ -604,6 +604,10 @@ int32_t out_quant_empty(const fp8_out_quantise* t, void* stream) {
                              as_stream(stream));
 }
 
+FusedQuant out_quant(const fp8_out_quantise* t) {
+    return FusedQuant{t->fmt, t->margin, t->bias_pred, t->bias, t->amax_bits, t->flags, t->q, t->ldq, (uint32_t*)t->ws};
+}
+
 // The checks that the four matmuls share, then the call.  e: everything but the
 // workspace's sums; out_cols: columns of the output; db: the column sums, or null.
 int32_t epilogue_mm(int mode, Epi& e, int64_t out_cols, void* db, int32_t db_dt, const fp8_out_quantise* quant, void* ws,
@@ -633,14 +637,11 @@ int32_t epilogue_mm(int mode, Epi& e, int64_t out_cols, void* db, int32_t db_dt,
     }
     e.sums = db ? (float*)ws : nullptr;
     e.sum_cols = out_cols;
-    int32_t lst = launch_epilogue_mm(mode, e, as_stream(stream));
-    if (lst == FP8_OK && db)
-        lst = launch_sums_finish((const float*)ws, epi_sum_rows(mode, e.M, e.N, e.K), out_cols, db, out_cols, nullptr, db_dt,
-                                 as_stream(stream));
-    if (lst != FP8_OK || !quant) return lst;
-    return launch_quantise(e.out, e.out_dt, e.M, out_cols, e.ldo, quant->fmt, quant->margin, quant->bias_pred, quant->bias,
-                           quant->amax_bits, quant->flags, quant->q, quant->ldq, quant->qT, quant->ldqT,
-                           (uint32_t*)quant->ws, as_stream(stream));
+    e.db = db, e.db_dt = db_dt;
+    FusedQuant fq{};
+    if (quant) fq = out_quant(quant);
+    return launch_epilogue_mm(mode, e, quant ? &fq : nullptr, quant ? quant->qT : nullptr, quant ? quant->ldqT : 0,
+                              as_stream(stream));
 }
 }  // namespace
 
@@ -730,9 +731,7 @@ int32_t gpt_layernorm_quantise(const void* x, int64_t ldx, const void* res, int6
     a.rows = rows, a.cols = cols, a.ldx = ldx, a.ldr = ldr, a.ldh = ldh, a.ldy = ldy, a.dt = dt, a.g_dt = g_dt;
     a.eps = eps, a.x = x, a.res = res, a.g = g, a.b = b, a.h = h, a.y = y, a.mean = mean, a.rstd = rstd;
     FusedQuant fq{};
-    if (quant)
-        fq = FusedQuant{quant->fmt, quant->margin, quant->bias_pred, quant->bias, quant->amax_bits, quant->flags, quant->q,
-                        quant->ldq, (uint32_t*)quant->ws};
+    if (quant) fq = out_quant(quant);
     return launch_layernorm(a, quant ? &fq : nullptr, as_stream(stream));
 }
 

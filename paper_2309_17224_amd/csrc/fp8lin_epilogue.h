@@ -12,62 +12,74 @@ namespace {
 constexpr bool epi_fwd(int mode) { return mode == kEpiAct || mode == kEpiGlu; }
 constexpr int epi_fa(int mode) { return epi_fwd(mode) ? FP8_E4M3 : FP8_E5M2; }  // format of A (B: E4M3)
 
-// Phi(x) = (1 + erf(x / sqrt 2)) / 2 = 1 - Phi(-x): for a = |x| it is h = e^(-a^2/2)
-// times half the scaled complementary error function of a / sqrt 2, which is
-// within 4e-9 of s P(s), s = 1 / (1 + 0.24 a), for a <= 20 (a least-squares fit,
-// reweighted towards the smallest largest relative error; 5e-7 in fp32), so the
-// tail keeps its relative accuracy.
-__device__ __forceinline__ float half_erfcx(float a) {
-    const float s = __builtin_amdgcn_rcpf(1.0f + 0.24f * a);
-    float p = 2.548838668e-02f;
-    p = fmaf(p, s, -1.244845439e-01f);
-    p = fmaf(p, s, 2.052491748e-01f);
-    p = fmaf(p, s, -1.441438550e-01f);
-    p = fmaf(p, s, 1.415055771e-01f);
-    p = fmaf(p, s, 2.803383015e-02f);
-    p = fmaf(p, s, 8.783841470e-02f);
-    p = fmaf(p, s, 8.890991091e-02f);
-    p = fmaf(p, s, 9.586130313e-02f);
-    p = fmaf(p, s, 9.574180156e-02f);
-    return p * s;
+// The VALU is what bounds the epilogues that have an exponential (a workgroup's 256
+// x 256 outputs: about 0.4 us an operation of each, 1.6 us an exponential or
+// reciprocal), so the forms below are the shortest that keep infinities, NaN and a
+// relative error of a few 2^-20: act(-inf) = 0, act(inf) = inf, slopes 0 and 1.
+constexpr float kMaxF = 3.402823466e38f;
+
+// h = Phi(-a) = (1 - erf(a / sqrt 2)) / 2, a = |x|: e = exp(-a^2 / 2) times half the
+// scaled complementary error function of a / sqrt 2, which is within 6.2e-7 of P(s),
+// s = 1 / (1 + 0.29 a), for a <= 9 (a least-squares fit, reweighted towards the
+// smallest largest relative error; 9.5e-7 in fp32), so the tail keeps its relative
+// accuracy.  e is left in *e, P in *p.
+__device__ __forceinline__ void gauss_tail(float x, float* e, float* p) {
+    *e = __builtin_amdgcn_exp2f(x * -0.72134752f * x);
+    const float s = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.29f, 1.0f));
+    float q = fmaf(-0.0970692119f, s, 0.317669847f);
+    q = fmaf(q, s, -0.145566512f);
+    q = fmaf(q, s, 0.222276692f);
+    q = fmaf(q, s, 0.0821047592f);
+    q = fmaf(q, s, 0.120924779f);
+    *p = fmaf(q, s, -0.000340452563f);
 }
 
-// x within [-top, top]; NaN stays.
-__device__ __forceinline__ float within(float x, float top) { return x < -top ? -top : x > top ? top : x; }
-
-// sigma(p ln 2) and sigma (1 - sigma), both to a few ulp at either end.
-__device__ __forceinline__ void sigmoid2(float p, float* s, float* ds) {
-    const float q = __builtin_amdgcn_exp2f(-fabsf(p)), r = __builtin_amdgcn_rcpf(1.0f + q);
-    *s = p < 0.0f ? q * r : r;
-    *ds = q * r * r;
+// q = 2^-p and sigma(p ln 2) = 1 / (1 + q).
+__device__ __forceinline__ float sigma2(float p, float* q) {
+    *q = __builtin_amdgcn_exp2f(-p);
+    return __builtin_amdgcn_rcpf(1.0f + *q);
 }
 
-// f = act(x), d = act'(x).  Beyond the clamps the exponentials are 0 in fp32;
-// they keep infinities (act(-inf) = -0, act(inf) = inf, slopes 0 and 1).
-__device__ __forceinline__ void act_of(int act, float x, float* f, float* d) {
-    if (act == FP8_ACT_GELU) {
-        const float c = within(x, 20.0f), e = __builtin_amdgcn_exp2f(c * c * -0.72134752f);
-        const float h = half_erfcx(fabsf(c)) * e, phi = c < 0.0f ? h : 1.0f - h;
-        *f = (x < 0.0f ? c : x) * phi;
-        *d = fmaf(c * e, 0.39894228f, phi);
-    } else if (act == FP8_ACT_GELU_TANH) {  // (1 + tanh u) / 2 = sigma(2 u), u = sqrt(2/pi) (x + 0.044715 x^3)
-        const float c = within(x, 20.0f), c2 = c * c;
-        float s, ds;
-        sigmoid2(c * fmaf(c2, 0.1029432397f, 2.302208198f), &s, &ds);  // 2 sqrt(2/pi) log2(e) {0.044715, 1}
-        *f = (x < 0.0f ? c : x) * s;
-        *d = fmaf(c * ds, fmaf(c2, 0.2140644488f, 1.595769122f), s);   // 2 sqrt(2/pi) {3 * 0.044715, 1}
-    } else if (act == FP8_ACT_SILU) {
-        const float c = within(x, 200.0f);
-        float s, ds;
-        sigmoid2(c * 1.442695041f, &s, &ds);
-        *f = (x < 0.0f ? c : x) * s;
-        *d = fmaf(c, ds, s);
-    } else if (act == FP8_ACT_RELU) {
+// f = act(x), d = act'(x) (what is not used costs nothing).
+// GELU: x Phi(x) = max(x, 0) - a h; its slope Phi(x) + x phi(x) is k = e (P - a /
+// sqrt(2 pi)) for x < 0 and 1 - k otherwise.
+// The others are x sigma(p(x)), with slope sigma (1 + x p' (1 - sigma)), 1 - sigma = q sigma.
+template <int ACT>
+__device__ __forceinline__ void act_t(float x, float* f, float* d) {
+    if constexpr (ACT == FP8_ACT_GELU) {
+        float e, p;
+        gauss_tail(x, &e, &p);
+        *f = fmaf(-fminf(fabsf(x), kMaxF), p * e, fmaxf(x, 0.0f));
+        const float k = e * fmaf(fminf(fabsf(x), 100.0f), -0.39894228f, p);
+        *d = x < 0.0f ? k : 1.0f - k;
+    } else if constexpr (ACT == FP8_ACT_GELU_TANH) {  // (1 + tanh u) / 2 = sigma(2 u), u = sqrt(2/pi) (x + 0.044715 x^3)
+        float q;
+        const float r = sigma2(x * fmaf(x * x, 0.1029432397f, 2.302208198f), &q);  // 2 sqrt(2/pi) log2(e) {0.044715, 1}
+        *f = fmaxf(x, -kMaxF) * r;
+        const float c = __builtin_amdgcn_fmed3f(x, -100.0f, 100.0f);
+        const float dp = c * fmaf(c * c, 0.2140644488f, 1.595769122f);  // 2 sqrt(2/pi) {3 * 0.044715, 1}
+        *d = fmaf(dp, fminf(q, 1e30f) * r, 1.0f) * r;
+    } else if constexpr (ACT == FP8_ACT_SILU) {
+        float q;
+        const float r = sigma2(x * 1.442695041f, &q);
+        *f = fmaxf(x, -kMaxF) * r;
+        *d = fmaf(__builtin_amdgcn_fmed3f(x, -1000.0f, 1000.0f), fminf(q, 1e30f) * r, 1.0f) * r;
+    } else if constexpr (ACT == FP8_ACT_RELU) {
         *f = x <= 0.0f ? 0.0f : x;
         *d = x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
     } else {
         *f = x;
         *d = 1.0f;
+    }
+}
+
+__device__ __forceinline__ void act_of(int act, float x, float* f, float* d) {
+    switch (act) {
+        case FP8_ACT_GELU: act_t<FP8_ACT_GELU>(x, f, d); break;
+        case FP8_ACT_GELU_TANH: act_t<FP8_ACT_GELU_TANH>(x, f, d); break;
+        case FP8_ACT_SILU: act_t<FP8_ACT_SILU>(x, f, d); break;
+        case FP8_ACT_RELU: act_t<FP8_ACT_RELU>(x, f, d); break;
+        default: act_t<FP8_ACT_NONE>(x, f, d);
     }
 }
 

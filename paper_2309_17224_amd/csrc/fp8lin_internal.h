@@ -178,11 +178,29 @@ struct Epi {
     int64_t ldres, ldkeep, ldz, ldo;
     float* sums;                 // backward, may be null: column sums of groups of rows, [epi_sum_rows, sum_cols]
     int64_t sum_cols;
+    void* db;                    // with sums: their sum over the groups, of type db_dt
+    int db_dt;
+    // set by launch_epilogue_mm: bf16 output and 32-bit offsets within a wave's rows;
+    // codes of the output written by the epilogue itself (q null: not)
+    int fast;
+    const int32_t* pred;
+    int32_t* used;
+    uint32_t* parts;
+    uint8_t *q, *qT;
+    int64_t ldq, ldqT;
 };
 MmRoute epi_route(int mode, int64_t M, int64_t N, int64_t K);
 int64_t epi_sum_rows(int mode, int64_t M, int64_t N, int64_t K);
-int32_t launch_epilogue_mm(int mode, const Epi& e, hipStream_t s);
+int64_t epi_b_cols(int mode, int64_t N);        // columns of B over all tiles: kEpiGlu: in blocks of 16 of each, filled up
+bool epi_big_tiles(int64_t M, int64_t cols);    // the kernels for any K: 256 x 128 tiles from 128 of them on, else 64 x 64
+// The matmul, the column sums and, with fq, the codes of its output (transposed to
+// qT if that is given); fq->ws: gemm_quantise_ws_words.
+int32_t launch_epilogue_mm(int mode, Epi& e, const struct FusedQuant* fq, uint8_t* qT, int64_t ldqT, hipStream_t s);
 void launch_ffn_small(int mode, int mb, int nb, const Epi& e, hipStream_t s);
+void launch_ffn_act(bool ragged, const Epi& e, hipStream_t s);
+void launch_ffn_glu(bool ragged, const Epi& e, hipStream_t s);
+void launch_ffn_act_bwd(bool ragged, const Epi& e, hipStream_t s);
+void launch_ffn_glu_bwd(bool ragged, const Epi& e, hipStream_t s);
 // out0[c] (c < n0) and out1[c - n0] = sum over the rows of part [rows, cols] fp32,
 // of type dt; either may be null.
 int32_t launch_sums_finish(const float* part, int64_t rows, int64_t cols, void* out0, int64_t n0, void* out1, int dt,

@@ -277,21 +277,28 @@ def test_far_values_and_nonfinite(gpu, act):
 PREDS = [None, 0, 1, -2, "alias"]
 
 
+# the format that the epilogue casts to itself, and another
+FORMATS = {"act": [(F.E4M3, 0), (F.E5M2, 2)], "glu": [(F.E4M3, 2), (F.E5_A, 0)], "act_bwd": [(F.E5M2, 0), (F.E4M3, 0)],
+           "glu_bwd": [(F.E5M2, -1), (F.E4_A, 1)]}
+
+
 def quantised(out, fmt, margin):
     return F.fp8_quantise(out, fmt, margin, want_qT=True)
 
 
-@pytest.mark.parametrize("shape", [(16, 1024, 256), (130, 70, 200), (700, 4099, 128), (2048, 4096, 256), (300, 520, 128)], ids=str)
+@pytest.mark.parametrize("shape", [(16, 1024, 256), (130, 70, 200), (700, 4099, 128), (2048, 4096, 256), (300, 520, 128), (700, 4104, 128), (2049, 2104, 256),
+                                   (515, 8200, 256)], ids=str)
 @pytest.mark.parametrize("kind", ["act", "glu", "act_bwd", "glu_bwd"])
 @pytest.mark.parametrize("pred", PREDS)
-def test_codes_are_those_of_the_output(gpu, shape, kind, pred):
+@pytest.mark.parametrize("nth", [0, 1])
+def test_codes_are_those_of_the_output(gpu, shape, kind, pred, nth):
     M, N, K = shape
     gen = torch.Generator().manual_seed(17 + M)
     fwd, wide = kind in ("act", "glu"), 2 if kind == "glu" else 1
     x8, _ = codes(gen, M, K, E4 if fwd else E5, gpu, False)
     w8, _ = codes(gen, wide * N, K, E4, gpu, False)
     cols = 2 * N if kind == "glu_bwd" else N
-    fmt, margin = {"act": (F.E4M3, 0), "glu": (F.E5M2, 1), "act_bwd": (F.E5M2, 0), "glu_bwd": (F.E4_A, -1)}[kind]
+    fmt, margin = FORMATS[kind][nth]
     z = torch.randn(M, cols, generator=gen).to(torch.bfloat16).to(gpu)
     args = (x8, word(6, gpu), w8, word(6, gpu))
     res = z if kind == "act" else None
@@ -324,6 +331,36 @@ def test_codes_are_those_of_the_output(gpu, shape, kind, pred):
     fq2 = F.FusedQuant(torch.empty_like(q), b, ws, fmt, margin, bias_pred=p)   # codes alone, dense
     call(fq2)
     assert torch.equal(fq2.q, q) and int(b) == int(bias)
+
+
+@pytest.mark.parametrize("M", [700, 1030, 2049])
+@pytest.mark.parametrize("kind", ["act", "act_bwd", "glu_bwd"])
+def test_codes_of_an_output_in_place(gpu, M, kind):
+    """y on res, dz on z, dgu on gu, rows that end inside a tile: nothing of what was written is taken for input."""
+    gen = torch.Generator().manual_seed(M)
+    N, K = 4096, 128
+    x8, _ = codes(gen, M, K, E4 if kind == "act" else E5, gpu, False)
+    w8, _ = codes(gen, N, K, E4, gpu, False)
+    fmt = F.E4M3 if kind == "act" else F.E5M2
+    cols = 2 * N if kind == "glu_bwd" else N
+    v = (0.001 * torch.randn(M, cols, generator=gen)).to(torch.bfloat16).to(gpu)
+    args = (x8, word(9, gpu), w8, word(9, gpu))
+
+    def call(src, out, fq):
+        if kind == "act":
+            return F.fp8_linear_fwd_act(*args, F.ACT_SILU, res=src, y=out, fq=fq)
+        if kind == "act_bwd":
+            return F.fp8_linear_bwd_dx_act(*args, src, F.ACT_GELU, dz=out, fq=fq)
+        return F.fp8_linear_bwd_dx_glu(*args, src, dgu=out, fq=fq)
+
+    apart = call(v, None, None)
+    q, qT, bias, amax, flags = quantised(apart, fmt, 0)
+    b = word(int(bias), gpu)
+    fq = F.FusedQuant(torch.empty_like(q), b, torch.empty(F.fp8_linear_quantise_ws_bytes(M, cols), dtype=torch.uint8, device=gpu),
+                      fmt, 0, bias_pred=b, amax_bits=word(0, gpu), qT=torch.empty_like(qT))
+    call(v, v, fq)
+    assert torch.equal(v, apart) and int(b) == int(bias) and int(fq.amax_bits) == int(amax)
+    assert torch.equal(fq.q, q) and torch.equal(fq.qT, qT)
 
 
 def test_codes_of_fp32_and_nonfinite_outputs(gpu):
