@@ -12,9 +12,9 @@
 // _ragged), and so is the choice among them.  The gated pair multiplies A by
 // both matrices in one tile whose B rows are blocks of 16 from them in turn, so
 // that one lane ends with the same columns of both products.
-// The sums go through LDS, 32 rows of a wave at a time, so that a lane gets eight
-// consecutive columns of one row: every global access is then a 16-byte piece of
-// a row run, and the epilogue's code exists once, in a loop.
+// The sums go through LDS, 16 rows of a wave at a time, so that a lane gets eight
+// consecutive columns of a row: every global access is then a 16-byte piece of a
+// row run.
 #pragma once
 
 #include "fp8lin_epilogue.h"
@@ -27,31 +27,45 @@ namespace {
 
 constexpr int pow2_up(int n) { return n <= 1 ? 1 : 2 * pow2_up((n + 1) / 2); }
 
-// Geometry of a wave's epilogue: MBLK x NBLK blocks of 16 x 16 sums, staged 32 rows
+// Geometry of a wave's epilogue: MBLK x NBLK blocks of 16 x 16 sums, staged 16 rows
 // at a time; an eight of columns to a lane, kNp consecutive rows of it one after
 // another (so that their codes' bytes end in one lane for the transposed copy).
 template <int MODE, int NBLK>
 struct EpiGeo {
     static constexpr bool kPair = MODE == kEpiGlu;
-    static constexpr int kRow = NBLK * 64 + 16;           // staging row, bytes
+    static constexpr int kRow = NBLK <= 2 ? 128 : NBLK <= 4 ? 256 : 512;  // staging row, bytes
     static constexpr int kOct = kPair ? NBLK : 2 * NBLK;  // eights of columns in a row
-    static constexpr int kLpr = pow2_up(kOct), kNp = kLpr / 2;  // lanes a row, rows of a lane
-    static_assert((!kPair || NBLK % 2 == 0) && kLpr <= 16 && kNp >= 1, "blocks of a wave");
+    static constexpr int kLpr = kOct <= 4 ? 4 : pow2_up(kOct), kNp = kLpr / 4;  // lanes a row, rows of a lane
+    static_assert((!kPair || NBLK % 2 == 0) && kLpr <= 16, "blocks of a wave");
 };
 
-// Stages rows 32 i2 .. 32 i2 + 31 of a wave's sums, unscaled by 2^sh.
-template <int I2, int MBLK, int NBLK>
-__device__ __forceinline__ void stage_sums(uint8_t* ep, const v4f (&acc)[MBLK][NBLK], int sh) {
-    constexpr int kRow = NBLK * 64 + 16;
-    const int lane = threadIdx.x & 63, frow = lane & 15, fg = lane >> 4;
+// 16-byte chunk c of staging row r (r < 16) is stored at chunk c ^ stage_swz(r): a
+// write has lanes on 16 rows and two neighbouring chunks, a read lanes on two rows
+// four apart and every second chunk, and either way the 16 lanes of a phase (see
+// fp8lin_gemm.hip) hit 16 distinct groups of banks.
+template <int ROW>
+__device__ __forceinline__ int stage_swz(int r) {
+    return (((r >> 2) & 1) | ((r & 3) << 1) | (((r >> 2) ^ (r >> 3)) & 1) << 3) & (ROW / 16 - 1);
+}
+
+// Stages rows 16 i .. 16 i + 15 of a wave's sums, unscaled by 2^sh.
+template <int ROW, int NBLK>
+__device__ __forceinline__ void stage_sums(uint8_t* ep, const v4f (&acc)[NBLK], int sh, int lane) {
+    const int frow = lane & 15, fg = lane >> 4, z = stage_swz<ROW>(frow);
 #pragma unroll
-    for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-        for (int j = 0; j < NBLK; ++j) {
-            const v4f a = acc[2 * I2 + ii][j];
-            *(float4*)(ep + (ii * 16 + frow) * kRow + (j * 16 + 4 * fg) * 4) =
-                make_float4(ldexpf(a[0], sh), ldexpf(a[1], sh), ldexpf(a[2], sh), ldexpf(a[3], sh));
-        }
+    for (int j = 0; j < NBLK; ++j) {
+        const v4f a = acc[j];
+        *(float4*)(ep + frow * ROW + (((4 * j + fg) ^ z) << 4)) =
+            make_float4(ldexpf(a[0], sh), ldexpf(a[1], sh), ldexpf(a[2], sh), ldexpf(a[3], sh));
+    }
+}
+
+// Eight staged sums of row r from chunk c on.
+template <int ROW>
+__device__ __forceinline__ void staged8(const uint8_t* ep, int r, int c, float4& a, float4& b) {
+    const int z = stage_swz<ROW>(r);
+    a = *(const float4*)(ep + r * ROW + ((c ^ z) << 4));
+    b = *(const float4*)(ep + r * ROW + (((c + 1) ^ z) << 4));
 }
 
 __device__ __forceinline__ void unpack8(uint4 w, float (&v)[8]) {
@@ -67,217 +81,234 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
     return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
 
-// Four words of four codes, one a row -> four words, one a column.
-__device__ __forceinline__ void transpose4(uint32_t (&r)[4]) {
-    const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
-    const uint32_t c = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), d = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
-    r[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
-    r[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
-    r[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
-    r[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
-}
+// Transposed codes of a tile in LDS: a column of codes is 256 bytes, one a row of the
+// tile, its 16-byte chunk q stored at chunk q ^ code_swz(column): the lanes of a
+// write (columns eight apart) and of a read (one column) hit distinct banks.
+__device__ __forceinline__ int code_swz(int col) { return (col ^ (col >> 3)) & 15; }
 
-// The codes c of NP consecutive rows (rows of them in the matrix) of eight columns
-// to the transposed copy: eight runs of NP bytes, ld apart.
+// The codes c of NP consecutive tile rows from `row` on of eight columns from `col` on.
 template <int NP>
-__device__ __forceinline__ void store_transposed(uint8_t* p, int64_t ld, const uint2 (&c)[NP], int rows) {
+__device__ __forceinline__ void put_codes(uint8_t* cs, int row, int col, const uint2 (&c)[NP]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        uint32_t t[(NP + 3) / 4][4];
+        uint32_t t[4];
 #pragma unroll
-        for (int g = 0; g < (NP + 3) / 4; ++g) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t[g][i] = 4 * g + i < NP ? (h ? c[(4 * g + i) % NP].y : c[(4 * g + i) % NP].x) : 0u;
-            transpose4(t[g]);
-        }
+        for (int i = 0; i < 4; ++i) t[i] = i < NP ? (h ? c[i % NP].y : c[i % NP].x) : 0u;
+        transpose4(t);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint8_t* q = p + (4 * h + i) * ld;
-            if (NP == 8 && rows >= 8) {
-                st8_any(q, t[0][i], t[(NP + 3) / 4 - 1][i]);
-            } else if (NP == 4 && rows >= 4) {
-                *(u32_any*)q = t[0][i];
-            } else {
-#pragma unroll
-                for (int r = 0; r < NP; ++r)
-                    if (r < rows) q[r] = (uint8_t)(t[r >> 2][i] >> (8 * (r & 3)));
-            }
+            const int n = col + 4 * h + i;
+            uint8_t* p = cs + n * 256 + (((row >> 4) ^ code_swz(n)) << 4) + (row & 15);
+            if (NP == 4) *(uint32_t*)p = t[i];
+            else if (NP == 2) *(uint16_t*)p = (uint16_t)t[i];
+            else *p = (uint8_t)t[i];
         }
     }
 }
 
-// One half (32 rows) of a wave's epilogue where every lane's eight columns are
-// all in the matrix (active) or all outside and the output is bf16.  zb, kb, ob, ..:
-// the wave's first element in each tensor (uniform), so that the lanes' offsets are
-// 32-bit.  rows: rows of the wave in the matrix (> 0).  What is read from memory is
-// under way before the sums are staged.
-template <int MODE, int ACT, int I2, int MBLK, int NBLK>
-__device__ __forceinline__ void half_epilogue(const Epi& e, uint8_t* ep, const v4f (&acc)[MBLK][NBLK], int64_t m0, int64_t n0,
-                                              int rows, bool active, int sh, int bq, const float (&ba)[8],
-                                              const float (&bu)[8], float (&sa)[8], float (&sb)[8], uint32_t& mag) {
+// Columns 0 .. cols - 1 of those codes to the transposed copy at q (the tile's first
+// column and row), rows of them in the matrix.
+__device__ __forceinline__ void store_codes(const uint8_t* cs, uint8_t* q, int64_t ld, int cols, int rows, int tid) {
+    const int c16 = tid & 15;
+    for (int n = tid >> 4; n < cols; n += kMainThreads / 16) {
+        const uint4 v = *(const uint4*)(cs + n * 256 + ((c16 ^ code_swz(n)) << 4));
+        uint8_t* p = q + n * ld + c16 * 16;
+        const int k = rows - c16 * 16;
+        if (k >= 16) {
+            st_stream(p, v);
+        } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < k) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+        }
+    }
+}
+
+// What a wave's epilogue needs beside the sums.
+template <int MODE, int NBLK>
+struct EpiWave {
+    static constexpr int kNp = EpiGeo<MODE, NBLK>::kNp;
+    int lane;
+    uint8_t *ep, *cs;        // 16 staging rows of its own; the tile's transposed codes
+    int64_t m0, n0;          // its first row and column of the output (uniform)
+    int rows;                // its rows in the matrix
+    int row0, col0;          // its first row and column of the tile's output
+    bool active;             // this lane's eight columns are in the matrix
+    int sh, bq;
+    float ba[8], bu[8];      // bias
+    float sa[8], sb[8];      // column sums
+    uint32_t mag;            // largest output (bf16 pattern)
+};
+
+// What the p-th of a lane's rows among rows 16 i .. 16 i + 15 needs from memory (bf16).
+template <int MODE, int NBLK>
+__device__ __forceinline__ void epi_load(const Epi& e, const EpiWave<MODE, NBLK>& w, int i, int p, uint4& x, uint4& u) {
+    using G = EpiGeo<MODE, NBLK>;
+    if (epi_fwd(MODE) && !(MODE == kEpiAct && e.res)) return;
+    const int oct = w.lane & (G::kLpr - 1), r0 = w.lane / G::kLpr * G::kNp;
+    const uint32_t ld = (uint32_t)(MODE == kEpiAct ? e.ldres : e.ldz);
+    const uint16_t* src = (MODE == kEpiAct ? (const uint16_t*)e.res : e.z) + w.m0 * ld + w.n0;
+    const uint32_t at = (uint32_t)min(16 * i + r0 + p, w.rows - 1) * ld + 8 * oct;
+    x = ld_stream(src + at);
+    if (MODE == kEpiGluBwd) u = ld_stream(src + e.N + at);
+}
+
+// Rows 16 i .. 16 i + 15 of a wave, where every lane's eight columns are all in
+// the matrix or all outside and the output is bf16.  The lanes' offsets from the wave's
+// first element of a tensor are 32-bit.  pre, pre2: epi_load of each row; with MORE those
+// of the next sixteen rows take their place as they are used.
+template <int MODE, int ACT, bool MORE, int NBLK>
+__device__ __forceinline__ void epi_rows(const Epi& e, EpiWave<MODE, NBLK>& w, const v4f (&acc)[NBLK], int i,
+                                         uint4 (&pre)[EpiGeo<MODE, NBLK>::kNp],
+                                         uint4 (&pre2)[EpiGeo<MODE, NBLK>::kNp]) {
     using G = EpiGeo<MODE, NBLK>;
     constexpr bool kPair = G::kPair, kTwo = MODE == kEpiGluBwd;
     constexpr int kNp = G::kNp, kFmt = epi_fwd(MODE) ? FP8_E4M3 : FP8_E5M2;
-    const int lane = threadIdx.x & 63, oct = lane & (G::kLpr - 1), r0 = lane / G::kLpr * kNp;
+    const int oct = w.lane & (G::kLpr - 1), r0 = w.lane / G::kLpr * kNp;
     const uint32_t col = 8 * oct;
-    uint4 pre[kNp], pre2[kTwo ? kNp : 1];
+    stage_sums<G::kRow>(w.ep, acc, w.sh, w.lane);
+    if (!w.active) return;
+    const int chunk = kPair ? (oct >> 1) * 8 + (oct & 1) * 2 : oct * 2;  // of the first sums; a pair's others 4 on
     const bool res = MODE == kEpiAct && e.res;
-    if (active && (!epi_fwd(MODE) || res)) {
-        const uint16_t* src = MODE == kEpiAct ? (const uint16_t*)e.res : e.z;
-        const uint32_t ld = (uint32_t)(MODE == kEpiAct ? e.ldres : e.ldz);
-        src += m0 * ld + n0;
-#pragma unroll
-        for (int p = 0; p < kNp; ++p) {
-            const uint32_t at = (uint32_t)min(32 * I2 + r0 + p, rows - 1) * ld + col;
-            pre[p] = ld16_any(src + at);
-            if (kTwo) pre2[p] = ld16_any(src + e.N + at);
-        }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    stage_sums<I2>(ep, acc, sh);
-    if (!active) return;
-    const uint8_t* src = ep + r0 * G::kRow + (kPair ? (oct >> 1) * 128 + (oct & 1) * 32 : oct * 32);
-    float4 nx[kPair ? 4 : 2];
+    uint16_t* ob = (uint16_t*)e.out + w.m0 * e.ldo + w.n0;
+    uint16_t* kb = e.keep + w.m0 * e.ldkeep + w.n0;
+    uint8_t* qb = e.q + w.m0 * e.ldq + w.n0;
+    uint2 c8[kNp];
+    float4 st[kPair ? 4 : 2];  // a row's sums, read while the row before is computed
     auto fetch = [&](int p) {
-        nx[0] = *(const float4*)(src + p * G::kRow);
-        nx[1] = *(const float4*)(src + p * G::kRow + 16);
-        if (kPair) {
-            nx[kPair ? 2 : 0] = *(const float4*)(src + p * G::kRow + 64);
-            nx[kPair ? 3 : 1] = *(const float4*)(src + p * G::kRow + 80);
-        }
+        staged8<G::kRow>(w.ep, r0 + p, chunk, st[0], st[1]);
+        if (kPair) staged8<G::kRow>(w.ep, r0 + p, chunk + 4, st[kPair ? 2 : 0], st[kPair ? 3 : 1]);
     };
     fetch(0);
-    uint16_t* ob = (uint16_t*)e.out + m0 * e.ldo + n0;
-    uint16_t* kb = e.keep + m0 * e.ldkeep + n0;
-    uint8_t* qb = e.q + m0 * e.ldq + n0;
-    uint2 c8[kNp], c8b[kTwo ? kNp : 1];
 #pragma unroll
     for (int p = 0; p < kNp; ++p) {
-        float t[8] = {nx[0].x, nx[0].y, nx[0].z, nx[0].w, nx[1].x, nx[1].y, nx[1].z, nx[1].w}, u[8], x[8], y[8], f, d;
+        float t[8] = {st[0].x, st[0].y, st[0].z, st[0].w, st[1].x, st[1].y, st[1].z, st[1].w}, u[8], x[8], y[8], f, d;
         if (kPair) {
-            const float4 a = nx[kPair ? 2 : 0], b = nx[kPair ? 3 : 1];
-            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            const float4 u0 = st[kPair ? 2 : 0], u1 = st[kPair ? 3 : 1];
+            const float v[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] = v[i];
+            for (int k = 0; k < 8; ++k) u[k] = v[k];
         }
         if (p + 1 < kNp) fetch(p + 1);
-        const int r = 32 * I2 + r0 + p;
-        const bool in = r < rows;
-        uint4 w, w2 = make_uint4(0u, 0u, 0u, 0u);
+        if (!epi_fwd(MODE) || res) unpack8(pre[p], x);
+        if (kTwo) unpack8(pre2[p], u);
+        if (MORE) epi_load(e, w, i + 1, p, pre[p], pre2[p]);
+        const int r = 16 * i + r0 + p;
+        const bool in = r < w.rows;
+        uint4 o, o2 = make_uint4(0u, 0u, 0u, 0u);
         if (epi_fwd(MODE)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                t[i] += ba[i];
-                if (kPair) u[i] += bu[i];
+            for (int k = 0; k < 8; ++k) {
+                t[k] += w.ba[k];
+                if (kPair) u[k] += w.bu[k];
             }
             if (e.keep) {
-                w = pack8(t);
-                if (kPair) w2 = pack8(u);
+                o = pack8(t);
+                if (kPair) o2 = pack8(u);
                 if (in) {
-                    st_stream(kb + ((uint32_t)r * (uint32_t)e.ldkeep + col), w);
-                    if (kPair) st_stream(kb + e.N + ((uint32_t)r * (uint32_t)e.ldkeep + col), w2);
+                    st_stream(kb + ((uint32_t)r * (uint32_t)e.ldkeep + col), o);
+                    if (kPair) st_stream(kb + e.N + ((uint32_t)r * (uint32_t)e.ldkeep + col), o2);
                 }
             }
-            if (res) unpack8(pre[p], x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                act_t<ACT>(t[i], &f, &d);
-                y[i] = kPair ? f * u[i] : res ? f + x[i] : f;
+            for (int k = 0; k < 8; ++k) {
+                act_t<ACT>(t[k], &f, &d);
+                y[k] = kPair ? f * u[k] : res ? f + x[k] : f;
             }
         } else {
-            unpack8(pre[p], x);
-            if (kTwo) unpack8(pre2[kTwo ? p : 0], u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                act_t<ACT>(x[i], &f, &d);
-                if (kTwo) x[i] = t[i] * f;
-                y[i] = (kTwo ? t[i] * u[i] : t[i]) * d;
+            for (int k = 0; k < 8; ++k) {
+                act_t<ACT>(x[k], &f, &d);
+                if (kTwo) x[k] = t[k] * f;
+                y[k] = (kTwo ? t[k] * u[k] : t[k]) * d;
             }
             if (e.sums && in) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    sa[i] += y[i];
-                    if (kTwo) sb[i] += x[i];
+                for (int k = 0; k < 8; ++k) {
+                    w.sa[k] += y[k];
+                    if (kTwo) w.sb[k] += x[k];
                 }
             }
-            if (kTwo) w2 = pack8(x);
+            if (kTwo) o2 = pack8(x);
         }
-        w = pack8(y);
+        o = pack8(y);
         if (in) {
-            st_stream(ob + ((uint32_t)r * (uint32_t)e.ldo + col), w);
-            if (kTwo) st_stream(ob + e.N + ((uint32_t)r * (uint32_t)e.ldo + col), w2);
+            st_stream(ob + ((uint32_t)r * (uint32_t)e.ldo + col), o);
+            if (kTwo) st_stream(ob + e.N + ((uint32_t)r * (uint32_t)e.ldo + col), o2);
         }
         if (e.q) {
-            c8[p] = codes8<kFmt>(w, bq);
-            if (in) mag = max(mag, mag8(w));
+            c8[p] = codes8<kFmt>(o, w.bq);
+            if (in) w.mag = max(w.mag, mag8(o));
             if (in) st8_any(qb + ((uint32_t)r * (uint32_t)e.ldq + col), c8[p].x, c8[p].y);
             if (kTwo) {
-                if (in) mag = max(mag, mag8(w2));
-                c8b[kTwo ? p : 0] = codes8<kFmt>(w2, bq);
-                if (in) st8_any(qb + e.N + ((uint32_t)r * (uint32_t)e.ldq + col), c8b[kTwo ? p : 0].x, c8b[kTwo ? p : 0].y);
+                const uint2 c = codes8<kFmt>(o2, w.bq);
+                if (in) w.mag = max(w.mag, mag8(o2));
+                if (in) st8_any(qb + e.N + ((uint32_t)r * (uint32_t)e.ldq + col), c.x, c.y);
             }
         }
     }
-    if (e.q && e.qT) {
-        uint8_t* q = e.qT + n0 * e.ldqT + m0 + ((uint32_t)(8 * oct) * (uint32_t)e.ldqT + 32 * I2 + r0);
-        store_transposed<kNp>(q, e.ldqT, c8, rows - (32 * I2 + r0));
-        if constexpr (kTwo) store_transposed<kNp>(q + e.N * e.ldqT, e.ldqT, c8b, rows - (32 * I2 + r0));
-    }
+    if (!kTwo && e.qT) put_codes<kNp>(w.cs, w.row0 + 16 * i + r0, w.col0 + 8 * oct, c8);
 }
 
 // The epilogue of one wave: MBLK x NBLK blocks of 16 x 16 sums (laid out as in
 // mm256_loop) of rows m0 .., columns n0 .. of the output (with kEpiGlu NBLK / 2
-// blocks of columns of each projection); ep: 32 rows of LDS of its own; srow: its
-// row of the column sums.  ACT < 0: the activation is e.act, and the epilogue exists
-// once, in a loop (tiles cut by the matrix's last columns, any K).  Returns the
-// largest output magnitude (bf16 pattern) where codes are written.
+// blocks of columns of each projection); srow: its row of the column sums.  ACT < 0:
+// the activation is e.act, and the epilogue exists once, in a loop (tiles cut by the
+// matrix's last columns, any K).  What is read from memory is under way while the
+// sixteen rows before are computed.
 template <int MODE, int ACT, int MBLK, int NBLK>
-__device__ __forceinline__ uint32_t wave_epilogue(const Epi& e, uint8_t* ep, const v4f (&acc)[MBLK][NBLK], int64_t m0,
-                                                  int64_t n0, int64_t srow, int bq) {
+__device__ __forceinline__ void wave_epilogue(const Epi& e, EpiWave<MODE, NBLK>& w, const v4f (&acc)[MBLK][NBLK], int64_t srow) {
     using G = EpiGeo<MODE, NBLK>;
-    static_assert(MBLK == 2 || MBLK == 4, "halves of a wave");
-    const int lane = threadIdx.x & 63;
-    const int sh = -(*e.ba + *e.bb);
-    const int oct = lane & (G::kLpr - 1), r0 = lane / G::kLpr * G::kNp;
-    const int64_t n = n0 + 8 * oct;
+    constexpr int kNp = G::kNp;
+    static_assert(MBLK <= 4, "rows of a wave");
+    const int oct = w.lane & (G::kLpr - 1), r0 = w.lane / G::kLpr * kNp;
+    const int64_t n = w.n0 + 8 * oct;
     const int nv = oct < G::kOct ? (int)min((int64_t)8, e.N - n) : 0;
-    const int rows = (int)min((int64_t)(16 * MBLK), e.M - m0);
-    float sa[8] = {}, sb[8] = {};
-    uint32_t mag = 0;
+    w.sh = -(*e.ba + *e.bb);
+    w.rows = (int)min((int64_t)(16 * MBLK), e.M - w.m0);
+    w.mag = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w.ba[k] = w.bu[k] = w.sa[k] = w.sb[k] = 0.0f;
     if (ACT >= 0 && e.fast && !__any(nv > 0 && nv < 8)) {
-        float ba[8] = {}, bu[8] = {};
-        if (epi_fwd(MODE) && e.bias && nv > 0) {
-            ld_vals<8>(e.bias, n, e.bias_dt, 8, ba);
-            if (MODE == kEpiGlu) ld_vals<8>(e.bias, e.N + n, e.bias_dt, 8, bu);
+        constexpr int kA = ACT >= 0 ? ACT : 0;
+        w.active = nv > 0;
+        if (epi_fwd(MODE) && e.bias && w.active) {
+            ld_vals<8>(e.bias, n, e.bias_dt, 8, w.ba);
+            if (MODE == kEpiGlu) ld_vals<8>(e.bias, e.N + n, e.bias_dt, 8, w.bu);
         }
-        if (rows > 0) {
-            constexpr int kA = ACT >= 0 ? ACT : 0;
-            half_epilogue<MODE, kA, 0>(e, ep, acc, m0, n0, rows, nv > 0, sh, bq, ba, bu, sa, sb, mag);
-            if constexpr (MBLK == 4) half_epilogue<MODE, kA, 1>(e, ep, acc, m0, n0, rows, nv > 0, sh, bq, ba, bu, sa, sb, mag);
+        if (w.rows > 0) {
+            uint4 x[kNp], u[kNp];
+            if (w.active) {
+#pragma unroll
+                for (int p = 0; p < kNp; ++p) epi_load(e, w, 0, p, x[p], u[p]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            epi_rows<MODE, kA, (MBLK > 1)>(e, w, acc[0], 0, x, u);
+            if constexpr (MBLK > 1) epi_rows<MODE, kA, (MBLK > 2)>(e, w, acc[1], 1, x, u);
+            if constexpr (MBLK > 2) epi_rows<MODE, kA, (MBLK > 3)>(e, w, acc[2], 2, x, u);
+            if constexpr (MBLK > 3) epi_rows<MODE, kA, false>(e, w, acc[3], 3, x, u);
         }
     } else {
-        const uint8_t* src = ep + r0 * G::kRow + (G::kPair ? (oct >> 1) * 128 + (oct & 1) * 32 : oct * 32);
-        auto half = [&](int i2) {
+        const int chunk = G::kPair ? (oct >> 1) * 8 + (oct & 1) * 2 : oct * 2;
+#pragma unroll
+        for (int i = 0; i < MBLK; ++i) {
+            stage_sums<G::kRow>(w.ep, acc[i], w.sh, w.lane);
+            const int r = 16 * i + r0;
 #pragma unroll 1
-            for (int p = 0; p < G::kNp; ++p) {
-                const int r = 32 * i2 + r0 + p;
-                if (nv <= 0 || r >= rows) continue;
-                const float4 t0 = *(const float4*)(src + p * G::kRow), t1 = *(const float4*)(src + p * G::kRow + 16);
+            for (int p = 0; p < kNp; ++p) {
+                if (nv <= 0 || r + p >= w.rows) continue;
+                float4 t0, t1, u0, u1;
+                staged8<G::kRow>(w.ep, r0 + p, chunk, t0, t1);
                 float t[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w}, u[8];
                 if (G::kPair) {
-                    const float4 u0 = *(const float4*)(src + p * G::kRow + 64), u1 = *(const float4*)(src + p * G::kRow + 80);
+                    staged8<G::kRow>(w.ep, r0 + p, chunk + 4, u0, u1);
                     const float v[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
 #pragma unroll
                     for (int k = 0; k < 8; ++k) u[k] = v[k];
                 }
-                epi_row<MODE, 8>(e, m0 + r, n, nv, t, u, sa, sb);
+                epi_row<MODE, 8>(e, w.m0 + r + p, n, nv, t, u, w.sa, w.sb);
             }
-        };
-        stage_sums<0>(ep, acc, sh);
-        half(0);
-        if constexpr (MBLK == 4) {
-            stage_sums<1>(ep, acc, sh);
-            half(1);
         }
     }
     if (!epi_fwd(MODE) && e.sums) {
@@ -285,27 +316,47 @@ __device__ __forceinline__ uint32_t wave_epilogue(const Epi& e, uint8_t* ep, con
         for (int k = 0; k < 8; ++k)
 #pragma unroll
             for (int off = G::kLpr; off < 64; off <<= 1) {
-                sa[k] += __shfl_xor(sa[k], off, 64);
-                if (MODE == kEpiGluBwd) sb[k] += __shfl_xor(sb[k], off, 64);
+                w.sa[k] += __shfl_xor(w.sa[k], off, 64);
+                if (MODE == kEpiGluBwd) w.sb[k] += __shfl_xor(w.sb[k], off, 64);
             }
         if (r0 == 0 && nv > 0) {
             float* s = e.sums + srow * e.sum_cols + n;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (k < nv) {
-                    s[k] = sa[k];
-                    if (MODE == kEpiGluBwd) s[e.N + k] = sb[k];
+                    s[k] = w.sa[k];
+                    if (MODE == kEpiGluBwd) s[e.N + k] = w.sb[k];
                 }
         }
     }
-    return mag;
 }
 
 // ------------------------------------------------------------ 256-row tiles
+// The kernel's first argument, read from its segment where this is called.
+__device__ __forceinline__ Epi late_args() {
+    struct Words {
+        uint64_t w[sizeof(Epi) / 8];
+    } v;
+    static_assert(sizeof(Epi) % 8 == 0, "argument words");
+    auto p = (const __attribute__((address_space(4))) uint64_t*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("; arguments of the epilogue" : "+s"(p));
+#pragma unroll
+    for (size_t i = 0; i < sizeof(Epi) / 8; ++i) v.w[i] = p[i];
+    return __builtin_bit_cast(Epi, v);
+}
+
+// The thread's number, likewise: what the epilogue derives from it is not kept from
+// the start.
+__device__ __forceinline__ int late_thread() {
+    int t = threadIdx.x;
+    asm volatile("; thread of the epilogue" : "+v"(t));
+    return t;
+}
+
 // Grid, tiles and the narrower last round as gemm_nt_256, over the columns of B
 // (kEpiGlu: of both matrices, in blocks of 16 in turn).
 template <int MODE, int ACT, int TN>
-__device__ __forceinline__ void ffn_tile(uint8_t* smem, int bid, int nb, const Epi& e, int tiles_m, int tiles_n, int col0) {
+__device__ __forceinline__ void ffn_tile(uint8_t* smem, int bid, int nb, const Epi& args, int tiles_m, int tiles_n, int col0) {
     constexpr bool kPair = MODE == kEpiGlu;
     const int w = threadIdx.x >> 6;
     const int g = __builtin_amdgcn_readfirstlane(w >> 2), sq = __builtin_amdgcn_readfirstlane(w & 3);
@@ -314,24 +365,42 @@ __device__ __forceinline__ void ffn_tile(uint8_t* smem, int bid, int nb, const E
     const int m0 = tm * kBM, n0 = col0 + tn * TN;
     const int wr0 = (sq >> 1) * 128 + g * 64, wc0 = (sq & 1) * (TN / 2);
     v4f acc[4][TN / 32];
-    mm256_loop<epi_fa(MODE), FP8_E4M3, TN, kPair>(smem, e.A, e.B, (int)e.M, (int)e.N, (int)e.K, m0, n0, acc);
+    mm256_loop<epi_fa(MODE), FP8_E4M3, TN, kPair>(smem, args.A, args.B, (int)args.M, (int)args.N, (int)args.K, m0, n0, acc);
+    // The epilogue's arguments are read here: held in registers through the main loop
+    // they would be spilled there.
+    const Epi e = late_args();
+    const int tid = late_thread(), lane = tid & 63;
     // The main loop's last barrier follows every read of the operand tiles, so
     // group 0 stages its sums while group 1 issues its last MFMAs.
-    static_assert(8 * 32 * (TN * 2 + 16) <= kSmemBytes - 64, "LDS budget");
-    const int bq = e.q ? clamp_bias(*e.pred) : 0;
-    const uint32_t mag = wave_epilogue<MODE, ACT, 4, TN / 32>(e, smem + w * 32 * (TN * 2 + 16), acc, m0 + wr0,
-                                                              (n0 + wc0) / (kPair ? 2 : 1), 4 * tm + wr0 / 64, bq);
-    if (e.q) {  // the workgroup's largest output for the exact bias
+    // LDS: the waves' staging rows, the transposed codes, the waves' maxima.
+    constexpr int kEpWave = 16 * EpiGeo<MODE, TN / 32>::kRow, kCols = kPair ? TN / 2 : TN;
+    static_assert(8 * kEpWave + kCols * 256 + 64 <= kSmemBytes && 8 * kEpWave % 16 == 0, "LDS budget");
+    EpiWave<MODE, TN / 32> wv;
+    wv.lane = lane;
+    wv.ep = smem + w * kEpWave;
+    wv.cs = smem + 8 * kEpWave;
+    wv.row0 = wr0;
+    wv.col0 = wc0 / (kPair ? 2 : 1);
+    wv.m0 = m0 + wr0;
+    wv.n0 = n0 / (kPair ? 2 : 1) + wv.col0;
+    wv.bq = e.q ? clamp_bias(*e.pred) : 0;
+    wave_epilogue<MODE, ACT>(e, wv, acc, 4 * tm + wr0 / 64);
+    if (e.q) {
+        // the transposed codes of whole columns, and the workgroup's largest output
+        // for the exact bias
         uint32_t* wmx = (uint32_t*)(smem + kSmemBytes - 64);
-        const uint32_t wv = wave_max_u32(mag);
-        if ((threadIdx.x & 63) == 0) wmx[w] = wv;
+        const uint32_t mx = wave_max_u32(wv.mag);
+        if (lane == 0) wmx[w] = mx;
         __syncthreads();
-        if (threadIdx.x == 0) {
+        const int64_t nt = n0 / (kPair ? 2 : 1);
+        const int cols = (int)min((int64_t)kCols, e.N - nt), rows = min(kBM, (int)e.M - m0);
+        if (MODE != kEpiGluBwd && e.qT) store_codes(wv.cs, e.qT + nt * e.ldqT + m0, e.ldqT, cols, rows, tid);
+        if (tid == 0) {
             uint32_t b = 0;
 #pragma unroll
             for (int v = 0; v < kMainThreads / 64; ++v) b = max(b, wmx[v]);
             e.parts[blockIdx.x] = b;
-            if (blockIdx.x == 0) *e.used = bq;
+            if (blockIdx.x == 0) *e.used = wv.bq;
         }
     }
 }
@@ -349,7 +418,7 @@ __global__ __launch_bounds__(kMainThreads) void ffn_256(Epi e, int tiles_m, int 
 template <int MODE, int BM, int BN, int WT>
 __global__ __launch_bounds__((BM / WT) * (BN / WT) * 64) void ffn_ragged(Epi e, int tiles_m, int tiles_n) {
     constexpr bool kPair = MODE == kEpiGlu;
-    constexpr int kWaves = (BM / WT) * (BN / WT), kStage = (BM + BN) * kRk, kEpWave = 32 * (WT * 4 + 16);
+    constexpr int kWaves = (BM / WT) * (BN / WT), kStage = (BM + BN) * kRk, kEpWave = 16 * EpiGeo<MODE, WT / 16>::kRow;
     constexpr int kSmem = 2 * kStage > kWaves * kEpWave ? 2 * kStage : kWaves * kEpWave;
     __shared__ __attribute__((aligned(128))) uint8_t smem[kSmem];
     const int w = threadIdx.x >> 6;
@@ -359,8 +428,12 @@ __global__ __launch_bounds__((BM / WT) * (BN / WT) * 64) void ffn_ragged(Epi e, 
     const int wr0 = (w / (BN / WT)) * WT, wc0 = (w % (BN / WT)) * WT;
     v4f acc[WT / 16][WT / 16];
     ragged_loop<epi_fa(MODE), FP8_E4M3, BM, BN, WT, kPair>(smem, e.A, e.B, e.M, e.N, e.K, m0, n0, acc);
-    wave_epilogue<MODE, -1, WT / 16, WT / 16>(e, smem + w * kEpWave, acc, m0 + wr0, (n0 + wc0) / (kPair ? 2 : 1),
-                                              (m0 + wr0) / WT, 0);
+    EpiWave<MODE, WT / 16> wv;
+    wv.lane = threadIdx.x & 63;
+    wv.ep = smem + w * kEpWave;
+    wv.m0 = m0 + wr0;
+    wv.n0 = (n0 + wc0) / (kPair ? 2 : 1);
+    wave_epilogue<MODE, -1>(e, wv, acc, (m0 + wr0) / WT);
 }
 
 // ------------------------------------------------------------ launches

@@ -1,6 +1,7 @@
 // The choice of kernel for the feed-forward matmuls (fp8lin_ffn.h), the column sums
 // that their backward epilogues leave in parts, and the quantise of their output.
 #include "fp8lin_mm.h"
+#include "fp8lin_vals.h"
 
 namespace fp8lin {
 namespace {
@@ -28,6 +29,70 @@ __global__ __launch_bounds__(256) void sums_finish_kernel(const float* __restric
         if (!out) return;
         if (dt == FP8_DT_BF16) ((uint16_t*)out)[at] = (uint16_t)f32_to_bf16_rne(v);
         else ((float*)out)[at] = v;
+    }
+}
+
+// ------------------------------------------------------------ transposed codes
+// qT [cols, rows] = q [rows, cols]^T, bytes: a workgroup's 256 rows x 128 columns
+// through LDS, so that both sides move 16-byte pieces of whole runs.  A column is 256
+// bytes of LDS, its 16-byte chunk c at chunk c ^ swz(column).
+constexpr int kTr = 256, kTc = 128;
+
+__global__ __launch_bounds__(256) void transpose_codes_kernel(const uint8_t* __restrict__ q, int64_t ldq,
+                                                              uint8_t* __restrict__ qT, int64_t ldqT, int64_t rows,
+                                                              int64_t cols) {
+    __shared__ __attribute__((aligned(16))) uint8_t cs[kTc * kTr];
+    auto swz = [](int col) { return (col ^ (col >> 4)) & 15; };
+    const int64_t tiles_m = (rows + kTr - 1) / kTr;
+    const int64_t m0 = blockIdx.x % tiles_m * kTr, n0 = blockIdx.x / tiles_m * kTc;
+    const int mr = (int)min((int64_t)kTr, rows - m0), nc = (int)min((int64_t)kTc, cols - n0);
+    uint4 v[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {  // four rows, sixteen columns a turn
+        const int i = threadIdx.x + 256 * h, r = (i >> 3) * 4, c = (i & 7) * 16;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[h][k] = make_uint4(0u, 0u, 0u, 0u);
+            const uint8_t* p = q + (m0 + r + k) * ldq + n0 + c;
+            if (r + k < mr && c + 16 <= nc) {
+                v[h][k] = ld_stream(p);
+            } else if (r + k < mr && c < nc) {
+                uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int b = 0; b < 16; ++b) w[b >> 2] |= c + b < nc ? (uint32_t)p[b] << (8 * (b & 3)) : 0u;
+                v[h][k] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = threadIdx.x + 256 * h, r = (i >> 3) * 4, c = (i & 7) * 16;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            uint32_t t[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[k] = g == 0 ? v[h][k].x : g == 1 ? v[h][k].y : g == 2 ? v[h][k].z : v[h][k].w;
+            transpose4(t);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int n = c + 4 * g + k;
+                *(uint32_t*)(cs + n * kTr + (((r >> 4) ^ swz(n)) << 4) + (r & 15)) = t[k];
+            }
+        }
+    }
+    __syncthreads();
+    const int c16 = threadIdx.x & 15, left = mr - c16 * 16;
+    for (int n = threadIdx.x >> 4; n < nc; n += 16) {
+        const uint4 x = *(const uint4*)(cs + n * kTr + ((c16 ^ swz(n)) << 4));
+        uint8_t* p = qT + (n0 + n) * ldqT + m0 + c16 * 16;
+        if (left >= 16) {
+            st16_any(p, x);
+        } else {
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int b = 0; b < 16; ++b)
+                if (b < left) p[b] = (uint8_t)(w[b >> 2] >> (8 * (b & 3)));
+        }
     }
 }
 
@@ -84,9 +149,19 @@ int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, uint8_t* qT, 
     if (st == FP8_OK && e.sums)
         st = launch_sums_finish(e.sums, epi_sum_rows(mode, e.M, e.N, e.K), cols, e.db, cols, nullptr, e.db_dt, s);
     if (st != FP8_OK || !fq) return st;
-    if (e.q)
-        return launch_quant_check(e.out, FP8_DT_BF16, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->ws + 1, parts,
-                                  (const int32_t*)fq->ws, fq->bias, fq->amax_bits, fq->flags, fq->q, fq->ldq, qT, ldqT, s);
+    if (e.q) {
+        // The codes of both gradients of a gated block's tile, transposed, are more than
+        // the LDS beside the staging rows (or the registers) holds: from the codes, once
+        // they are final.
+        const bool apart = qT && mode == kEpiGluBwd;
+        st = launch_quant_check(e.out, FP8_DT_BF16, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->ws + 1, parts,
+                                (const int32_t*)fq->ws, fq->bias, fq->amax_bits, fq->flags, fq->q, fq->ldq,
+                                apart ? nullptr : qT, apart ? 0 : ldqT, s);
+        if (st != FP8_OK || !apart) return st;
+        hipLaunchKernelGGL(transpose_codes_kernel, dim3((unsigned)((e.M + kTr - 1) / kTr * ((cols + kTc - 1) / kTc))),
+                           dim3(256), 0, s, fq->q, fq->ldq, qT, ldqT, e.M, cols);
+        return hip_status();
+    }
     return launch_quantise(e.out, e.out_dt, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->pred, fq->bias, fq->amax_bits,
                            fq->flags, fq->q, fq->ldq, qT, ldqT, fq->ws, s);
 }

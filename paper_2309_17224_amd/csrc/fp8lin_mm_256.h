@@ -36,25 +36,22 @@ __device__ __forceinline__ void mm256_loop(uint8_t* __restrict__ smem, const uin
     // group (0: waves 0-3, 1: waves 4-7) and quadrant; wave-uniform
     const int g = __builtin_amdgcn_readfirstlane(w >> 2), sq = __builtin_amdgcn_readfirstlane(w & 3);
 
-    // Loader (group 0): wave sq fills rows [64 sq, 64 sq + 64) of the A tile
-    // and [TN/4 sq, TN/4 (sq + 1)) of the B tile, 8 rows per copy (voff[0..7]
-    // for A, voff[8..] for B); lane -> row r = (first row) + 8 i + lane / 8 and
-    // physical chunk lane % 8, which holds logical chunk (lane % 8) ^
+    // Loaders: wave sq of group 0 fills rows [64 sq, 64 sq + 64) of the A tile, of
+    // group 1 rows [TN/4 sq, TN/4 (sq + 1)) of the B tile, 8 rows per copy (voff[i] is
+    // that of the group's own operand); lane -> row r = (first row) + 8 i + lane / 8
+    // and physical chunk lane % 8, which holds logical chunk (lane % 8) ^
     // chunk_swz(r).  Rows past the matrix edge re-read the last row (their
     // outputs are not stored).  Offsets are relative to the tile's first row,
     // so they fit 32 bits for K < 2^22.
     const int lrow = lane >> 3;
-    uint32_t voff[kNc];
+    uint32_t voff[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int r = sq * 64 + i * 8 + lrow;
-        voff[i] = (uint32_t)((min(m0 + r, M - 1) - m0) * K + ((lane & 7) ^ chunk_swz(r)) * 16);
-    }
-#pragma unroll
-    for (int i = 0; i < kNbw; ++i) {
-        const int r = sq * (TN / 4) + i * 8 + lrow;
-        const int src = PAIR ? min(n0 / 2 + pair_row(r), N - 1) - n0 / 2 : min(n0 + r, N - 1) - n0;
-        voff[8 + i] = (uint32_t)(src * K + ((lane & 7) ^ chunk_swz(r)) * 16);
+        const int r = (g == 0 ? sq * 64 : sq * (TN / 4)) + i * 8 + lrow;
+        const int src = g == 0 ? min(m0 + r, M - 1) - m0
+                        : PAIR ? min(n0 / 2 + pair_row(r), N - 1) - n0 / 2
+                               : min(n0 + r, N - 1) - n0;
+        voff[i] = (uint32_t)(src * K + ((lane & 7) ^ chunk_swz(r)) * 16);
     }
     const uint8_t* baseA = A + (int64_t)m0 * K;
     const uint8_t* baseB = B + (int64_t)(PAIR ? n0 / 2 : n0) * K;
@@ -67,7 +64,7 @@ __device__ __forceinline__ void mm256_loop(uint8_t* __restrict__ smem, const uin
     auto dma = [&](int d, int stage, int k0) {  // stage: of A for d < 8, of B for d >= 8
         // a copy's eight rows lie in one block of 16: which of the pair is wave-uniform
         const bool up = PAIR && d >= 8 && ((sq * (TN / 64) + ((d - 8) >> 1)) & 1);
-        lds_dma16_s((d >= 8 ? baseB : baseA) + k0 + (up ? second : 0), voff[d],
+        lds_dma16_s((d >= 8 ? baseB : baseA) + k0 + (up ? second : 0), voff[d & 7],
                     d >= 8 ? lds_b + (d - 8) * 8 * kBK + stage * kBStage : lds_a + d * 8 * kBK + stage * kTileBytes);
     };
 

@@ -85,5 +85,15 @@ __device__ __forceinline__ void st_vals(void* base, int64_t at, int dt, int nv, 
     }
 }
 
+// Four words of four codes, one a row -> four words, one a column.
+__device__ __forceinline__ void transpose4(uint32_t (&r)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
+    const uint32_t c = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), d = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+    r[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    r[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    r[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    r[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
 }  // namespace
 }  // namespace fp8lin
