@@ -156,9 +156,9 @@ __device__ __forceinline__ void epi_load(const Epi& e, const EpiWave<MODE, NBLK>
 
 // Rows 16 i .. 16 i + 15 of a wave, where every lane's eight columns are all in
 // the matrix or all outside and the output is bf16.  The lanes' offsets from the wave's
-// first element of a tensor are 32-bit.  pre, pre2: epi_load of each row; with MORE those
-// of the next sixteen rows take their place as they are used.
-template <int MODE, int ACT, bool MORE, int NBLK>
+// first element of a tensor are 32-bit.  pre, pre2: epi_load of each row; those of the
+// rows AHEAD sixteens on take their place as they are used (LEFT sixteens are left).
+template <int MODE, int ACT, int AHEAD, int LEFT, int NBLK>
 __device__ __forceinline__ void epi_rows(const Epi& e, EpiWave<MODE, NBLK>& w, const v4f (&acc)[NBLK], int i,
                                          uint4 (&pre)[EpiGeo<MODE, NBLK>::kNp],
                                          uint4 (&pre2)[EpiGeo<MODE, NBLK>::kNp]) {
@@ -193,7 +193,7 @@ __device__ __forceinline__ void epi_rows(const Epi& e, EpiWave<MODE, NBLK>& w, c
         if (p + 1 < kNp) fetch(p + 1);
         if (!epi_fwd(MODE) || res) unpack8(pre[p], x);
         if (kTwo) unpack8(pre2[p], u);
-        if (MORE) epi_load(e, w, i + 1, p, pre[p], pre2[p]);
+        if (AHEAD < LEFT) epi_load(e, w, i + AHEAD, p, pre[p], pre2[p]);
         const int r = 16 * i + r0 + p;
         const bool in = r < w.rows;
         uint4 o, o2 = make_uint4(0u, 0u, 0u, 0u);
@@ -278,16 +278,21 @@ __device__ __forceinline__ void wave_epilogue(const Epi& e, EpiWave<MODE, NBLK>&
             if (MODE == kEpiGlu) ld_vals<8>(e.bias, e.N + n, e.bias_dt, 8, w.bu);
         }
         if (w.rows > 0) {
-            uint4 x[kNp], u[kNp];
+            // of a gated block's backward pass, with two tensors to read, sixteen rows ahead;
+            // otherwise 32 (the registers that the sums leave)
+            constexpr int kAhead = MODE == kEpiGluBwd ? 1 : 2;
+            uint4 x[kAhead][kNp], u[kAhead][kNp];
             if (w.active) {
 #pragma unroll
-                for (int p = 0; p < kNp; ++p) epi_load(e, w, 0, p, x[p], u[p]);
+                for (int i = 0; i < kAhead && i < MBLK; ++i)
+#pragma unroll
+                    for (int p = 0; p < kNp; ++p) epi_load(e, w, i, p, x[i][p], u[i][p]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            epi_rows<MODE, kA, (MBLK > 1)>(e, w, acc[0], 0, x, u);
-            if constexpr (MBLK > 1) epi_rows<MODE, kA, (MBLK > 2)>(e, w, acc[1], 1, x, u);
-            if constexpr (MBLK > 2) epi_rows<MODE, kA, (MBLK > 3)>(e, w, acc[2], 2, x, u);
-            if constexpr (MBLK > 3) epi_rows<MODE, kA, false>(e, w, acc[3], 3, x, u);
+            epi_rows<MODE, kA, kAhead, MBLK>(e, w, acc[0], 0, x[0], u[0]);
+            if constexpr (MBLK > 1) epi_rows<MODE, kA, kAhead, MBLK - 1>(e, w, acc[1], 1, x[1 % kAhead], u[1 % kAhead]);
+            if constexpr (MBLK > 2) epi_rows<MODE, kA, kAhead, MBLK - 2>(e, w, acc[2], 2, x[0], u[0]);
+            if constexpr (MBLK > 3) epi_rows<MODE, kA, kAhead, MBLK - 3>(e, w, acc[3], 3, x[1 % kAhead], u[1 % kAhead]);
         }
     } else {
         const int chunk = G::kPair ? (oct >> 1) * 8 + (oct & 1) * 2 : oct * 2;
