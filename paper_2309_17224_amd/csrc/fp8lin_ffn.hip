@@ -7,17 +7,25 @@ namespace fp8lin {
 namespace {
 
 // ------------------------------------------------------------ column sums
-// out[c] = sum of the rows of part [rows, cols], in order within each of 16
-// slices of them, then over the slices: 16 columns a workgroup.  Columns from n0
-// on go to out1.
-__global__ __launch_bounds__(256) void sums_finish_kernel(const float* __restrict__ part, int rows, int64_t cols,
-                                                          void* out0, int64_t n0, void* out1, int dt) {
-    __shared__ float red[16][17];
-    const int c = threadIdx.x & 15, s = threadIdx.x >> 4;
-    const int64_t col = (int64_t)blockIdx.x * 16 + c;
+// out[c] = sum of the rows of part [rows, cols]: 64 columns a workgroup, each of its 16
+// waves every 16th row, eight loads at a time, in order; then over the waves.  Columns
+// from n0 on go to out1.
+__global__ __launch_bounds__(1024) void sums_finish_kernel(const float* __restrict__ part, int rows, int64_t cols,
+                                                           void* out0, int64_t n0, void* out1, int dt) {
+    __shared__ float red[16][64];
+    const int c = threadIdx.x & 63, s = threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * 64 + c;
     float v = 0.0f;
-    if (col < cols)
-        for (int r = s; r < rows; r += 16) v += part[(int64_t)r * cols + col];
+    if (col < cols) {
+        const float* p = part + col;
+        for (int r0 = s; r0 < rows; r0 += 128) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = p[(int64_t)min(r0 + 16 * k, rows - 1) * cols];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v += r0 + 16 * k < rows ? x[k] : 0.0f;
+        }
+    }
     red[s][c] = v;
     __syncthreads();
     if (s == 0 && col < cols) {
@@ -115,7 +123,7 @@ int64_t epi_sum_rows(int mode, int64_t M, int64_t N, int64_t K) {
 
 int32_t launch_sums_finish(const float* part, int64_t rows, int64_t cols, void* out0, int64_t n0, void* out1, int dt,
                            hipStream_t s) {
-    hipLaunchKernelGGL(sums_finish_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(256), 0, s, part, (int)rows, cols,
+    hipLaunchKernelGGL(sums_finish_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, (int)rows, cols,
                        out0, n0, out1, dt);
     return hip_status();
 }

@@ -41,6 +41,67 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
     return s[0];
 }
 
+// Two such sums in one exchange; red: two slots for every wave.
+template <int T>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float2* red) {
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if (T == 64) return;
+    const int w = threadIdx.x >> 6;
+    __syncthreads();  // earlier sums have been read
+    if ((threadIdx.x & 63) == 0) red[w] = make_float2(a, b);
+    __syncthreads();
+    constexpr int kW = T / 64;
+    const float2* p = red + w / kW * kW;
+    float2 s[kW];
+#pragma unroll
+    for (int i = 0; i < kW; ++i) s[i] = p[i];
+#pragma unroll
+    for (int d = 1; d < kW; d *= 2)
+#pragma unroll
+        for (int i = 0; i + d < kW; i += 2 * d) s[i].x += s[i + d].x, s[i].y += s[i + d].y;
+    a = s[0].x;
+    b = s[0].y;
+}
+
+// Eight values as they lie in memory, read once (the first nv of them; the rest 0).
+template <int DT>
+struct Raw8 {
+    uint4 w[DT == FP8_DT_F32 ? 2 : 1];
+};
+
+template <int DT>
+__device__ __forceinline__ Raw8<DT> ld_raw8(const void* base, int64_t at, int nv) {
+    Raw8<DT> r;
+    if (nv >= 8) {
+#pragma unroll
+        for (int k = 0; k < (DT == FP8_DT_F32 ? 2 : 1); ++k)
+            r.w[k] = ld_stream((const char*)base + at * (DT == FP8_DT_F32 ? 4 : 2) + 16 * k);
+    } else {
+        float v[8];
+        ld_vals<8>(base, at, DT, nv, v);
+        if (DT == FP8_DT_F32) {
+            r.w[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            r.w[DT == FP8_DT_F32 ? 1 : 0] =
+                make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        } else {  // the upper halves, exact
+            r.w[0] = make_uint4(__float_as_uint(v[0]) >> 16 | (__float_as_uint(v[1]) & 0xFFFF0000u),
+                                __float_as_uint(v[2]) >> 16 | (__float_as_uint(v[3]) & 0xFFFF0000u),
+                                __float_as_uint(v[4]) >> 16 | (__float_as_uint(v[5]) & 0xFFFF0000u),
+                                __float_as_uint(v[6]) >> 16 | (__float_as_uint(v[7]) & 0xFFFF0000u));
+        }
+    }
+    return r;
+}
+
+template <int DT>
+__device__ __forceinline__ void values8(const Raw8<DT>& r, float (&v)[8]) {
+    const uint32_t w[8] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w, r.w[DT == FP8_DT_F32 ? 1 : 0].x,
+                           r.w[DT == FP8_DT_F32 ? 1 : 0].y, r.w[DT == FP8_DT_F32 ? 1 : 0].z, r.w[DT == FP8_DT_F32 ? 1 : 0].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = DT == FP8_DT_F32 ? __uint_as_float(w[i]) : i & 1 ? hi_f(w[i >> 1]) : lo_f(w[i >> 1]);
+}
+
 // One value of v rounded to type DT.
 template <int DT>
 __device__ __forceinline__ float rounded(float v) {
@@ -61,32 +122,43 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
     const int64_t row = live ? r : a.rows - 1, cols = a.cols;
     const bool in_regs = cols <= (int64_t)8 * T * CH;
     float h[CH][8];
-    auto load = [&](int64_t c, float (&v)[8]) {
-        const int nv = (int)min((int64_t)8, cols - c);
-        ld_vals<8>(a.x, row * a.ldx + c, DT, nv, v);
+    auto sum_res = [&](const Raw8<DT>& x, const Raw8<DT>& y, float (&v)[8]) {
+        values8(x, v);
         if (a.res) {
             float w[8];
-            ld_vals<8>(a.res, row * a.ldr + c, DT, nv, w);
+            values8(y, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = rounded<DT>(v[i] + w[i]);
         }
     };
+    auto load = [&](int64_t c, float (&v)[8]) {
+        const int nv = (int)min((int64_t)8, cols - c);
+        Raw8<DT> x = ld_raw8<DT>(a.x, row * a.ldx + c, nv), y{};
+        if (a.res) y = ld_raw8<DT>(a.res, row * a.ldr + c, nv);
+        sum_res(x, y, v);
+    };
     float sum = 0.0f;
     if (in_regs) {
+        Raw8<DT> x[CH], y[CH];  // every load of the row under way before the first is used
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const int64_t c = (int64_t)8 * (tid + T * k);
-            if (c < cols) {
-                load(c, h[k]);
-            } else {
+            x[k] = y[k] = Raw8<DT>{};
+            if (c < cols) x[k] = ld_raw8<DT>(a.x, row * a.ldx + c, (int)min((int64_t)8, cols - c));
+        }
+        if (a.res) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[k][i] = 0.0f;
+            for (int k = 0; k < CH; ++k) {
+                const int64_t c = (int64_t)8 * (tid + T * k);
+                if (c < cols) y[k] = ld_raw8<DT>(a.res, row * a.ldr + c, (int)min((int64_t)8, cols - c));
             }
         }
 #pragma unroll
-        for (int k = 0; k < CH; ++k)
+        for (int k = 0; k < CH; ++k) {
+            sum_res(x[k], y[k], h[k]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += h[k][i];
+        }
     } else {
         for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
             float v[8];
@@ -169,64 +241,87 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
 // too wide for that, read twice, and the column sums are colsum_kernel's.
 template <int DT, int T, int CH>
 __global__ __launch_bounds__(T < kNormBlock ? kNormBlock : T) void layernorm_bwd_kernel(NormArgs a, float* __restrict__ part) {
+    // Two eights a thread leave no registers for the next row or the gain.
+    constexpr bool kAhead = CH <= 1;
     constexpr int kBlock = T < kNormBlock ? kNormBlock : T, kCh = CH > 0 ? CH : 1;
-    __shared__ float red[2 * (kBlock / 64)];
+    __shared__ float2 red[kBlock / 64];
     const int tid = threadIdx.x % T;
     const int64_t slot = (int64_t)blockIdx.x * (kBlock / T) + threadIdx.x / T, slots = (int64_t)gridDim.x * (kBlock / T);
     const int64_t cols = a.cols;
     const float inv = 1.0f / (float)cols;
-    float g[kCh][8], sg[kCh][8], sb[kCh][8];
-#pragma unroll
-    for (int k = 0; k < kCh; ++k) {
+    float g[8] = {}, sg[kCh][8], sb[kCh][8];
+    auto gain = [&](int k) {
         const int64_t c = (int64_t)8 * (tid + T * k);
-        const int nv = (int)max((int64_t)0, min((int64_t)8, cols - c));
+        if (c < cols) ld_vals<8>(a.g, c, a.g_dt, (int)min((int64_t)8, cols - c), g);
+    };
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sg[k][i] = sb[k][i] = g[k][i] = 0.0f;
-        if (CH > 0 && nv > 0) ld_vals<8>(a.g, c, a.g_dt, nv, g[k]);
-    }
+    for (int k = 0; k < kCh; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sg[k][i] = sb[k][i] = 0.0f;
+    if (CH == 1) gain(0);
     // every thread of a block takes the same number of turns (the sums are the block's)
     const int64_t turns = (a.rows - (int64_t)blockIdx.x * (kBlock / T) + slots - 1) / slots;
-    for (int64_t turn = 0; turn < turns; ++turn) {
-        const int64_t r = slot + turn * slots;
-        const bool live = r < a.rows;
-        const int64_t row = live ? r : a.rows - 1;
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float xh[kCh][8], dy[kCh][8], c1 = 0.0f, c2 = 0.0f;
-        auto load = [&](int64_t c, float (&x)[8], float (&d)[8]) {
-            const int nv = (int)min((int64_t)8, cols - c);
-            ld_vals<8>(a.x, row * a.ldx + c, DT, nv, x);
-            ld_vals<8>(a.dy, row * a.lddy + c, DT, nv, d);
+    // what a row needs, one row ahead: while a row's sums go round the block, the next
+    // row is on its way
+    Raw8<DT> xr[kCh], dr[kCh], er[kCh];
+    float mean = 0.0f, rstd = 0.0f, mean_n = 0.0f, rstd_n = 0.0f;
+    auto row_of = [&](int64_t turn) { return min(slot + turn * slots, a.rows - 1); };
+    auto ahead = [&](int64_t turn) {
+        const int64_t row = row_of(turn);
+        mean_n = a.mean[row];
+        rstd_n = a.rstd[row];
+        if (CH == 0) return;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean) * rstd;
-        };
-        auto finish = [&](int64_t c, const float (&x)[8], const float (&d)[8], const float (&gg)[8]) {
-            if (!live || c >= cols) return;
+        for (int k = 0; k < kCh; ++k) {
+            const int64_t c = (int64_t)8 * (tid + T * k);
             const int nv = (int)min((int64_t)8, cols - c);
+            xr[k] = dr[k] = er[k] = Raw8<DT>{};
+            if (c < cols) {
+                xr[k] = ld_raw8<DT>(a.x, row * a.ldx + c, nv);
+                dr[k] = ld_raw8<DT>(a.dy, row * a.lddy + c, nv);
+                if (kAhead && a.dres) er[k] = ld_raw8<DT>(a.dres, row * a.lddr + c, nv);
+            }
+        }
+    };
+    if (kAhead) ahead(0);
+    for (int64_t turn = 0; turn < turns; ++turn) {
+        const int64_t r = slot + turn * slots, row = row_of(turn);
+        const bool live = r < a.rows;
+        if (!kAhead) ahead(turn);
+        mean = mean_n;
+        rstd = rstd_n;
+        float xh[kCh][8], dy[kCh][8], c1 = 0.0f, c2 = 0.0f;
+        Raw8<DT> e[kCh];
+        auto finish = [&](int64_t c, const float (&x)[8], const float (&d)[8], const float (&gg)[8], const Raw8<DT>& ee) {
+            if (!live || c >= cols) return;
             float y[8], w[8];
-            if (a.dres) ld_vals<8>(a.dres, r * a.lddr + c, DT, nv, w);
+            values8(ee, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 y[i] = rstd * (d[i] * gg[i] - c1 - x[i] * c2);
                 if (a.dres) y[i] += w[i];
             }
-            st_vals<8>(a.y, r * a.ldy + c, DT, nv, y);
+            st_vals<8>(a.y, r * a.ldy + c, DT, (int)min((int64_t)8, cols - c), y);
+        };
+        auto centre = [&](const Raw8<DT>& x, const Raw8<DT>& d, int nv, float (&xv)[8], float (&dv)[8]) {
+            values8(x, xv);
+            values8(d, dv);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) xv[i] = i < nv ? (xv[i] - mean) * rstd : 0.0f;
         };
         if (CH > 0) {
 #pragma unroll
             for (int k = 0; k < kCh; ++k) {
-                const int64_t c = (int64_t)8 * (tid + T * k);
-                if (c < cols) {
-                    load(c, xh[k], dy[k]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) xh[k][i] = dy[k][i] = 0.0f;
-                }
+                centre(xr[k], dr[k], (int)min((int64_t)8, cols - (int64_t)8 * (tid + T * k)), xh[k], dy[k]);
+                e[k] = er[k];
             }
+            if (kAhead && turn + 1 < turns) ahead(turn + 1);
 #pragma unroll
-            for (int k = 0; k < kCh; ++k)
+            for (int k = 0; k < kCh; ++k) {
+                if (CH > 1) gain(k);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float w = dy[k][i] * g[k][i];
+                    const float w = dy[k][i] * g[i];
                     c1 += w;
                     c2 = fmaf(w, xh[k][i], c2);
                     if (live) {
@@ -234,31 +329,44 @@ __global__ __launch_bounds__(T < kNormBlock ? kNormBlock : T) void layernorm_bwd
                         sb[k][i] += dy[k][i];
                     }
                 }
+            }
         } else {
+            if (turn + 1 < turns) ahead(turn + 1);
             for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
                 const int nv = (int)min((int64_t)8, cols - c);
                 float gg[8];
-                load(c, xh[0], dy[0]);
+                centre(ld_raw8<DT>(a.x, row * a.ldx + c, nv), ld_raw8<DT>(a.dy, row * a.lddy + c, nv), nv, xh[0], dy[0]);
                 ld_vals<8>(a.g, c, a.g_dt, nv, gg);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float w = i < nv ? dy[0][i] * gg[i] : 0.0f;
+                    const float w = dy[0][i] * gg[i];
                     c1 += w;
                     c2 = fmaf(w, xh[0][i], c2);
                 }
             }
         }
-        c1 = row_sum<T>(c1, red) * inv;
-        c2 = row_sum<T>(c2, red + kBlock / 64) * inv;
+        row_sum2<T>(c1, c2, red);
+        c1 *= inv;
+        c2 *= inv;
         if (CH > 0) {
 #pragma unroll
-            for (int k = 0; k < kCh; ++k) finish((int64_t)8 * (tid + T * k), xh[k], dy[k], g[k]);
+            for (int k = 0; k < kCh; ++k) {
+                if (CH > 1) {
+                    gain(k);
+                    const int64_t c = (int64_t)8 * (tid + T * k);
+                    if (a.dres && c < cols) e[k] = ld_raw8<DT>(a.dres, row * a.lddr + c, (int)min((int64_t)8, cols - c));
+                }
+                finish((int64_t)8 * (tid + T * k), xh[k], dy[k], g, e[k]);
+            }
         } else {
             for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
+                const int nv = (int)min((int64_t)8, cols - c);
                 float gg[8];
-                load(c, xh[0], dy[0]);
-                ld_vals<8>(a.g, c, a.g_dt, (int)min((int64_t)8, cols - c), gg);
-                finish(c, xh[0], dy[0], gg);
+                Raw8<DT> ee{};
+                centre(ld_raw8<DT>(a.x, row * a.ldx + c, nv), ld_raw8<DT>(a.dy, row * a.lddy + c, nv), nv, xh[0], dy[0]);
+                if (a.dres) ee = ld_raw8<DT>(a.dres, row * a.lddr + c, nv);
+                ld_vals<8>(a.g, c, a.g_dt, nv, gg);
+                finish(c, xh[0], dy[0], gg, ee);
             }
         }
     }
@@ -275,34 +383,44 @@ __global__ __launch_bounds__(T < kNormBlock ? kNormBlock : T) void layernorm_bwd
 }
 
 // ------------------------------------------------------------- column sums
-// A workgroup sums 512 columns over every gridDim.y-th group of kSumRows rows,
-// a wave each fourth row; its waves' sums are added in order: one row of part for
-// each blockIdx.y.  NORM: the layer norm's two sums instead, of dy xh into
-// columns [0, cols) and dy into [cols, 2 cols).
-constexpr int kSumRows = 64;
+// A workgroup sums 512 columns over `per` consecutive rows, a wave each fourth row,
+// eight rows' loads at a time; its waves' sums are added in order: one row of part for
+// each blockIdx.y.  With one group of rows in all, the result itself goes to out0, out1
+// (of type out_dt; either may be null).  NORM: the layer norm's two sums, of dy xh into
+// columns [0, cols) (out0) and dy into [cols, 2 cols) (out1).
 template <int DT, bool NORM>
-__global__ __launch_bounds__(256) void colsum_kernel(NormArgs a, float* __restrict__ part) {
-    constexpr int kNs = NORM ? 2 : 1;
+__global__ __launch_bounds__(256) void colsum_kernel(NormArgs a, int64_t per, float* __restrict__ part, void* out0,
+                                                     void* out1, int out_dt) {
+    constexpr int kNs = NORM ? 2 : 1, kDepth = NORM ? 4 : 8;
     __shared__ float red[kNs][4][512];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t c = (int64_t)blockIdx.x * 512 + 8 * lane;
     const int nv = (int)max((int64_t)0, min((int64_t)8, a.cols - c));
     float s[kNs][8] = {};
     if (nv > 0) {
-        for (int64_t r0 = (int64_t)blockIdx.y * kSumRows; r0 < a.rows; r0 += (int64_t)gridDim.y * kSumRows) {
-            const int64_t end = min(r0 + kSumRows, a.rows);
-#pragma unroll 4
-            for (int64_t r = r0 + w; r < end; r += 4) {
-                float d[8], x[8];
-                ld_vals<8>(a.dy, r * a.lddy + c, DT, nv, d);
+        const int64_t end = min(((int64_t)blockIdx.y + 1) * per, a.rows);
+        for (int64_t r0 = (int64_t)blockIdx.y * per + w; r0 < end; r0 += 4 * kDepth) {
+            Raw8<DT> d[kDepth], x[kDepth];
+#pragma unroll
+            for (int k = 0; k < kDepth; ++k) {
+                const int64_t r = min(r0 + 4 * k, a.rows - 1);
+                d[k] = ld_raw8<DT>(a.dy, r * a.lddy + c, nv);
+                if (NORM) x[k] = ld_raw8<DT>(a.x, r * a.ldx + c, nv);
+            }
+#pragma unroll
+            for (int k = 0; k < kDepth; ++k) {
+                const int64_t r = r0 + 4 * k;
+                if (r >= end) break;
+                float dv[8], xv[8];
+                values8(d[k], dv);
                 if (NORM) {
-                    ld_vals<8>(a.x, r * a.ldx + c, DT, nv, x);
+                    values8(x[k], xv);
                     const float mean = a.mean[r], rstd = a.rstd[r];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s[0][i] = fmaf(d[i], (x[i] - mean) * rstd, s[0][i]);
+                    for (int i = 0; i < 8; ++i) s[0][i] = fmaf(dv[i], (xv[i] - mean) * rstd, s[0][i]);
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s[kNs - 1][i] += d[i];
+                for (int i = 0; i < 8; ++i) s[kNs - 1][i] += dv[i];
             }
         }
     }
@@ -315,15 +433,27 @@ __global__ __launch_bounds__(256) void colsum_kernel(NormArgs a, float* __restri
         const int64_t col = (int64_t)blockIdx.x * 512 + i;
         if (col >= a.cols) break;
 #pragma unroll
-        for (int k = 0; k < kNs; ++k)
-            part[(int64_t)blockIdx.y * kNs * a.cols + k * a.cols + col] =
-                (red[k][0][i] + red[k][1][i]) + (red[k][2][i] + red[k][3][i]);
+        for (int k = 0; k < kNs; ++k) {
+            const float v = (red[k][0][i] + red[k][1][i]) + (red[k][2][i] + red[k][3][i]);
+            if (gridDim.y > 1) {
+                part[(int64_t)blockIdx.y * kNs * a.cols + k * a.cols + col] = v;
+            } else if (void* out = k ? out1 : out0) {
+                if (out_dt == FP8_DT_BF16) ((uint16_t*)out)[col] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+                else ((float*)out)[col] = v;
+            }
+        }
     }
 }
 
 // ------------------------------------------------------------- host side
 constexpr int64_t kNormWidest = 16384;  // columns a row's threads hold in the backward pass
-constexpr int64_t kSumGroups = 256;     // rows of partial column sums, at most
+
+// Rows of a group of colsum_kernel: about 1024 workgroups, groups of 16 rows (four to a
+// wave) at least.
+int64_t sum_group(int64_t rows, int64_t cols) {
+    const int64_t wide = (cols + 511) / 512, groups = std::max<int64_t>(1, std::min<int64_t>(256, 1024 / wide));
+    return std::max<int64_t>(16, (rows + groups - 1) / groups);
+}
 
 // Threads of a row in the backward pass: 8 columns each, 16 beyond 8192.
 int bwd_threads(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024; }
@@ -336,8 +466,8 @@ int64_t bwd_blocks(int64_t rows, int64_t cols) {
 }  // namespace
 
 int64_t colsum_rows(int64_t rows, int64_t cols) {
-    (void)cols;
-    return std::max<int64_t>(1, std::min<int64_t>((rows + kSumRows - 1) / kSumRows, kSumGroups));
+    const int64_t per = sum_group(rows, cols);
+    return (rows + per - 1) / per;
 }
 
 int64_t norm_sum_rows(int64_t rows, int64_t cols) {
@@ -399,10 +529,13 @@ int32_t launch_layernorm_bwd(const NormArgs& a, float* dg, float* db, float* par
     if (st != FP8_OK || !want) return st;
     if (a.cols > kNormWidest) {
         const dim3 grid((unsigned)((a.cols + 511) / 512), (unsigned)sums);
-        if (a.dt == FP8_DT_BF16) hipLaunchKernelGGL((colsum_kernel<FP8_DT_BF16, true>), grid, dim3(256), 0, s, a, part);
-        else hipLaunchKernelGGL((colsum_kernel<FP8_DT_F32, true>), grid, dim3(256), 0, s, a, part);
+        const int64_t per = sum_group(a.rows, a.cols);
+        if (a.dt == FP8_DT_BF16)
+            hipLaunchKernelGGL((colsum_kernel<FP8_DT_BF16, true>), grid, dim3(256), 0, s, a, per, part, dg, db, FP8_DT_F32);
+        else
+            hipLaunchKernelGGL((colsum_kernel<FP8_DT_F32, true>), grid, dim3(256), 0, s, a, per, part, dg, db, FP8_DT_F32);
         st = hip_status();
-        if (st != FP8_OK) return st;
+        if (st != FP8_OK || sums == 1) return st;
     }
     return launch_sums_finish(part, sums, 2 * a.cols, dg, a.cols, db, FP8_DT_F32, s);
 }
@@ -416,10 +549,14 @@ int32_t launch_colsum(const void* x, int dt, int64_t rows, int64_t cols, int64_t
     a.lddy = ldx;
     const int64_t sums = colsum_rows(rows, cols);
     const dim3 grid((unsigned)((cols + 511) / 512), (unsigned)sums);
-    if (dt == FP8_DT_BF16) hipLaunchKernelGGL((colsum_kernel<FP8_DT_BF16, false>), grid, dim3(256), 0, s, a, part);
-    else hipLaunchKernelGGL((colsum_kernel<FP8_DT_F32, false>), grid, dim3(256), 0, s, a, part);
+    const int64_t per = sum_group(rows, cols);
+    void* none = nullptr;
+    if (dt == FP8_DT_BF16)
+        hipLaunchKernelGGL((colsum_kernel<FP8_DT_BF16, false>), grid, dim3(256), 0, s, a, per, part, out, none, out_dt);
+    else
+        hipLaunchKernelGGL((colsum_kernel<FP8_DT_F32, false>), grid, dim3(256), 0, s, a, per, part, out, none, out_dt);
     const int32_t st = hip_status();
-    if (st != FP8_OK) return st;
+    if (st != FP8_OK || sums == 1) return st;
     return launch_sums_finish(part, sums, cols, out, cols, nullptr, out_dt, s);
 }
 
