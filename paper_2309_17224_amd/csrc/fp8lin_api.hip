@@ -1,6 +1,7 @@
 // C entry points of libfp8lin.so (declared and documented in fp8lin.h).
 // Each call checks its arguments on the host, then enqueues kernels on the
 // caller's stream; nothing is allocated, kept or synchronised.
+#include <algorithm>
 #include <mutex>
 
 #include "fp8lin_internal.h"
@@ -377,7 +378,11 @@ int32_t fp8_linear_bwd_dx_bias(const uint8_t* dy8, const int32_t* bg, const uint
 
 size_t fp8_linear_quantise_ws_bytes(int64_t M, int64_t N) {
     if (M <= 0 || N <= 0 || M > kMaxDim || N > kMaxDim) return 0;
-    return (size_t)gemm_quantise_ws_words(M, N) * sizeof(uint32_t);
+    // a word for each workgroup of a matmul in small tiles that casts its output itself
+    // (the feed-forward calls; those of more workgroups leave it to the quantise)
+    constexpr int64_t kSmallTiles = 4096;
+    const int64_t blocks = ((M + 15) / 16) * ((N + 15) / 16);
+    return (size_t)std::max(gemm_quantise_ws_words(M, N), 1 + std::min(blocks, kSmallTiles)) * sizeof(uint32_t);
 }
 
 namespace {
@@ -400,7 +405,7 @@ int32_t gemm_quantise_common(const uint8_t* a, int fa, const int32_t* ba, const 
     if (!aligned(c, 2) || !aligned(ba, 4) || !aligned(bb, 4) || !aligned(ws, 4)) return FP8_EINVAL;
     if (!operands_ok(a, b, kc)) return FP8_EINVAL;
     if (ldq < cols || (qT && ldqT < rows)) return FP8_EINVAL;
-    if (ws_bytes < fp8_linear_quantise_ws_bytes(rows, cols)) return FP8_EINVAL;
+    if (ws_bytes < (size_t)gemm_quantise_ws_words(rows, cols) * sizeof(uint32_t)) return FP8_EINVAL;
     if (rows > INT32_MAX || cols > INT32_MAX) return FP8_ENOTSUP;
     return launch_gemm_nt_quantise(a, fa, ba, b, FP8_E4M3, bb, c, rows, cols, kc, fmt, margin, pred, bias,
                                    amax_bits, flags, q, ldq, qT, ldqT, (uint32_t*)ws, as_stream(stream));
@@ -614,7 +619,7 @@ int32_t epilogue_mm(int mode, Epi& e, int64_t out_cols, void* db, int32_t db_dt,
                     size_t ws_bytes, void* stream) {
     if (!sizes_ok(e.M, e.N, e.K) || !act_ok(e.act) || !dt_ok(e.out_dt)) return FP8_EINVAL;
     const bool empty = e.M == 0 || e.N == 0;
-    const int32_t st = out_quant_checks(quant, e.M, out_cols, quant ? fp8_linear_quantise_ws_bytes(e.M, out_cols) : 0);
+    const int32_t st = out_quant_checks(quant, e.M, out_cols, quant ? (size_t)gemm_quantise_ws_words(e.M, out_cols) * 4 : 0);
     if (st != FP8_OK) return st;
     if (db && (!dt_ok(db_dt) || !aligned(db, esize(db_dt)))) return FP8_EINVAL;
     if (!empty) {
@@ -640,8 +645,8 @@ int32_t epilogue_mm(int mode, Epi& e, int64_t out_cols, void* db, int32_t db_dt,
     e.db = db, e.db_dt = db_dt;
     FusedQuant fq{};
     if (quant) fq = out_quant(quant);
-    return launch_epilogue_mm(mode, e, quant ? &fq : nullptr, quant ? quant->qT : nullptr, quant ? quant->ldqT : 0,
-                              as_stream(stream));
+    return launch_epilogue_mm(mode, e, quant ? &fq : nullptr, quant ? (int64_t)(quant->ws_bytes / 4) : 0,
+                              quant ? quant->qT : nullptr, quant ? quant->ldqT : 0, as_stream(stream));
 }
 }  // namespace
 

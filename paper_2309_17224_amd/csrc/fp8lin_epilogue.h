@@ -86,11 +86,12 @@ __device__ __forceinline__ void act_of(int act, float x, float* f, float* d) {
 // Columns n .. n + W - 1 (nv of them valid) of row m: t the unscaled sums (with
 // kEpiGlu the gate's, u the up projection's).  Every output is rounded once,
 // from fp32.  The column sums of a backward epilogue are added to sa (with
-// kEpiGluBwd: the gate's, sb the up projection's).
+// kEpiGluBwd: the gate's, sb the up projection's).  y: the output before its rounding
+// (with kEpiGluBwd the gate's, x the up projection's).
 template <int MODE, int W>
 __device__ __forceinline__ void epi_row(const Epi& e, int64_t m, int64_t n, int nv, float (&t)[W], float (&u)[W],
-                                        float (&sa)[W], float (&sb)[W]) {
-    float f, d, x[W], y[W];
+                                        float (&sa)[W], float (&sb)[W], float (&y)[W], float (&x)[W]) {
+    float f, d;
     if (epi_fwd(MODE)) {
         if (e.bias) {
             ld_vals<W>(e.bias, n, e.bias_dt, nv, x);

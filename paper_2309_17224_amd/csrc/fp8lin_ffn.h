@@ -312,7 +312,8 @@ __device__ __forceinline__ void wave_epilogue(const Epi& e, EpiWave<MODE, NBLK>&
 #pragma unroll
                     for (int k = 0; k < 8; ++k) u[k] = v[k];
                 }
-                epi_row<MODE, 8>(e, w.m0 + r + p, n, nv, t, u, w.sa, w.sb);
+                float y[8], x[8];
+                epi_row<MODE, 8>(e, w.m0 + r + p, n, nv, t, u, w.sa, w.sb, y, x);
             }
         }
     }

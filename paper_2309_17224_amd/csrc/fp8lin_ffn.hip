@@ -128,22 +128,28 @@ int32_t launch_sums_finish(const float* part, int64_t rows, int64_t cols, void* 
     return hip_status();
 }
 
-int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, uint8_t* qT, int64_t ldqT, hipStream_t s) {
+int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, int64_t ws_words, uint8_t* qT, int64_t ldqT,
+                           hipStream_t s) {
     const MmRoute r = epi_route(mode, e.M, e.N, e.K);
     const int64_t cols = mode == kEpiGluBwd ? 2 * e.N : e.N;
     // 32-bit offsets within a wave's rows (64) and, for transposed codes, columns (128)
     constexpr int64_t kFar = 1 << 22;
     e.fast = e.out_dt == FP8_DT_BF16 && e.ldo <= kFar && e.ldres <= kFar && e.ldkeep <= kFar && e.ldz <= kFar;
     e.q = nullptr;
-    int parts = 0;
-    if (fq && fq->pred && r.kernel == kMm256 && e.fast && e.N % 8 == 0 && fq->ldq <= kFar && ldqT <= kFar &&
-        fq->fmt == (mode == kEpiAct || mode == kEpiGlu ? FP8_E4M3 : FP8_E5M2)) {
+    // Codes from the epilogue, with the predicted bias: where each workgroup finds a word
+    // for its largest output, in the format of the matmul that reads them.
+    int64_t parts = 0;
+    if (fq && fq->pred && e.out_dt == FP8_DT_BF16 && fq->fmt == (mode == kEpiAct || mode == kEpiGlu ? FP8_E4M3 : FP8_E5M2)) {
         const int64_t bc = epi_b_cols(mode, e.N);
-        const int tm = (int)((e.M + 255) / 256), tn = (int)((bc + 255) / 256);
-        int ndp, tw, tn2;
-        mm256_split(tm, tn, bc, ndp, tw, tn2);
-        parts = tm * (ndp + tn2);
-        if (1 + parts <= gemm_quantise_ws_words(e.M, cols)) {
+        if (r.kernel == kMmStream) {
+            parts = stream_workgroups(e.M, bc, r.mb, r.nb);
+        } else if (r.kernel == kMm256 && e.fast && e.N % 8 == 0 && fq->ldq <= kFar && ldqT <= kFar) {
+            const int tm = (int)((e.M + 255) / 256), tn = (int)((bc + 255) / 256);
+            int ndp, tw, tn2;
+            mm256_split(tm, tn, bc, ndp, tw, tn2);
+            parts = (int64_t)tm * (ndp + tn2);
+        }
+        if (parts > 0 && 1 + parts <= ws_words) {
             e.pred = fq->pred, e.used = (int32_t*)fq->ws, e.parts = fq->ws + 1;
             e.q = fq->q, e.ldq = fq->ldq, e.qT = qT, e.ldqT = ldqT;
         }
@@ -161,8 +167,8 @@ int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, uint8_t* qT, 
         // The codes of both gradients of a gated block's tile, transposed, are more than
         // the LDS beside the staging rows (or the registers) holds: from the codes, once
         // they are final.
-        const bool apart = qT && mode == kEpiGluBwd;
-        st = launch_quant_check(e.out, FP8_DT_BF16, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->ws + 1, parts,
+        const bool apart = qT && mode == kEpiGluBwd && r.kernel == kMm256;
+        st = launch_quant_check(e.out, FP8_DT_BF16, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->ws + 1, (int)parts,
                                 (const int32_t*)fq->ws, fq->bias, fq->amax_bits, fq->flags, fq->q, fq->ldq,
                                 apart ? nullptr : qT, apart ? 0 : ldqT, s);
         if (st != FP8_OK || !apart) return st;

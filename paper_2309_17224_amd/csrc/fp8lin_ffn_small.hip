@@ -16,7 +16,8 @@ struct Finish {
     static constexpr bool kPlain = false, kPair = MODE == kEpiGlu;
 
     template <int MB, int NB, int SLOTS>
-    static __device__ __forceinline__ void finish(const Epi& e, const v4f* red, int m0, int n0) {
+    static __device__ __forceinline__ void finish(const Epi& e, const v4f* red, uint32_t* wmx, int m0, int n0) {
+        constexpr int kFmt = epi_fwd(MODE) ? FP8_E4M3 : FP8_E5M2;
         const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, frow = lane & 15, fg = lane >> 4;
         const int sh = -(*e.ba + *e.bb);
         auto total = [&](int b, float (&y)[4]) {
@@ -26,6 +27,28 @@ struct Finish {
 #pragma unroll
             for (int v = 0; v < 4; ++v) y[v] = ldexpf(sum[v], sh);
         };
+        // Four codes of row m from column n on; transposed they are single bytes, of
+        // sixteen rows side by side over the lanes.
+        const int bq = e.q ? clamp_bias(*e.pred) : 0;
+        uint32_t mag = 0;
+        auto codes = [&](const float (&y)[4], int64_t m, int64_t n, int nv) {
+            const uint32_t lo = pack_bf16x2(nv > 0 ? y[0] : 0.0f, nv > 1 ? y[1] : 0.0f);
+            const uint32_t hi = pack_bf16x2(nv > 2 ? y[2] : 0.0f, nv > 3 ? y[3] : 0.0f);
+            uint32_t c = cast4_bf16<kFmt>(lo, hi, bq);
+            if (__builtin_expect(any_nan_bf16(lo, hi), 0)) {
+                const uint32_t h[4] = {lo & 0xFFFFu, lo >> 16, hi & 0xFFFFu, hi >> 16};
+                c = nan_patch<kFmt>(c, h);
+            }
+            mag = max(mag, max(max(lo & 0x7FFFu, (lo >> 16) & 0x7FFFu), max(hi & 0x7FFFu, (hi >> 16) & 0x7FFFu)));
+            uint8_t* p = e.q + m * e.ldq + n;
+            if (nv >= 4) *(u32_any*)p = c;
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                if (v < nv) {
+                    if (nv < 4) p[v] = (uint8_t)(c >> (8 * v));
+                    if (e.qT) e.qT[(n + v) * e.ldqT + m] = (uint8_t)(c >> (8 * v));
+                }
+        };
         constexpr int kStep = kPair ? 2 : 1, kPerRow = NB / kStep;
         for (int b = w; b < MB * kPerRow; b += stream_threads(MB) / 64) {
             const int mb = b / kPerRow, nb = b % kPerRow;
@@ -34,7 +57,14 @@ struct Finish {
             float t[4], u[4], sa[4] = {}, sb[4] = {};
             total(mb * NB + nb * kStep, t);
             if (kPair) total(mb * NB + nb * kStep + 1, u);
-            if (nv > 0 && m < e.M) epi_row<MODE, 4>(e, m, n, nv, t, u, sa, sb);
+            if (nv > 0 && m < e.M) {
+                float y[4], x[4];
+                epi_row<MODE, 4>(e, m, n, nv, t, u, sa, sb, y, x);
+                if (e.q) {
+                    codes(y, m, n, nv);
+                    if (MODE == kEpiGluBwd) codes(x, m, e.N + n, nv);
+                }
+            }
             if (!epi_fwd(MODE) && e.sums) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
@@ -52,6 +82,18 @@ struct Finish {
                             if (MODE == kEpiGluBwd) s[e.N + v] = sb[v];
                         }
                 }
+            }
+        }
+        if (e.q) {  // the workgroup's largest output, for the exact bias
+            const uint32_t wv = wave_max_u32(mag);
+            if (lane == 0) wmx[w] = wv;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                uint32_t b = 0;
+#pragma unroll
+                for (int v = 0; v < stream_threads(MB) / 64; ++v) b = max(b, wmx[v]);
+                e.parts[blockIdx.x] = b;
+                if (blockIdx.x == 0) *e.used = bq;
             }
         }
     }

@@ -194,8 +194,9 @@ int64_t epi_sum_rows(int mode, int64_t M, int64_t N, int64_t K);
 int64_t epi_b_cols(int mode, int64_t N);        // columns of B over all tiles: kEpiGlu: in blocks of 16 of each, filled up
 bool epi_big_tiles(int64_t M, int64_t cols);    // the kernels for any K: 256 x 128 tiles from 128 of them on, else 64 x 64
 // The matmul, the column sums and, with fq, the codes of its output (transposed to
-// qT if that is given); fq->ws: gemm_quantise_ws_words.
-int32_t launch_epilogue_mm(int mode, Epi& e, const struct FusedQuant* fq, uint8_t* qT, int64_t ldqT, hipStream_t s);
+// qT if that is given); fq->ws: ws_words >= gemm_quantise_ws_words.
+int32_t launch_epilogue_mm(int mode, Epi& e, const struct FusedQuant* fq, int64_t ws_words, uint8_t* qT, int64_t ldqT,
+                           hipStream_t s);
 void launch_ffn_small(int mode, int mb, int nb, const Epi& e, hipStream_t s);
 void launch_ffn_act(bool ragged, const Epi& e, hipStream_t s);
 void launch_ffn_glu(bool ragged, const Epi& e, hipStream_t s);

@@ -168,7 +168,7 @@ __global__ __launch_bounds__(stream_threads(MB)) void gemm_nt_stream(typename E:
                 for (int j = 0; j < kNbw; ++j) red[((slot * MB + mb0 + i) * NB + nb0 + j) * 64 + lane] = acc[i][j];
         }
         __syncthreads();
-        E::template finish<MB, NB, kSlots>(p, red, m0, n0);
+        E::template finish<MB, NB, kSlots>(p, red, wmx, m0, n0);
     } else {
         uint32_t mx = 0;
         const int bb = *p.bb;

@@ -723,6 +723,8 @@ class OutQuantise(ctypes.Structure):
                 ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t)]
 
 
+# (A call of these is a few microseconds of host work, as long as its kernel where the
+# tensors are small: what is right is looked at once, what is wrong is named apart.)
 def _gpu(t: torch.Tensor, name: str) -> int:
     """The GPU of a call's first operand: the current one, whose stream runs the call."""
     dev = t.get_device()
@@ -732,31 +734,48 @@ def _gpu(t: torch.Tensor, name: str) -> int:
 
 
 def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dev: int, dtype=_BF16) -> int:
-    """Row stride of a tensor [rows, cols] of one or of several types, with contiguous rows, on GPU dev."""
-    if t.dtype is not dtype and (not isinstance(dtype, tuple) or t.dtype not in dtype):
+    """Row stride of a tensor [rows, cols] of a type with contiguous rows, on GPU dev."""
+    if t.dtype is dtype and t.shape == (rows, cols) and t.get_device() == dev:
+        if t.is_contiguous():
+            return cols or 1
+        ld, one = t.stride()
+        if (one == 1 or cols <= 1) and (ld >= cols or rows <= 1):
+            return ld if rows > 1 else cols or 1
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or shape[0] != rows or shape[1] != cols or (cols > 1 and stride[1] != 1):
-        raise ValueError(f"{name}: expected [{rows}, {cols}] with contiguous rows, got {tuple(shape)}")
     if t.get_device() != dev:
         raise ValueError(f"{name}: on {t.device}, the call on GPU {dev}")
-    if rows > 1 and stride[0] < cols:  # an expanded tensor's rows lie on each other
-        raise ValueError(f"{name}: rows {stride[0]} elements apart, {cols} long")
-    return stride[0] if rows > 1 else max(cols, 1)
+    raise ValueError(f"{name}: expected [{rows}, {cols}] with contiguous rows that do not overlap, "
+                     f"got {tuple(t.shape)}, strides {t.stride()}")
 
 
 def _vec(t: torch.Tensor, name: str, n: int, dev: int, dtypes) -> int:
     """Address of a contiguous vector of n elements (any shape) of one of the types on GPU dev."""
+    if t.dtype in dtypes and t.numel() == n and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
     if t.dtype not in dtypes:
         raise TypeError(f"{name}: expected one of {dtypes}, got {t.dtype}")
-    if t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(t.shape)}")
     if t.get_device() != dev:
         raise ValueError(f"{name}: on {t.device}, the call on GPU {dev}")
-    return t.data_ptr()
+    raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(t.shape)}, strides {t.stride()}")
+
+
+def _float(t: torch.Tensor, name: str) -> torch.dtype:
+    dt = t.dtype
+    if dt is not _BF16 and dt is not torch.float32:
+        raise TypeError(f"{name}: expected torch.bfloat16 or torch.float32, got {dt}")
+    return dt
+
+
+def _stream_on(stream, dev: int):
+    """The stream of a call on GPU dev, the current one."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream(stream)
 
 
 _FLOATS = (torch.bfloat16, torch.float32)
+_F32 = (torch.float32,)
 _INT = (torch.int32,)
 _U8 = (torch.uint8,)
 
@@ -775,7 +794,7 @@ def _scratch(ws, nbytes: int, dev: int, device, stream):
         ws = _made(max(nbytes, 4), torch.uint8, device, stream)
     elif ws.get_device() != dev or not ws.is_contiguous():
         raise ValueError(f"ws: expected a contiguous tensor on GPU {dev}")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
 def _out_quantise(fq: FusedQuant | None, rows: int, cols: int, dev: int):
@@ -797,14 +816,22 @@ def _ref(quant):
 
 
 def _operands(a8, ba, b8, bb, names):
-    """Checks of a matmul's operands [M, K] and [N, K]: M, N, K and the GPU."""
+    """Checks of a matmul's operands [M, K] and [N, K] and their biases: their addresses, M, N, K and
+    the GPU."""
     dev = _gpu(a8, names[0])
+    u8, i32 = torch.uint8, torch.int32
+    if a8.dtype is u8 and b8.dtype is u8 and ba.dtype is i32 and bb.dtype is i32:
+        sa, sb = a8.shape, b8.shape
+        if (len(sa) == 2 and len(sb) == 2 and sa[1] == sb[1] and a8.is_contiguous() and b8.is_contiguous()
+                and ba.numel() == 1 and bb.numel() == 1 and b8.get_device() == dev and ba.get_device() == dev
+                and bb.get_device() == dev):
+            return (a8.data_ptr(), ba.data_ptr(), b8.data_ptr(), bb.data_ptr()), sa[0], sb[0], sa[1], dev
     if a8.dim() != 2 or b8.dim() != 2 or a8.shape[1] != b8.shape[1]:
         raise ValueError(f"{names[0]}, {names[2]}: expected [M, K] and [N, K], got {tuple(a8.shape)} and {tuple(b8.shape)}")
-    M, K = a8.shape
-    N = b8.shape[0]
-    return (_vec(a8, names[0], M * K, dev, _U8), _vec(ba, names[1], 1, dev, _INT), _vec(b8, names[2], N * K, dev, _U8),
-            _vec(bb, names[3], 1, dev, _INT)), M, N, K, dev
+    for t, name, n, kind in ((a8, names[0], a8.numel(), _U8), (ba, names[1], 1, _INT), (b8, names[2], b8.numel(), _U8),
+                             (bb, names[3], 1, _INT)):
+        _vec(t, name, n, dev, kind)
+    raise ValueError(f"{names}: unusable operands")
 
 
 _FWD_NAMES = ("x8", "bx", "w8t", "bw")
@@ -824,13 +851,14 @@ def fp8_linear_fwd_act(x8, bx, w8t, bw, act: int = ACT_NONE, bias=None, res=None
     ops, M, N, K, dev = _operands(x8, bx, w8t, bw, _FWD_NAMES)
     if y is None:
         y = _made((M, N), torch.bfloat16 if out_dt == DT_BF16 else torch.float32, x8.device, stream)
-    ldy = _rows(y, "y", M, N, dev, _FLOATS)
+    dt = _float(y, "y")
+    ldy = _rows(y, "y", M, N, dev, dt)
     b, b_dt = (None, 0) if bias is None else (_vec(bias, "bias", N, dev, _FLOATS), _dt(bias))
-    ldr = 0 if res is None else _rows(res, "res", M, N, dev, y.dtype)
-    ldz = 0 if z is None else _rows(z, "z", M, N, dev)
-    quant = _out_quantise(fq, M, N, dev)
-    st = lib().fp8_linear_fwd_act(*ops, b, b_dt, act, _p(res), ldr, _p(z), ldz, y.data_ptr(), _dt(y), ldy, M, N, K,
-                                  _ref(quant), _stream(stream))
+    r, ldr = (None, 0) if res is None else (res.data_ptr(), _rows(res, "res", M, N, dev, dt))
+    zp, ldz = (None, 0) if z is None else (z.data_ptr(), _rows(z, "z", M, N, dev))
+    quant = None if fq is None else _out_quantise(fq, M, N, dev)
+    st = lib().fp8_linear_fwd_act(*ops, b, b_dt, act, r, ldr, zp, ldz, y.data_ptr(), DT_BF16 if dt is _BF16 else DT_F32,
+                                  ldy, M, N, K, _ref(quant), _stream_on(stream, dev))
     if st:
         _check("fp8_linear_fwd_act", st)
     return y
@@ -849,10 +877,10 @@ def fp8_linear_fwd_glu(x8, bx, w8t, bw, act: int = ACT_SILU, bias=None, gu=None,
         a = _made((M, N), torch.bfloat16, x8.device, stream)
     lda = _rows(a, "a", M, N, dev)
     b, b_dt = (None, 0) if bias is None else (_vec(bias, "bias", N2, dev, _FLOATS), _dt(bias))
-    ldgu = 0 if gu is None else _rows(gu, "gu", M, N2, dev)
-    quant = _out_quantise(fq, M, N, dev)
-    st = lib().fp8_linear_fwd_glu(*ops, b, b_dt, act, _p(gu), ldgu, a.data_ptr(), lda, M, N, K, _ref(quant),
-                                  _stream(stream))
+    g, ldgu = (None, 0) if gu is None else (gu.data_ptr(), _rows(gu, "gu", M, N2, dev))
+    quant = None if fq is None else _out_quantise(fq, M, N, dev)
+    st = lib().fp8_linear_fwd_glu(*ops, b, b_dt, act, g, ldgu, a.data_ptr(), lda, M, N, K, _ref(quant),
+                                  _stream_on(stream, dev))
     if st:
         _check("fp8_linear_fwd_glu", st)
     return a
@@ -875,13 +903,13 @@ def _linear_bwd(name, dy8, bg, w8, bw, saved, saved_name, act, out, out_name, wi
     if out is None:
         out = _made((M, cols), torch.bfloat16, dy8.device, stream)
     ldo = _rows(out, out_name, M, cols, dev)
-    quant = _out_quantise(fq, M, cols, dev)
+    quant = None if fq is None else _out_quantise(fq, M, cols, dev)
     d, d_dt, w = None, 0, (None, 0)
     if db is not None:
         d, d_dt = _vec(db, "db", cols, dev, _FLOATS), _dt(db)
         w = _scratch(ws, gpt_bias_grad_ws_bytes(M, cols) if ws is None else 0, dev, dy8.device, stream)
     st = getattr(lib(), name)(*ops, saved.data_ptr(), lds, act, out.data_ptr(), ldo, d, d_dt, M, N, K, _ref(quant), *w,
-                              _stream(stream))
+                              _stream_on(stream, dev))
     if st:
         _check(name, st)
     return out
@@ -909,12 +937,12 @@ def gpt_bias_grad(dy, db=None, ws=None, stream=None):
     where it is made here).  Returns db."""
     dev = _gpu(dy, "dy")
     rows, cols = dy.shape
-    ld = _rows(dy, "dy", rows, cols, dev, _FLOATS)
+    ld = _rows(dy, "dy", rows, cols, dev, _float(dy, "dy"))
     if db is None:
         db = _made((cols,), torch.float32, dy.device, stream)
     d = _vec(db, "db", cols, dev, _FLOATS)
     w = _scratch(ws, gpt_bias_grad_ws_bytes(rows, cols) if ws is None else 0, dev, dy.device, stream)
-    st = lib().gpt_bias_grad(dy.data_ptr(), _dt(dy), rows, cols, ld, d, _dt(db), *w, _stream(stream))
+    st = lib().gpt_bias_grad(dy.data_ptr(), _dt(dy), rows, cols, ld, d, _dt(db), *w, _stream_on(stream, dev))
     if st:
         _check("gpt_bias_grad", st)
     return db
@@ -931,18 +959,20 @@ def gpt_layernorm_quantise(x, g, b=None, eps=1e-5, res=None, h=None, y=None, mea
     of a bf16 y, ws of gpt_layernorm_ws_bytes(rows) bytes, no qT.  Returns y."""
     dev = _gpu(x, "x")
     rows, cols = x.shape
-    ldx = _rows(x, "x", rows, cols, dev, _FLOATS)
+    dt = _float(x, "x")
+    ldx = _rows(x, "x", rows, cols, dev, dt)
     if y is None:
-        y = _made((rows, cols), x.dtype, x.device, stream)
-    ldy = _rows(y, "y", rows, cols, dev, x.dtype)
-    ldr = 0 if res is None else _rows(res, "res", rows, cols, dev, x.dtype)
-    ldh = 0 if h is None else _rows(h, "h", rows, cols, dev, x.dtype)
+        y = _made((rows, cols), dt, x.device, stream)
+    ldy = _rows(y, "y", rows, cols, dev, dt)
+    r, ldr = (None, 0) if res is None else (res.data_ptr(), _rows(res, "res", rows, cols, dev, dt))
+    hp, ldh = (None, 0) if h is None else (h.data_ptr(), _rows(h, "h", rows, cols, dev, dt))
     gp = _vec(g, "g", cols, dev, _FLOATS)
     bp = None if b is None else _vec(b, "b", cols, dev, (g.dtype,))
-    stats = [None if t is None else _vec(t, "mean, rstd", rows, dev, (torch.float32,)) for t in (mean, rstd)]
-    quant = _out_quantise(fq, rows, cols, dev)
-    st = lib().gpt_layernorm_quantise(x.data_ptr(), ldx, _p(res), ldr, _dt(x), gp, bp, _dt(g), rows, cols, float(eps),
-                                      _p(h), ldh, y.data_ptr(), ldy, *stats, _ref(quant), _stream(stream))
+    mp = None if mean is None else _vec(mean, "mean", rows, dev, _F32)
+    sp = None if rstd is None else _vec(rstd, "rstd", rows, dev, _F32)
+    quant = None if fq is None else _out_quantise(fq, rows, cols, dev)
+    st = lib().gpt_layernorm_quantise(x.data_ptr(), ldx, r, ldr, DT_BF16 if dt is _BF16 else DT_F32, gp, bp, _dt(g), rows,
+                                      cols, eps, hp, ldh, y.data_ptr(), ldy, mp, sp, _ref(quant), _stream_on(stream, dev))
     if st:
         _check("gpt_layernorm_quantise", st)
     return y
@@ -962,25 +992,25 @@ def gpt_layernorm_bwd(dy, h, g, mean, rstd, dres=None, dx=None, dg=None, db=None
     normalised.  Returns (dx, dg, db)."""
     dev = _gpu(dy, "dy")
     rows, cols = dy.shape
-    dt = dy.dtype
-    lddy = _rows(dy, "dy", rows, cols, dev, _FLOATS)
+    dt = _float(dy, "dy")
+    lddy = _rows(dy, "dy", rows, cols, dev, dt)
     ldh = _rows(h, "h", rows, cols, dev, dt)
-    lddr = 0 if dres is None else _rows(dres, "dres", rows, cols, dev, dt)
+    r, lddr = (None, 0) if dres is None else (dres.data_ptr(), _rows(dres, "dres", rows, cols, dev, dt))
     if dx is None:
         dx = _made((rows, cols), dt, dy.device, stream)
     lddx = _rows(dx, "dx", rows, cols, dev, dt)
     if want_params:
         dg = _made((cols,), torch.float32, dy.device, stream) if dg is None else dg
         db = _made((cols,), torch.float32, dy.device, stream) if db is None else db
-    f32 = (torch.float32,)
-    sums = [None if t is None else _vec(t, "dg, db", cols, dev, f32) for t in (dg, db)]
+    gp = None if dg is None else _vec(dg, "dg", cols, dev, _F32)
+    bp = None if db is None else _vec(db, "db", cols, dev, _F32)
     w = (None, 0)
     if dg is not None or db is not None:
         w = _scratch(ws, gpt_layernorm_bwd_ws_bytes(rows, cols) if ws is None else 0, dev, dy.device, stream)
-    st = lib().gpt_layernorm_bwd(dy.data_ptr(), lddy, h.data_ptr(), ldh, _p(dres), lddr, _dt(dy),
-                                 _vec(g, "g", cols, dev, _FLOATS), _dt(g), _vec(mean, "mean", rows, dev, f32),
-                                 _vec(rstd, "rstd", rows, dev, f32), rows, cols, dx.data_ptr(), lddx, *sums, *w,
-                                 _stream(stream))
+    st = lib().gpt_layernorm_bwd(dy.data_ptr(), lddy, h.data_ptr(), ldh, r, lddr, DT_BF16 if dt is _BF16 else DT_F32,
+                                 _vec(g, "g", cols, dev, _FLOATS), _dt(g), _vec(mean, "mean", rows, dev, _F32),
+                                 _vec(rstd, "rstd", rows, dev, _F32), rows, cols, dx.data_ptr(), lddx, gp, bp, *w,
+                                 _stream_on(stream, dev))
     if st:
         _check("gpt_layernorm_bwd", st)
     return dx, dg, db
