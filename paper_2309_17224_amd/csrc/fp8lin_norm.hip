@@ -445,6 +445,50 @@ __global__ __launch_bounds__(256) void colsum_kernel(NormArgs a, int64_t per, fl
     }
 }
 
+// The sums of few rows in one launch: 64 columns a workgroup, 128 rows at a time over
+// its 1024 threads, all of up to four such loads under way; then over the lanes and waves
+// in a fixed order.
+constexpr int64_t kFewRows = 1024;
+template <int DT>
+__global__ __launch_bounds__(1024) void colsum_few_kernel(const void* __restrict__ x, int64_t rows, int64_t cols,
+                                                          int64_t ldx, void* __restrict__ out, int out_dt) {
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + 8 * (lane & 7);
+    const int nv = (int)max((int64_t)0, min((int64_t)8, cols - c));
+    float s[8] = {};
+    for (int64_t r0 = 8 * w + (lane >> 3); r0 < rows; r0 += 512) {
+        Raw8<DT> v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = Raw8<DT>{};
+            if (nv > 0 && r0 + 128 * k < rows) v[k] = ld_raw8<DT>(x, (r0 + 128 * k) * ldx + c, nv);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float f[8];
+            values8(v[k], f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] += f[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int off = 8; off < 64; off <<= 1) s[i] += __shfl_xor(s[i], off, 64);
+        if (lane < 8) red[w][8 * lane + i] = s[i];
+    }
+    __syncthreads();
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    if (w == 0 && col < cols) {
+        float v = red[0][lane];
+#pragma unroll
+        for (int k = 1; k < 16; ++k) v += red[k][lane];
+        if (out_dt == FP8_DT_BF16) ((uint16_t*)out)[col] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+        else ((float*)out)[col] = v;
+    }
+}
+
 // ------------------------------------------------------------- host side
 constexpr int64_t kNormWidest = 16384;  // columns a row's threads hold in the backward pass
 
@@ -459,8 +503,11 @@ int64_t sum_group(int64_t rows, int64_t cols) {
 int bwd_threads(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024; }
 
 int64_t bwd_blocks(int64_t rows, int64_t cols) {
+    // Every block leaves a row of partial sums: as many as compute units, of few rows
+    // twice that (two rows a turn behind one another rather than three or more).
     const int t = bwd_threads(cols), per = t < kNormBlock ? kNormBlock / t : 1;
-    return std::min<int64_t>((rows + per - 1) / per, 256);
+    const int64_t all = (rows + per - 1) / per;
+    return all <= 1024 && t <= kNormBlock ? std::min<int64_t>((all + 1) / 2, 512) : std::min<int64_t>(all, 256);
 }
 
 }  // namespace
@@ -542,6 +589,14 @@ int32_t launch_layernorm_bwd(const NormArgs& a, float* dg, float* db, float* par
 
 int32_t launch_colsum(const void* x, int dt, int64_t rows, int64_t cols, int64_t ldx, void* out, int out_dt, float* part,
                       hipStream_t s) {
+    if (rows <= kFewRows) {
+        const dim3 grid((unsigned)((cols + 63) / 64));
+        if (dt == FP8_DT_BF16)
+            hipLaunchKernelGGL((colsum_few_kernel<FP8_DT_BF16>), grid, dim3(1024), 0, s, x, rows, cols, ldx, out, out_dt);
+        else
+            hipLaunchKernelGGL((colsum_few_kernel<FP8_DT_F32>), grid, dim3(1024), 0, s, x, rows, cols, ldx, out, out_dt);
+        return hip_status();
+    }
     NormArgs a{};
     a.rows = rows;
     a.cols = cols;
