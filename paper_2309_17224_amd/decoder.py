@@ -16,6 +16,9 @@ its own FP8-AMAX bias per call (Sec. 2.3 Eq. 3, Sec. 3).  The layer:
   a   = silu(gate) * up            -> E4 codes, bias   (fused quantise)
   out = h1 + a8 . Wd8
 
+With fused_glu the two lines of gu and a are one matmul (fp8_linear_fwd_glu) that
+keeps gate and up in fp32 and writes a alone.
+
 Each fused quantise casts with the previous call's bias as a prediction and
 re-casts only if the exact bias differs, so the codes are always those of the
 exact FP8-AMAX bias.  Buffers are allocated once; a call launches kernels only
@@ -85,10 +88,12 @@ class DecoderLayer:
 
     BIAS_PER = ("tensor", "sequence")
 
-    def __init__(self, cfg: LayerConfig, weights: dict, device, bias_per: str = "tensor"):
+    def __init__(self, cfg: LayerConfig, weights: dict, device, bias_per: str = "tensor", fused_glu: bool = False):
         if bias_per not in self.BIAS_PER:
             raise ValueError(f"bias_per must be one of {self.BIAS_PER}")
-        self.bias_per = bias_per
+        if fused_glu and bias_per != "tensor":
+            raise ValueError("fused_glu: the gated matmul takes one bias for all rows")
+        self.bias_per, self.fused_glu = bias_per, bool(fused_glu)
         self.cfg = c = cfg
         dev = self.dev = torch.device(device)
         R, d, nh, nkv, dh, ffn = c.rows, c.d_model, c.n_heads, c.n_kv_heads, c.d_head, c.ffn
@@ -115,8 +120,8 @@ class DecoderLayer:
         self.o = torch.empty((R, d), **bf)
         self.h1 = torch.empty((R, d), **bf)
         self.hn = _Act(R, d, F.llama_rmsnorm_ws_bytes(R), dev)
-        self.gu = torch.empty((R, 2 * ffn), **bf)
-        self.act = _Act(R, ffn, F.llama_swiglu_ws_bytes(), dev)
+        self.gu = None if fused_glu else torch.empty((R, 2 * ffn), **bf)
+        self.act = _Act(R, ffn, F.fp8_linear_quantise_ws_bytes(R, ffn) if fused_glu else F.llama_swiglu_ws_bytes(), dev)
         self.down = torch.empty((R, d), **bf)
         self.out = torch.empty((R, d), **bf)
         self.nseg = (R + c.seq_len - 1) // c.seq_len
@@ -156,9 +161,15 @@ class DecoderLayer:
             ("residual+rmsnorm+quantise mlp", "glue", 4 * R * d + 5 * R * d,
              lambda: F.llama_rmsnorm_quantise(self.o, self.g_mlp, LLAMA_EPS, res=self.H, h=self.h1,
                                               y=self.hn.x, fq=self.hn.fq())),
+        ] + ([
+            ("gate_up+swiglu+quantise", "gemm_fwd", 2 * R * 2 * ffn * d,
+             lambda: F.fp8_linear_fwd_glu(self.hn.q, self.hn.bias, self.w8t["gate_up"], self.bw("gate_up"), F.ACT_SILU,
+                                          a=self.act.x, fq=self.act.fq())),
+        ] if self.fused_glu else [
             lin("gate_up", self.hn, self.gu),
             ("swiglu+quantise", "glue", 4 * R * ffn + 3 * R * ffn,
              lambda: F.llama_swiglu_quantise(self.gu, ffn, a=self.act.x, fq=self.act.fq())),
+        ]) + [
             lin("down", self.act, self.down),
             ("residual", "glue", 6 * R * d, lambda: F.llama_residual_add(self.h1, self.down, out=self.out)),
         ]
@@ -258,7 +269,7 @@ class CachedDecoderLayer(DecoderLayer):
 
     def __init__(self, cfg: LayerConfig, weights: dict, device, n_seqs: int, max_pages: int, page_size: int = 64,
                  n_pages: int | None = None, kv_fmt: int = F.E4M3, max_rows: int | None = None, window: int = 0,
-                 cache: F.KVCache | None = None):
+                 cache: F.KVCache | None = None, fused_glu: bool = False):
         dev = torch.device(device)
         n_pages = n_seqs * max_pages if n_pages is None else n_pages
         self.cache = F.KVCache(n_pages, cfg.n_kv_heads, cfg.d_head, page_size, kv_fmt, dev) if cache is None else cache
@@ -269,7 +280,7 @@ class CachedDecoderLayer(DecoderLayer):
                                 torch.full((n_seqs, max_pages), -1, **i32))
         self.max_rows = cfg.rows if max_rows is None else max_rows
         self.window = window
-        super().__init__(cfg, weights, device)
+        super().__init__(cfg, weights, device, fused_glu=fused_glu)
         self.table = F.llama_rope_table(max_pages * self.cache.page_size, cfg.d_head, ROPE_THETA, device=dev)
         self.att.ws = F.cache_attention_workspace(cfg.rows, cfg.n_heads, self.cache, self.seqs, self.max_rows)
         self.att.x.zero_()
