@@ -571,6 +571,9 @@ int32_t llama_residual_add(const void *a, const void *b, void *out, int64_t n, v
  * the transposed codes, row stride ldqT.  ws: workspace of the call's size, 4-byte
  * aligned; scratch, distinct for calls that may run at the same time.
  * An empty output has amax 0, bias 0 and FP8_FLAG_ZERO.
+ *
+ * Sizes that the launches cannot count (rows or columns of 2^31 - 255 and more, tiles
+ * of 2^32 threads in all) are FP8_ENOTSUP.
  */
 typedef struct fp8_out_quantise {
     int32_t fmt, margin;
@@ -612,7 +615,7 @@ int32_t fp8_linear_fwd_act(const uint8_t *x8, const int32_t *bx, const uint8_t *
  * gu:     out, optional, bf16 [M, 2 N]: g and u, rounded, for fp8_linear_bwd_dx_glu
  *         (a is of the unrounded ones).
  * a:      out, bf16 [M, N].  quant: codes of a, ws of fp8_linear_quantise_ws_bytes(M, N).
- * N is at most 2^30 - 16 (FP8_ENOTSUP beyond).
+ * N is at most 2^30 - 256 (FP8_ENOTSUP beyond).
  */
 int32_t fp8_linear_fwd_glu(const uint8_t *x8, const int32_t *bx, const uint8_t *w8t, const int32_t *bw,
                            const void *bias, int32_t bias_dt, int32_t act, void *gu, int64_t ldgu, void *a, int64_t lda,
@@ -649,7 +652,7 @@ int32_t fp8_linear_bwd_dx_act(const uint8_t *dy8, const int32_t *bg, const uint8
  * db:    out, optional, [2 K]: the sums over rows, as in fp8_linear_bwd_dx_act.
  * quant: codes of dgu, ws of fp8_linear_quantise_ws_bytes(M, 2 K).
  * ws:    with db, gpt_bias_grad_ws_bytes(M, 2 K) bytes.
- * K is at most 2^30 - 16 (FP8_ENOTSUP beyond).
+ * K is at most 2^30 - 256 (FP8_ENOTSUP beyond).
  */
 int32_t fp8_linear_bwd_dx_glu(const uint8_t *dy8, const int32_t *bg, const uint8_t *w8, const int32_t *bw,
                               const void *gu, int64_t ldgu, int32_t act, void *dgu, int64_t lddgu, void *db,

@@ -633,7 +633,8 @@ int32_t epilogue_mm(int mode, Epi& e, int64_t out_cols, void* db, int32_t db_dt,
         if ((mode == kEpiActBwd || mode == kEpiGluBwd) && !rows_at(e.z, e.ldz, wide, 2)) return FP8_EINVAL;
         if (db && (!ws || !aligned(ws, 4) || ws_bytes < gpt_bias_grad_ws_bytes(e.M, out_cols))) return FP8_EINVAL;
         const bool pair = mode == kEpiGlu || mode == kEpiGluBwd;
-        if (e.M > INT32_MAX || e.N > (pair ? ((int64_t)1 << 30) - 16 : INT32_MAX)) return FP8_ENOTSUP;
+        constexpr int64_t kMost = INT32_MAX - 255;  // the last row and column of a tile are 32-bit
+        if (e.M > kMost || e.N > (pair ? ((int64_t)1 << 30) - 256 : kMost)) return FP8_ENOTSUP;
     }
     if (empty) {
         const int32_t qst = out_quant_empty(quant, stream);

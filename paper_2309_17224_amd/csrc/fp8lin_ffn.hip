@@ -1,5 +1,7 @@
 // The choice of kernel for the feed-forward matmuls (fp8lin_ffn.h), the column sums
 // that their backward epilogues leave in parts, and the quantise of their output.
+#include <algorithm>
+
 #include "fp8lin_mm.h"
 #include "fp8lin_vals.h"
 
@@ -7,36 +9,38 @@ namespace fp8lin {
 namespace {
 
 // ------------------------------------------------------------ column sums
-// out[c] = sum of the rows of part [rows, cols]: 64 columns a workgroup, each of its 16
-// waves every 16th row, eight loads at a time, in order; then over the waves.  Columns
-// from n0 on go to out1.
+// out[c] = sum of the rows of part [rows, cols]: 64 columns a workgroup at a time, each of
+// its 16 waves every 16th row, eight loads at a time, in order; then over the waves.
+// Columns from n0 on go to out1.
 __global__ __launch_bounds__(1024) void sums_finish_kernel(const float* __restrict__ part, int rows, int64_t cols,
                                                            void* out0, int64_t n0, void* out1, int dt) {
     __shared__ float red[16][64];
     const int c = threadIdx.x & 63, s = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + c;
-    float v = 0.0f;
-    if (col < cols) {
-        const float* p = part + col;
-        for (int r0 = s; r0 < rows; r0 += 128) {
-            float x[8];
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < cols; c0 += (int64_t)gridDim.x * 64) {
+        const int64_t col = c0 + c;
+        float v = 0.0f;
+        if (col < cols) {
+            const float* p = part + col;
+            for (int r0 = s; r0 < rows; r0 += 128) {
+                float x[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = p[(int64_t)min(r0 + 16 * k, rows - 1) * cols];
+                for (int k = 0; k < 8; ++k) x[k] = p[(int64_t)min(r0 + 16 * k, rows - 1) * cols];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v += r0 + 16 * k < rows ? x[k] : 0.0f;
+                for (int k = 0; k < 8; ++k) v += r0 + 16 * k < rows ? x[k] : 0.0f;
+            }
         }
-    }
-    red[s][c] = v;
-    __syncthreads();
-    if (s == 0 && col < cols) {
-        v = red[0][c];
-#pragma unroll
-        for (int k = 1; k < 16; ++k) v += red[k][c];
+        red[s][c] = v;
+        __syncthreads();
         void* out = col < n0 ? out0 : out1;
-        const int64_t at = col < n0 ? col : col - n0;
-        if (!out) return;
-        if (dt == FP8_DT_BF16) ((uint16_t*)out)[at] = (uint16_t)f32_to_bf16_rne(v);
-        else ((float*)out)[at] = v;
+        if (s == 0 && col < cols && out) {
+            v = red[0][c];
+#pragma unroll
+            for (int k = 1; k < 16; ++k) v += red[k][c];
+            const int64_t at = col < n0 ? col : col - n0;
+            if (dt == FP8_DT_BF16) ((uint16_t*)out)[at] = (uint16_t)f32_to_bf16_rne(v);
+            else ((float*)out)[at] = v;
+        }
+        __syncthreads();  // red may be written again
     }
 }
 
@@ -123,8 +127,8 @@ int64_t epi_sum_rows(int mode, int64_t M, int64_t N, int64_t K) {
 
 int32_t launch_sums_finish(const float* part, int64_t rows, int64_t cols, void* out0, int64_t n0, void* out1, int dt,
                            hipStream_t s) {
-    hipLaunchKernelGGL(sums_finish_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, (int)rows, cols,
-                       out0, n0, out1, dt);
+    hipLaunchKernelGGL(sums_finish_kernel, dim3((unsigned)std::min<int64_t>((cols + 63) / 64, kMaxSumBlocks)), dim3(1024), 0,
+                       s, part, (int)rows, cols, out0, n0, out1, dt);
     return hip_status();
 }
 
@@ -136,23 +140,27 @@ int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, int64_t ws_wo
     constexpr int64_t kFar = 1 << 22;
     e.fast = e.out_dt == FP8_DT_BF16 && e.ldo <= kFar && e.ldres <= kFar && e.ldkeep <= kFar && e.ldz <= kFar;
     e.q = nullptr;
+    const int64_t bc = epi_b_cols(mode, e.N);
+    int64_t blocks;
+    if (r.kernel == kMmStream) {
+        blocks = stream_workgroups(e.M, bc, r.mb, r.nb);
+    } else if (r.kernel == kMm256) {
+        const int tm = (int)((e.M + 255) / 256), tn = (int)((bc + 255) / 256);
+        int ndp, tw, tn2;
+        mm256_split(tm, tn, bc, ndp, tw, tn2);
+        blocks = (int64_t)tm * (ndp + tn2);
+    } else {
+        blocks = ((e.M + 255) / 256) * ((bc + 127) / 128);  // at most 128 of the smaller tiles are four times as many
+    }
+    if (blocks > UINT32_MAX / 512) return FP8_ENOTSUP;  // workgroups of up to 512 threads; a launch has fewer than 2^32
     // Codes from the epilogue, with the predicted bias: where each workgroup finds a word
     // for its largest output, in the format of the matmul that reads them.
-    int64_t parts = 0;
-    if (fq && fq->pred && e.out_dt == FP8_DT_BF16 && fq->fmt == (mode == kEpiAct || mode == kEpiGlu ? FP8_E4M3 : FP8_E5M2)) {
-        const int64_t bc = epi_b_cols(mode, e.N);
-        if (r.kernel == kMmStream) {
-            parts = stream_workgroups(e.M, bc, r.mb, r.nb);
-        } else if (r.kernel == kMm256 && e.fast && e.N % 8 == 0 && fq->ldq <= kFar && ldqT <= kFar) {
-            const int tm = (int)((e.M + 255) / 256), tn = (int)((bc + 255) / 256);
-            int ndp, tw, tn2;
-            mm256_split(tm, tn, bc, ndp, tw, tn2);
-            parts = (int64_t)tm * (ndp + tn2);
-        }
-        if (parts > 0 && 1 + parts <= ws_words) {
-            e.pred = fq->pred, e.used = (int32_t*)fq->ws, e.parts = fq->ws + 1;
-            e.q = fq->q, e.ldq = fq->ldq, e.qT = qT, e.ldqT = ldqT;
-        }
+    const bool casts = r.kernel == kMmStream ||
+                       (r.kernel == kMm256 && e.fast && e.N % 8 == 0 && fq && fq->ldq <= kFar && ldqT <= kFar);
+    if (fq && fq->pred && e.out_dt == FP8_DT_BF16 && casts && 1 + blocks <= ws_words &&
+        fq->fmt == (mode == kEpiAct || mode == kEpiGlu ? FP8_E4M3 : FP8_E5M2)) {
+        e.pred = fq->pred, e.used = (int32_t*)fq->ws, e.parts = fq->ws + 1;
+        e.q = fq->q, e.ldq = fq->ldq, e.qT = qT, e.ldqT = ldqT;
     }
     if (r.kernel == kMmStream) launch_ffn_small(mode, r.mb, r.nb, e, s);
     else if (mode == kEpiAct) launch_ffn_act(r.kernel == kMmRagged, e, s);
@@ -168,7 +176,7 @@ int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, int64_t ws_wo
         // the LDS beside the staging rows (or the registers) holds: from the codes, once
         // they are final.
         const bool apart = qT && mode == kEpiGluBwd && r.kernel == kMm256;
-        st = launch_quant_check(e.out, FP8_DT_BF16, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->ws + 1, (int)parts,
+        st = launch_quant_check(e.out, FP8_DT_BF16, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->ws + 1, (int)blocks,
                                 (const int32_t*)fq->ws, fq->bias, fq->amax_bits, fq->flags, fq->q, fq->ldq,
                                 apart ? nullptr : qT, apart ? 0 : ldqT, s);
         if (st != FP8_OK || !apart) return st;

@@ -445,7 +445,7 @@ __global__ __launch_bounds__(256) void colsum_kernel(NormArgs a, int64_t per, fl
     }
 }
 
-// The sums of few rows in one launch: 64 columns a workgroup, 128 rows at a time over
+// The sums of few rows in one launch: 64 columns a workgroup at a time, 128 rows at a time over
 // its 1024 threads, all of up to four such loads under way; then over the lanes and waves
 // in a fixed order.
 constexpr int64_t kFewRows = 1024;
@@ -454,42 +454,46 @@ __global__ __launch_bounds__(1024) void colsum_few_kernel(const void* __restrict
                                                           int64_t ldx, void* __restrict__ out, int out_dt) {
     __shared__ float red[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + 8 * (lane & 7);
-    const int nv = (int)max((int64_t)0, min((int64_t)8, cols - c));
-    float s[8] = {};
-    for (int64_t r0 = 8 * w + (lane >> 3); r0 < rows; r0 += 512) {
-        Raw8<DT> v[4];
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < cols; c0 += (int64_t)gridDim.x * 64) {
+        const int64_t c = c0 + 8 * (lane & 7);
+        const int nv = (int)max((int64_t)0, min((int64_t)8, cols - c));
+        float s[8] = {};
+        for (int64_t r0 = 8 * w + (lane >> 3); r0 < rows; r0 += 512) {
+            Raw8<DT> v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[k] = Raw8<DT>{};
-            if (nv > 0 && r0 + 128 * k < rows) v[k] = ld_raw8<DT>(x, (r0 + 128 * k) * ldx + c, nv);
+            for (int k = 0; k < 4; ++k) {
+                v[k] = Raw8<DT>{};
+                if (nv > 0 && r0 + 128 * k < rows) v[k] = ld_raw8<DT>(x, (r0 + 128 * k) * ldx + c, nv);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float f[8];
+                values8(v[k], f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] += f[i];
+            }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float f[8];
-            values8(v[k], f);
+        for (int i = 0; i < 8; ++i) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += f[i];
+            for (int off = 8; off < 64; off <<= 1) s[i] += __shfl_xor(s[i], off, 64);
+            if (lane < 8) red[w][8 * lane + i] = s[i];
         }
-    }
+        __syncthreads();
+        const int64_t col = c0 + lane;
+        if (w == 0 && col < cols) {
+            float v = red[0][lane];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-#pragma unroll
-        for (int off = 8; off < 64; off <<= 1) s[i] += __shfl_xor(s[i], off, 64);
-        if (lane < 8) red[w][8 * lane + i] = s[i];
-    }
-    __syncthreads();
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
-    if (w == 0 && col < cols) {
-        float v = red[0][lane];
-#pragma unroll
-        for (int k = 1; k < 16; ++k) v += red[k][lane];
-        if (out_dt == FP8_DT_BF16) ((uint16_t*)out)[col] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
-        else ((float*)out)[col] = v;
+            for (int k = 1; k < 16; ++k) v += red[k][lane];
+            if (out_dt == FP8_DT_BF16) ((uint16_t*)out)[col] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+            else ((float*)out)[col] = v;
+        }
+        __syncthreads();  // red may be written again
     }
 }
 
 // ------------------------------------------------------------- host side
+constexpr int64_t kMaxNormBlocks = 1 << 23;  // of a launch
 constexpr int64_t kNormWidest = 16384;  // columns a row's threads hold in the backward pass
 
 // Rows of a group of colsum_kernel: about 1024 workgroups, groups of 16 rows (four to a
@@ -525,13 +529,29 @@ int64_t norm_sum_rows(int64_t rows, int64_t cols) {
 
 int32_t launch_layernorm(const NormArgs& a, const FusedQuant* fq, hipStream_t s) {
     const bool quant = fq && fq->q;
-    int grid = 0;
+    int64_t grid = 0;
+    int32_t st = FP8_OK;
     auto go = [&](auto D, auto Tt, auto C, auto Fm) {
         constexpr int kT = decltype(Tt)::value;
-        grid = (int)((a.rows + kNormBlock / kT - 1) / (kNormBlock / kT));
-        hipLaunchKernelGGL((layernorm_kernel<decltype(D)::value, kT, decltype(C)::value, decltype(Fm)::value>), dim3(grid),
-                           dim3(kNormBlock), 0, s, a, quant ? fq->pred : nullptr, quant ? (int32_t*)fq->ws : nullptr,
-                           quant ? fq->ws + 1 : nullptr, quant ? fq->q : nullptr, quant ? fq->ldq : (int64_t)0);
+        constexpr int64_t kPer = kNormBlock / kT;
+        grid = (a.rows + kPer - 1) / kPer;
+        // (a launch has fewer than 2^32 threads)
+        for (int64_t b0 = 0; b0 < grid && st == FP8_OK; b0 += kMaxNormBlocks) {
+            const int64_t r0 = b0 * kPer, nb = std::min(grid - b0, kMaxNormBlocks), size = decltype(D)::value == FP8_DT_F32 ? 4 : 2;
+            NormArgs p = a;
+            p.rows = std::min(a.rows - r0, nb * kPer);
+            p.x = (const char*)a.x + r0 * a.ldx * size;
+            p.y = (char*)a.y + r0 * a.ldy * size;
+            if (a.res) p.res = (const char*)a.res + r0 * a.ldr * size;
+            if (a.h) p.h = (char*)a.h + r0 * a.ldh * size;
+            if (a.mean) p.mean = a.mean + r0;
+            if (a.rstd) p.rstd = a.rstd + r0;
+            hipLaunchKernelGGL((layernorm_kernel<decltype(D)::value, kT, decltype(C)::value, decltype(Fm)::value>),
+                               dim3((unsigned)nb), dim3(kNormBlock), 0, s, p, quant ? fq->pred : nullptr,
+                               quant ? (int32_t*)fq->ws : nullptr, quant ? fq->ws + 1 + b0 : nullptr,
+                               quant ? fq->q + r0 * fq->ldq : nullptr, quant ? fq->ldq : (int64_t)0);
+            st = hip_status();
+        }
     };
     auto size = [&](auto D, auto Fm) {
         if (a.cols <= 512) go(D, IC<64>{}, IC<1>{}, Fm);
@@ -543,9 +563,8 @@ int32_t launch_layernorm(const NormArgs& a, const FusedQuant* fq, hipStream_t s)
     if (a.dt == FP8_DT_F32) size(IC<FP8_DT_F32>{}, IC<-1>{});
     else if (!quant) size(IC<FP8_DT_BF16>{}, IC<-1>{});
     else with_fmt(fq->fmt, [&](auto Fm) { size(IC<FP8_DT_BF16>{}, Fm); });
-    const int32_t st = hip_status();
     if (st != FP8_OK || !quant) return st;
-    return launch_quant_check(a.y, FP8_DT_BF16, a.rows, a.cols, a.ldy, fq->fmt, fq->margin, fq->ws + 1, grid,
+    return launch_quant_check(a.y, FP8_DT_BF16, a.rows, a.cols, a.ldy, fq->fmt, fq->margin, fq->ws + 1, (int)grid,
                               (const int32_t*)fq->ws, fq->bias, fq->amax_bits, fq->flags, fq->q, fq->ldq, nullptr, 0, s);
 }
 
@@ -590,7 +609,7 @@ int32_t launch_layernorm_bwd(const NormArgs& a, float* dg, float* db, float* par
 int32_t launch_colsum(const void* x, int dt, int64_t rows, int64_t cols, int64_t ldx, void* out, int out_dt, float* part,
                       hipStream_t s) {
     if (rows <= kFewRows) {
-        const dim3 grid((unsigned)((cols + 63) / 64));
+        const dim3 grid((unsigned)std::min<int64_t>((cols + 63) / 64, kMaxSumBlocks));
         if (dt == FP8_DT_BF16)
             hipLaunchKernelGGL((colsum_few_kernel<FP8_DT_BF16>), grid, dim3(1024), 0, s, x, rows, cols, ldx, out, out_dt);
         else

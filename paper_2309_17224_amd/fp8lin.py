@@ -627,6 +627,8 @@ class FusedQuant:
         self.amax_bits, self.flags, self.qT = amax_bits, flags, qT
 
     def args(self):
+        if self.qT is not None:
+            raise ValueError("fq.qT: this call writes no transposed codes")
         return (self.fmt, self.margin, _p(self.bias_pred), _p(self.bias), _p(self.amax_bits), _p(self.flags),
                 _p(self.q), _ld(self.q), _p(self.ws), self.ws.numel() * self.ws.element_size())
 

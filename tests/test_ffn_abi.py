@@ -122,6 +122,22 @@ def test_unsupported(L):
     assert call(L, "fp8_linear_bwd_dx_glu", K=wide, ldz=2 * wide, lddz=2 * wide, db=None) == F.ENOTSUP
 
 
+def test_more_than_a_launch_counts(L):
+    """The last row and column of a tile are 32-bit, and so is the number of a launch's threads."""
+    for M in ((1 << 31) - 1, (1 << 31) - 255):
+        assert call(L, "fp8_linear_fwd_act", M=M) == F.ENOTSUP
+        assert call(L, "fp8_linear_bwd_dx_act", M=M, ws_bytes=1 << 62, db=None) == F.ENOTSUP
+    wide = (1 << 31) - 256
+    assert call(L, "fp8_linear_fwd_act", N=wide, M=1 << 20, ldy=wide, ldz=wide, ldres=wide) == F.ENOTSUP
+
+
+def test_a_fused_quantise_without_transposed_codes_refuses_them():
+    t = torch.zeros(4, 4, dtype=torch.uint8)
+    fq = F.FusedQuant(t, torch.zeros(1, dtype=torch.int32), torch.zeros(8, dtype=torch.uint8), qT=t)
+    with pytest.raises(ValueError, match="qT"):
+        fq.args()
+
+
 def test_nothing_to_do_launches_nothing(L):
     """No output and no quantise: OK whatever the pointers."""
     assert call(L, "fp8_linear_fwd_act", M=0, x8=None, y=None) == F.OK
