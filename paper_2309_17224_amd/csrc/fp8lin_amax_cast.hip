@@ -22,6 +22,7 @@
 // outputs leave as coalesced stores (whole 128-byte lines for the transpose).
 #include <type_traits>
 
+#include "fp8lin_sums.h"
 #include "fp8lin_fp8.h"
 #include "fp8lin_internal.h"
 
@@ -596,6 +597,26 @@ __global__ __launch_bounds__(kCastThreads) void quant_pass2_kernel(
                                     have_used, margin, bias, amax_bits, flags, q, ldq, qT, ldqT, tiles_c, ncast);
 }
 
+// Pass 2 in the first ncheck workgroups, column sums of 64 columns in each of the others.
+template <int DT, int FMT, bool EDGE>
+__global__ __launch_bounds__(kCastThreads) void quant_pass2_sums_kernel(
+    const void* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
+    const uint32_t* __restrict__ parts, int nparts, const int32_t* __restrict__ used, int32_t margin,
+    int32_t* __restrict__ bias, uint32_t* __restrict__ amax_bits, uint32_t* __restrict__ flags,
+    uint8_t* __restrict__ q, int64_t ldq, uint8_t* __restrict__ qT, int64_t ldqT, int64_t tiles_c, int64_t ncast,
+    int ncheck, ColumnSums sums) {
+    __shared__ __attribute__((aligned(16))) uint8_t tile[kCastCols * kCastRows];
+    __shared__ uint32_t red[kCastThreads / 64];
+    __shared__ uint32_t amax_s;
+    static_assert(sizeof(float[16][64]) <= sizeof(tile), "LDS of the sums");
+    if ((int)blockIdx.x < ncheck)
+        quant_pass2_body<DT, FMT, EDGE>(blockIdx.x, ncheck, tile, red, amax_s, x, rows, cols, ldx, parts, nparts, used, 1,
+                                        margin, bias, amax_bits, flags, q, ldq, qT, ldqT, tiles_c, ncast);
+    else
+        sum_rows64<kCastThreads / 64>(*(float(*)[16][64])tile, sums.part, sums.rows, sums.cols,
+                                      (int64_t)((int)blockIdx.x - ncheck) * 64, sums.out, sums.cols, nullptr, sums.dt);
+}
+
 // ------------------------------------------------ delayed scaling
 // The second launch of fp8_quantise_delayed (one workgroup): the tensor's amax
 // from the tile maxima of pass 1 (cast with the bias in *bias, recorded in
@@ -831,11 +852,20 @@ template <int DT, int FMT>
 void launch_quant_check_t(const void* x, int64_t rows, int64_t cols, int64_t ldx, int32_t margin,
                           const uint32_t* parts, int nparts, const int32_t* used, int32_t* bias,
                           uint32_t* amax_bits, uint32_t* flags, uint8_t* q, int64_t ldq, uint8_t* qT,
-                          int64_t ldqT, hipStream_t s) {
+                          int64_t ldqT, hipStream_t s, const ColumnSums* sums) {
     const int64_t tiles_c = (cols + kCastCols - 1) / kCastCols;
     const int64_t ncast = ((rows + kCastRows - 1) / kCastRows) * tiles_c;
     const int nb2 = (int)(ncast < kQuantPass2MaxBlocks ? ncast : kQuantPass2MaxBlocks);
     with_edge(has_edge(rows, cols), [&](auto E) {
+        if constexpr (DT == FP8_DT_BF16 && FMT == FP8_E5M2) {
+            if (sums) {
+                hipLaunchKernelGGL((quant_pass2_sums_kernel<DT, FMT, decltype(E)::value>),
+                                   dim3((unsigned)(nb2 + (sums->cols + 63) / 64)), dim3(kCastThreads), 0, s, x, rows, cols,
+                                   ldx, parts, nparts, used, margin, bias, amax_bits, flags, q, ldq, qT, ldqT, tiles_c,
+                                   ncast, nb2, *sums);
+                return;
+            }
+        }
         hipLaunchKernelGGL((quant_pass2_kernel<DT, FMT, decltype(E)::value>), dim3(nb2), dim3(kCastThreads), 0, s, x, rows,
                            cols, ldx, parts, nparts, used, 1, margin, bias, amax_bits, flags, q, ldq, qT, ldqT, tiles_c,
                            ncast);
@@ -1136,10 +1166,11 @@ int32_t launch_cast(const void* x, int dt, int64_t rows, int64_t cols, int64_t l
 int32_t launch_quant_check(const void* x, int dt, int64_t rows, int64_t cols, int64_t ldx, int fmt,
                            int32_t margin, const uint32_t* parts, int nparts, const int32_t* used,
                            int32_t* bias, uint32_t* amax_bits, uint32_t* flags, uint8_t* q, int64_t ldq,
-                           uint8_t* qT, int64_t ldqT, hipStream_t s) {
+                           uint8_t* qT, int64_t ldqT, hipStream_t s, const ColumnSums* sums) {
+    if (sums && (dt != FP8_DT_BF16 || fmt != FP8_E5M2)) return FP8_ENOTSUP;
     with_dt_fmt(dt, fmt, [&](auto D, auto F) {
         launch_quant_check_t<decltype(D)::value, decltype(F)::value>(x, rows, cols, ldx, margin, parts, nparts, used,
-                                                                     bias, amax_bits, flags, q, ldq, qT, ldqT, s);
+                                                                     bias, amax_bits, flags, q, ldq, qT, ldqT, s, sums);
     });
     return hip_status();
 }

@@ -3,44 +3,52 @@
 #include <algorithm>
 
 #include "fp8lin_mm.h"
+#include "fp8lin_sums.h"
 #include "fp8lin_vals.h"
 
 namespace fp8lin {
 namespace {
 
 // ------------------------------------------------------------ column sums
-// out[c] = sum of the rows of part [rows, cols]: 64 columns a workgroup at a time, each of
-// its 16 waves every 16th row, eight loads at a time, in order; then over the waves.
-// Columns from n0 on go to out1.
 __global__ __launch_bounds__(1024) void sums_finish_kernel(const float* __restrict__ part, int rows, int64_t cols,
                                                            void* out0, int64_t n0, void* out1, int dt) {
     __shared__ float red[16][64];
-    const int c = threadIdx.x & 63, s = threadIdx.x >> 6;
-    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < cols; c0 += (int64_t)gridDim.x * 64) {
-        const int64_t col = c0 + c;
-        float v = 0.0f;
-        if (col < cols) {
-            const float* p = part + col;
-            for (int r0 = s; r0 < rows; r0 += 128) {
-                float x[8];
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < cols; c0 += (int64_t)gridDim.x * 64)
+        sum_rows64<16>(red, part, rows, cols, c0, out0, n0, out1, dt);
+}
+
+// The same where there are many rows of few columns: 32 columns a workgroup, 32 sums of
+// every 32nd row each.  512 rows of 1536 sums (layer norm of 4096 x 768, its two launches)
+// 13.4 -> 12.0 us, of 4096 sums (4096 x 2048) 19.8 -> 18.3; 16 columns are slower, 64-byte
+// runs being half a line.
+constexpr int kFineRows = 256, kFineCols = 8192;
+__global__ __launch_bounds__(1024) void sums_finish_fine_kernel(const float* __restrict__ part, int rows, int64_t cols,
+                                                                void* out0, int64_t n0, void* out1, int dt) {
+    constexpr int C = 32, kS = 1024 / C;
+    __shared__ float red[16][C];
+    const int c = threadIdx.x % C, s = threadIdx.x / C;
+    const int64_t col = (int64_t)blockIdx.x * C + c;
+    const float* p = part + min(col, cols - 1);
+    float v = 0.0f;
+    for (int r0 = s; r0 < rows; r0 += 8 * kS) {
+        float x[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = p[(int64_t)min(r0 + 16 * k, rows - 1) * cols];
+        for (int k = 0; k < 8; ++k) x[k] = p[(int64_t)min(r0 + kS * k, rows - 1) * cols];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v += r0 + 16 * k < rows ? x[k] : 0.0f;
-            }
-        }
-        red[s][c] = v;
-        __syncthreads();
-        void* out = col < n0 ? out0 : out1;
-        if (s == 0 && col < cols && out) {
-            v = red[0][c];
+        for (int k = 0; k < 8; ++k) v += r0 + kS * k < rows ? x[k] : 0.0f;
+    }
 #pragma unroll
-            for (int k = 1; k < 16; ++k) v += red[k][c];
-            const int64_t at = col < n0 ? col : col - n0;
-            if (dt == FP8_DT_BF16) ((uint16_t*)out)[at] = (uint16_t)f32_to_bf16_rne(v);
-            else ((float*)out)[at] = v;
-        }
-        __syncthreads();  // red may be written again
+    for (int off = C; off < 64; off <<= 1) v += __shfl_xor(v, off, 64);
+    if ((threadIdx.x & 63) < C) red[threadIdx.x >> 6][c] = v;
+    __syncthreads();
+    void* out = col < n0 ? out0 : out1;
+    if (s == 0 && col < cols && out) {
+        v = red[0][c];
+#pragma unroll
+        for (int k = 1; k < 16; ++k) v += red[k][c];
+        const int64_t at = col < n0 ? col : col - n0;
+        if (dt == FP8_DT_BF16) ((uint16_t*)out)[at] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+        else ((float*)out)[at] = v;
     }
 }
 
@@ -110,6 +118,11 @@ __global__ __launch_bounds__(256) void transpose_codes_kernel(const uint8_t* __r
 
 }  // namespace
 
+// Rows of partial sums up to which the launch that checks the codes' bias adds them up too
+// (it costs a launch less and has fewer waves: 32 rows of a 509 x 2048 output 14.1 -> 13.1 us
+// the whole call, 256 rows of 16384 x 4096 154.9 -> 154.4; 512 rows 156.0 -> 159.4).
+constexpr int kJoinRows = 256;
+
 int64_t epi_b_cols(int mode, int64_t N) { return mode == kEpiGlu ? 2 * ((N + 15) / 16 * 16) : N; }
 
 bool epi_big_tiles(int64_t M, int64_t cols) { return ((M + 255) / 256) * ((cols + 127) / 128) >= 128; }
@@ -127,6 +140,11 @@ int64_t epi_sum_rows(int mode, int64_t M, int64_t N, int64_t K) {
 
 int32_t launch_sums_finish(const float* part, int64_t rows, int64_t cols, void* out0, int64_t n0, void* out1, int dt,
                            hipStream_t s) {
+    if (rows > kFineRows && cols <= kFineCols) {
+        hipLaunchKernelGGL(sums_finish_fine_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(1024), 0, s, part, (int)rows,
+                           cols, out0, n0, out1, dt);
+        return hip_status();
+    }
     hipLaunchKernelGGL(sums_finish_kernel, dim3((unsigned)std::min<int64_t>((cols + 63) / 64, kMaxSumBlocks)), dim3(1024), 0,
                        s, part, (int)rows, cols, out0, n0, out1, dt);
     return hip_status();
@@ -168,8 +186,11 @@ int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, int64_t ws_wo
     else if (mode == kEpiActBwd) launch_ffn_act_bwd(r.kernel == kMmRagged, e, s);
     else launch_ffn_glu_bwd(r.kernel == kMmRagged, e, s);
     int32_t st = hip_status();
-    if (st == FP8_OK && e.sums)
-        st = launch_sums_finish(e.sums, epi_sum_rows(mode, e.M, e.N, e.K), cols, e.db, cols, nullptr, e.db_dt, s);
+    // The column sums, with the check of the codes' bias in one launch where both are due.
+    ColumnSums sums{e.sums, e.sums ? (int)epi_sum_rows(mode, e.M, e.N, e.K) : 0, e.db_dt, cols, e.db};
+    const bool join = e.q && e.sums && sums.rows <= kJoinRows;
+    if (st == FP8_OK && e.sums && !join)
+        st = launch_sums_finish(e.sums, sums.rows, cols, e.db, cols, nullptr, e.db_dt, s);
     if (st != FP8_OK || !fq) return st;
     if (e.q) {
         // The codes of both gradients of a gated block's tile, transposed, are more than
@@ -178,7 +199,7 @@ int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, int64_t ws_wo
         const bool apart = qT && mode == kEpiGluBwd && r.kernel == kMm256;
         st = launch_quant_check(e.out, FP8_DT_BF16, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->ws + 1, (int)blocks,
                                 (const int32_t*)fq->ws, fq->bias, fq->amax_bits, fq->flags, fq->q, fq->ldq,
-                                apart ? nullptr : qT, apart ? 0 : ldqT, s);
+                                apart ? nullptr : qT, apart ? 0 : ldqT, s, join ? &sums : nullptr);
         if (st != FP8_OK || !apart) return st;
         hipLaunchKernelGGL(transpose_codes_kernel, dim3((unsigned)((e.M + kTr - 1) / kTr * ((cols + kTc - 1) / kTc))),
                            dim3(256), 0, s, fq->q, fq->ldq, qT, ldqT, e.M, cols);

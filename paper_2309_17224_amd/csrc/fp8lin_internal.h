@@ -63,11 +63,18 @@ int32_t launch_quantise_delayed(const void* x, int dt, int64_t rows, int64_t col
 
 // The exact-bias check and recast of fp8_quantise's second pass for a tensor
 // x whose per-tile maxima (nparts of them, any tiling) and the prediction its
-// codes were cast with (*used) were written by another kernel.
+// codes were cast with (*used) were written by another kernel.  sums (bf16 x and E5M2
+// only): column sums to add up in the same launch.
+struct ColumnSums {
+    const float* part;  // [rows, cols]
+    int rows, dt;
+    int64_t cols;
+    void* out;          // [cols] of type dt
+};
 int32_t launch_quant_check(const void* x, int dt, int64_t rows, int64_t cols, int64_t ldx, int fmt,
                            int32_t margin, const uint32_t* parts, int nparts, const int32_t* used,
                            int32_t* bias, uint32_t* amax_bits, uint32_t* flags, uint8_t* q, int64_t ldq,
-                           uint8_t* qT, int64_t ldqT, hipStream_t s);
+                           uint8_t* qT, int64_t ldqT, hipStream_t s, const ColumnSums* sums = nullptr);
 
 // Matmul with bf16 output C whose epilogue also casts C to format qfmt with
 // the predicted bias *pred and writes y8 (and y8t if non-null), followed by

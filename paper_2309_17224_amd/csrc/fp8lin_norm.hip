@@ -237,7 +237,8 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
 
 // ------------------------------------------------------------- backward
 // A row's threads hold its columns and, of every row they take, add their part
-// of the column sums: one row of part for each group of T threads.  CH == 0: rows
+// of the column sums: one row of part for each workgroup, its groups of T threads added in
+// order.  CH == 0: rows
 // too wide for that, read twice, and the column sums are colsum_kernel's.
 template <int DT, int T, int CH>
 __global__ __launch_bounds__(T < kNormBlock ? kNormBlock : T) void layernorm_bwd_kernel(NormArgs a, float* __restrict__ part) {
@@ -371,7 +372,22 @@ __global__ __launch_bounds__(T < kNormBlock ? kNormBlock : T) void layernorm_bwd
         }
     }
     if (CH > 0 && part) {
-        float* p = part + slot * 2 * cols;
+        constexpr int kGroups = kBlock / T;
+        if constexpr (kGroups > 1) {
+            __shared__ float sums[kGroups - 1][16][T];
+            const int grp = threadIdx.x / T;
+            if (grp > 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sums[grp - 1][i][tid] = sg[0][i], sums[grp - 1][8 + i][tid] = sb[0][i];
+            }
+            __syncthreads();
+            if (grp > 0) return;
+#pragma unroll
+            for (int k = 0; k < kGroups - 1; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sg[0][i] += sums[k][i][tid], sb[0][i] += sums[k][8 + i][tid];
+        }
+        float* p = part + (int64_t)blockIdx.x * 2 * cols;
 #pragma unroll
         for (int k = 0; k < kCh; ++k) {
             const int64_t c = (int64_t)8 * (tid + T * k);
@@ -507,11 +523,14 @@ int64_t sum_group(int64_t rows, int64_t cols) {
 int bwd_threads(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024; }
 
 int64_t bwd_blocks(int64_t rows, int64_t cols) {
-    // Every block leaves a row of partial sums: as many as compute units, of few rows
-    // twice that (two rows a turn behind one another rather than three or more).
+    // Every block leaves a row of partial sums, which bounds them: blocks of up to four rows
+    // at a time are small enough for two on a compute unit, each hiding the other's
+    // exchanges (16384 x 1024 in 256, 512 and 1024 of them: 41.7, 26.8, 27.4 us; 4096 x 2048
+    // 25.0, 19.8, 25.0), with at least two rows one after another; of wider rows one
+    // (8192 x 5120 in 256 and 512: 62.5, 66.8; 2000 x 4096 18.0, 21.9; 16384 x 4096 81.3, 77.8).
     const int t = bwd_threads(cols), per = t < kNormBlock ? kNormBlock / t : 1;
     const int64_t all = (rows + per - 1) / per;
-    return all <= 1024 && t <= kNormBlock ? std::min<int64_t>((all + 1) / 2, 512) : std::min<int64_t>(all, 256);
+    return t <= kNormBlock ? std::min<int64_t>((all + 1) / 2, 512) : std::min<int64_t>(all, 256);
 }
 
 }  // namespace
@@ -523,8 +542,7 @@ int64_t colsum_rows(int64_t rows, int64_t cols) {
 
 int64_t norm_sum_rows(int64_t rows, int64_t cols) {
     if (cols > kNormWidest) return colsum_rows(rows, cols);
-    const int t = bwd_threads(cols);
-    return bwd_blocks(rows, cols) * (t < kNormBlock ? kNormBlock / t : 1);
+    return bwd_blocks(rows, cols);
 }
 
 int32_t launch_layernorm(const NormArgs& a, const FusedQuant* fq, hipStream_t s) {
