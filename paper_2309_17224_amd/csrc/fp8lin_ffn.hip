@@ -54,7 +54,9 @@ __global__ __launch_bounds__(1024) void sums_finish_fine_kernel(const float* __r
 
 // ------------------------------------------------------------ transposed codes
 // qT [cols, rows] = q [rows, cols]^T, bytes: a workgroup's 256 rows x 128 columns
-// through LDS, so that both sides move 16-byte pieces of whole runs.  A column is 256
+// through LDS, so that both sides move 16-byte pieces of whole runs: memory bounds it
+// (4096 x 22016: 31 us, 5.8 TB/s; the whole quantise after the matmul instead of the
+// codes in its epilogue and this: 286 instead of 263 us).  A column is 256
 // bytes of LDS, its 16-byte chunk c at chunk c ^ swz(column).
 constexpr int kTr = 256, kTc = 128;
 
