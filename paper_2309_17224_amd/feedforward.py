@@ -72,6 +72,16 @@ class _Block:
                              f"{tuple(x.shape)} on {x.device}")
         return x
 
+    def _own(self, name: str, x: torch.Tensor) -> None:
+        """x copied into the block's tensor of that name, whose address a captured graph has."""
+        t = getattr(self, name, None)
+        if t is None:
+            setattr(self, name, x.detach().clone(memory_format=torch.contiguous_format))
+        elif t.dtype != x.dtype:
+            raise TypeError(f"{name}: the block was set up with {t.dtype}, got {x.dtype}")
+        else:
+            t.copy_(x)
+
     def _needs_training(self) -> None:
         if not self.train:
             raise RuntimeError("this block was made for inference (train=False)")
@@ -103,9 +113,9 @@ class GptFeedForward(_Block):
     """out = h + act(LayerNorm(h) W1 + b1) W2 + b2 for `rows` tokens of d columns.
 
     set_weights(W1 [d, ffn], b1 [ffn], W2 [ffn, d], b2 [d], g [d], b [d]) casts the
-    weights (after every update; biases, gain and b are kept by reference).
-    forward(h) returns out.  backward(dout) returns dh and leaves dw1, dw2, dg, db
-    (fp32) and db1, db2 (of the biases' type)."""
+    weights and copies the rest, after every update (a captured graph follows it).
+    forward(h) returns out; h has to stay as it is until backward.  backward(dout)
+    returns dh and leaves dw1, dw2, dg, db (fp32) and db1, db2 (of the biases' type)."""
 
     def __init__(self, rows: int, d: int, ffn: int, device, act: int = F.ACT_GELU, eps: float = 1e-5, train: bool = True):
         super().__init__(rows, device, act, train)
@@ -113,7 +123,7 @@ class GptFeedForward(_Block):
         self.w1, self.w2 = self._fp8(d, ffn, plain=train), self._fp8(ffn, d, plain=train)
         self.xn, self.a, self.out = self._new(rows, d), self._new(rows, ffn), self._new(rows, d)
         self.xn8, self.a8 = self._fp8(rows, d, transposed=train), self._fp8(rows, ffn, transposed=train)
-        self.z = self.mean = self.rstd = None
+        self.z = self.mean = self.rstd = self.db1 = self.db2 = None
         if train:
             f32 = torch.float32
             self.z, self.mean, self.rstd = self._new(rows, ffn), self._new(rows, dtype=f32), self._new(rows, dtype=f32)
@@ -130,14 +140,17 @@ class GptFeedForward(_Block):
                                (g, "g", (d,)), (b, "b", (d,))):
             if tuple(x.shape) != shape or x.device != self.dev:
                 raise ValueError(f"{name}: expected {shape} on {self.dev}, got {tuple(x.shape)} on {x.device}")
+        for name, x in (("b1", b1), ("b2", b2), ("g", g), ("b", b)):
+            self._own(name, x)
+        if self.train and self.db1 is None:
+            self.db1, self.db2 = torch.empty_like(self.b1), torch.empty_like(self.b2)
         self._quantise(W1, self.w1, F.E4M3, predict=False)
         self._quantise(W2, self.w2, F.E4M3, predict=False)
-        self.b1, self.b2, self.g, self.b = b1, b2, g, b
-        if self.train:
-            self.db1, self.db2 = torch.empty_like(b1), torch.empty_like(b2)
 
     def forward(self, h: torch.Tensor) -> torch.Tensor:
         self.h = self._take(h, "h", self.d)
+        if self.train and h.untyped_storage().data_ptr() == self.out.untyped_storage().data_ptr():
+            raise ValueError("h: the block's own output, which this call overwrites before backward reads it")
         # the layer norm casts its rows itself where no transposed codes are needed
         F.gpt_layernorm_quantise(h, self.g, self.b, self.eps, y=self.xn, mean=self.mean, rstd=self.rstd,
                                  fq=None if self.train else self._fq(self.xn8, F.E4M3))

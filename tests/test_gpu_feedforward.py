@@ -290,3 +290,45 @@ def test_cached_layer_over_the_gated_matmul(gpu):
         outs.append(m.run()[:2].clone())
     for a, b in ((outs[0], outs[2]), (outs[1], outs[3])):
         assert rel_f(np_bits(a), np_bits(b)) <= 2.0 ** -4
+
+
+# ------------------------------------------------------------------ weights that change under a captured graph
+def test_captured_step_follows_its_weights(gpu):
+    """set_weights between replays, of new tensors that do not stay: the graph reads the new
+    weights, biases and gain and writes the gradients that the block shows."""
+    rows, d, ffn = 40, 256, 768
+    block, w, h, dout = gpt(gpu, rows, d, ffn, F.ACT_GELU, 11)
+    eager = gpt(gpu, rows, d, ffn, F.ACT_GELU, 11)[0]
+
+    def step():
+        block.forward(h)
+        block.backward(dout)
+
+    step()
+    block.capture(step)
+    for turn in range(3):
+        new = {k: (v.to(gpu) * (1.5 + turn)).to(v.dtype) for k, v in w.items()}
+        block.set_weights(**new)
+        del new
+        junk = [torch.full((n,), 7.0, dtype=BF, device=gpu) for n in (d, ffn) for _ in range(8)]
+        block.replay()
+        eager.set_weights(**{k: (v.to(gpu) * (1.5 + turn)).to(v.dtype) for k, v in w.items()})
+        eager.forward(h)
+        eager.backward(dout)
+        for name in ("out", "dh", "dw1", "dw2", "db1", "db2", "dg", "db"):
+            assert torch.equal(getattr(block, name), getattr(eager, name)), (turn, name)
+        assert all(bool((t == 7).all()) for t in junk)
+    with pytest.raises(TypeError):
+        block.set_weights(**{k: v.to(gpu).float() if k == "b1" else v.to(gpu) for k, v in w.items()})
+
+
+def test_a_block_does_not_train_on_its_own_output(gpu):
+    """forward(out) would overwrite what backward reads."""
+    block, _, h, _ = gpt(gpu, 4, 64, 128, F.ACT_GELU, 1)
+    with pytest.raises(ValueError, match="own output"):
+        block.forward(block.forward(h))
+    infer = gpt(gpu, 4, 64, 128, F.ACT_GELU, 1, train=False)[0]
+    out = infer.forward(h).clone()
+    want = infer.forward(out).clone()
+    infer.forward(h)
+    assert torch.equal(infer.forward(infer.out), want)
