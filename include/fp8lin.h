@@ -677,7 +677,8 @@ int32_t gpt_bias_grad(const void *dy, int32_t dt, int64_t rows, int64_t cols, in
  * mean, rstd: out, optional, fp32 [rows], for gpt_layernorm_bwd.
  * quant: optional, codes of y (bf16 only, without qT: FP8_ENOTSUP otherwise); its ws
  *        of gpt_layernorm_ws_bytes(rows) bytes.
- * eps >= 0.  Statistics in fp32, the variance of the centred values.
+ * eps >= 0.  Statistics in fp32, the variance of the centred values; a row's outputs
+ * do not depend on the number of rows.
  */
 size_t gpt_layernorm_ws_bytes(int64_t rows);
 int32_t gpt_layernorm_quantise(const void *x, int64_t ldx, const void *res, int64_t ldr, int32_t dt, const void *g,

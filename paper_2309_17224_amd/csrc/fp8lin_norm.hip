@@ -112,6 +112,21 @@ __device__ __forceinline__ float rounded(float v) {
 }
 
 // ------------------------------------------------------------- forward
+// The sum over a row of what each of its T threads has in parts.  A wave that holds a row
+// alone has a part for each wave of a block that would, and adds them in that block's
+// order: a row's bits do not depend on how many rows there are.
+template <int T, int G>
+__device__ __forceinline__ float parts_sum(float (&v)[G], float* red) {
+    if constexpr (G == 1) return row_sum<T>(v[0], red);
+#pragma unroll
+    for (int i = 0; i < G; ++i) v[i] = wave_sum(v[i]);
+#pragma unroll
+    for (int d = 1; d < G; d *= 2)
+#pragma unroll
+        for (int i = 0; i + d < G; i += 2 * d) v[i] += v[i + d];
+    return v[0];
+}
+
 template <int DT, int T, int CH, int FMT>
 __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const int32_t* __restrict__ pred,
                                                                int32_t* __restrict__ used, uint32_t* __restrict__ parts,
@@ -124,6 +139,7 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
     const bool live = r < a.rows;
     const int64_t row = live ? r : a.rows - 1, cols = a.cols;
     const bool in_regs = cols <= (int64_t)8 * T * CH;
+    constexpr int kParts = T > 64 ? 1 : CH < 4 ? CH : 4;
     float h[CH][8];
     auto sum_res = [&](const Raw8<DT>& x, const Raw8<DT>& y, float (&v)[8]) {
         values8(x, v);
@@ -140,7 +156,7 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
         if (a.res) y = ld_raw8<DT>(a.res, row * a.ldr + c, nv);
         sum_res(x, y, v);
     };
-    float sum = 0.0f;
+    float sum[kParts] = {};
     if (in_regs) {
         Raw8<DT> x[CH], y[CH];  // every load of the row under way before the first is used
 #pragma unroll
@@ -160,36 +176,36 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
         for (int k = 0; k < CH; ++k) {
             sum_res(x[k], y[k], h[k]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += h[k][i];
+            for (int i = 0; i < 8; ++i) sum[k % kParts] += h[k][i];
         }
     } else {
         for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
             float v[8];
             load(c, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += v[i];
+            for (int i = 0; i < 8; ++i) sum[0] += v[i];
         }
     }
-    const float mean = row_sum<T>(sum, red) / (float)cols;
-    float ss = 0.0f;
-    auto centred = [&](int64_t c, const float (&v)[8]) {
+    const float mean = parts_sum<T>(sum, red) / (float)cols;
+    float ss[kParts] = {};
+    auto centred = [&](int64_t c, const float (&v)[8], float& s) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float d = c + i < cols ? v[i] - mean : 0.0f;
-            ss = fmaf(d, d, ss);
+            s = fmaf(d, d, s);
         }
     };
     if (in_regs) {
 #pragma unroll
-        for (int k = 0; k < CH; ++k) centred((int64_t)8 * (tid + T * k), h[k]);
+        for (int k = 0; k < CH; ++k) centred((int64_t)8 * (tid + T * k), h[k], ss[k % kParts]);
     } else {
         for (int64_t c = 8 * tid; c < cols; c += 8 * T) {
             float v[8];
             load(c, v);
-            centred(c, v);
+            centred(c, v, ss[0]);
         }
     }
-    const float rstd = 1.0f / sqrtf(row_sum<T>(ss, red) / (float)cols + a.eps);
+    const float rstd = 1.0f / sqrtf(parts_sum<T>(ss, red) / (float)cols + a.eps);
     if (live && tid == 0) {
         if (a.mean) a.mean[r] = mean;
         if (a.rstd) a.rstd[r] = rstd;
@@ -575,8 +591,17 @@ int32_t launch_layernorm(const NormArgs& a, const FusedQuant* fq, hipStream_t s)
         }
     };
     auto size = [&](auto D, auto Fm) {
+        // A wave for a row needs no exchange in LDS and no barrier, which counts where rows
+        // queue for the compute units; a block for a row has the shorter way through it.
+        // Plain and with codes, us: 64 x 768 by a wave 4.0, 7.4, by a block 3.6, 6.6; 4096 x
+        // 768 5.6, 9.7 and 9.0, 14.7; 1000 x 1283 6.5, 10.4 and 5.3, 8.8; 2000 x 1283 7.6,
+        // 11.4 and 7.4, 12.7; 8192 x 1283 17.5, 25.8 and 21.8, 35.3; 8192 x 2560 21.4, 34.4
+        // and 22.5, 43.0; 8192 x 4096 26.8, 47.6 and 28.5, 48.4, with a residual 43.4 and 40.8.
         if (a.cols <= 512) go(D, IC<64>{}, IC<1>{}, Fm);
-        else if (a.cols <= 1024) go(D, IC<64>{}, IC<2>{}, Fm);
+        else if (a.cols <= 1024 && a.rows > 768) go(D, IC<64>{}, IC<2>{}, Fm);
+        else if (a.cols <= 2048 && a.rows >= 2000) go(D, IC<64>{}, IC<4>{}, Fm);
+        else if (a.cols <= 2048) go(D, IC<256>{}, IC<1>{}, Fm);
+        else if (a.cols <= 2560 && a.rows >= 3000) go(D, IC<64>{}, IC<8>{}, Fm);
         else if (a.cols <= 4096) go(D, IC<256>{}, IC<2>{}, Fm);
         else if (a.cols <= 8192) go(D, IC<256>{}, IC<4>{}, Fm);
         else go(D, IC<256>{}, IC<8>{}, Fm);

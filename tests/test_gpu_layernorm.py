@@ -76,6 +76,33 @@ def test_forward(gpu, size, dt, res, gdt, pad, off):
     assert torch.equal(y2, ys.t)
 
 
+# rows by waves and by blocks, on both sides of each border
+@pytest.mark.parametrize("size", [(768, 1000), (769, 521), (1999, 1031), (2000, 1283), (2003, 2048), (2999, 2056), (3000, 2560),
+                                  (3001, 2051), (3000, 2561)], ids=str)
+@pytest.mark.parametrize("dt,res,gdt,pad,off", [(torch.bfloat16, True, torch.bfloat16, 3, 1), (torch.float32, False, torch.float32, 0, 0)])
+def test_forward_of_many_rows(gpu, size, dt, res, gdt, pad, off):
+    test_forward(gpu, size, dt, res, gdt, pad, off)
+
+
+@pytest.mark.parametrize("size", [(770, 1000), (2001, 1290), (3001, 2104)], ids=str)
+def test_codes_of_many_rows(gpu, size):
+    for pred in (None, 0, 1):
+        test_codes_are_those_of_the_output(gpu, size, pred, F.E4M3)
+
+
+@pytest.mark.parametrize("cols", [500, 768, 1001, 1283, 2048, 2560, 5000])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_a_row_is_the_same_in_any_batch(gpu, cols, dt):
+    _, x, g, b = data(3001, cols, dt, cols)
+    x, g, b = x.to(gpu), g.to(gpu), b.to(gpu)
+    seen = []
+    for n in (3, 768, 769, 1999, 2000, 3001):
+        mean, rstd = torch.empty(n, device=gpu), torch.empty(n, device=gpu)
+        seen.append((F.gpt_layernorm_quantise(x[:n], g, b, mean=mean, rstd=rstd)[:3], mean[:3], rstd[:3]))
+    for other in seen[1:]:
+        assert all(torch.equal(p, q) for p, q in zip(seen[0], other))
+
+
 @pytest.mark.parametrize("size", SIZES + [(300, 96), (1111, 1024), (600, 640)], ids=str)
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("res,gdt,pad,off", [(False, torch.float32, 0, 0), (True, torch.bfloat16, 3, 1)])
