@@ -140,6 +140,7 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
     const int64_t row = live ? r : a.rows - 1, cols = a.cols;
     const bool in_regs = cols <= (int64_t)8 * T * CH;
     constexpr int kParts = T > 64 ? 1 : CH < 4 ? CH : 4;
+    const int bq = kQuant ? fused_bias(pred, used) : 0;
     float h[CH][8];
     auto sum_res = [&](const Raw8<DT>& x, const Raw8<DT>& y, float (&v)[8]) {
         values8(x, v);
@@ -211,7 +212,6 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
         if (a.rstd) a.rstd[r] = rstd;
     }
     const bool cast = kQuant && pred;
-    const int bq = kQuant ? fused_bias(pred, used) : 0;
     uint32_t mag = 0;
     auto store = [&](int64_t c, const float (&v)[8]) {
         if (!live || c >= cols) return;
@@ -232,7 +232,8 @@ __global__ __launch_bounds__(kNormBlock) void layernorm_kernel(NormArgs a, const
             if (cast) {
                 const uint2 c8 = codes8<FMT < 0 ? 0 : FMT>(w, bq);
                 uint8_t* p = q + r * ldq + c;
-                if (nv == 8) st8_any(p, c8.x, c8.y);
+                // (plain stores: 8192 x 5120 65.9 us, 1000 x 8192 14.6; so 64.6, 13.6)
+                if (nv == 8) __builtin_nontemporal_store((u32x2_any{c8.x, c8.y}), (u32x2_any*)p);
                 else
                     for (int i = 0; i < nv; ++i) p[i] = (uint8_t)((i < 4 ? c8.x : c8.y) >> (8 * (i & 3)));
             }
