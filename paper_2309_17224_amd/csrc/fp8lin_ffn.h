@@ -60,16 +60,19 @@ __device__ __forceinline__ int stage_swz(int r) {
     return (((r >> 2) & 1) | ((r & 3) << 1) | (((r >> 2) ^ (r >> 3)) & 1) << 3) & (ROW / 16 - 1);
 }
 
-// Stages rows 16 i .. 16 i + 15 of a wave's sums, unscaled by 2^sh.
+// Stages rows 16 i .. 16 i + 15 of a wave's sums, unscaled by 2^sh, for its other lanes
+// to read, after they have read the sixteen before.
 template <int ROW, int NBLK>
 __device__ __forceinline__ void stage_sums(uint8_t* ep, const v4f (&acc)[NBLK], int sh, int lane) {
     const int frow = lane & 15, fg = lane >> 4, z = stage_swz<ROW>(frow);
+    wave_lds_order();
 #pragma unroll
     for (int j = 0; j < NBLK; ++j) {
         const v4f a = acc[j];
         *(float4*)(ep + frow * ROW + (((4 * j + fg) ^ z) << 4)) =
             make_float4(ldexpf(a[0], sh), ldexpf(a[1], sh), ldexpf(a[2], sh), ldexpf(a[3], sh));
     }
+    wave_lds_order();
 }
 
 // Eight staged sums of row r from chunk c on.

@@ -133,6 +133,7 @@ __device__ __forceinline__ void gemm_tile(
         if (QF >= 0) bq = clamp_bias(*qo.pred);
 #pragma unroll
         for (int i2 = 0; i2 < 2; ++i2) {
+            wave_lds_order();  // the rows before have been read
 #pragma unroll
             for (int ii = 0; ii < 2; ++ii) {
                 const int i = 2 * i2 + ii;
@@ -157,6 +158,7 @@ __device__ __forceinline__ void gemm_tile(
                     *(uint2*)(ep + (ii * 16 + frow) * kEpRowBf16 + (j * 16 + 4 * fg) * 2) = make_uint2(lo, hi);
                 }
             }
+            wave_lds_order();
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
                 const int row = 4 * t + prow, c16 = lane & 15;
@@ -229,6 +231,7 @@ __device__ __forceinline__ void gemm_tile(
         uint8_t* ep = smem + w * 32 * kEpRowF32;
 #pragma unroll
         for (int i2 = 0; i2 < 2; ++i2) {
+            wave_lds_order();  // the rows before have been read
 #pragma unroll
             for (int ii = 0; ii < 2; ++ii) {
                 const int i = 2 * i2 + ii;
@@ -244,6 +247,7 @@ __device__ __forceinline__ void gemm_tile(
                         make_float4(y[0], y[1], y[2], y[3]);
                 }
             }
+            wave_lds_order();
 #pragma unroll
             for (int t = 0; t < 16; ++t) {
                 const int row = 2 * t + (lane >> 5), c32 = lane & 31;

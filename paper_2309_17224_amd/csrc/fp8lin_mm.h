@@ -53,6 +53,16 @@ __device__ __forceinline__ void ws_barrier() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// What one lane of a wave has written to LDS before this, the others read after it, and
+// what was read before may be overwritten after it.  A wave's LDS operations are carried
+// out in order, so no instruction is needed; but without this the compiler may move a
+// lane's access over another lane's that its own does not overlap.
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // The two 16-byte pieces of an MFMA operand fragment, as one 8-register vector.
 __device__ __forceinline__ v8i ld_frag(const uint8_t* p, int fo0, int fo1) {
     const uint4 p0 = *(const uint4*)(p + fo0);
