@@ -597,7 +597,7 @@ __global__ __launch_bounds__(kCastThreads) void quant_pass2_kernel(
                                     have_used, margin, bias, amax_bits, flags, q, ldq, qT, ldqT, tiles_c, ncast);
 }
 
-// Pass 2 in the first ncheck workgroups, column sums of 64 columns in each of the others.
+// Pass 2 in the first ncheck workgroups, column sums of 64 columns in each of the others, in turn.
 template <int DT, int FMT, bool EDGE>
 __global__ __launch_bounds__(kCastThreads) void quant_pass2_sums_kernel(
     const void* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
@@ -613,8 +613,9 @@ __global__ __launch_bounds__(kCastThreads) void quant_pass2_sums_kernel(
         quant_pass2_body<DT, FMT, EDGE>(blockIdx.x, ncheck, tile, red, amax_s, x, rows, cols, ldx, parts, nparts, used, 1,
                                         margin, bias, amax_bits, flags, q, ldq, qT, ldqT, tiles_c, ncast);
     else
-        sum_rows64<kCastThreads / 64>(*(float(*)[16][64])tile, sums.part, sums.rows, sums.cols,
-                                      (int64_t)((int)blockIdx.x - ncheck) * 64, sums.out, sums.cols, nullptr, sums.dt);
+        for (int64_t c0 = (int64_t)((int)blockIdx.x - ncheck) * 64; c0 < sums.cols; c0 += (int64_t)((int)gridDim.x - ncheck) * 64)
+            sum_rows64<kCastThreads / 64>(*(float(*)[16][64])tile, sums.part, sums.rows, sums.cols, c0, sums.out, sums.cols,
+                                          nullptr, sums.dt);
 }
 
 // ------------------------------------------------ delayed scaling
@@ -855,12 +856,13 @@ void launch_quant_check_t(const void* x, int64_t rows, int64_t cols, int64_t ldx
                           int64_t ldqT, hipStream_t s, const ColumnSums* sums) {
     const int64_t tiles_c = (cols + kCastCols - 1) / kCastCols;
     const int64_t ncast = ((rows + kCastRows - 1) / kCastRows) * tiles_c;
-    const int nb2 = (int)(ncast < kQuantPass2MaxBlocks ? ncast : kQuantPass2MaxBlocks);
+    const CheckSumBlocks blocks = check_sum_blocks(rows, cols, sums ? sums->cols : 0);
+    const int nb2 = (int)blocks.check;
     with_edge(has_edge(rows, cols), [&](auto E) {
         if constexpr (DT == FP8_DT_BF16 && FMT == FP8_E5M2) {
             if (sums) {
                 hipLaunchKernelGGL((quant_pass2_sums_kernel<DT, FMT, decltype(E)::value>),
-                                   dim3((unsigned)(nb2 + (sums->cols + 63) / 64)), dim3(kCastThreads), 0, s, x, rows, cols,
+                                   dim3((unsigned)(nb2 + blocks.sums)), dim3(kCastThreads), 0, s, x, rows, cols,
                                    ldx, parts, nparts, used, margin, bias, amax_bits, flags, q, ldq, qT, ldqT, tiles_c,
                                    ncast, nb2, *sums);
                 return;
@@ -1161,6 +1163,11 @@ int32_t launch_cast(const void* x, int dt, int64_t rows, int64_t cols, int64_t l
         launch_cast_t<decltype(D)::value, decltype(F)::value>(x, rows, cols, ldx, bias, q, ldq, qT, ldqT, s);
     });
     return hip_status();
+}
+
+CheckSumBlocks check_sum_blocks(int64_t rows, int64_t cols, int64_t sum_cols) {
+    const int64_t ncast = ((rows + kCastRows - 1) / kCastRows) * ((cols + kCastCols - 1) / kCastCols);
+    return {ncast < kQuantPass2MaxBlocks ? ncast : kQuantPass2MaxBlocks, sum_blocks(sum_cols)};
 }
 
 int32_t launch_quant_check(const void* x, int dt, int64_t rows, int64_t cols, int64_t ldx, int fmt,

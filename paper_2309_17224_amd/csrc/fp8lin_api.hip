@@ -893,6 +893,13 @@ int32_t fp8lin_epi_route(int32_t mode, int64_t M, int64_t N, int64_t K, int32_t*
     return r.kernel;
 }
 
+// Workgroups (of 256 threads) of the launch that checks the codes of a [rows, cols] output
+// and adds up its column sums.
+int64_t fp8lin_check_sum_blocks(int64_t rows, int64_t cols) {
+    const CheckSumBlocks b = check_sum_blocks(rows, cols, cols);
+    return b.check + b.sums;
+}
+
 // Tile i of the small-tile kernel; 0 past the last one.
 int32_t fp8lin_mm_tile(int32_t i, int32_t* mb, int32_t* nb) { return stream_tile_at(i, mb, nb) ? 1 : 0; }
 

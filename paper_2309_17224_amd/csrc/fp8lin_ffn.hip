@@ -147,8 +147,8 @@ int32_t launch_sums_finish(const float* part, int64_t rows, int64_t cols, void* 
                            cols, out0, n0, out1, dt);
         return hip_status();
     }
-    hipLaunchKernelGGL(sums_finish_kernel, dim3((unsigned)std::min<int64_t>((cols + 63) / 64, kMaxSumBlocks)), dim3(1024), 0,
-                       s, part, (int)rows, cols, out0, n0, out1, dt);
+    hipLaunchKernelGGL(sums_finish_kernel, dim3((unsigned)sum_blocks(cols)), dim3(1024), 0, s, part, (int)rows, cols,
+                       out0, n0, out1, dt);
     return hip_status();
 }
 

@@ -209,9 +209,15 @@ void launch_ffn_act(bool ragged, const Epi& e, hipStream_t s);
 void launch_ffn_glu(bool ragged, const Epi& e, hipStream_t s);
 void launch_ffn_act_bwd(bool ragged, const Epi& e, hipStream_t s);
 void launch_ffn_glu_bwd(bool ragged, const Epi& e, hipStream_t s);
-// Workgroups of 1024 threads that take columns in turn where there are more of them (a
-// launch has fewer than 2^32 threads).
+// Workgroups (of up to 1024 threads) that add up 64 columns each, in turn where there are
+// more of them: a launch has fewer than 2^32 threads.
 constexpr int64_t kMaxSumBlocks = 1 << 16;
+inline int64_t sum_blocks(int64_t cols) { return cols < 64 * kMaxSumBlocks ? (cols + 63) / 64 : kMaxSumBlocks; }
+// Workgroups of launch_quant_check with column sums: those that check, and those that add.
+struct CheckSumBlocks {
+    int64_t check, sums;
+};
+CheckSumBlocks check_sum_blocks(int64_t rows, int64_t cols, int64_t sum_cols);
 // out0[c] (c < n0) and out1[c - n0] = sum over the rows of part [rows, cols] fp32,
 // of type dt; either may be null.
 int32_t launch_sums_finish(const float* part, int64_t rows, int64_t cols, void* out0, int64_t n0, void* out1, int dt,

@@ -656,7 +656,7 @@ int32_t launch_layernorm_bwd(const NormArgs& a, float* dg, float* db, float* par
 int32_t launch_colsum(const void* x, int dt, int64_t rows, int64_t cols, int64_t ldx, void* out, int out_dt, float* part,
                       hipStream_t s) {
     if (rows <= kFewRows) {
-        const dim3 grid((unsigned)std::min<int64_t>((cols + 63) / 64, kMaxSumBlocks));
+        const dim3 grid((unsigned)sum_blocks(cols));
         if (dt == FP8_DT_BF16)
             hipLaunchKernelGGL((colsum_few_kernel<FP8_DT_BF16>), grid, dim3(1024), 0, s, x, rows, cols, ldx, out, out_dt);
         else
