@@ -43,7 +43,8 @@ __device__ __forceinline__ float sigma2(float p, float* q) {
 // f = act(x), d = act'(x) (what is not used costs nothing).
 // GELU: x Phi(x) = max(x, 0) - a h; its slope Phi(x) + x phi(x) is k = e (P - a /
 // sqrt(2 pi)) for x < 0 and 1 - k otherwise.
-// The others are x sigma(p(x)), with slope sigma (1 + x p' (1 - sigma)), 1 - sigma = q sigma.
+// The others are x sigma(p(x)), with slope sigma (1 + x p' (1 - sigma)), 1 - sigma = q sigma
+// (with an infinite q sigma is 0, and q only has to be finite).
 template <int ACT>
 __device__ __forceinline__ void act_t(float x, float* f, float* d) {
     if constexpr (ACT == FP8_ACT_GELU) {
@@ -58,12 +59,12 @@ __device__ __forceinline__ void act_t(float x, float* f, float* d) {
         *f = fmaxf(x, -kMaxF) * r;
         const float c = __builtin_amdgcn_fmed3f(x, -100.0f, 100.0f);
         const float dp = c * fmaf(c * c, 0.2140644488f, 1.595769122f);  // 2 sqrt(2/pi) {3 * 0.044715, 1}
-        *d = fmaf(dp, fminf(q, 1e30f) * r, 1.0f) * r;
+        *d = fmaf(dp, fminf(q, kMaxF) * r, 1.0f) * r;
     } else if constexpr (ACT == FP8_ACT_SILU) {
         float q;
         const float r = sigma2(x * 1.442695041f, &q);
         *f = fmaxf(x, -kMaxF) * r;
-        *d = fmaf(__builtin_amdgcn_fmed3f(x, -1000.0f, 1000.0f), fminf(q, 1e30f) * r, 1.0f) * r;
+        *d = fmaf(__builtin_amdgcn_fmed3f(x, -1000.0f, 1000.0f), fminf(q, kMaxF) * r, 1.0f) * r;
     } else if constexpr (ACT == FP8_ACT_RELU) {
         *f = x <= 0.0f ? 0.0f : x;
         *d = x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
