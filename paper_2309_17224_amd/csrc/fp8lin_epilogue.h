@@ -14,24 +14,28 @@ constexpr int epi_fa(int mode) { return epi_fwd(mode) ? FP8_E4M3 : FP8_E5M2; }  
 
 // The VALU is what bounds the epilogues that have an exponential (a workgroup's 256
 // x 256 outputs: about 0.4 us an operation of each, 1.6 us an exponential or
-// reciprocal), so the forms below are the shortest that keep infinities, NaN and a
-// relative error of a few 2^-20: act(-inf) = 0, act(inf) = inf, slopes 0 and 1.
+// reciprocal), so the forms below are the shortest that keep infinities, NaN and, relative
+// to the value (of a slope, to its two terms), an error of (1 + |p| / 4) 2^-20 where the
+// exponential is 2^-p: its argument's rounding, the larger the further out.  Exponentials
+// and reciprocals below 2^-126 are 0: then |x| 2^-125 of a value is lost, and of a slope as
+// much of either term.  act(-inf) = 0, act(inf) = inf, slopes 0 and 1.
 constexpr float kMaxF = 3.402823466e38f;
 
 // h = Phi(-a) = (1 - erf(a / sqrt 2)) / 2, a = |x|: e = exp(-a^2 / 2) times half the
-// scaled complementary error function of a / sqrt 2, which is within 6.2e-7 of P(s),
-// s = 1 / (1 + 0.29 a), for a <= 9 (a least-squares fit, reweighted towards the
-// smallest largest relative error; 9.5e-7 in fp32), so the tail keeps its relative
+// scaled complementary error function of a / sqrt 2, which is within 2.5e-7 of P(s),
+// s = 1 / (1 + 0.255 a), for a <= 13.2, where e ends (the smallest largest relative error,
+// by a linear program over 3000 points; 6e-7 in fp32), so the tail keeps its relative
 // accuracy.  e is left in *e, P in *p.
 __device__ __forceinline__ void gauss_tail(float x, float* e, float* p) {
     *e = __builtin_amdgcn_exp2f(x * -0.72134752f * x);
-    const float s = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.29f, 1.0f));
-    float q = fmaf(-0.0970692119f, s, 0.317669847f);
-    q = fmaf(q, s, -0.145566512f);
-    q = fmaf(q, s, 0.222276692f);
-    q = fmaf(q, s, 0.0821047592f);
-    q = fmaf(q, s, 0.120924779f);
-    *p = fmaf(q, s, -0.000340452563f);
+    const float s = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.255f, 1.0f));
+    float q = fmaf(-0.0861081492f, s, 0.300115732f);
+    q = fmaf(q, s, -0.213540407f);
+    q = fmaf(q, s, 0.251808977f);
+    q = fmaf(q, s, 0.0317131988f);
+    q = fmaf(q, s, 0.115948818f);
+    q = fmaf(q, s, 0.0999695562f);
+    *p = fmaf(q, s, 9.23959189e-05f);
 }
 
 // q = 2^-p and sigma(p ln 2) = 1 / (1 + q).

@@ -79,7 +79,7 @@ def ones(rows, cols, kind, gpu):
 
 
 @pytest.mark.parametrize("rows", ROWS)
-@pytest.mark.parametrize("act", ACTS[1:])
+@pytest.mark.parametrize("act", ACTS)
 def test_values(gpu, rows, act):
     M, kernel = ROWS[rows]
     assert R.epilogue(0, M, N, K)[0] == R.epilogue(1, M, N, K)[0] == kernel
