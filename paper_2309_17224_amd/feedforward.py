@@ -80,7 +80,7 @@ class _Block:
         elif t.dtype != x.dtype:
             raise TypeError(f"{name}: the block was set up with {t.dtype}, got {x.dtype}")
         else:
-            t.copy_(x)
+            t.copy_(x.detach())  # of a parameter the values alone, without an autograd history
 
     def _needs_training(self) -> None:
         if not self.train:
