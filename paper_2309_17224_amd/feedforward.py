@@ -72,13 +72,21 @@ class _Block:
                              f"{tuple(x.shape)} on {x.device}")
         return x
 
+    def _check(self, x: torch.Tensor, name: str, *shape: int) -> None:
+        """A weight (its rows contiguous), bias or gain that a call can take."""
+        if tuple(x.shape) != shape or x.device != self.dev:
+            raise ValueError(f"{name}: expected {shape} on {self.dev}, got {tuple(x.shape)} on {x.device}")
+        if x.dtype not in (BF16, torch.float32):
+            raise TypeError(f"{name}: expected bfloat16 or float32, got {x.dtype}")
+        rows, cols = shape if len(shape) == 2 else (1, 1)
+        if (cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols):
+            raise ValueError(f"{name}: expected contiguous rows that do not overlap, got strides {x.stride()}")
+
     def _own(self, name: str, x: torch.Tensor) -> None:
         """x copied into the block's tensor of that name, whose address a captured graph has."""
         t = getattr(self, name, None)
         if t is None:
             setattr(self, name, x.detach().clone(memory_format=torch.contiguous_format))
-        elif t.dtype != x.dtype:
-            raise TypeError(f"{name}: the block was set up with {t.dtype}, got {x.dtype}")
         else:
             t.copy_(x.detach())  # of a parameter the values alone, without an autograd history
 
@@ -113,7 +121,8 @@ class GptFeedForward(_Block):
     """out = h + act(LayerNorm(h) W1 + b1) W2 + b2 for `rows` tokens of d columns.
 
     set_weights(W1 [d, ffn], b1 [ffn], W2 [ffn, d], b2 [d], g [d], b [d]) casts the
-    weights and copies the rest, after every update (a captured graph follows it).
+    weights and copies the rest, after every update (a captured graph follows it); each
+    bf16 or fp32, g and b of one type, biases and gain of the types of the first time.
     forward(h) returns out; h has to stay as it is until backward.  backward(dout)
     returns dh and leaves dw1, dw2, dg, db (fp32) and db1, db2 (of the biases' type)."""
 
@@ -138,8 +147,13 @@ class GptFeedForward(_Block):
         d, ffn = self.d, self.ffn
         for x, name, shape in ((W1, "W1", (d, ffn)), (b1, "b1", (ffn,)), (W2, "W2", (ffn, d)), (b2, "b2", (d,)),
                                (g, "g", (d,)), (b, "b", (d,))):
-            if tuple(x.shape) != shape or x.device != self.dev:
-                raise ValueError(f"{name}: expected {shape} on {self.dev}, got {tuple(x.shape)} on {x.device}")
+            self._check(x, name, *shape)
+        if g.dtype != b.dtype:
+            raise TypeError(f"g and b: expected one type, got {g.dtype} and {b.dtype}")
+        for name, x in (("b1", b1), ("b2", b2), ("g", g), ("b", b)):
+            t = getattr(self, name, None)
+            if t is not None and t.dtype != x.dtype:
+                raise TypeError(f"{name}: the block was set up with {t.dtype}, got {x.dtype}")
         for name, x in (("b1", b1), ("b2", b2), ("g", g), ("b", b)):
             self._own(name, x)
         if self.train and self.db1 is None:
@@ -195,9 +209,8 @@ class GatedFeedForward(_Block):
             self.dwgu, self.dwd = self._new(d, 2 * ffn, dtype=torch.float32), self._new(ffn, d, dtype=torch.float32)
 
     def set_weights(self, Wgu, Wd) -> None:
-        for x, name, shape in ((Wgu, "Wgu", (self.d, 2 * self.ffn)), (Wd, "Wd", (self.ffn, self.d))):
-            if tuple(x.shape) != shape or x.device != self.dev:
-                raise ValueError(f"{name}: expected {shape} on {self.dev}, got {tuple(x.shape)} on {x.device}")
+        self._check(Wgu, "Wgu", self.d, 2 * self.ffn)
+        self._check(Wd, "Wd", self.ffn, self.d)
         self._quantise(Wgu, self.wgu, F.E4M3, predict=False)
         self._quantise(Wd, self.wd, F.E4M3, predict=False)
 

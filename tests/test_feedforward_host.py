@@ -39,3 +39,53 @@ def test_parameters_are_copied_without_their_graph(gpt):
         for name in ("b1", "b2", "g", "b"):
             t = getattr(gpt, name)
             assert not t.requires_grad and t.grad_fn is None and torch.equal(t, w[name])
+
+
+def refused(block, error, match, **other):
+    """set_weights raises, and has neither cast nor copied anything."""
+    before = {n: None if getattr(block, n, None) is None else getattr(block, n).clone() for n in ("b1", "b2", "g", "b")}
+    casts = len(block.casts)
+    with pytest.raises(error, match=match):
+        block.set_weights(**weights(7, **other))
+    assert len(block.casts) == casts
+    for n, t in before.items():
+        now = getattr(block, n, None)
+        assert (now is None) == (t is None) and (t is None or torch.equal(now, t)), n
+
+
+@pytest.mark.parametrize("again", [False, True])
+def test_unusable_weights_are_refused_before_anything_changes(gpt, again):
+    if again:
+        gpt.set_weights(**weights())
+    v = lambda n, dt=BF: torch.ones(n, dtype=dt)  # noqa: E731
+    refused(gpt, TypeError, "g and b", g=v(D, F32))
+    refused(gpt, TypeError, "g and b", b=v(D, F32))
+    for name, n in (("b1", FFN), ("b2", D), ("g", D), ("b", D)):
+        refused(gpt, TypeError, name, **{name: v(n, torch.float16)})
+        refused(gpt, ValueError, name, **{name: v(n + 1)})
+    for name, shape in (("W1", (D, FFN)), ("W2", (FFN, D))):
+        refused(gpt, TypeError, name, **{name: torch.ones(shape, dtype=torch.float16)})
+        refused(gpt, ValueError, name, **{name: torch.ones(shape[::-1], dtype=BF).t()})   # columns contiguous, not rows
+        refused(gpt, ValueError, name, **{name: torch.ones((shape[0], 1), dtype=BF).expand(shape)})
+
+
+def test_biases_keep_their_types(gpt):
+    """Each bias of its own type; what the block was set up with stays, since a captured graph has its tensors."""
+    gpt.set_weights(**weights(b1=torch.ones(FFN, dtype=F32), g=torch.ones(D), b=torch.ones(D)))
+    assert gpt.db1.dtype == F32 and gpt.db2.dtype == BF
+    refused(gpt, TypeError, "b1", b1=torch.ones(FFN, dtype=BF))
+    refused(gpt, TypeError, "b", g=torch.ones(D, dtype=BF), b=torch.ones(D, dtype=BF))
+
+
+def test_gated_weights_are_refused_before_either_is_cast(monkeypatch):
+    block = FF.GatedFeedForward(4, D, FFN, "cpu")
+    casts = []
+    monkeypatch.setattr(block, "_quantise", lambda x, t, fmt, predict=True: casts.append(x))
+    good = torch.ones((D, 2 * FFN), dtype=BF), torch.ones((FFN, D), dtype=BF)
+    for error, bad in ((TypeError, torch.ones((FFN, D), dtype=torch.float16)), (ValueError, torch.ones((D, FFN), dtype=BF)),
+                       (ValueError, torch.ones((D, FFN), dtype=BF).t())):
+        with pytest.raises(error, match="Wd"):
+            block.set_weights(good[0], bad)
+    assert not casts
+    block.set_weights(*good)
+    assert len(casts) == 2
