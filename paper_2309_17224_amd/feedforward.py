@@ -47,6 +47,7 @@ class _Block:
         self.rows, self.act, self.train = rows, act, train
         self.dev = torch.empty(0, device=device).device
         self.graph = None
+        self.weighed = self.ran = False  # set_weights, and then forward, have run
 
     def _new(self, *shape, dtype=BF16):
         return torch.empty(shape, dtype=dtype, device=self.dev)
@@ -90,9 +91,15 @@ class _Block:
         else:
             t.copy_(x.detach())  # of a parameter the values alone, without an autograd history
 
+    def _needs_weights(self) -> None:
+        if not self.weighed:
+            raise RuntimeError("forward: the block has no weights yet (set_weights)")
+
     def _needs_training(self) -> None:
         if not self.train:
             raise RuntimeError("this block was made for inference (train=False)")
+        if not self.ran:
+            raise RuntimeError("backward: no forward has run yet")
 
     def capture(self, step):
         """Record step() (calls of this block, on tensors that stay) into a HIP graph;
@@ -114,6 +121,8 @@ class _Block:
         return g
 
     def replay(self) -> None:
+        if self.graph is None:
+            raise RuntimeError("replay: nothing was recorded yet (capture)")
         self.graph.replay()
 
 
@@ -160,9 +169,11 @@ class GptFeedForward(_Block):
             self.db1, self.db2 = torch.empty_like(self.b1), torch.empty_like(self.b2)
         self._quantise(W1, self.w1, F.E4M3, predict=False)
         self._quantise(W2, self.w2, F.E4M3, predict=False)
+        self.weighed = True
 
     def forward(self, h: torch.Tensor) -> torch.Tensor:
-        self.h = self._take(h, "h", self.d)
+        self._needs_weights()
+        self._take(h, "h", self.d)
         if self.train and h.untyped_storage().data_ptr() == self.out.untyped_storage().data_ptr():
             raise ValueError("h: the block's own output, which this call overwrites before backward reads it")
         # the layer norm casts its rows itself where no transposed codes are needed
@@ -172,8 +183,9 @@ class GptFeedForward(_Block):
             self._quantise(self.xn, self.xn8, F.E4M3)
         F.fp8_linear_fwd_act(self.xn8.q, self.xn8.bias, self.w1.qT, self.w1.bias, self.act, bias=self.b1, z=self.z, y=self.a,
                              fq=self._fq(self.a8, F.E4M3))
-        return F.fp8_linear_fwd_act(self.a8.q, self.a8.bias, self.w2.qT, self.w2.bias, F.ACT_NONE, bias=self.b2, res=h,
-                                    y=self.out)
+        F.fp8_linear_fwd_act(self.a8.q, self.a8.bias, self.w2.qT, self.w2.bias, F.ACT_NONE, bias=self.b2, res=h, y=self.out)
+        self.h, self.ran = h, True
+        return self.out
 
     def backward(self, dout: torch.Tensor) -> torch.Tensor:
         self._needs_training()
@@ -213,12 +225,16 @@ class GatedFeedForward(_Block):
         self._check(Wd, "Wd", self.ffn, self.d)
         self._quantise(Wgu, self.wgu, F.E4M3, predict=False)
         self._quantise(Wd, self.wd, F.E4M3, predict=False)
+        self.weighed = True
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
+        self._needs_weights()
         self._quantise(self._take(x, "x", self.d), self.x8, F.E4M3)
         F.fp8_linear_fwd_glu(self.x8.q, self.x8.bias, self.wgu.qT, self.wgu.bias, self.act, gu=self.gu, a=self.a,
                              fq=self._fq(self.a8, F.E4M3))
-        return F.fp8_linear_fwd(self.a8.q, self.a8.bias, self.wd.qT, self.wd.bias, y=self.y)
+        F.fp8_linear_fwd(self.a8.q, self.a8.bias, self.wd.qT, self.wd.bias, y=self.y)
+        self.ran = True
+        return self.y
 
     def backward(self, dy: torch.Tensor) -> torch.Tensor:
         self._needs_training()

@@ -89,3 +89,21 @@ def test_gated_weights_are_refused_before_either_is_cast(monkeypatch):
     assert not casts
     block.set_weights(*good)
     assert len(casts) == 2
+
+
+def test_calls_out_of_order_are_refused(gpt):
+    x = torch.ones((4, D), dtype=BF)
+    gated = FF.GatedFeedForward(4, D, FFN, "cpu")
+    for block in (gpt, gated):
+        with pytest.raises(RuntimeError, match="set_weights"):
+            block.forward(x)
+        with pytest.raises(RuntimeError, match="forward"):
+            block.backward(x)
+        with pytest.raises(RuntimeError, match="capture"):
+            block.replay()
+    gpt.set_weights(**weights())
+    with pytest.raises(RuntimeError, match="forward"):
+        gpt.backward(x)
+    infer = FF.GatedFeedForward(4, D, FFN, "cpu", train=False)
+    with pytest.raises(RuntimeError, match="inference"):
+        infer.backward(x)
