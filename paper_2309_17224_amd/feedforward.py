@@ -36,6 +36,11 @@ from .linear import Fp8Tensor
 BF16 = torch.bfloat16
 
 
+def _index(dev: torch.device) -> int:
+    """The GPU of a device, -1 of the host."""
+    return dev.index if dev.type == "cuda" else -1
+
+
 class _Block:
     """Buffers shared by the two blocks: FP8 forms of tensors, each with its workspace."""
 
@@ -67,7 +72,14 @@ class _Block:
         F.fp8_quantise(x, fmt, 0, bias_pred=t.bias if predict else None, bias=t.bias, amax_bits=t.amax, flags=t.flags,
                        q=t.q, qT=t.qT, want_q=t.q is not None, want_qT=t.qT is not None, ws=t.qws)
 
+    def _on_current_gpu(self) -> None:
+        """The calls of a block run on the current GPU's stream."""
+        gpu = _index(self.dev)
+        if gpu >= 0 and F._current() != gpu:
+            raise ValueError(f"the block is on {self.dev}, which is not the current GPU")
+
     def _take(self, x: torch.Tensor, name: str, cols: int) -> torch.Tensor:
+        self._on_current_gpu()
         if x.shape != (self.rows, cols) or x.dtype != BF16 or x.device != self.dev:
             raise ValueError(f"{name}: expected bfloat16 [{self.rows}, {cols}] on {self.dev}, got {x.dtype} "
                              f"{tuple(x.shape)} on {x.device}")
@@ -75,6 +87,7 @@ class _Block:
 
     def _check(self, x: torch.Tensor, name: str, *shape: int) -> None:
         """A weight (its rows contiguous), bias or gain that a call can take."""
+        self._on_current_gpu()
         if tuple(x.shape) != shape or x.device != self.dev:
             raise ValueError(f"{name}: expected {shape} on {self.dev}, got {tuple(x.shape)} on {x.device}")
         if x.dtype not in (BF16, torch.float32):

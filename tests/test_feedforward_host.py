@@ -107,3 +107,17 @@ def test_calls_out_of_order_are_refused(gpt):
     infer = FF.GatedFeedForward(4, D, FFN, "cpu", train=False)
     with pytest.raises(RuntimeError, match="inference"):
         infer.backward(x)
+
+
+def test_a_block_of_another_gpu_is_refused(gpt, monkeypatch):
+    """Calls run on the current GPU's stream: a block on another is refused before any is made."""
+    x = torch.ones((4, D), dtype=BF)
+    gpt.set_weights(**weights())
+    casts = len(gpt.casts)
+    gpt.ran = True
+    monkeypatch.setattr(FF, "_index", lambda dev: 1)
+    monkeypatch.setattr(F, "_current", lambda: 0)
+    for call in (lambda: gpt.set_weights(**weights(1)), lambda: gpt.forward(x), lambda: gpt.backward(x)):
+        with pytest.raises(ValueError, match="current GPU"):
+            call()
+    assert len(gpt.casts) == casts and torch.equal(gpt.b1, weights()["b1"])
