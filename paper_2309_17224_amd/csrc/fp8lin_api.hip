@@ -893,6 +893,17 @@ int32_t fp8lin_epi_route(int32_t mode, int64_t M, int64_t N, int64_t K, int32_t*
     return r.kernel;
 }
 
+// How the 256-row kernel of a feed-forward matmul splits its columns (those of both
+// projections with kEpiGlu): ndp tiles 256 wide, then tn2 of width tw.  0 where it takes another.
+int32_t fp8lin_epi_split(int32_t mode, int64_t M, int64_t N, int64_t K, int32_t* ndp, int32_t* tw, int32_t* tn2) {
+    if (epi_route(mode, M, N, K).kernel != kMm256) return 0;
+    const int64_t cols = epi_b_cols(mode, N);
+    int a, b, c;
+    mm256_split((int)((M + 255) / 256), (int)((cols + 255) / 256), cols, a, b, c);
+    *ndp = a, *tw = b, *tn2 = c;
+    return 1;
+}
+
 // Workgroups (of 256 threads) of the launch that checks the codes of a [rows, cols] output
 // and adds up its column sums.
 int64_t fp8lin_check_sum_blocks(int64_t rows, int64_t cols) {
