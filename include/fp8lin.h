@@ -560,6 +560,13 @@ int32_t llama_residual_add(const void *a, const void *b, void *out, int64_t n, v
  * gated pair of projections (SwiGLU).  The matmuls below do in their epilogue what
  * follows the product (or, backward, what follows the grad-input product on its
  * way to the linear before); fp32 arithmetic throughout, every output rounded once.
+ * A product's sums are the matrix core's, as in the other matmuls: within 2^-11 of the
+ * sum of the products' magnitudes (about 1.5e-5 of a sum in practice, which moves about
+ * one bf16 output in 200 by a step).  Activations and, of a slope, its two terms are
+ * within (1 + |p| / 4) 2^-20 of themselves, 2^-p being the exponential that they take (p =
+ * x^2 / (2 ln 2), 2 u / ln 2 with the tanh's argument u, x / ln 2), for an fp32 output too;
+ * where it is below 2^-126, |x| 2^-125 may be lost (of a term of a slope, 2^-125 times its
+ * other factor).
  * Tensors are row-major with row strides (ld*, in elements) of any length from
  * the row's on and start on their element size; FP8 operands are as in
  * fp8_linear_fwd and fp8_linear_bwd_dx (dense, 16-byte aligned).  Outputs must not

@@ -1,7 +1,5 @@
 // The choice of kernel for the feed-forward matmuls (fp8lin_ffn.h), the column sums
 // that their backward epilogues leave in parts, and the quantise of their output.
-#include <algorithm>
-
 #include "fp8lin_mm.h"
 #include "fp8lin_sums.h"
 #include "fp8lin_vals.h"
@@ -195,9 +193,9 @@ int32_t launch_epilogue_mm(int mode, Epi& e, const FusedQuant* fq, int64_t ws_wo
         st = launch_sums_finish(e.sums, sums.rows, cols, e.db, cols, nullptr, e.db_dt, s);
     if (st != FP8_OK || !fq) return st;
     if (e.q) {
-        // The codes of both gradients of a gated block's tile, transposed, are more than
-        // the LDS beside the staging rows (or the registers) holds: from the codes, once
-        // they are final.
+        // The codes of both gradients of a gated block's tile, transposed, are 128 KB, and
+        // whole rows of eight waves staged another 64 (half rows would leave room): from the
+        // codes, once they are final.
         const bool apart = qT && mode == kEpiGluBwd && r.kernel == kMm256;
         st = launch_quant_check(e.out, FP8_DT_BF16, e.M, cols, e.ldo, fq->fmt, fq->margin, fq->ws + 1, (int)blocks,
                                 (const int32_t*)fq->ws, fq->bias, fq->amax_bits, fq->flags, fq->q, fq->ldq,

@@ -4,8 +4,9 @@
 // through LDS in a fixed order as there; each wave then takes whole blocks of 16
 // x 16 outputs (with kEpiGlu the two blocks of a pair), a lane four columns of a
 // row.  The weight's stream bounds it where there are few rows (16 x 28672 x 8192 gated:
-// 70 us, 6.7 TB/s; 1 x 4096 x 11008 with bias and residual: 12 us, 3.7 TB/s, one round of
-// workgroups that each wait for their first rows), launches and latency where both sides
+// 70 us, 6.7 TB/s; 1 x 4096 x 11008 with bias and residual: 12 us, 3.7 TB/s, since a 16 x 16
+// tile has two stages of 16 KB on the way, half of each copies of the one row of
+// activations: 4 MB of weights at a time over the chip), launches and latency where both sides
 // are small (509 x 2048 x 768 backward with codes and bias gradient: 10 us, with the launch
 // that finishes both 13).
 #include "fp8lin_epilogue.h"

@@ -10,7 +10,10 @@
 // mean is taken first), and each output is rounded once.  8192 x 5120 with residual and
 // codes: 80 us, 4.7 TB/s, near the rate of a device copy (16384 x 4096 without them 5.1);
 // backward of 4096 x 8192 with the residual's gradient 55 us, 4.9 TB/s, and 4 for the sums
-// of its partial rows.
+// of its partial rows.  fp32: 8192 x 5120 76 us forward (4.4 TB/s), 113 backward (4.5).
+// Backward beyond 8192 columns, two eights a thread: 4096 x 12288 96 us (3.1 TB/s), fp32 171;
+// 21 and 26 registers are spilled there (7 of fp32 rows of 4097 columns and more).  Beyond
+// 16384 rows are read again: 4096 x 20480 148 us forward, 224 backward (2.3).
 #include <algorithm>
 
 #include "fp8lin_glue.h"
@@ -533,7 +536,9 @@ constexpr int64_t kMaxNormBlocks = 1 << 23;  // of a launch
 constexpr int64_t kNormWidest = 16384;  // columns a row's threads hold in the backward pass
 
 // Rows of a group of colsum_kernel: about 1024 workgroups, groups of 16 rows (four to a
-// wave) at least.
+// wave) at least.  A turn of 32 rows (16 of the layer norm's sums) past a group's end is loaded and not
+// added: of 4096 x 5120 64 rows for the 41 of a group (15.1 us with the second launch, 2.8
+// TB/s; 8192 x 4096, 64 for 64, 18.1 us, 3.7).
 int64_t sum_group(int64_t rows, int64_t cols) {
     const int64_t wide = (cols + 511) / 512, groups = std::max<int64_t>(1, std::min<int64_t>(256, 1024 / wide));
     return std::max<int64_t>(16, (rows + groups - 1) / groups);
@@ -598,6 +603,7 @@ int32_t launch_layernorm(const NormArgs& a, const FusedQuant* fq, hipStream_t s)
         // 768 5.6, 9.7 and 9.0, 14.7; 1000 x 1283 6.5, 10.4 and 5.3, 8.8; 2000 x 1283 7.6,
         // 11.4 and 7.4, 12.7; 8192 x 1283 17.5, 25.8 and 21.8, 35.3; 8192 x 2560 21.4, 34.4
         // and 22.5, 43.0; 8192 x 4096 26.8, 47.6 and 28.5, 48.4, with a residual 43.4 and 40.8.
+        // The borders lie between these sizes; nearer to them the two were not measured.
         if (a.cols <= 512) go(D, IC<64>{}, IC<1>{}, Fm);
         else if (a.cols <= 1024 && a.rows > 768) go(D, IC<64>{}, IC<2>{}, Fm);
         else if (a.cols <= 2048 && a.rows >= 2000) go(D, IC<64>{}, IC<4>{}, Fm);
