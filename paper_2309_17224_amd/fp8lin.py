@@ -773,6 +773,8 @@ def _stream_on(stream, dev: int):
     """The stream of a call on GPU dev, the current one."""
     if stream is None and _raw_stream is not None:
         return _raw_stream(dev)
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"stream: of GPU {stream.device_index}, the call on GPU {dev}")
     return _stream(stream)
 
 
